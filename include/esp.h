@@ -308,6 +308,113 @@ int esp_gemm_scratch_bytes(size_t* bytes_out);
 int esp_gemm_bf16(int32_t impl, int32_t rows, int32_t n_out, int32_t k_in, const void* x, const void* w, float* y,
                   void* scratch, size_t scratch_bytes, void* cuda_stream);
 
+/* ---- operators over a paged key/value cache ----
+ * For a server that keeps keys and values in pages: what it has to run between the projections of a layer and its output
+ * projection, for decode steps, draft trees and chunks of prompts, in one ragged batch.  Token-major tensors hold the new tokens
+ * of all sequences one behind the other.  Everything is asynchronous on cuda_stream and on the current device, whose memory every
+ * [device] pointer is.  The calls allocate nothing and keep nothing, so they can be captured into a CUDA graph; a replay reads
+ * lengths, tables and tensors as they are then. */
+
+/* `n_heads` vectors of head_dim adjacent elements for each token: head h of token t starts at data + t * token_stride +
+ * h * head_stride (elements).  Strides of tensors that are read may be zero. */
+typedef struct {
+    void* data;        /* [device] */
+    int64_t token_stride, head_stride;
+    int32_t n_heads;
+} esp_heads;
+
+/* Pages of keys and values: token s of page p of head h starts at p * page_stride + s * token_stride + h * head_stride (elements)
+ * behind k and behind v. */
+typedef struct {
+    void* k;           /* [device] */
+    void* v;           /* [device] */
+    int64_t page_stride, token_stride, head_stride;
+    int32_t n_pages, page_size, n_kv_heads;
+    int32_t head_dim;  /* 32, 64 or 128 */
+    int32_t dtype;     /* as in esp_model_cfg; the token-major tensors have it too */
+} esp_paged_cache;
+
+/* The sequences of one call.  Sequence b has the new tokens q_start[b] .. q_start[b+1] - 1 of the token-major tensors and kv_len[b]
+ * positions with them: new token i stands at position kv_len[b] - n + i, n = q_start[b+1] - q_start[b].  Position p lives in slot
+ * p % page_size of page page_table[b][p / page_size].  A position below 0 (kv_len[b] < n) is padding: nothing is cached
+ * for it, it sees nothing.  Tokens before q_start[0] and from q_start[batch] on are left alone.
+ * The device checks what the host cannot see: a sequence whose q_start leaves 0 .. n_tokens, falls, or spans more than max_new tokens, or
+ * whose kv_len is negative or beyond its table's pages, is left out as a whole; a page number outside 0 .. n_pages - 1 where a
+ * position needs one makes the sequence's results meaningless (no other memory is touched).  Both are recorded in *status. */
+typedef struct {
+    int32_t batch;
+    int32_t max_new;            /* no sequence has more new tokens than this */
+    const int32_t* q_start;     /* [device] [batch + 1] */
+    const int32_t* kv_len;      /* [device] [batch] */
+    const int32_t* page_table;  /* [device] [batch][table_pages], rows table_stride entries apart */
+    int32_t table_pages, table_stride;
+    int32_t* status;            /* [device] or NULL: word that a kernel sets to a device error code when it finds one; only the caller clears it */
+} esp_paged_batch;
+
+/* Rotary positions.  The first rotary_dim elements of a head form rotary_dim / 2 pairs: elements i and i + rotary_dim / 2, or 2i
+ * and 2i + 1 when interleaved.  Pair i of a token at position p turns by p * f_i, and its length is multiplied by `amplitude`; the
+ * other elements stay.  f_i = base^(-2i / rotary_dim) radians, then by `scaling`:
+ *   ESP_ROPE_PLAIN      as it is
+ *   ESP_ROPE_LINEAR     f / factor (position interpolation)
+ *   ESP_ROPE_BASE       base replaced by base * factor^(rotary_dim / (rotary_dim - 2))
+ *   ESP_ROPE_ROTATIONS  with r = original_len * f / 2 pi turns in the original length: f / factor where r < low, f where r > high,
+ *                       between them f * (w + (1 - w) / factor), w = (r - low) / (high - low)
+ *   ESP_ROPE_INDEX      the same with w linear in i instead: 1 up to the pair that turns `high` times in the original length (its index
+ *                       rounded down, at least 0), 0 from the one that turns `low` times on (rounded up, at most rotary_dim - 1) */
+enum { ESP_ROPE_PLAIN = 0, ESP_ROPE_LINEAR = 1, ESP_ROPE_BASE = 2, ESP_ROPE_ROTATIONS = 3, ESP_ROPE_INDEX = 4 };
+#define ESP_ROPE_MAX_DIM 256
+typedef struct {
+    int32_t rotary_dim;   /* even, 2 .. ESP_ROPE_MAX_DIM */
+    int32_t interleaved;  /* 0 or 1 */
+    int32_t scaling;
+    int32_t original_len; /* positions the frequencies were made for (ROTATIONS, INDEX) */
+    float base, factor, low, high, amplitude;
+} esp_rope_cfg;
+
+/* f_i in radians per position: out [host] [rotary_dim / 2].  No GPU is needed. */
+int esp_rope_frequencies(const esp_rope_cfg* rope, double* out);
+
+/* Writes the table that the rotating operators read: the frequencies as 64-bit fractions of a turn, so that the angle of any 32-bit
+ * position is exact to 2^-31 of a turn.  table [device], 16-byte aligned, esp_rope_table_bytes bytes; made once per configuration. */
+int esp_rope_table_bytes(const esp_rope_cfg* rope, size_t* bytes_out);
+int esp_rope_table(const esp_rope_cfg* rope, void* table, size_t table_bytes, void* cuda_stream);
+
+/* Per-head RMSNorm of queries and keys and the rotation of their positions in one pass:
+ *   y = x * gain / sqrt(mean(x^2) + eps) over the head's elements (gain NULL: y = x), then the rotation (rope NULL: none).
+ * q, k and their outputs: n_tokens tokens of heads of head_dim elements, 1 .. ESP_ROPE_MAX_DIM; an output may be its input (same data and strides),
+ * otherwise they do not overlap; either pair may be NULL.  gains [device] [head_dim] in the tensors' dtype; positions [device] [n_tokens], any
+ * 32-bit value.  Arithmetic in fp32, one rounding at the end. */
+int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const esp_heads* q, const esp_heads* k, const void* q_gain, const void* k_gain,
+                     float eps, const esp_rope_cfg* rope, const void* rope_table, const int32_t* positions, const esp_heads* q_out,
+                     const esp_heads* k_out, void* cuda_stream);
+
+/* Appends the new tokens' keys and values to the pages: k normed (k_gain) and rotated as above, v as it is.  With q (may be NULL,
+ * with q_out) the queries are normed and rotated in the same launch; rows of q_out that belong to no position are left alone.
+ * positions [device] [n_tokens] gives the rotation's positions where they are not the slots' (the rows of a draft tree share
+ * positions); NULL: the slot's position.  Two tokens of a call must not share a slot. */
+int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* k, const esp_heads* v,
+                     const esp_heads* q, const void* q_gain, const void* k_gain, float eps, const esp_rope_cfg* rope, const void* rope_table,
+                     const int32_t* positions, const esp_heads* q_out, void* cuda_stream);
+
+/* Attention of the new tokens over the pages, their own keys and values (appended before) among them:
+ *   out = softmax(scale * q k^T) v over the visible positions; query head h reads key/value head h / (n_heads of q / n_kv_heads).
+ * anc NULL: a token at position p sees positions p - window + 1 .. p (window 0: 0 .. p).  anc [device] [n_tokens][2] uint64: a draft tree -- a
+ * token sees every position before its block and the block rows whose bits are set in its mask (max_new <= ESP_MAX_ROWS, window 0; bits of rows
+ * that the block does not have are ignored).  A token that sees nothing gets zeros.  scale 0: 1 / sqrt(head_dim).
+ * lse [device] or NULL: [n_tokens][n_heads of q] fp32, the logarithm of the sum of exp(scale * q k) over the visible positions,
+ * -infinity where there are none.  out must not overlap q.
+ * What a token does not see does not reach its result: slots behind kv_len may hold anything, and an infinite or undefined value reaches
+ * only the tokens that see it.  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);
+ * the same call gives the same bits.
+ * scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
+int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
+int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const uint64_t* anc,
+                        int32_t window, float scale, const esp_heads* out, float* lse, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
+/* The status word of a batch: waits for cuda_stream, copies *status [device] to *device_status_out [host] (may be NULL) and returns ESP_OK
+ * if it is 0, ESP_E_DEVICE otherwise. */
+int esp_paged_status(const int32_t* status, void* cuda_stream, int32_t* device_status_out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,10 +29,12 @@ EXPORTS = ["esp_workspace_bytes", "esp_init", "esp_prefill", "esp_step", "esp_st
            "esp_debug_state", "esp_debug_capture", "esp_debug_set_gemm", "esp_debug_set_layer_kernel", "esp_debug_layer_timeline", "esp_step_profiled", "esp_get_stats",
            "esp_debug_wait_selftest", "esp_debug_gumbel", "esp_free",
            "esp_tree_attention_scratch_bytes", "esp_tree_attention", "esp_tree_attention_status", "esp_tree_attention_static", "esp_gemm_scratch_bytes",
-           "esp_gemm_bf16"]
+           "esp_gemm_bf16",
+           "esp_rope_frequencies", "esp_rope_table_bytes", "esp_rope_table", "esp_qk_norm_rope", "esp_paged_append",
+           "esp_paged_attention_scratch_bytes", "esp_paged_attention", "esp_paged_status"]
 
 __all__ = ["EspError", "esp_model_cfg", "esp_spec_cfg", "esp_weights", "esp_stats", "load_library", "model_cfg",
-           "spec_cfg", "Handle", "ESP_MAX_ROWS", "ESP_MAX_PROBES", "ESP_MAX_KPRIME", "ESP_PREFILL_CHUNK", "ESP_MAX_UNREAD_STEPS", "ESP_STATIC_SCRATCH_BYTES", "EXPORTS", "LIB_PATH", "KINDS"] + EXPORTS
+           "spec_cfg", "Handle", "esp_heads", "esp_paged_cache", "esp_paged_batch", "esp_rope_cfg", "rope_cfg", "PagedCache", "PagedBatch", "ESP_ROPE_MAX_DIM", "ESP_MAX_ROWS", "ESP_MAX_PROBES", "ESP_MAX_KPRIME", "ESP_PREFILL_CHUNK", "ESP_MAX_UNREAD_STEPS", "ESP_STATIC_SCRATCH_BYTES", "EXPORTS", "LIB_PATH", "KINDS"] + EXPORTS
 
 
 class EspError(RuntimeError):
@@ -69,7 +71,38 @@ class esp_stats(ctypes.Structure):
                 ("device_error", ctypes.c_int32), ("kernels_per_step", ctypes.c_int32), ("rows_hist", ctypes.c_int64 * 4)]
 
 
+class esp_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+
+class esp_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("page_stride", "token_stride", "head_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class esp_paged_batch(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_new", ctypes.c_int32), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("table_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("status", ctypes.c_void_p)]
+
+
+class esp_rope_cfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rotary_dim", "interleaved", "scaling", "original_len")] + \
+               [(n, ctypes.c_float) for n in ("base", "factor", "low", "high", "amplitude")]
+
+
 _lib = None
+_P, _I, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+# (with the types declared once, a call hands over plain numbers: a call per layer has no time for wrapping each argument)
+_ARGTYPES = {
+    "esp_rope_frequencies": [_P, _P],
+    "esp_rope_table_bytes": [_P, _P],
+    "esp_rope_table": [_P, _P, ctypes.c_size_t, _P],
+    "esp_qk_norm_rope": [_I, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P, _P],
+    "esp_paged_append": [_I, _P, _P, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P],
+    "esp_paged_attention_scratch_bytes": [_I, _I, _P],
+    "esp_paged_attention": [_I, _P, _P, _P, _P, _I, _F, _P, _P, _P, ctypes.c_size_t, _P],
+    "esp_paged_status": [_P, _P, _P],
+}
 
 
 def load_library(path: Optional[str] = None):
@@ -83,6 +116,8 @@ def load_library(path: Optional[str] = None):
         lib = ctypes.CDLL(p)
         for name in EXPORTS:
             getattr(lib, name).restype = None if name == "esp_free" else ctypes.c_int
+        for name, types in _ARGTYPES.items():
+            getattr(lib, name).argtypes = types
         if path is not None:
             return lib
         _lib = lib
@@ -276,6 +311,183 @@ def esp_gemm_bf16(impl: int, rows: int, n_out: int, k_in: int, x, w, y, scratch,
     _check(load_library().esp_gemm_bf16(ctypes.c_int32(impl), ctypes.c_int32(rows), ctypes.c_int32(n_out), ctypes.c_int32(k_in),
                                         _vp(x), _vp(w), _vp(y), _vp(scratch), ctypes.c_size_t(scratch_bytes), _vp(stream)),
            "esp_gemm_bf16")
+
+
+# ---------------------------------------------------------------- operators over a paged key/value cache
+# These take the tensors themselves ([tokens, heads, head_dim], the last dimension dense) and read shapes, strides and types off them; what does not
+# fit together raises EspError(ESP_E_ARG) before the library is called.
+ESP_ROPE_MAX_DIM = 256
+ROPE_SCALINGS = ("none", "linear", "base", "rotations", "index")
+
+
+def rope_cfg(rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, original_len: int = 8192,
+             low: float = 1.0, high: Optional[float] = None, amplitude: float = 1.0) -> esp_rope_cfg:
+    """esp_rope_cfg.  scaling: none, linear, base, rotations or index (see esp.h); high: turns above which a pair is kept, by default 4 for
+    "rotations" and 32 for "index"."""
+    if scaling not in ROPE_SCALINGS:
+        raise EspError(-1, f"rope_cfg(scaling={scaling!r})")
+    if high is None:
+        high = 32.0 if scaling == "index" else 4.0
+    return esp_rope_cfg(int(rotary_dim), int(bool(interleaved)), ROPE_SCALINGS.index(scaling), int(original_len), base, factor, low, high, amplitude)
+
+
+def esp_rope_frequencies(rope: esp_rope_cfg) -> np.ndarray:
+    """Radians per position of every rotated pair (fp64)."""
+    out = np.zeros(ESP_ROPE_MAX_DIM // 2, np.float64)
+    _check(load_library().esp_rope_frequencies(ctypes.byref(rope), out.ctypes.data), "esp_rope_frequencies")
+    return out[:rope.rotary_dim // 2].copy()
+
+
+def esp_rope_table_bytes(rope: esp_rope_cfg) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().esp_rope_table_bytes(ctypes.byref(rope), ctypes.byref(out)), "esp_rope_table_bytes")
+    return out.value
+
+
+def _need(ok: bool, where: str, what: str):
+    if not ok:
+        raise EspError(-8, f"{where} ({what})")
+
+
+def _device(where: str) -> int:
+    import torch
+    _need(torch.cuda.is_available(), where, "no CUDA device")
+    return torch.cuda.current_device()
+
+
+def esp_rope_table(rope: esp_rope_cfg, table, stream=None):
+    """Fills `table` (a CUDA tensor of esp_rope_table_bytes bytes or more), once per configuration."""
+    _need(table.get_device() == _device("esp_rope_table") and table.is_contiguous(), "esp_rope_table", "table: another device, or not dense")
+    _check(load_library().esp_rope_table(ctypes.byref(rope), table.data_ptr(), table.numel() * table.element_size(), _stream(stream)), "esp_rope_table")
+
+
+def _stream(stream):
+    return getattr(stream, "cuda_stream", stream)
+
+
+_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1}
+
+
+def _heads(x, like, where: str, name: str) -> esp_heads:
+    """x [tokens, heads, head_dim] as esp_heads; `like`: (tokens, head_dim, dtype, device) it has to have."""
+    shape, stride = x.shape, x.stride()
+    if not (len(shape) == 3 and shape[0] == like[0] and shape[2] == like[1] and (stride[2] == 1 or shape[2] == 1) and x.dtype == like[2] and
+            x.get_device() == like[3]):
+        raise EspError(-8, f"{where} ({name}: {tuple(shape)} {x.dtype} on {x.device}, strides {stride}; wanted [{like[0]}, heads, {like[1]}] "
+                           f"{like[2]} on device {like[3]}, last dimension dense)")
+    return esp_heads(x.data_ptr(), stride[0], stride[1], shape[1])
+
+
+def _vector(x, n: int, dtype, device: int, where: str, name: str):
+    """Address of a dense tensor of n elements (None: NULL)."""
+    if x is None:
+        return None
+    if not (x.numel() == n and x.is_contiguous() and str(x.dtype) in (dtype if isinstance(dtype, tuple) else (dtype,)) and x.get_device() == device):
+        raise EspError(-8, f"{where} ({name}: {tuple(x.shape)} {x.dtype} on {x.device}; wanted {n} dense elements of {dtype} on device {device})")
+    return x.data_ptr()
+
+
+class PagedCache:
+    """Pages of keys and values.  k, v [pages, kv_heads, page_size, head_dim] (order "head") or [pages, page_size, kv_heads, head_dim] (order "token"),
+    fp32 or bf16, any strides that both share with a dense last dimension.  Keeps the tensors alive."""
+
+    def __init__(self, k, v, order: str = "head"):
+        where = "PagedCache"
+        _need(order in ("head", "token"), where, f"order {order!r}")
+        _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device, where, "k and v differ")
+        _need(str(k.dtype) in _DTYPES and (k.stride(3) == 1 or k.shape[3] == 1), where, "type, or last dimension not dense")
+        h, s = (1, 2) if order == "head" else (2, 1)
+        self.k, self.v, self.order = k, v, order
+        self.dtype, self.device, self.head_dim = k.dtype, k.get_device(), k.shape[3]
+        self.c = esp_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(s), k.stride(h), k.shape[0], k.shape[s], k.shape[h], k.shape[3],
+                                 _DTYPES[str(k.dtype)])
+        self.ref = ctypes.byref(self.c)
+
+
+class PagedBatch:
+    """The sequences of a call: q_start [batch + 1], kv_len [batch], page_table [batch, pages] int32 on the GPU (their contents are read when a call runs),
+    max_new: most new tokens of a sequence, status: an int32 tensor of one element or None.  Keeps the tensors alive."""
+
+    def __init__(self, q_start, kv_len, page_table, max_new: int, status=None):
+        where = "PagedBatch"
+        n = kv_len.numel()
+        _need(page_table.dim() == 2 and page_table.shape[0] == n and q_start.numel() == n + 1, where, "q_start, kv_len and page_table do not fit together")
+        for t in (q_start, kv_len, status):
+            _need(t is None or (str(t.dtype) == "torch.int32" and t.is_contiguous() and t.get_device() == page_table.get_device()), where, "int32, dense, one device")
+        _need(str(page_table.dtype) == "torch.int32" and (page_table.stride(1) == 1 or page_table.shape[1] <= 1) and
+              (page_table.stride(0) >= page_table.shape[1] or n <= 1), where, "page_table: int32 rows")
+        _need(status is None or status.numel() >= 1, where, "status")
+        self.q_start, self.kv_len, self.page_table, self.status = q_start, kv_len, page_table, status
+        self.device = page_table.get_device()
+        self.c = esp_paged_batch(n, int(max_new), q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
+                                 page_table.stride(0) if n > 1 else page_table.shape[1],
+                                 None if status is None else status.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def esp_qk_norm_rope(q, k, q_out, k_out, rope: Optional[esp_rope_cfg] = None, rope_table=None, positions=None, q_gain=None, k_gain=None, eps: float = 1e-6,
+                     stream=None):
+    """Per-head RMSNorm (where a gain is given) and rotation (where `rope` is) of q and k into q_out and k_out; one pair may be None."""
+    where = "esp_qk_norm_rope"
+    x = q if q is not None else k
+    _need(x is not None and x.dim() == 3 and str(x.dtype) in _DTYPES, where, "q or k [tokens, heads, head_dim], fp32 or bf16")
+    like = (x.shape[0], x.shape[2], x.dtype, _device(where))
+    views = [None if t is None else ctypes.byref(_heads(t, like, where, n)) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    dt = str(x.dtype)
+    _check(load_library().esp_qk_norm_rope(
+        _DTYPES[dt], like[0], like[1], views[0], views[1], _vector(q_gain, like[1], dt, like[3], where, "q_gain"),
+        _vector(k_gain, like[1], dt, like[3], where, "k_gain"), eps, None if rope is None else ctypes.byref(rope),
+        _table(rope, rope_table, like[3], where), _vector(positions, like[0], "torch.int32", like[3], where, "positions"), views[2], views[3], _stream(stream)), where)
+
+
+def _table(rope, table, device: int, where: str):
+    if rope is None or table is None:
+        return None
+    _need(table.get_device() == device and table.numel() * table.element_size() >= 4 * rope.rotary_dim, where, "rope_table")
+    return table.data_ptr()
+
+
+def esp_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Optional[esp_rope_cfg] = None, rope_table=None, positions=None, k_gain=None, q=None,
+                     q_out=None, q_gain=None, eps: float = 1e-6, stream=None):
+    """Appends the new tokens' k (normed and rotated as asked) and v to the pages; with q, norms and rotates the queries into q_out in the same launch."""
+    where = "esp_paged_append"
+    dev = _device(where)
+    _need(cache.device == dev and batch.device == dev, where, "cache and batch on the current device")
+    like = (k.shape[0], cache.head_dim, cache.dtype, dev)
+    views = [None if t is None else ctypes.byref(_heads(t, like, where, n)) for t, n in ((k, "k"), (v, "v"), (q, "q"), (q_out, "q_out"))]
+    dt = str(cache.dtype)
+    _check(load_library().esp_paged_append(
+        like[0], cache.ref, batch.ref, views[0], views[1], views[2], _vector(q_gain, like[1], dt, dev, where, "q_gain"),
+        _vector(k_gain, like[1], dt, dev, where, "k_gain"), eps, None if rope is None else ctypes.byref(rope), _table(rope, rope_table, dev, where),
+        _vector(positions, like[0], "torch.int32", dev, where, "positions"), views[3], _stream(stream)), where)
+
+
+def esp_paged_attention_scratch_bytes(n_q_heads: int, head_dim: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().esp_paged_attention_scratch_bytes(n_q_heads, head_dim, ctypes.byref(out)), "esp_paged_attention_scratch_bytes")
+    return out.value
+
+
+def esp_paged_attention(cache: PagedCache, batch: PagedBatch, q, out, scratch, scratch_bytes: int, anc=None, window: int = 0, scale: float = 0.0, lse=None,
+                        stream=None):
+    """Attention of the new tokens over the pages into `out`: causal, with a window, or with the ancestor masks `anc` [tokens, 2] (64-bit words) of draft trees."""
+    where = "esp_paged_attention"
+    dev = _device(where)
+    _need(cache.device == dev and batch.device == dev and scratch.get_device() == dev, where, "cache, batch and scratch on the current device")
+    _need(scratch.numel() * scratch.element_size() >= scratch_bytes, where, "scratch_bytes")
+    like = (q.shape[0], cache.head_dim, cache.dtype, dev)
+    hq, ho = _heads(q, like, where, "q"), _heads(out, like, where, "out")
+    _check(load_library().esp_paged_attention(
+        like[0], cache.ref, batch.ref, ctypes.byref(hq), _vector(anc, 2 * like[0], ("torch.int64", "torch.uint64"), dev, where, "anc"), window, scale,
+        ctypes.byref(ho), _vector(lse, like[0] * hq.n_heads, "torch.float32", dev, where, "lse"), scratch.data_ptr(), scratch_bytes, _stream(stream)), where)
+
+
+def esp_paged_status(batch: PagedBatch, stream=None) -> int:
+    """The batch's status word (0); raises EspError(ESP_E_DEVICE) if a kernel has set it."""
+    _need(batch.status is not None, "esp_paged_status", "the batch has no status word")
+    st = ctypes.c_int32(0)
+    _check(load_library().esp_paged_status(batch.status.data_ptr(), _stream(stream), ctypes.byref(st)), "esp_paged_status")
+    return st.value
 
 
 # ---------------------------------------------------------------- convenience: a handle that keeps its tensors alive

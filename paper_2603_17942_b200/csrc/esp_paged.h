@@ -1,0 +1,65 @@
+// Operators over a paged key/value cache: what their kernels are given, and the launches behind the C entry points.
+#pragma once
+
+#include "esp_common.cuh"
+
+namespace esp {
+
+struct HeadsView {      // as esp_heads; p NULL: absent
+    void* p;
+    long long tok, head;
+    int32_t n;
+};
+
+// Where token s of page p of head h lives: p * page + s * tok + h * head elements behind k and v.
+struct PagesView {
+    void *k, *v;
+    long long page, tok, head;
+    int32_t n_pages, page_size;
+};
+
+struct SeqTable {
+    const int32_t *q_start, *kv_len, *table;
+    int32_t batch, table_stride, max_new, n_tokens;
+    int32_t kv_cap;     // positions a row of the table can hold
+    int32_t* status;
+};
+
+struct NormRopeArgs {
+    HeadsView q, k, v, q_out, k_out;
+    const void *q_gain, *k_gain;
+    const uint64_t* freq;        // [pairs] fractions of a turn per position, 2^64 = one turn
+    const int32_t* positions;    // NULL: the slot's position (append)
+    int32_t n_tokens, D, pairs, interleaved;
+    float eps, amplitude;
+    PagesView pages;             // append: where k and v go
+    SeqTable seq;
+    int32_t append;
+};
+
+struct PagedAttnArgs {
+    HeadsView q, out;
+    float* lse;
+    PagesView pages;
+    SeqTable seq;
+    const unsigned long long* anc;
+    int32_t Hq, Hkv, group, D, window;
+    float scale_log2;
+    int32_t rows;           // tokens of a tile: rows * group (token, head) pairs
+    int32_t pairs;          // pairs of a tile's partial in the scratch
+    int32_t n_cta;          // CTAs the work is dealt to
+    int32_t vec;            // CUDA-core kernel: rows can be read four elements at a time
+    float* part_o;          // [n_cta][2][pairs][D] split partials: weighted values, not divided by the sum
+    float2* part_ml;        // [n_cta][2][pairs] their (maximum in the log2 domain, sum)
+};
+
+// Partials a launch may need at most: two tiles of 256 pairs for each of 148 CTAs, or as much in smaller tiles.
+constexpr int PAGED_MAX_PAIRS = 256;
+constexpr int PAGED_MAX_CTAS = 148;
+
+int launch_norm_rope(int dtype, const NormRopeArgs& a, cudaStream_t s);
+void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStream_t s);
+int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s);
+int launch_paged_merge(int dtype, const PagedAttnArgs& a, int chunk, int min_units, cudaStream_t s);
+
+}  // namespace esp
