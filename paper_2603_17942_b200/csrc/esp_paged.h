@@ -60,6 +60,8 @@ constexpr int PAGED_MAX_CTAS = 148;
 int launch_norm_rope(int dtype, const NormRopeArgs& a, cudaStream_t s);
 void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStream_t s);
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s);
+bool paged_tc_supported(int dtype, const PagedAttnArgs& a);
+int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s);
 int launch_paged_merge(int dtype, const PagedAttnArgs& a, int chunk, int min_units, cudaStream_t s);
 
 }  // namespace esp

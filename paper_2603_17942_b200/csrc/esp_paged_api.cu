@@ -265,7 +265,8 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     };
     a.vec = by4(a.q.p, a.q.tok, a.q.head, 0) && by4(a.pages.k, a.pages.page, a.pages.tok, a.pages.head) && by4(a.pages.v, 0, 0, 0);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    if (launch_paged_simt(cache->dtype, a, n_sm, s)) return ESP_E_CUDA;
+    const int rc = paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s) : launch_paged_simt(cache->dtype, a, n_sm, s);
+    if (rc) return ESP_E_CUDA;
     return cuda_ok(cudaGetLastError());
 }
 

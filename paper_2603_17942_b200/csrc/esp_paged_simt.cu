@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
     constexpr int PR = MP / 16;                       // pairs of a thread
     constexpr int DV = D >= 64 ? D / 64 : 1;          // float4 columns of a thread (D = 32: the first eight tx have one)
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    pdl_launch_dependents();
     if (!deal<CK, false>(a, blockIdx.x, 1, &sm.deal)) return;
     Cursor c = sm.deal.at;
     const long long total = sm.deal.total, begin = sm.deal.unit, end = cta_begin(total, sm.deal.ctas, blockIdx.x + 1);
@@ -308,8 +309,7 @@ int run_merge_d(const PagedAttnArgs& a, int min_units, cudaStream_t s) {
 
 int launch_paged_merge(int dtype, const PagedAttnArgs& a, int chunk, int min_units, cudaStream_t s) {
     if (dtype == 0) return run_merge_d<float, CK>(a, min_units, s);
-    if (chunk == 64) return run_merge_d<__nv_bfloat16, 64>(a, min_units, s);
-    return -1;
+    return chunk == 64 ? run_merge_d<__nv_bfloat16, 64>(a, min_units, s) : run_merge_d<__nv_bfloat16, 128>(a, min_units, s);
 }
 
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {

@@ -1,0 +1,509 @@
+// Attention over pages on the Blackwell tensor cores: bf16, heads of 64 or 128, blocks of several tokens.
+//
+// A CTA takes tiles of up to 256 (token, query head) pairs that share a KV head, as two subtiles of 128, and walks their keys 128 at
+// a time.  Keys and values come by TMA, page by page (boxes of as many tokens as page size and chunk have in common), into a ring of
+// stages that both subtiles share:
+//   S_s = Q_s K^T    tcgen05.mma, both operands K-major in shared memory, S_s (128 x 128 fp32) in tensor memory;
+//   softmax          one thread per pair (= tensor-memory lane): mask, running maximum and sum in the log2 domain, P as bf16 back over S_s;
+//   O_s += P_s V     tcgen05.mma with P_s as the tensor-memory operand, V MN-major as the pages have it; O_s stays in tensor memory.
+//                    The reference of the exponentials follows the maximum lazily: it moves, and O_s is rescaled, only after a growth of 2^8.
+// The tensor cores work on one subtile while the softmax of the other runs; products are issued in the order P_0 V, Q_0 K^T (next chunk),
+// P_1 V, Q_1 K^T, and run in that order, so S_s may be overwritten as soon as the P_s V that read P_s from it has been issued, and S_s
+// arriving says that O_s is complete.
+// Weights of keys that a pair does not see are zero, but zero times an infinite value is no number: in chunks that not every pair sees
+// as a whole, two warps set values that are no finite numbers to zero in shared memory before the product, and the pairs that see them get them
+// when the tile is finished.
+// Roles: warp 0 TMA, warp 1 issues the products, warps 2 and 3 look after the values, warps 4-7 and 8-11 softmax and output of a
+// subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
+#include <string.h>
+
+#include "esp_paged.cuh"
+#include "esp_tc.cuh"
+
+namespace esp {
+
+namespace {
+
+using namespace tc;
+using namespace paged;
+
+constexpr int CK = 128;                   // keys per chunk
+constexpr int SUB = 128;                  // pairs per subtile
+constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
+constexpr int THREADS = 384;
+constexpr int TMEM_COLS = 512;            // S0, S1, O0, O1: 128 columns each
+constexpr int ODD_RING = 8;               // tiles whose note on odd values is kept: more than the ring's stages can hold values of
+
+template <int D>
+struct Cfg {
+    static constexpr int HALVES = D / 64;
+    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;         // 128 rows of a head
+    static constexpr int STAGES = D == 128 ? 5 : 8;
+    static constexpr int OFF_KV = 2 * TILE_BYTES;
+    static constexpr int OFF_BAR = OFF_KV + STAGES * TILE_BYTES;
+    static constexpr int SMEM = 1024 + OFF_BAR + 512;
+    // kind::f16 instruction descriptors: D = f32, A = B = bf16, M = 128; Q K^T: N = 128 keys; P V: N = D, V is MN-major
+    static constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+    static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+    // keys and values take stages in turn: with an odd number of stages a stage holds values on every other pass
+    __device__ static uint32_t v_parity(uint32_t it) { return (STAGES % 2 ? it / STAGES / 2 : it / STAGES) & 1; }
+};
+
+struct TcParams {
+    CUtensorMap map_q;        // [tokens][heads][D], box 64 x group x rows of a subtile
+    CUtensorMap map_k;        // [pages][heads][slots][D], box 64 x box_rows
+    CUtensorMap map_v;
+    PagedAttnArgs a;
+    int32_t box_rows, sub_rows, out_vec;
+};
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+// 2^x as one special-function instruction (relative error about 2^-22, far below the rounding of the weight to bf16)
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// A chunk that some pair of the tile does not see as a whole (the last one of the cache, the diagonal, the window's edge, the tree).
+__device__ __forceinline__ bool is_edge(const PagedAttnArgs& a, const Cursor& c, int p0) {
+    const int L = c.s.kv - c.s.n;
+    const int hi = a.anc ? L : L + c.x.r0 + 1;
+    const int lo = a.window > 0 ? L + c.x.r0 + c.x.nr - a.window : 0;
+    return p0 + CK > hi || p0 < lo;
+}
+// the 128 keys of the chunk at p0 as bits: which of them the pair sees
+__device__ __forceinline__ void chunk_bits(const RowMask& m, int p0, int L, int n, uint32_t (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int lo = max(m.lo - p0 - 32 * i, 0), hi = min(m.hi - p0 - 32 * i, 32);
+        w[i] = hi > lo ? (hi - lo >= 32 ? 0xffffffffu : ((1u << (hi - lo)) - 1u) << lo) : 0u;
+    }
+    if (m.b0 | m.b1) {
+        // block row j stands at position L + j: bit j goes to bit j + L - p0
+        unsigned long long b0 = m.b0, b1 = m.b1;
+        if (n < 64) { b0 &= (1ull << n) - 1ull; b1 = 0; }
+        else if (n < 128) b1 &= (1ull << (n - 64)) - 1ull;
+        const int up = L - p0;
+        if (up >= 64 && up < 128) { b1 = b0 << (up - 64); b0 = 0; }
+        else if (up > 0 && up < 64) { b1 = (b1 << up) | (b0 >> (64 - up)); b0 <<= up; }
+        else if (up < 0 && up > -64) { b0 = (b0 >> -up) | (b1 << (64 + up)); b1 >>= -up; }
+        else if (up <= -64 && up > -128) { b0 = b1 >> (-up - 64); b1 = 0; }
+        else if (up != 0) b0 = b1 = 0;
+        w[0] |= (uint32_t)b0; w[1] |= (uint32_t)(b0 >> 32); w[2] |= (uint32_t)b1; w[3] |= (uint32_t)(b1 >> 32);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__ TcParams p) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ Deal s_deal;
+    __shared__ int s_odd[2][ODD_RING];     // [warp 2, 3] a value that some pair sees is no finite number
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);   // [STAGES] keys or values have landed
+    uint64_t* empty = full + C::STAGES;                                // [STAGES] their products have completed
+    uint64_t* v_ok = empty + C::STAGES;                                // [STAGES] the values have been looked after
+    uint64_t* s_full = v_ok + C::STAGES;                               // [2] scores of a subtile's chunk
+    uint64_t* p_ready = s_full + 2;                                    // [2] its weights
+    uint64_t* o_full = p_ready + 2;                                    // [2] the piece's last P V has completed
+    uint64_t* o_free = o_full + 2;                                     // [2] the accumulator has been read
+    uint64_t* q_full = o_free + 2;
+    uint64_t* q_empty = q_full + 1;
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(q_empty + 1);
+    volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+
+    const PagedAttnArgs& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&p.map_k);
+        prefetch_tensormap(&p.map_v);
+        prefetch_tensormap(&p.map_q);
+        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&v_ok[i], 2); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        *s_abort = 0;
+        for (int i = 0; i < ODD_RING; ++i) s_odd[0][i] = s_odd[1][i] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_launch_dependents();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    const bool any = deal<CK, false>(a, blockIdx.x, 1, &s_deal);
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *s_tmem;
+    unsigned char* sQ = smem;
+    unsigned char* sKV = smem + C::OFF_KV;
+    const long long begin = any ? s_deal.unit : 0, end = any ? cta_begin(s_deal.total, s_deal.ctas, blockIdx.x + 1) : 0;
+
+    if (warp == 0) {
+        // ---------------- TMA: keys and values of a chunk in turn; a lane per box
+        const int n_boxes = CK / p.box_rows;
+        const int box = lane % n_boxes, half = lane / n_boxes;
+        const bool active = half < C::HALVES;
+        uint32_t it = 0, n_it = 0;      // stages filled, pieces
+        bool ok = true;
+        Cursor c = s_deal.at;
+        for (long long u = begin; u < end && ok; ++n_it) {
+            const Piece pc = make_piece(c, begin, u, end);
+            for (int j = 0; j < pc.n && ok; ++j) {
+                const int pos = (pc.c0 + j) * CK + box * p.box_rows;
+                int page = a.pages.n_pages, slot = 0;       // a page that there is not reads as zeros
+                if (active && pos < c.s.kv) {
+                    const int index = pos / a.pages.page_size;
+                    const int pg = load_page(a.seq, a.pages, c.b, index);
+                    if (pg >= 0) page = pg;
+                    slot = pos - index * a.pages.page_size;
+                }
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++it) {
+                    const int st = it % C::STAGES;
+                    if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], ((it / C::STAGES) & 1) ^ 1, s_abort))) { ok = false; break; }
+                    if (lane == 0) mbar_expect_tx(&full[st], C::TILE_BYTES);
+                    __syncwarp();
+                    if (active) tma_load_4d(sKV + st * C::TILE_BYTES + half * HALF_BYTES + box * p.box_rows * 128, kv ? &p.map_v : &p.map_k, half * 64, slot, c.kvh, page, &full[st]);
+                    if (kv == 0 && j == 0) {                // the piece's queries behind its first keys
+                        if (!__all_sync(0xffffffffu, mbar_wait(q_empty, (n_it & 1) ^ 1, s_abort))) { ok = false; break; }
+                        if (lane == 0) {
+                            const int subs = c.x.nr > p.sub_rows ? 2 : 1;
+                            mbar_expect_tx(q_full, subs * C::HALVES * p.sub_rows * a.group * 128);
+                            for (int s = 0; s < subs; ++s)
+                                for (int h = 0; h < C::HALVES; ++h)
+                                    tma_load_3d(sQ + s * C::TILE_BYTES + h * HALF_BYTES, &p.map_q, h * 64, c.kvh * a.group, c.s.start + c.x.r0 + s * p.sub_rows, q_full);
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+            u += pc.n;
+            if (u < end) next_tile<CK>(a, c);
+        }
+        if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
+    } else if (warp == 1) {
+        // ---------------- products: the warp walks its loop as a whole, one lane issues
+        const bool leader{elect_lane()};
+        const uint32_t q_addr = smem_u32(sQ), kv_addr = smem_u32(sKV);
+        uint32_t it = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // stages used, pieces, chunks and pieces of each subtile
+        bool ok = true;
+        Cursor c = s_deal.at;
+        for (long long u = begin; u < end && ok; ++n_it) {
+            const Piece pc = make_piece(c, begin, u, end);
+            const int subs = c.x.nr > p.sub_rows ? 2 : 1;
+            auto issue_qk = [&](int s, int st) {
+                const uint32_t k_addr = kv_addr + st * C::TILE_BYTES, qa = q_addr + s * C::TILE_BYTES;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
+                    if (leader) umma(tmem_base + s * 128, smem_desc(qa + off, 16), smem_desc(k_addr + off, 16), C::IDESC_QK, kk > 0 ? 1u : 0u);
+                }
+                if (leader) umma_commit(&s_full[s]);
+            };
+            ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&full[it % C::STAGES], (it / C::STAGES) & 1, s_abort));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int s = 0; s < subs; ++s) issue_qk(s, it % C::STAGES);
+            if (leader) umma_commit(&empty[it % C::STAGES]);
+            if (leader && pc.n == 1) umma_commit(q_empty);
+            for (int j = 0; j < pc.n && ok; ++j, it += 2) {
+                const uint32_t vt = it + 1, kt = it + 2;                        // this chunk's values, the next one's keys
+                for (int s = 0; s < subs && ok; ++s) {
+                    const uint32_t g = s ? g1 : g0, np = s ? pieces1 : pieces0;
+                    ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[s], (g + j) & 1, s_abort) &&
+                                                     (s > 0 || mbar_wait(&v_ok[vt % C::STAGES], C::v_parity(vt), s_abort)) &&
+                                                     (j > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t v_addr = kv_addr + (vt % C::STAGES) * C::TILE_BYTES;
+#pragma unroll
+                    for (int kk = 0; kk < CK / 16; ++kk)
+                        if (leader) umma_ta(tmem_base + 256 + s * 128, tmem_base + s * 128 + kk * 8, smem_desc(v_addr + kk * 16 * 128, HALF_BYTES), C::IDESC_PV,
+                                            (j > 0 || kk > 0) ? 1u : 0u);
+                    if (leader && s == subs - 1) umma_commit(&empty[vt % C::STAGES]);
+                    if (leader && j == pc.n - 1) umma_commit(&o_full[s]);
+                    if (j + 1 < pc.n) {
+                        if (s == 0) {
+                            ok = __all_sync(0xffffffffu, mbar_wait(&full[kt % C::STAGES], (kt / C::STAGES) & 1, s_abort));
+                            if (!ok) break;
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        }
+                        issue_qk(s, kt % C::STAGES);
+                        if (leader && s == subs - 1) umma_commit(&empty[kt % C::STAGES]);
+                        if (leader && s == subs - 1 && j + 2 == pc.n) umma_commit(q_empty);
+                    }
+                }
+            }
+            g0 += pc.n;
+            ++pieces0;
+            if (subs == 2) { g1 += pc.n; ++pieces1; }
+            u += pc.n;
+            if (u < end) next_tile<CK>(a, c);
+        }
+        if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
+    } else if (warp < 4) {
+        // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
+        uint32_t it = 1, n_it = 0;
+        bool ok = true;
+        Cursor c = s_deal.at;
+        for (long long u = begin; u < end && ok; ++n_it) {
+            const Piece pc = make_piece(c, begin, u, end);
+            if (lane == 0) s_odd[warp - 2][(n_it + 1) % ODD_RING] = 0;
+            for (int j = 0; j < pc.n; ++j, it += 2) {
+                const int st = it % C::STAGES, p0 = (pc.c0 + j) * CK;
+                if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (it / C::STAGES) & 1, s_abort))) { ok = false; break; }
+                if (is_edge(a, c, p0)) {
+                    // a lane takes every other row of 16 bytes; its key follows from the row
+                    bool odd = false;
+                    for (int i = (warp - 2) * 32 + lane; i < C::TILE_BYTES / 16; i += 64) {
+                        uint4* at = reinterpret_cast<uint4*>(sKV + st * C::TILE_BYTES) + i;
+                        uint4 x = *at;
+                        uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+                        bool here = false;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; here = true; }
+                            if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0x0000ffffu; here = true; }
+                        }
+                        if (here) {
+                            *at = x;
+                            odd = odd || p0 + ((i >> 3) & 127) < c.s.kv;
+                        }
+                    }
+                    if (odd) s_odd[warp - 2][n_it % ODD_RING] = 1;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive(&v_ok[st]);
+            }
+            u += pc.n;
+            if (u < end) next_tile<CK>(a, c);
+        }
+        if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
+    } else {
+        // ---------------- softmax and output of subtile sub: a thread per pair
+        const int sub = (warp - 4) >> 2, q4 = warp & 3, row = q4 * 32 + lane;
+        const uint32_t s_addr = tmem_base + ((uint32_t)(q4 * 32) << 16) + sub * 128, o_addr = s_addr + 256;
+        uint32_t g = 0, np = 0, n_it = 0;
+        bool ok = true;
+        Cursor c = s_deal.at;
+        for (long long u = begin; u < end && ok; ++n_it) {
+            const Piece pc = make_piece(c, begin, u, end);
+            const int L = c.s.kv - c.s.n;
+            if (sub == 0 || c.x.nr > p.sub_rows) {
+                const int pair = sub * p.sub_rows * a.group + row;               // of the tile
+                const bool valid = row < p.sub_rows * a.group && pair < c.x.nr * a.group;
+                const int trow = pair / a.group, head = c.kvh * a.group + pair - trow * a.group;
+                RowMask mask;
+                mask.lo = mask.hi = 0;
+                mask.b0 = mask.b1 = 0;
+                if (valid) mask = row_mask(a, c.s, c.x.r0 + trow);
+                const bool live = __any_sync(0xffffffffu, valid);
+                float m_run = -INFINITY, l_run = 0.f;
+                for (int j = 0; j < pc.n; ++j, ++g) {
+                    // (a wait that fails takes the whole warp out: the accesses to tensor memory are warp-wide)
+                    if (!__all_sync(0xffffffffu, mbar_wait(&s_full[sub], g & 1, s_abort))) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (live) {
+                        const int p0 = (pc.c0 + j) * CK;
+                        uint32_t sv[128];
+                        tmem_ld128(s_addr, sv);
+                        if (!__all_sync(0xffffffffu, p0 >= mask.lo && p0 + CK <= mask.hi)) {
+                            uint32_t w[4];
+                            chunk_bits(mask, p0, L, c.s.n, w);
+#pragma unroll
+                            for (int i = 0; i < 128; ++i) sv[i] = (w[i >> 5] >> (i & 31)) & 1u ? sv[i] : 0xff800000u;
+                        }
+                        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int i = 0; i < 128; i += 8)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) m4[e] = fmaxf(fmaxf(m4[e], __uint_as_float(sv[i + 2 * e])), __uint_as_float(sv[i + 2 * e + 1]));
+                        const float cmax = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
+                        const bool move = m_run == -INFINITY ? cmax != -INFINITY : cmax - m_run > 8.f;
+                        const float m_new = move ? cmax : m_run;
+                        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+                        if (j > 0 && __any_sync(0xffffffffu, move)) {
+                            // O <- O * 2^(old - new); S arriving said that O is complete
+                            const float alpha = exp2f(m_run - m_use);
+#pragma unroll
+                            for (int b = 0; b < D / 32; ++b) {
+                                uint32_t o[32];
+                                tmem_ld32(o_addr + b * 32, o);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st32(o_addr + b * 32, o);
+                            }
+                            l_run *= alpha;
+                        }
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int b = 0; b < 4; b += 2) {
+                            uint32_t pk[32];
+#pragma unroll
+                            for (int i = 0; i < 64; i += 2) {
+                                const float p0_ = ex2(fmaf(__uint_as_float(sv[b * 32 + i]), a.scale_log2, -m_use));
+                                const float p1_ = ex2(fmaf(__uint_as_float(sv[b * 32 + i + 1]), a.scale_log2, -m_use));
+                                sum[i & 2] += p0_;
+                                sum[(i & 2) + 1] += p1_;
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(p0_, p1_);
+                                pk[i >> 1] = *reinterpret_cast<const uint32_t*>(&b2);
+                            }
+                            tmem_st32(s_addr + b * 16, pk);
+                        }
+                        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        m_run = m_new;
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_ready[sub]);
+                }
+                if (!ok) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(&o_full[sub], np & 1, s_abort))) { ok = false; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                ++np;
+                if (live) {
+                    const bool odd = (*reinterpret_cast<volatile int*>(&s_odd[0][n_it % ODD_RING]) | *reinterpret_cast<volatile int*>(&s_odd[1][n_it % ODD_RING])) != 0;
+                    const int token = c.s.start + c.x.r0 + trow;
+                    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+                    const size_t at = ((size_t)blockIdx.x * 2 + (pc.slot < 0 ? 0 : pc.slot)) * a.pairs + pair;
+#pragma unroll 1
+                    for (int b = 0; b < D / 32; ++b) {
+                        uint32_t o[32];
+                        tmem_ld32(o_addr + b * 32, o);
+                        if (odd && valid) {
+                            // the values that were set to zero, for the pairs that see them
+                            for (int j = 0; j < pc.n; ++j) {
+                                const int p0 = (pc.c0 + j) * CK;
+                                if (!is_edge(a, c, p0)) continue;
+                                for (int pos = p0; pos < min(p0 + CK, c.s.kv); ++pos) {
+                                    if (!sees(mask, pos, L, c.s.kv)) continue;
+                                    const int index = pos / a.pages.page_size;
+                                    const int page = load_page(a.seq, a.pages, c.b, index);
+                                    if (page < 0) continue;
+                                    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(a.pages.v) + page * a.pages.page +
+                                                             (pos - index * a.pages.page_size) * a.pages.tok + c.kvh * a.pages.head + b * 32;
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) {
+                                        const float x = to_f32(v[i]);
+                                        if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+                                    }
+                                }
+                            }
+                        }
+                        if (valid && pc.slot < 0) {
+                            __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(a.out.p) + out_offset(a.out, token, head) + b * 32;
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                                pk[i >> 1] = *reinterpret_cast<const uint32_t*>(&b2);
+                            }
+                            if (p.out_vec) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(y + i * 8) = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) y[i] = __ushort_as_bfloat16((unsigned short)(pk[i >> 1] >> ((i & 1) * 16)));
+                            }
+                        } else if (valid) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<uint4*>(a.part_o + at * D + b * 32 + i * 4) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                    if (valid && pc.slot >= 0) a.part_ml[at] = make_float2(m_run, l_run);
+                    if (valid && pc.slot < 0 && a.lse) a.lse[(size_t)token * a.Hq + head] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * 0.6931471805599453f;
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&o_free[sub]);
+            }
+            u += pc.n;
+            if (u < end) next_tile<CK>(a, c);
+        }
+        if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
+    }
+    // ---------------- teardown (every thread arrives here)
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (*s_abort) {
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);   // let copies in flight land before shared memory goes away
+    }
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+int gcd(int x, int y) { return y ? gcd(y, x % y) : x; }
+
+template <int D>
+int run_tc(TcParams& p, cudaStream_t s) {
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_paged_tc<D>), Cfg<D>::SMEM)) return -1;
+    k_paged_tc<D><<<p.a.n_cta, THREADS, Cfg<D>::SMEM, s>>>(p);
+    return 0;
+}
+
+}  // namespace
+
+bool paged_tma_pages(const PagedAttnArgs& a, int chunk, int* box_rows) {
+    // boxes of whole swizzle groups of eight rows; every stride a multiple of 16 bytes
+    *box_rows = gcd(a.pages.page_size, chunk);
+    auto al = [](long long x) { return x % 8 == 0; };
+    return *box_rows % 8 == 0 && reinterpret_cast<uintptr_t>(a.pages.k) % 16 == 0 && reinterpret_cast<uintptr_t>(a.pages.v) % 16 == 0 && al(a.pages.page) &&
+           al(a.pages.tok) && al(a.pages.head) && a.pages.page_size <= (1 << 30);
+}
+int paged_page_map(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows) {
+    EncodeFn enc = get_encode();
+    if (!enc) return -1;
+    auto bytes = [&](long long stride) { return (cuuint64_t)(stride > 0 ? stride * 2 : a.D * 2); };      // (a dimension of one element: any stride)
+    cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.pages.page_size, (cuuint64_t)a.Hkv, (cuuint64_t)a.pages.n_pages};
+    cuuint64_t strides[3] = {bytes(a.pages.tok), bytes(a.pages.head), bytes(a.pages.page)};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? 0 : -1;
+}
+
+bool paged_tc_supported(int dtype, const PagedAttnArgs& a) {
+    int box = 0;
+    return dtype == 1 && (a.D == 64 || a.D == 128) && a.group <= SUB && paged_tma_pages(a, CK, &box) && reinterpret_cast<uintptr_t>(a.q.p) % 16 == 0 &&
+           a.q.tok % 8 == 0 && a.q.head % 8 == 0 && (a.q.tok > 0 || a.seq.n_tokens == 1) && (a.q.head > 0 || a.Hq == 1);
+}
+
+int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s) {
+    TcParams p;
+    memset(&p, 0, sizeof(p));
+    if (!paged_tma_pages(a, CK, &p.box_rows)) return -1;
+    if (paged_page_map(&p.map_k, a, a.pages.k, p.box_rows) || paged_page_map(&p.map_v, a, a.pages.v, p.box_rows)) return -1;
+    p.sub_rows = SUB / a.group;
+    {
+        EncodeFn enc = get_encode();
+        cuuint64_t dims[3] = {(cuuint64_t)a.D, (cuuint64_t)a.Hq, (cuuint64_t)a.seq.n_tokens};
+        cuuint64_t strides[2] = {(cuuint64_t)(a.q.head > 0 ? a.q.head * 2 : a.D * 2), (cuuint64_t)(a.q.tok > 0 ? a.q.tok * 2 : a.D * 2)};
+        cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)p.sub_rows};
+        const cuuint32_t estr[3] = {1, 1, 1};
+        if (enc(&p.map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.q.p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return -1;
+    }
+    a.rows = 2 * p.sub_rows;
+    a.pairs = 2 * SUB;
+    a.n_cta = n_sm;
+    p.out_vec = reinterpret_cast<uintptr_t>(a.out.p) % 16 == 0 && a.out.tok % 8 == 0 && a.out.head % 8 == 0;
+    p.a = a;
+    const int rc = a.D == 128 ? run_tc<128>(p, s) : run_tc<64>(p, s);
+    return rc ? rc : launch_paged_merge(1, a, CK, 1, s);
+}
+
+}  // namespace esp
