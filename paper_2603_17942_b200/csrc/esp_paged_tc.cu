@@ -32,6 +32,10 @@ constexpr int SUB = 128;                  // pairs per subtile
 constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
 constexpr int THREADS = 384;
 constexpr int TMEM_COLS = 512;            // S0, S1, O0, O1: 128 columns each
+// Keys and values share the ring's stages in turn, but have barriers of their own that go by the chunk: whoever waits on a barrier waits for each of
+// its phases and is needed for the next one.  (With a barrier per stage the warps that look after the values were needed for every other
+// phase only, could be one phase late or early, and a wait ran out once in a thousand calls.)
+constexpr int NB = 4;                     // more chunks than the ring can hold values of
 constexpr int ODD_RING = 8;               // tiles whose note on odd values is kept: more than the ring's stages can hold values of
 
 template <int D>
@@ -45,8 +49,6 @@ struct Cfg {
     // kind::f16 instruction descriptors: D = f32, A = B = bf16, M = 128; Q K^T: N = 128 keys; P V: N = D, V is MN-major
     static constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
-    // keys and values take stages in turn: with an odd number of stages a stage holds values on every other pass
-    __device__ static uint32_t v_parity(uint32_t it) { return (STAGES % 2 ? it / STAGES / 2 : it / STAGES) & 1; }
 };
 
 struct TcParams {
@@ -106,10 +108,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     __shared__ Deal s_deal;
     __shared__ int s_odd[2][ODD_RING];     // [warp 2, 3] a value that some pair sees is no finite number
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);   // [STAGES] keys or values have landed
-    uint64_t* empty = full + C::STAGES;                                // [STAGES] their products have completed
-    uint64_t* v_ok = empty + C::STAGES;                                // [STAGES] the values have been looked after
-    uint64_t* s_full = v_ok + C::STAGES;                               // [2] scores of a subtile's chunk
+    uint64_t* empty = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // [STAGES] the products with what it held have completed
+    uint64_t* k_full = empty + C::STAGES;                              // [NB] keys of a chunk have landed
+    uint64_t* v_full = k_full + NB;                                    // [NB] values of a chunk have landed
+    uint64_t* v_ok = v_full + NB;                                      // [NB] they have been looked after
+    uint64_t* s_full = v_ok + NB;                                      // [2] scores of a subtile's chunk
     uint64_t* p_ready = s_full + 2;                                    // [2] its weights
     uint64_t* o_full = p_ready + 2;                                    // [2] the piece's last P V has completed
     uint64_t* o_free = o_full + 2;                                     // [2] the accumulator has been read
@@ -124,7 +127,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         prefetch_tensormap(&p.map_k);
         prefetch_tensormap(&p.map_v);
         prefetch_tensormap(&p.map_q);
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&v_ok[i], 2); }
+        for (int i = 0; i < C::STAGES; ++i) mbar_init(&empty[i], 1);
+        for (int i = 0; i < NB; ++i) { mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&v_ok[i], 2); }
         for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
@@ -169,9 +173,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 for (int kv = 0; kv < 2; ++kv, ++it) {
                     const int st = it % C::STAGES;
                     if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], ((it / C::STAGES) & 1) ^ 1, s_abort))) { ok = false; break; }
-                    if (lane == 0) mbar_expect_tx(&full[st], C::TILE_BYTES);
+                    uint64_t* full = (kv ? v_full : k_full) + (it >> 1) % NB;
+                    if (lane == 0) mbar_expect_tx(full, C::TILE_BYTES);
                     __syncwarp();
-                    if (active) tma_load_4d(sKV + st * C::TILE_BYTES + half * HALF_BYTES + box * p.box_rows * 128, kv ? &p.map_v : &p.map_k, half * 64, slot, c.kvh, page, &full[st]);
+                    if (active) tma_load_4d(sKV + st * C::TILE_BYTES + half * HALF_BYTES + box * p.box_rows * 128, kv ? &p.map_v : &p.map_k, half * 64, slot, c.kvh, page, full);
                     if (kv == 0 && j == 0) {                // the piece's queries behind its first keys
                         if (!__all_sync(0xffffffffu, mbar_wait(q_empty, (n_it & 1) ^ 1, s_abort))) { ok = false; break; }
                         if (lane == 0) {
@@ -193,7 +198,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         // ---------------- products: the warp walks its loop as a whole, one lane issues
         const bool leader{elect_lane()};
         const uint32_t q_addr = smem_u32(sQ), kv_addr = smem_u32(sKV);
-        uint32_t it = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // stages used, pieces, chunks and pieces of each subtile
+        uint32_t ch = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // chunks, pieces, chunks and pieces of each subtile
         bool ok = true;
         Cursor c = s_deal.at;
         for (long long u = begin; u < end && ok; ++n_it) {
@@ -208,36 +213,36 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 }
                 if (leader) umma_commit(&s_full[s]);
             };
-            ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&full[it % C::STAGES], (it / C::STAGES) & 1, s_abort));
+            ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&k_full[ch % NB], (ch / NB) & 1, s_abort));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int s = 0; s < subs; ++s) issue_qk(s, it % C::STAGES);
-            if (leader) umma_commit(&empty[it % C::STAGES]);
+            for (int s = 0; s < subs; ++s) issue_qk(s, 2 * ch % C::STAGES);
+            if (leader) umma_commit(&empty[2 * ch % C::STAGES]);
             if (leader && pc.n == 1) umma_commit(q_empty);
-            for (int j = 0; j < pc.n && ok; ++j, it += 2) {
-                const uint32_t vt = it + 1, kt = it + 2;                        // this chunk's values, the next one's keys
+            for (int j = 0; j < pc.n && ok; ++j, ++ch) {
+                const uint32_t vs = (2 * ch + 1) % C::STAGES, ks = (2 * ch + 2) % C::STAGES;     // stages of this chunk's values, of the next one's keys
                 for (int s = 0; s < subs && ok; ++s) {
                     const uint32_t g = s ? g1 : g0, np = s ? pieces1 : pieces0;
                     ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[s], (g + j) & 1, s_abort) &&
-                                                     (s > 0 || mbar_wait(&v_ok[vt % C::STAGES], C::v_parity(vt), s_abort)) &&
+                                                     (s > 0 || mbar_wait(&v_ok[ch % NB], (ch / NB) & 1, s_abort)) &&
                                                      (j > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t v_addr = kv_addr + (vt % C::STAGES) * C::TILE_BYTES;
+                    const uint32_t v_addr = kv_addr + vs * C::TILE_BYTES;
 #pragma unroll
                     for (int kk = 0; kk < CK / 16; ++kk)
                         if (leader) umma_ta(tmem_base + 256 + s * 128, tmem_base + s * 128 + kk * 8, smem_desc(v_addr + kk * 16 * 128, HALF_BYTES), C::IDESC_PV,
                                             (j > 0 || kk > 0) ? 1u : 0u);
-                    if (leader && s == subs - 1) umma_commit(&empty[vt % C::STAGES]);
+                    if (leader && s == subs - 1) umma_commit(&empty[vs]);
                     if (leader && j == pc.n - 1) umma_commit(&o_full[s]);
                     if (j + 1 < pc.n) {
                         if (s == 0) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(&full[kt % C::STAGES], (kt / C::STAGES) & 1, s_abort));
+                            ok = __all_sync(0xffffffffu, mbar_wait(&k_full[(ch + 1) % NB], ((ch + 1) / NB) & 1, s_abort));
                             if (!ok) break;
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         }
-                        issue_qk(s, kt % C::STAGES);
-                        if (leader && s == subs - 1) umma_commit(&empty[kt % C::STAGES]);
+                        issue_qk(s, ks);
+                        if (leader && s == subs - 1) umma_commit(&empty[ks]);
                         if (leader && s == subs - 1 && j + 2 == pc.n) umma_commit(q_empty);
                     }
                 }
@@ -251,15 +256,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
     } else if (warp < 4) {
         // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
-        uint32_t it = 1, n_it = 0;
+        uint32_t ch = 0, n_it = 0;
         bool ok = true;
         Cursor c = s_deal.at;
         for (long long u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             if (lane == 0) s_odd[warp - 2][(n_it + 1) % ODD_RING] = 0;
-            for (int j = 0; j < pc.n; ++j, it += 2) {
-                const int st = it % C::STAGES, p0 = (pc.c0 + j) * CK;
-                if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (it / C::STAGES) & 1, s_abort))) { ok = false; break; }
+            for (int j = 0; j < pc.n; ++j, ++ch) {
+                const int st = (2 * ch + 1) % C::STAGES, p0 = (pc.c0 + j) * CK;
+                if (!__all_sync(0xffffffffu, mbar_wait(&v_full[ch % NB], (ch / NB) & 1, s_abort))) { ok = false; break; }
                 if (is_edge(a, c, p0)) {
                     // a lane takes every other row of 16 bytes; its key follows from the row
                     bool odd = false;
@@ -282,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                if (lane == 0) mbar_arrive(&v_ok[st]);
+                if (lane == 0) mbar_arrive(&v_ok[ch % NB]);
             }
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);

@@ -581,6 +581,22 @@ def test_the_same_call_gives_the_same_bits(dtype, n, kv):
         assert torch.equal(first, again) and torch.equal(l1, l2)
 
 
+@pytest.mark.parametrize("dtype,D,n,kv", [("bf16", 128, [1] * 8, [9000] * 8), ("bf16", 128, [600, 68], [4000, 9000]), ("bf16", 64, [3, 300], [16000, 5000]), ("fp32", 64, [1, 20], [5000, 900])])
+def test_many_calls_behind_one_another(dtype, D, n, kv):
+    """Three hundred calls without a pause, on inputs larger than what the GPU keeps on chip among them: no wait runs out, every call gives the same bits."""
+    b = Batch(n, kv, 16, 8, D, dtype, seed=2)
+    q = _randn(_gen(7), b.tokens, 32, D, dtype=DT[dtype])
+    sc, nb = _scratch(32, D)
+    first, wrong = torch.empty_like(q), torch.zeros((), dtype=torch.int64, device="cuda")
+    P.esp_paged_attention(b.cache, b.batch, q, first, sc, nb)
+    out = torch.empty_like(q)
+    for _ in range(300):
+        P.esp_paged_attention(b.cache, b.batch, q, out, sc, nb)
+        wrong += (out != first).sum()
+    assert int(wrong) == 0
+    b.ok()
+
+
 def test_nothing_to_do():
     b = Batch([0, 0], [5, 0], 16, 2, 128, "bf16", seed=2, front=2, back=1)
     q = _randn(_gen(7), 3, 8, 128, dtype=torch.bfloat16)
