@@ -17,8 +17,8 @@
 // subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
 #include <string.h>
 
+#include "esp_attn_tc.cuh"
 #include "esp_paged.cuh"
-#include "esp_tc.cuh"
 
 namespace esp {
 
@@ -65,11 +65,12 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
-// 2^x as one special-function instruction (relative error about 2^-22, far below the rounding of the weight to bf16)
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
 }
 
 // A chunk that some pair of the tile does not see as a whole (the last one of the cache, the diagonal, the window's edge, the tree).
@@ -150,6 +151,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     unsigned char* sKV = smem + C::OFF_KV;
     const long long begin = any ? s_deal.unit : 0, end = any ? cta_begin(s_deal.total, s_deal.ctas, blockIdx.x + 1) : 0;
 
+    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; a softmax thread holds its 128 scores at once
+    if (warp < 4) { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         // ---------------- TMA: keys and values of a chunk in turn; a lane per box
         const int n_boxes = CK / p.box_rows;
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             if (u < end) next_tile<CK>(a, c);
         }
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
-    } else if (warp < 4) {
+    } else {
         // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
         uint32_t ch = 0, n_it = 0;
         bool ok = true;
@@ -293,7 +296,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             if (u < end) next_tile<CK>(a, c);
         }
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
-    } else {
+    } } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---------------- softmax and output of subtile sub: a thread per pair
         const int sub = (warp - 4) >> 2, q4 = warp & 3, row = q4 * 32 + lane;
         const uint32_t s_addr = tmem_base + ((uint32_t)(q4 * 32) << 16) + sub * 128, o_addr = s_addr + 256;
@@ -336,9 +340,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         const bool move = m_run == -INFINITY ? cmax != -INFINITY : cmax - m_run > 8.f;
                         const float m_new = move ? cmax : m_run;
                         const float m_use = m_new == -INFINITY ? 0.f : m_new;
+                        const float alpha = m_run == m_use ? 1.f : exp2f(m_run - m_use);
+                        const uint64_t scale2 = attn::pack2(a.scale_log2, a.scale_log2), neg_m2 = attn::pack2(-m_use, -m_use);
+                        uint64_t sum2[2] = {0, 0};
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                float w0, w1;
+                                attn::unpack2(attn::fma2(attn::pack2(__uint_as_float(sv[b * 32 + i]), __uint_as_float(sv[b * 32 + i + 1])), scale2, neg_m2), w0, w1);
+                                w0 = attn::ex2_approx(w0);
+                                w1 = attn::ex2_approx(w1);
+                                sum2[(i >> 1) & 1] = attn::add2(sum2[(i >> 1) & 1], attn::pack2(w0, w1));
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
+                                pk[i >> 1] = *reinterpret_cast<const uint32_t*>(&b2);
+                            }
+                            tmem_st16(s_addr + b * 16, pk);
+                        }
+                        float c0, c1;
+                        attn::unpack2(attn::add2(sum2[0], sum2[1]), c0, c1);
+                        l_run = fmaf(l_run, alpha, c0 + c1);
+                        m_run = m_new;
                         if (j > 0 && __any_sync(0xffffffffu, move)) {
-                            // O <- O * 2^(old - new); S arriving said that O is complete
-                            const float alpha = exp2f(m_run - m_use);
+                            // O <- O * 2^(old - new); S arriving said that O is complete.  (Here, where the scores' registers are free again)
 #pragma unroll
                             for (int b = 0; b < D / 32; ++b) {
                                 uint32_t o[32];
@@ -347,25 +372,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                                 for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
                                 tmem_st32(o_addr + b * 32, o);
                             }
-                            l_run *= alpha;
                         }
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int b = 0; b < 4; b += 2) {
-                            uint32_t pk[32];
-#pragma unroll
-                            for (int i = 0; i < 64; i += 2) {
-                                const float p0_ = ex2(fmaf(__uint_as_float(sv[b * 32 + i]), a.scale_log2, -m_use));
-                                const float p1_ = ex2(fmaf(__uint_as_float(sv[b * 32 + i + 1]), a.scale_log2, -m_use));
-                                sum[i & 2] += p0_;
-                                sum[(i & 2) + 1] += p1_;
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(p0_, p1_);
-                                pk[i >> 1] = *reinterpret_cast<const uint32_t*>(&b2);
-                            }
-                            tmem_st32(s_addr + b * 16, pk);
-                        }
-                        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                        m_run = m_new;
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
