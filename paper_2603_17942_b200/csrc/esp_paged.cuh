@@ -1,9 +1,8 @@
 // How the attention over pages deals its work, shared by its kernels.
 //
 // The pairs (token, query head) of one sequence and KV head are cut into tiles of `rows` tokens; a tile has to walk the chunks of CK
-// keys that any of its tokens can see.  All (sequence, KV head, tile, chunk) units of the batch form one line, and CTA c takes the units
-// [W c / G, W (c + 1) / G): every CTA gets the same number of chunks whatever the lengths are, and nobody on the host has to know
-// them.  A tile that lies in one CTA is finished there; the pieces of a tile that several CTAs share are stored as split partials
+// keys that any of its tokens can see.  All (sequence, KV head, tile, chunk) units of the batch form one line, cut into equal shares for
+// the CTAs: every CTA gets the same number of chunks, or one more, whatever the lengths are, and nobody on the host has to know them.  A tile that lies in one CTA is finished there; the pieces of a tile that several CTAs share are stored as split partials
 // (weighted values, maximum, sum) and joined by the merge kernel in the order of the CTAs, so a call always gives the same bits.
 // A CTA's pieces of shared tiles are its first and its last, so two slots per CTA are enough.
 #pragma once
@@ -54,130 +53,123 @@ __device__ __forceinline__ Tile make_tile(const PagedAttnArgs& a, const Seq& s, 
 }
 __device__ __forceinline__ int n_tiles(const PagedAttnArgs& a, const Seq& s) { return (s.n + a.rows - 1) / a.rows; }
 
-// Where a unit lies: everything a CTA needs to walk on from there.
+// Where a CTA stands on the line: a tile, and the CTA's own range of units.
 struct Cursor {
-    long long tile_u;     // first unit of the tile
+    uint32_t tile_u;      // first unit of the tile
     int b, kvh, t;
     Seq s;
     Tile x;
 };
-struct Deal {             // in shared memory, filled by deal()
-    long long total;
-    int ctas;             // CTAs that take part: each of them has at least one unit
-    Cursor at;            // the tile that holds the unit asked for
-    long long scan[32];
-    long long unit;
-    int owner, owner_b;
-    long long owner_rest, owner_u;
+struct Share {            // CTA c of `ctas` has `each` units, the first `more` CTAs one more
+    uint32_t each, more;
+    int ctas;
+    __device__ __forceinline__ uint32_t begin(int c) const { return (uint32_t)c * each + min((uint32_t)c, more); }
+    __device__ __forceinline__ int cta_of(uint32_t u) const {
+        const uint32_t wide = more * (each + 1);
+        return (int)(u < wide ? u / (each + 1) : more + (u - wide) / each);
+    }
 };
-
-__device__ __forceinline__ long long cta_begin(long long total, int ctas, int c) { return total * c / ctas; }
-__device__ __forceinline__ int cta_of_unit(long long total, int ctas, long long u) { return (int)(((u + 1) * ctas + total - 1) / total - 1); }
+__device__ __forceinline__ uint32_t warp_sum_u32(uint32_t v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ uint32_t warp_scan_u32(uint32_t v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
+    }
+    return v;
+}
 
 // Chunks of all tiles of a sequence (one KV head).  All 32 lanes call it together with a sequence each; long ones are counted by the whole warp.
 template <int CK>
-__device__ __forceinline__ long long seq_chunks(const PagedAttnArgs& a, const Seq& s, int lane) {
+__device__ __forceinline__ uint32_t seq_chunks(const PagedAttnArgs& a, const Seq& s, int lane) {
     const int T = n_tiles(a, s);
-    long long w = 0;
-    if (T <= 16)
+    uint32_t w = 0;
+    if (T <= 4)
         for (int t = 0; t < T; ++t) w += make_tile<CK>(a, s, t).nc;
-    for (uint32_t big = __ballot_sync(0xffffffffu, T > 16); big; big &= big - 1) {
+    for (uint32_t big = __ballot_sync(0xffffffffu, T > 4); big; big &= big - 1) {
         const int src = __ffs(big) - 1;
         Seq o;
         o.start = 0;
         o.n = __shfl_sync(0xffffffffu, s.n, src);
         o.kv = __shfl_sync(0xffffffffu, s.kv, src);
         const int To = n_tiles(a, o);
-        long long p = 0;
+        uint32_t p = 0;
         for (int t = lane; t < To; t += 32) p += make_tile<CK>(a, o, t).nc;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) p += __shfl_xor_sync(0xffffffffu, p, d);
+        p = warp_sum_u32(p);
         if (lane == src) w = p;
     }
     return w;
 }
 
-// Called by all threads of a block (a multiple of 32, at most 1024): counts the batch's units and finds the tile that holds the first unit of
-// CTA `cta` (or, LAST, the last unit of it).  false: the CTA has no units.
-template <int CK, bool LAST>
-__device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int min_units, Deal* d) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    const int per = (a.seq.batch + blockDim.x - 1) / blockDim.x;        // consecutive sequences of a thread
-    const int b0 = min((int)threadIdx.x * per, a.seq.batch), b1 = min(b0 + per, a.seq.batch);
-    long long mine = 0;
+// Called by all lanes of a warp, each warp that needs to know for itself (no barrier, nothing shared): counts the batch's units and finds the tile in
+// which CTA `cta` starts.  false: the CTA has no units.  A batch of 2^31 units or more (months of work) is refused on the device.
+template <int CK>
+__device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, Share& share, Cursor& at) {
+    const int per = (a.seq.batch + 31) >> 5;                             // consecutive sequences of a lane
+    const int b0 = lane * per;
+    uint32_t mine = 0;
+    unsigned long long wide = 0;
+    Seq s;
     for (int i = 0; i < per; ++i) {                                      // the same trips in every lane
-        Seq s;
         s.start = s.n = s.kv = 0;
-        if (b0 + i < b1) s = load_seq(a.seq, b0 + i);
-        mine += seq_chunks<CK>(a, s, lane) * a.Hkv;
+        if (b0 + i < a.seq.batch) s = load_seq(a.seq, b0 + i);
+        const unsigned long long w = (unsigned long long)seq_chunks<CK>(a, s, lane) * a.Hkv;
+        wide += w;
+        mine += (uint32_t)w;
     }
-    long long incl = mine;
+    if (__any_sync(0xffffffffu, wide >> 26)) {                           // (32 lanes below 2^26 each stay below 2^31)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
+        for (int o = 16; o > 0; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+        if (wide >> 31) {
+            set_error(a.seq.status, DEV_E_CAPACITY);
+            return false;
+        }
     }
-    if (lane == 31) d->scan[warp] = incl;
-    __syncthreads();
-    long long before = incl - mine, total = 0;
-    for (int w = 0; w < n_warps; ++w) {
-        if (w < warp) before += d->scan[w];
-        total += d->scan[w];
-    }
-    const int ctas = (int)max(1ll, min((long long)a.n_cta, (total + min_units - 1) / min_units));
-    if (total == 0 || cta >= ctas) return false;                         // the same answer in every thread
-    const long long unit = LAST ? cta_begin(total, ctas, cta + 1) - 1 : cta_begin(total, ctas, cta);
-    if (before <= unit && unit < before + mine) {
-        d->total = total;
-        d->ctas = ctas;
-        d->unit = unit;
-        d->owner = threadIdx.x;
-        d->owner_b = b0;
-        d->owner_u = before;
-    }
-    __syncthreads();
-    if (warp == (d->owner >> 5)) {
-        // the warp walks the owner's sequences, then the tiles of the one that holds the unit
-        long long u0 = d->owner_u;
-        int b = d->owner_b;
-        Seq s;
-        long long Wt;
-        for (;; ++b) {
-            s = load_seq(a.seq, b);                                      // the same sequence in every lane
+    const uint32_t incl = warp_scan_u32(mine, lane), total = __shfl_sync(0xffffffffu, incl, 31);
+    share.ctas = (int)min((uint32_t)a.n_cta, (total + a.min_units - 1) / a.min_units);
+    if (cta >= share.ctas) return false;                                 // (nothing to do at all: no CTAs)
+    share.each = total / share.ctas;
+    share.more = total - share.each * share.ctas;
+    const uint32_t unit = share.begin(cta), before = incl - mine;
+    const int owner = __ffs(__ballot_sync(0xffffffffu, before <= unit && unit < incl)) - 1;
+    uint32_t u0 = __shfl_sync(0xffffffffu, before, owner), Wt;
+    at.b = owner * per;
+    if (per == 1) {
+        at.s.start = __shfl_sync(0xffffffffu, s.start, owner);
+        at.s.n = __shfl_sync(0xffffffffu, s.n, owner);
+        at.s.kv = __shfl_sync(0xffffffffu, s.kv, owner);
+        Wt = (__shfl_sync(0xffffffffu, incl, owner) - u0) / a.Hkv;
+    } else {
+        for (;; ++at.b) {                                                // the same sequence in every lane
+            at.s = load_seq(a.seq, at.b);
+            const int T = n_tiles(a, at.s);
             Wt = 0;
-            const int T = n_tiles(a, s);
-            for (int t = lane; t < T; t += 32) Wt += make_tile<CK>(a, s, t).nc;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) Wt += __shfl_xor_sync(0xffffffffu, Wt, o);
-            if (unit < u0 + Wt * a.Hkv) break;
+            for (int t = lane; t < T; t += 32) Wt += make_tile<CK>(a, at.s, t).nc;
+            Wt = warp_sum_u32(Wt);
+            if (unit - u0 < Wt * a.Hkv) break;
             u0 += Wt * a.Hkv;
         }
-        const int kvh = (int)((unit - u0) / Wt);
-        u0 += kvh * Wt;
-        for (int t0 = 0;; t0 += 32) {
-            const int t = t0 + lane;
-            int nc = 0;
-            if (t < n_tiles(a, s)) nc = make_tile<CK>(a, s, t).nc;
-            long long in = nc;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(0xffffffffu, in, o);
-                if (lane >= o) in += v;
-            }
-            const bool here = unit >= u0 + in - nc && unit < u0 + in;
-            if (here) {
-                d->at.tile_u = u0 + in - nc;
-                d->at.b = b;
-                d->at.kvh = kvh;
-                d->at.t = t;
-                d->at.s = s;
-                d->at.x = make_tile<CK>(a, s, t);
-            }
-            if (__ballot_sync(0xffffffffu, here)) break;
-            u0 += __shfl_sync(0xffffffffu, in, 31);
-        }
     }
-    __syncthreads();
+    at.kvh = (int)((unit - u0) / Wt);
+    u0 += at.kvh * Wt;
+    for (int t0 = 0;; t0 += 32) {
+        const int t = t0 + lane;
+        const uint32_t nc = t < n_tiles(a, at.s) ? make_tile<CK>(a, at.s, t).nc : 0;
+        const uint32_t in = warp_scan_u32(nc, lane);
+        const uint32_t here = __ballot_sync(0xffffffffu, unit - u0 < in);  // the first lane behind the unit has its tile
+        if (here) {
+            const int src = __ffs(here) - 1;
+            at.t = t0 + src;
+            at.tile_u = u0 + __shfl_sync(0xffffffffu, in - nc, src);
+            break;
+        }
+        u0 += __shfl_sync(0xffffffffu, in, 31);
+    }
+    at.x = make_tile<CK>(a, at.s, at.t);
     return true;
 }
 
@@ -202,14 +194,29 @@ struct Piece {
     int c0, n;
     int slot;             // -1: the whole tile, finished here; else the CTA's slot for the split partial
 };
-__device__ __forceinline__ Piece make_piece(const Cursor& c, long long begin, long long u, long long end) {
+__device__ __forceinline__ Piece make_piece(const Cursor& c, uint32_t begin, uint32_t u, uint32_t end) {
     Piece p;
     const int off = (int)(u - c.tile_u);
-    p.n = (int)min((long long)(c.x.nc - off), end - u);
+    p.n = (int)min((uint32_t)(c.x.nc - off), end - u);
     p.c0 = c.x.c0 + off;
     p.slot = p.n == c.x.nc ? -1 : (begin >= c.tile_u ? 0 : 1);
     return p;
 }
+
+// What the merge kernel has to know of the tile whose first piece is CTA c's last one, if other CTAs have the rest.
+__device__ __forceinline__ MergeDesc make_desc(const PagedAttnArgs& a, const Cursor& c, const Share& share, const Piece& p, int cta) {
+    MergeDesc d;
+    d.token = c.s.start + c.x.r0;
+    d.pairs = c.x.nr * a.group;
+    d.head0 = c.kvh * a.group;
+    d.parts = (share.cta_of(c.tile_u + c.x.nc - 1) - cta + 1) * 2 + p.slot;
+    return d;
+}
+// split partials: quad dq of a pair's weighted values, in the order in which a warp with a lane per pair writes them
+__device__ __forceinline__ size_t part_quad(const PagedAttnArgs& a, int cta, int slot, int dq, int pair) {
+    return ((size_t)(cta * 2 + slot) * (a.D / 4) + dq) * a.pairs + pair;
+}
+__device__ __forceinline__ size_t part_row(const PagedAttnArgs& a, int cta, int slot, int pair) { return (size_t)(cta * 2 + slot) * a.pairs + pair; }
 
 // What token i of its sequence sees of position pos (< kv).
 struct RowMask {

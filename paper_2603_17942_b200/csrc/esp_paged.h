@@ -37,6 +37,11 @@ struct NormRopeArgs {
     int32_t append;
 };
 
+struct MergeDesc {        // a tile that several CTAs share
+    int32_t token, pairs, head0;
+    int32_t parts;        // 2 x CTAs that have a piece of it + the first one's slot; 0: no such tile
+};
+
 struct PagedAttnArgs {
     HeadsView q, out;
     float* lse;
@@ -48,20 +53,24 @@ struct PagedAttnArgs {
     int32_t rows;           // tokens of a tile: rows * group (token, head) pairs
     int32_t pairs;          // pairs of a tile's partial in the scratch
     int32_t n_cta;          // CTAs the work is dealt to
+    int32_t min_units;      // fewer CTAs rather than fewer chunks than this for each
     int32_t vec;            // CUDA-core kernel: rows can be read four elements at a time
-    float* part_o;          // [n_cta][2][pairs][D] split partials: weighted values, not divided by the sum
+    int32_t out_vec;        // rows of out can be written four elements at a time
+    MergeDesc* desc;        // [n_cta]
+    float4* part_o;         // [n_cta][2][D / 4][pairs] split partials: weighted values, not divided by the sum
     float2* part_ml;        // [n_cta][2][pairs] their (maximum in the log2 domain, sum)
 };
 
-// Partials a launch may need at most: two tiles of 256 pairs for each of 148 CTAs, or as much in smaller tiles.
+// Partials a launch may need at most: two tiles of 256 pairs for each of 148 SMs, or as much in smaller tiles.
 constexpr int PAGED_MAX_PAIRS = 256;
-constexpr int PAGED_MAX_CTAS = 148;
+constexpr int PAGED_MAX_SMS = 148;
+constexpr int PAGED_MAX_CTAS = PAGED_MAX_SMS * 8;
 
 int launch_norm_rope(int dtype, const NormRopeArgs& a, cudaStream_t s);
 void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStream_t s);
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s);
 bool paged_tc_supported(int dtype, const PagedAttnArgs& a);
 int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s);
-int launch_paged_merge(int dtype, const PagedAttnArgs& a, int chunk, int min_units, cudaStream_t s);
+int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s);
 
 }  // namespace esp

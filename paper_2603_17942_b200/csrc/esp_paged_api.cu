@@ -221,12 +221,12 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
     return cuda_ok(cudaGetLastError());
 }
 
-// scratch layout: [split partials: weighted values][split partials: (maximum, sum)]
+// scratch layout: [split tiles][split partials: weighted values][split partials: (maximum, sum)]
 int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_t* bytes_out) {
     if (!bytes_out || n_q_heads < 1) return ESP_E_ARG;
     if (head_dim != 32 && head_dim != 64 && head_dim != 128) return ESP_E_BADCFG;
-    const size_t rows = (size_t)PAGED_MAX_CTAS * 2 * PAGED_MAX_PAIRS;
-    *bytes_out = rows * head_dim * sizeof(float) + rows * sizeof(float2);
+    const size_t rows = (size_t)PAGED_MAX_SMS * 2 * PAGED_MAX_PAIRS;
+    *bytes_out = sizeof(MergeDesc) * PAGED_MAX_CTAS + rows * head_dim * sizeof(float) + rows * sizeof(float2);
     return ESP_OK;
 }
 
@@ -246,7 +246,7 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     if (n_tokens == 0 || batch->batch == 0 || batch->max_new == 0) return ESP_OK;
     int n_sm = current_sm_count();
     if (n_sm < 1) return ESP_E_CUDA;
-    if (n_sm > PAGED_MAX_CTAS) n_sm = PAGED_MAX_CTAS;
+    if (n_sm > PAGED_MAX_SMS) n_sm = PAGED_MAX_SMS;
     PagedAttnArgs a;
     memset(&a, 0, sizeof(a));
     a.q = view_of(q, n_tokens); a.out = view_of(out, n_tokens); a.lse = lse;
@@ -256,13 +256,16 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     a.Hq = q->n_heads; a.Hkv = cache->n_kv_heads; a.group = a.Hq / a.Hkv; a.D = cache->head_dim;
     a.window = window > paged::KV_LIMIT ? 0 : window;      // no position is that far back
     a.scale_log2 = (float)(1.4426950408889634 * (scale != 0.f ? (double)scale : 1.0 / sqrt((double)a.D)));
-    const size_t rows = (size_t)PAGED_MAX_CTAS * 2 * PAGED_MAX_PAIRS;
-    a.part_o = reinterpret_cast<float*>(scratch);
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * a.D);
+    const size_t rows = (size_t)PAGED_MAX_SMS * 2 * PAGED_MAX_PAIRS;
+    a.min_units = 1;
+    a.desc = reinterpret_cast<MergeDesc*>(scratch);
+    a.part_o = reinterpret_cast<float4*>(a.desc + PAGED_MAX_CTAS);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * (a.D / 4));
     const size_t es = elem_size(cache->dtype), quad = 4 * es;
     auto by4 = [&](const void* p, int64_t s0, int64_t s1, int64_t s2) {
         return reinterpret_cast<uintptr_t>(p) % quad == 0 && s0 % 4 == 0 && s1 % 4 == 0 && s2 % 4 == 0;
     };
+    a.out_vec = by4(a.out.p, a.out.tok, a.out.head, 0);
     a.vec = by4(a.q.p, a.q.tok, a.q.head, 0) && by4(a.pages.k, a.pages.page, a.pages.tok, a.pages.head) && by4(a.pages.v, 0, 0, 0);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     const int rc = paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s) : launch_paged_simt(cache->dtype, a, n_sm, s);

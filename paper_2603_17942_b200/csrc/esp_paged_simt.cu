@@ -22,7 +22,6 @@ struct SimtSmem {
     float v[CK][D];
     float p[MP][CK + 4];
     long long base[CK];               // element offset of the chunk's keys in the pages, -1: none
-    Deal deal;
 };
 
 template <typename T, bool VEC>
@@ -34,6 +33,19 @@ __device__ __forceinline__ float4 load4(const T* x) {
         return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
     }
 }
+template <typename T>
+__device__ __forceinline__ void store4(T* y, const float4& x, bool vec) {
+    if constexpr (sizeof(T) == 4) {
+        if (vec) { *reinterpret_cast<float4*>(y) = x; return; }
+    } else {
+        if (vec) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
+            *reinterpret_cast<uint2*>(y) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            return;
+        }
+    }
+    y[0] = from_f32<T>(x.x); y[1] = from_f32<T>(x.y); y[2] = from_f32<T>(x.z); y[3] = from_f32<T>(x.w);
+}
 __device__ __forceinline__ bool finite4(const float4& x) { return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w); }
 
 template <typename T, int D, int MP, bool VEC>
@@ -44,12 +56,18 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
     constexpr int DV = D >= 64 ? D / 64 : 1;          // float4 columns of a thread (D = 32: the first eight tx have one)
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     pdl_launch_dependents();
-    if (!deal<CK, false>(a, blockIdx.x, 1, &sm.deal)) return;
-    Cursor c = sm.deal.at;
-    const long long total = sm.deal.total, begin = sm.deal.unit, end = cta_begin(total, sm.deal.ctas, blockIdx.x + 1);
+    Share share;
+    Cursor c;
+    MergeDesc desc;
+    desc.parts = 0;
+    if (!deal<CK>(a, blockIdx.x, tid & 31, share, c)) {
+        if (tid == 0) a.desc[blockIdx.x] = desc;
+        return;
+    }
+    const uint32_t begin = share.begin(blockIdx.x), end = share.begin(blockIdx.x + 1);
     const bool dims = D >= 64 || tx < 8;
 
-    for (long long u = begin; u < end;) {
+    for (uint32_t u = begin; u < end;) {
         const Piece pc = make_piece(c, begin, u, end);
         const int L = c.s.kv - c.s.n, n_pairs = c.x.nr * a.group;
         __syncthreads();                              // the previous piece is done with shared memory
@@ -195,86 +213,72 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
                 T* y = reinterpret_cast<T*>(a.out.p) + out_offset(a.out, token, head);
                 if (dims)
 #pragma unroll
-                    for (int j = 0; j < DV; ++j) {
-                        T* z = y + tx * 4 + 64 * j;
-                        z[0] = from_f32<T>(o[i][j].x * inv); z[1] = from_f32<T>(o[i][j].y * inv);
-                        z[2] = from_f32<T>(o[i][j].z * inv); z[3] = from_f32<T>(o[i][j].w * inv);
-                    }
+                    for (int j = 0; j < DV; ++j)
+                        store4<T>(y + tx * 4 + 64 * j, make_float4(o[i][j].x * inv, o[i][j].y * inv, o[i][j].z * inv, o[i][j].w * inv), a.out_vec);
                 if (a.lse && tx == 0) a.lse[(size_t)token * a.Hq + head] = l_run[i] == 0.f ? -INFINITY : (m_run[i] + log2f(l_run[i])) * 0.6931471805599453f;
             } else {
-                const size_t at = ((size_t)blockIdx.x * 2 + pc.slot) * a.pairs + pr;
                 if (dims)
 #pragma unroll
-                    for (int j = 0; j < DV; ++j) *reinterpret_cast<float4*>(a.part_o + at * D + tx * 4 + 64 * j) = o[i][j];
-                if (tx == 0) a.part_ml[at] = make_float2(m_run[i], l_run[i]);
+                    for (int j = 0; j < DV; ++j) a.part_o[part_quad(a, blockIdx.x, pc.slot, tx + 16 * j, pr)] = o[i][j];
+                if (tx == 0) a.part_ml[part_row(a, blockIdx.x, pc.slot, pr)] = make_float2(m_run[i], l_run[i]);
             }
         }
+        if (pc.slot >= 0 && pc.c0 == c.x.c0) desc = make_desc(a, c, share, pc, blockIdx.x);
         u += pc.n;
         if (u < end) next_tile<CK>(a, c);
     }
+    if (tid == 0) a.desc[blockIdx.x] = desc;
 }
 
-// Block (c, slice): the tile whose first piece CTA c has as its last one, if other CTAs have the rest; a warp per pair, which weighs
-// the partials by 2^(m - max m) in the order of the CTAs.  The dealing is looked up while the kernel in front still runs.
-constexpr int MERGE_WARPS = 8;
+// The tile whose first piece CTA c has as its last one (c = blockIdx.x), if other CTAs have the rest: the partials are weighed by 2^(m - max m) in the
+// order of the CTAs.  A lane takes four quads of one pair; a warp has LP pairs side by side, as the partials lie.
+constexpr int MERGE_WARPS = 8, MERGE_QUADS = 4;
 
-template <typename T, int D, int CKM>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge(const __grid_constant__ PagedAttnArgs a, int min_units) {
-    __shared__ Deal sd;
-    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool any = deal<CKM, true>(a, c, min_units, &sd);
-    const Cursor& t = sd.at;
-    const bool split = any && t.tile_u >= cta_begin(sd.total, sd.ctas, c) && t.tile_u + t.x.nc > cta_begin(sd.total, sd.ctas, c + 1);
+template <typename T, int D>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge(const __grid_constant__ PagedAttnArgs a) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x;
+    const int LP = min(32, a.pairs), LQ = 32 / LP, WQ = LQ * MERGE_QUADS;       // pairs and quads side by side, quads of a warp
+    const int cols = (D / 4 + WQ - 1) / WQ;                                     // warps for the quads of a pair
+    const int task = blockIdx.y * MERGE_WARPS + warp, pr = (task / cols) * LP + lane % LP, q0 = (task % cols) * WQ + lane / LP;
     pdl_wait();
-    if (!split) return;
-    const int c_last = cta_of_unit(sd.total, sd.ctas, t.tile_u + t.x.nc - 1);
+    const int4 dd = __ldcg(reinterpret_cast<const int4*>(a.desc + c));
+    const int token = dd.x, n_pairs = dd.y, head0 = dd.z, n = dd.w >> 1, first_slot = dd.w & 1;
+    if (n == 0 || pr >= n_pairs || q0 >= D / 4) return;
     // CTA c has the tile's first piece in slot 0 if the tile is where it starts; the CTAs behind it have theirs in slot 0
-    const int first_slot = cta_begin(sd.total, sd.ctas, c) >= t.tile_u ? 0 : 1;
-    const int n_pairs = t.x.nr * a.group;
-    for (int pr = blockIdx.y * MERGE_WARPS + warp; pr < n_pairs; pr += gridDim.y * MERGE_WARPS) {
-        auto at = [&](int cta) { return ((size_t)cta * 2 + (cta == c ? first_slot : 0)) * a.pairs + pr; };
-        float m = -INFINITY;
-        for (int k = c + lane; k <= c_last; k += 32) m = fmaxf(m, __ldcg(a.part_ml + at(k)).x);
-        m = warp_max(m);
-        const float m_use = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        float o[D / 32];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
-        for (int k0 = c; k0 <= c_last; k0 += 32) {
-            float w = 0.f, lk = 0.f;
-            if (k0 + lane <= c_last) {
-                const float2 ml = __ldcg(a.part_ml + at(k0 + lane));
-                w = exp2f(ml.x - m_use);
-                lk = ml.y * w;
-            }
-            const int n = min(32, c_last - k0 + 1);
+    const float2* ml = a.part_ml + part_row(a, c, 0, pr);
+    float m = -INFINITY;
 #pragma unroll 4
-            for (int j = 0; j < n; ++j) {
-                const float wj = __shfl_sync(0xffffffffu, w, j);
-                l += __shfl_sync(0xffffffffu, lk, j);
-                const float* src = a.part_o + at(k0 + j) * D + lane * (D / 32);
-                float x[D / 32];
-                if constexpr (D == 128) {
-                    const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
-                    x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
-                } else if constexpr (D == 64) {
-                    const float2 y = __ldcg(reinterpret_cast<const float2*>(src));
-                    x[0] = y.x; x[1] = y.y;
-                } else {
-                    x[0] = __ldcg(src);
-                }
+    for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(ml + (size_t)(2 * k + (k == 0 ? first_slot : 0)) * a.pairs).x);
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 o[MERGE_QUADS];
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) o[i] = fmaf(wj, x[i], o[i]);
-            }
+    for (int i = 0; i < MERGE_QUADS; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int k = 0; k < n; ++k) {
+        const int sl = 2 * k + (k == 0 ? first_slot : 0);
+        const float2 x = __ldcg(ml + (size_t)sl * a.pairs);
+        float4 v[MERGE_QUADS];
+#pragma unroll
+        for (int i = 0; i < MERGE_QUADS; ++i)
+            v[i] = q0 + i * LQ < D / 4 ? __ldcg(a.part_o + part_quad(a, c, sl, q0 + i * LQ, pr)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float w = exp2f(x.x - m_use);
+        l = fmaf(x.y, w, l);
+#pragma unroll
+        for (int i = 0; i < MERGE_QUADS; ++i) {
+            o[i].x = fmaf(v[i].x, w, o[i].x); o[i].y = fmaf(v[i].y, w, o[i].y);
+            o[i].z = fmaf(v[i].z, w, o[i].z); o[i].w = fmaf(v[i].w, w, o[i].w);
         }
-        const int row = pr / a.group, head = t.kvh * a.group + pr - row * a.group, token = t.s.start + t.x.r0 + row;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* y = reinterpret_cast<T*>(a.out.p) + out_offset(a.out, token, head) + lane * (D / 32);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) y[i] = from_f32<T>(o[i] * inv);
-        if (a.lse && lane == 0) a.lse[(size_t)token * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     }
+    const int row = pr / a.group, head = head0 + pr - row * a.group;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* y = reinterpret_cast<T*>(a.out.p) + out_offset(a.out, token + row, head);
+#pragma unroll
+    for (int i = 0; i < MERGE_QUADS; ++i) {
+        const int q = q0 + i * LQ;
+        if (q < D / 4) store4<T>(y + 4 * q, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
+    }
+    if (a.lse && q0 == 0) a.lse[(size_t)(token + row) * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, int MP, bool VEC>
@@ -294,22 +298,19 @@ int run_simt_t(const PagedAttnArgs& a, cudaStream_t s) {
     return a.D == 32 ? run_simt_d<T, 32>(a, s) : (a.D == 64 ? run_simt_d<T, 64>(a, s) : run_simt_d<T, 128>(a, s));
 }
 
-template <typename T, int D, int CKM>
-int run_merge(const PagedAttnArgs& a, int min_units, cudaStream_t s) {
-    const int slices = (a.rows * a.group + MERGE_WARPS - 1) / MERGE_WARPS;
+template <typename T, int D>
+int run_merge(const PagedAttnArgs& a, cudaStream_t s) {
+    const int lp = a.pairs < 32 ? a.pairs : 32, wq = 32 / lp * MERGE_QUADS;
+    const int tasks = (a.rows * a.group + lp - 1) / lp * ((D / 4 + wq - 1) / wq);
     if (a.n_cta < 2) return 0;
-    return launch_k(k_paged_merge<T, D, CKM>, dim3(a.n_cta - 1, slices), dim3(MERGE_WARPS * 32), 0, s, true, a, min_units) != cudaSuccess;
-}
-template <typename T, int CKM>
-int run_merge_d(const PagedAttnArgs& a, int min_units, cudaStream_t s) {
-    return a.D == 32 ? run_merge<T, 32, CKM>(a, min_units, s) : (a.D == 64 ? run_merge<T, 64, CKM>(a, min_units, s) : run_merge<T, 128, CKM>(a, min_units, s));
+    return launch_k(k_paged_merge<T, D>, dim3(a.n_cta - 1, (tasks + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, true, a) != cudaSuccess;
 }
 
 }  // namespace
 
-int launch_paged_merge(int dtype, const PagedAttnArgs& a, int chunk, int min_units, cudaStream_t s) {
-    if (dtype == 0) return run_merge_d<float, CK>(a, min_units, s);
-    return chunk == 64 ? run_merge_d<__nv_bfloat16, 64>(a, min_units, s) : run_merge_d<__nv_bfloat16, 128>(a, min_units, s);
+int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s) {
+    if (dtype == 0) return a.D == 32 ? run_merge<float, 32>(a, s) : (a.D == 64 ? run_merge<float, 64>(a, s) : run_merge<float, 128>(a, s));
+    return a.D == 32 ? run_merge<__nv_bfloat16, 32>(a, s) : (a.D == 64 ? run_merge<__nv_bfloat16, 64>(a, s) : run_merge<__nv_bfloat16, 128>(a, s));
 }
 
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {
@@ -319,7 +320,7 @@ int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {
     if (a.rows < 1) return -1;                      // more than 64 query heads share a KV head
     a.n_cta = n_sm * (a.pairs == 16 ? 4 : 2);
     const int rc = dtype == 0 ? run_simt_t<float>(a, s) : run_simt_t<__nv_bfloat16>(a, s);
-    return rc ? rc : launch_paged_merge(dtype, a, CK, 1, s);
+    return rc ? rc : launch_paged_merge(dtype, a, s);
 }
 
 }  // namespace esp

@@ -1,20 +1,21 @@
 // Attention over pages on the Blackwell tensor cores: bf16, heads of 64 or 128, blocks of several tokens.
 //
 // A CTA takes tiles of up to 256 (token, query head) pairs that share a KV head, as two subtiles of 128, and walks their keys 128 at
-// a time.  Keys and values come by TMA, page by page (boxes of as many tokens as page size and chunk have in common), into a ring of
+// a time.  Keys and values come by TMA, page by page (boxes of as many tokens as page size and chunk have in common), into rings of
 // stages that both subtiles share:
 //   S_s = Q_s K^T    tcgen05.mma, both operands K-major in shared memory, S_s (128 x 128 fp32) in tensor memory;
 //   softmax          one thread per pair (= tensor-memory lane): mask, running maximum and sum in the log2 domain, P as bf16 back over S_s;
 //   O_s += P_s V     tcgen05.mma with P_s as the tensor-memory operand, V MN-major as the pages have it; O_s stays in tensor memory.
 //                    The reference of the exponentials follows the maximum lazily: it moves, and O_s is rescaled, only after a growth of 2^8.
 // The tensor cores work on one subtile while the softmax of the other runs; products are issued in the order P_0 V, Q_0 K^T (next chunk),
-// P_1 V, Q_1 K^T, and run in that order, so S_s may be overwritten as soon as the P_s V that read P_s from it has been issued, and S_s
-// arriving says that O_s is complete.
+// P_1 V, Q_1 K^T, and run in that order, so S_s may be overwritten as soon as the P_s V that reads P_s from it has been issued, and S_s
+// arriving says that O_s is complete.  (A warp for each subtile's products interleaves them, and the tensor cores take longer: chunk of 2048 behind
+// 6144 347 us against 262.)
 // Weights of keys that a pair does not see are zero, but zero times an infinite value is no number: in chunks that not every pair sees
-// as a whole, two warps set values that are no finite numbers to zero in shared memory before the product, and the pairs that see them get them
+// as a whole, a warp sets values that are no finite numbers to zero in shared memory before the product, and the pairs that see them get them
 // when the tile is finished.
-// Roles: warp 0 TMA, warp 1 issues the products, warps 2 and 3 look after the values, warps 4-7 and 8-11 softmax and output of a
-// subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
+// Roles: warps 0 and 2 TMA (keys and queries, values), warp 1 issues the products, warp 3 looks after the values, warps 4-7 and 8-11 softmax and
+// output of a subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
 #include <string.h>
 
 #include "esp_attn_tc.cuh"
@@ -32,19 +33,17 @@ constexpr int SUB = 128;                  // pairs per subtile
 constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
 constexpr int THREADS = 384;
 constexpr int TMEM_COLS = 512;            // S0, S1, O0, O1: 128 columns each
-// Keys and values share the ring's stages in turn, but have barriers of their own that go by the chunk: whoever waits on a barrier waits for each of
-// its phases and is needed for the next one.  (With a barrier per stage the warps that look after the values were needed for every other
-// phase only, could be one phase late or early, and a wait ran out once in a thousand calls.)
-constexpr int NB = 4;                     // more chunks than the ring can hold values of
-constexpr int ODD_RING = 8;               // tiles whose note on odd values is kept: more than the ring's stages can hold values of
+constexpr int ODD_RING = 8;               // tiles whose note on odd values is kept: more than the stages can hold values of
 
 template <int D>
 struct Cfg {
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;         // 128 rows of a head
-    static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int OFF_KV = 2 * TILE_BYTES;
-    static constexpr int OFF_BAR = OFF_KV + STAGES * TILE_BYTES;
+    // Rings of their own for keys and values: whoever waits on a barrier has to see each of its phases and to be needed for the next one.  (With one
+    // ring for both, whose stages held keys and values in turn, the warps that look at the values alone lost a phase once in a thousand calls.)
+    static constexpr int KST = D == 128 ? 2 : 4, VST = D == 128 ? 3 : 4;
+    static constexpr int OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + KST * TILE_BYTES;
+    static constexpr int OFF_BAR = OFF_V + VST * TILE_BYTES;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     // kind::f16 instruction descriptors: D = f32, A = B = bf16, M = 128; Q K^T: N = 128 keys; P V: N = D, V is MN-major
     static constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -71,6 +70,69 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+
+__device__ __forceinline__ float max3_nan(float x, float y, float z) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
+    return d;
+}
+// 2^x of a pair on the FMA pipe: x = n + f, |f| <= 1/2, a polynomial of degree 5 in f (fitted for the smallest relative error with p(0) = 1:
+// 1.1e-7), n added to the exponent.  Below -126 the result stays at 2^-126.
+__device__ __forceinline__ void ex2_poly2(float& x0, float& x1) {
+    const uint64_t magic = attn::pack2(12582912.f, 12582912.f), neg_magic = attn::pack2(-12582912.f, -12582912.f), minus_one = attn::pack2(-1.f, -1.f);
+    const uint64_t x = attn::pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const uint64_t t = attn::add2(x, magic);                       // the low bits are n
+    const uint64_t f = attn::fma2(attn::add2(t, neg_magic), minus_one, x);
+    uint64_t r = attn::pack2(0.001326472731307149f, 0.001326472731307149f);
+    r = attn::fma2(r, f, attn::pack2(0.009671512991189957f, 0.009671512991189957f));
+    r = attn::fma2(r, f, attn::pack2(0.05550733581185341f, 0.05550733581185341f));
+    r = attn::fma2(r, f, attn::pack2(0.24022242426872253f, 0.24022242426872253f));
+    r = attn::fma2(r, f, attn::pack2(0.6931470036506653f, 0.6931470036506653f));
+    r = attn::fma2(r, f, attn::pack2(1.f, 1.f));
+    float t0, t1;
+    attn::unpack2(t, t0, t1);
+    attn::unpack2(r, x0, x1);
+    x0 = __int_as_float(__float_as_int(x0) + (__float_as_int(t0) << 23));
+    x1 = __int_as_float(__float_as_int(x1) + (__float_as_int(t1) << 23));
+}
+// The weights of a row's 128 scores, as bf16 over the scores' columns; their sum.  The first 64 are announced on ready[0] as soon as they stand, so that their product
+// with V runs beside the other half's exponentials.
+// WHOLE: every key is seen, and POLY of eight pairs take the FMA pipe instead of the special-function unit, which alone would need as long as the
+// tensor cores do; masked scores (-infinity) have to give exactly 0 and take the special-function unit.
+constexpr uint32_t POLY_PAIRS = 0;      // of the 16 pairs of 32 columns: 3 of 8
+template <bool WHOLE>
+__device__ __forceinline__ float weights(const uint32_t (&sv)[128], uint32_t s_addr, float scale_log2, float m_use, uint64_t* ready) {
+    const uint64_t scale2 = attn::pack2(scale_log2, scale_log2), neg_m2 = attn::pack2(-m_use, -m_use);
+    uint64_t sum2[2] = {0, 0};
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float w0, w1;
+            attn::unpack2(attn::fma2(attn::pack2(__uint_as_float(sv[b * 32 + 2 * i]), __uint_as_float(sv[b * 32 + 2 * i + 1])), scale2, neg_m2), w0, w1);
+            if (WHOLE && ((POLY_PAIRS >> i) & 1u)) {
+                ex2_poly2(w0, w1);
+            } else {
+                w0 = attn::ex2_approx(w0);
+                w1 = attn::ex2_approx(w1);
+            }
+            sum2[i & 1] = attn::add2(sum2[i & 1], attn::pack2(w0, w1));
+            const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
+            pk[i] = *reinterpret_cast<const uint32_t*>(&b2);
+        }
+        tmem_st16(s_addr + b * 16, pk);
+        if (b & 1) {
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(&ready[b >> 1]);
+        }
+    }
+    float c0, c1;
+    attn::unpack2(attn::add2(sum2[0], sum2[1]), c0, c1);
+    return c0 + c1;
 }
 
 // A chunk that some pair of the tile does not see as a whole (the last one of the cache, the diagonal, the window's edge, the tree).
@@ -106,16 +168,16 @@ template <int D>
 __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__ TcParams p) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ Deal s_deal;
-    __shared__ int s_odd[2][ODD_RING];     // [warp 2, 3] a value that some pair sees is no finite number
+    __shared__ int s_odd[ODD_RING];        // a value that some pair sees is no finite number
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* empty = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // [STAGES] the products with what it held have completed
-    uint64_t* k_full = empty + C::STAGES;                              // [NB] keys of a chunk have landed
-    uint64_t* v_full = k_full + NB;                                    // [NB] values of a chunk have landed
-    uint64_t* v_ok = v_full + NB;                                      // [NB] they have been looked after
-    uint64_t* s_full = v_ok + NB;                                      // [2] scores of a subtile's chunk
-    uint64_t* p_ready = s_full + 2;                                    // [2] its weights
-    uint64_t* o_full = p_ready + 2;                                    // [2] the piece's last P V has completed
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR); // [KST] keys of a chunk have landed
+    uint64_t* k_empty = k_full + C::KST;                               // [KST] both subtiles' Q K^T have completed
+    uint64_t* v_full = k_empty + C::KST;                               // [VST] values of a chunk have landed
+    uint64_t* v_ok = v_full + C::VST;                                  // [VST] they have been looked after
+    uint64_t* v_empty = v_ok + C::VST;                                 // [VST] both subtiles' P V have completed
+    uint64_t* s_full = v_empty + C::VST;                               // [2] scores of a subtile's chunk
+    uint64_t* p_ready = s_full + 2;                                    // [2][2] its weights, by halves of the chunk
+    uint64_t* o_full = p_ready + 4;                                    // [2] the piece's last P V has completed
     uint64_t* o_free = o_full + 2;                                     // [2] the accumulator has been read
     uint64_t* q_full = o_free + 2;
     uint64_t* q_empty = q_full + 1;
@@ -128,13 +190,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         prefetch_tensormap(&p.map_k);
         prefetch_tensormap(&p.map_v);
         prefetch_tensormap(&p.map_q);
-        for (int i = 0; i < C::STAGES; ++i) mbar_init(&empty[i], 1);
-        for (int i = 0; i < NB; ++i) { mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&v_ok[i], 2); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
+        for (int i = 0; i < C::KST; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < C::VST; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_ok[i], 1); mbar_init(&v_empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[2 * i], 4); mbar_init(&p_ready[2 * i + 1], 4); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         *s_abort = 0;
-        for (int i = 0; i < ODD_RING; ++i) s_odd[0][i] = s_odd[1][i] = 0;
+        for (int i = 0; i < ODD_RING; ++i) s_odd[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -143,55 +205,61 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     }
     pdl_launch_dependents();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    const bool any = deal<CK, false>(a, blockIdx.x, 1, &s_deal);
+    Share share;
+    Cursor c;                              // every warp deals for itself and walks its own copy
+    const bool any = deal<CK>(a, blockIdx.x, lane, share, c);
+    const uint32_t begin = any ? share.begin(blockIdx.x) : 0, end = any ? share.begin(blockIdx.x + 1) : 0;
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *s_tmem;
     unsigned char* sQ = smem;
-    unsigned char* sKV = smem + C::OFF_KV;
-    const long long begin = any ? s_deal.unit : 0, end = any ? cta_begin(s_deal.total, s_deal.ctas, blockIdx.x + 1) : 0;
+    unsigned char *sK = smem + C::OFF_K, *sV = smem + C::OFF_V;
 
     // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; a softmax thread holds its 128 scores at once
     if (warp < 4) { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 0) {
-        // ---------------- TMA: keys and values of a chunk in turn; a lane per box
-        const int n_boxes = CK / p.box_rows;
-        const int box = lane % n_boxes, half = lane / n_boxes;
-        const bool active = half < C::HALVES;
-        uint32_t it = 0, n_it = 0;      // stages filled, pieces
+    if (warp == 0 || warp == 2) {
+        // ---------------- TMA: warp 0 keys and queries, warp 2 values.  The lanes look up a chunk's pages, one lane issues box after box (a copy
+        // issued by every lane for itself runs lane by lane, at some 50 cycles each)
+        const bool is_v = warp == 2;
+        const int n_boxes = CK / p.box_rows, box = lane & (n_boxes - 1);        // (a power of two: it divides the chunk)
+        const CUtensorMap* map = is_v ? &p.map_v : &p.map_k;
+        uint32_t ch = 0, n_it = 0;      // chunks, pieces
         bool ok = true;
-        Cursor c = s_deal.at;
-        for (long long u = begin; u < end && ok; ++n_it) {
+        for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
-            for (int j = 0; j < pc.n && ok; ++j) {
+            for (int j = 0; j < pc.n; ++j, ++ch) {
                 const int pos = (pc.c0 + j) * CK + box * p.box_rows;
                 int page = a.pages.n_pages, slot = 0;       // a page that there is not reads as zeros
-                if (active && pos < c.s.kv) {
+                if (pos < c.s.kv) {
                     const int index = pos / a.pages.page_size;
                     const int pg = load_page(a.seq, a.pages, c.b, index);
                     if (pg >= 0) page = pg;
                     slot = pos - index * a.pages.page_size;
                 }
+                const uint32_t n_st = is_v ? C::VST : C::KST, st = ch % n_st;
+                if (!__all_sync(0xffffffffu, mbar_wait((is_v ? v_empty : k_empty) + st, ((ch / n_st) & 1) ^ 1, s_abort))) { ok = false; break; }
+                uint64_t* full = (is_v ? v_full : k_full) + st;
+                if (lane == 0) mbar_expect_tx(full, C::TILE_BYTES);
+                unsigned char* dst = (is_v ? sV : sK) + st * C::TILE_BYTES;
+#pragma unroll 4
+                for (int i = 0; i < n_boxes; ++i) {
+                    const int pg = __shfl_sync(0xffffffffu, page, i), sl = __shfl_sync(0xffffffffu, slot, i);
+                    if (lane == 0) {
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++it) {
-                    const int st = it % C::STAGES;
-                    if (!__all_sync(0xffffffffu, mbar_wait(&empty[st], ((it / C::STAGES) & 1) ^ 1, s_abort))) { ok = false; break; }
-                    uint64_t* full = (kv ? v_full : k_full) + (it >> 1) % NB;
-                    if (lane == 0) mbar_expect_tx(full, C::TILE_BYTES);
-                    __syncwarp();
-                    if (active) tma_load_4d(sKV + st * C::TILE_BYTES + half * HALF_BYTES + box * p.box_rows * 128, kv ? &p.map_v : &p.map_k, half * 64, slot, c.kvh, page, full);
-                    if (kv == 0 && j == 0) {                // the piece's queries behind its first keys
-                        if (!__all_sync(0xffffffffu, mbar_wait(q_empty, (n_it & 1) ^ 1, s_abort))) { ok = false; break; }
-                        if (lane == 0) {
-                            const int subs = c.x.nr > p.sub_rows ? 2 : 1;
-                            mbar_expect_tx(q_full, subs * C::HALVES * p.sub_rows * a.group * 128);
-                            for (int s = 0; s < subs; ++s)
-                                for (int h = 0; h < C::HALVES; ++h)
-                                    tma_load_3d(sQ + s * C::TILE_BYTES + h * HALF_BYTES, &p.map_q, h * 64, c.kvh * a.group, c.s.start + c.x.r0 + s * p.sub_rows, q_full);
-                        }
-                        __syncwarp();
+                        for (int h = 0; h < C::HALVES; ++h) tma_load_4d(dst + h * HALF_BYTES + i * p.box_rows * 128, map, h * 64, sl, c.kvh, pg, full);
                     }
                 }
+                if (!is_v && j == 0) {                      // the piece's queries behind its first keys
+                    if (!__all_sync(0xffffffffu, mbar_wait(q_empty, (n_it & 1) ^ 1, s_abort))) { ok = false; break; }
+                    if (lane == 0) {
+                        const int subs = c.x.nr > p.sub_rows ? 2 : 1;
+                        mbar_expect_tx(q_full, subs * C::HALVES * p.sub_rows * a.group * 128);
+                        for (int s = 0; s < subs; ++s)
+                            for (int h = 0; h < C::HALVES; ++h)
+                                tma_load_3d(sQ + s * C::TILE_BYTES + h * HALF_BYTES, &p.map_q, h * 64, c.kvh * a.group, c.s.start + c.x.r0 + s * p.sub_rows, q_full);
+                    }
+                }
+                __syncwarp();
             }
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);
@@ -200,54 +268,61 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     } else if (warp == 1) {
         // ---------------- products: the warp walks its loop as a whole, one lane issues
         const bool leader{elect_lane()};
-        const uint32_t q_addr = smem_u32(sQ), kv_addr = smem_u32(sKV);
+        const uint64_t q_desc = smem_desc(smem_u32(sQ), 16), k_desc = smem_desc(smem_u32(sK), 16), v_desc = smem_desc(smem_u32(sV), HALF_BYTES);
         uint32_t ch = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // chunks, pieces, chunks and pieces of each subtile
         bool ok = true;
-        Cursor c = s_deal.at;
-        for (long long u = begin; u < end && ok; ++n_it) {
+        auto issue_qk = [&](int s, int st) {
+            uint64_t da = q_desc + (uint32_t)(s * C::TILE_BYTES >> 4), db = k_desc + (uint32_t)(st * C::TILE_BYTES >> 4);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                if (leader) umma(tmem_base + s * 128, da, db, C::IDESC_QK, kk > 0 ? 1u : 0u);
+                const uint32_t step = kk == 3 ? (HALF_BYTES - 96) >> 4 : 32 >> 4;      // the next 32 bytes of the row, or the row in the other half
+                da += step;
+                db += step;
+            }
+            if (leader) umma_commit(&s_full[s]);
+        };
+        for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int subs = c.x.nr > p.sub_rows ? 2 : 1;
-            auto issue_qk = [&](int s, int st) {
-                const uint32_t k_addr = kv_addr + st * C::TILE_BYTES, qa = q_addr + s * C::TILE_BYTES;
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
-                    if (leader) umma(tmem_base + s * 128, smem_desc(qa + off, 16), smem_desc(k_addr + off, 16), C::IDESC_QK, kk > 0 ? 1u : 0u);
-                }
-                if (leader) umma_commit(&s_full[s]);
-            };
-            ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&k_full[ch % NB], (ch / NB) & 1, s_abort));
+            ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&k_full[ch % C::KST], (ch / C::KST) & 1, s_abort));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int s = 0; s < subs; ++s) issue_qk(s, 2 * ch % C::STAGES);
-            if (leader) umma_commit(&empty[2 * ch % C::STAGES]);
+            for (int s = 0; s < subs; ++s) issue_qk(s, ch % C::KST);
+            if (leader) umma_commit(&k_empty[ch % C::KST]);
             if (leader && pc.n == 1) umma_commit(q_empty);
             for (int j = 0; j < pc.n && ok; ++j, ++ch) {
-                const uint32_t vs = (2 * ch + 1) % C::STAGES, ks = (2 * ch + 2) % C::STAGES;     // stages of this chunk's values, of the next one's keys
+                const uint32_t vs = ch % C::VST, ks = (ch + 1) % C::KST;     // stages of this chunk's values, of the next one's keys
+                const bool more = j + 1 < pc.n;
                 for (int s = 0; s < subs && ok; ++s) {
                     const uint32_t g = s ? g1 : g0, np = s ? pieces1 : pieces0;
-                    ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[s], (g + j) & 1, s_abort) &&
-                                                     (s > 0 || mbar_wait(&v_ok[ch % NB], (ch / NB) & 1, s_abort)) &&
-                                                     (j > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)));
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t v_addr = kv_addr + vs * C::TILE_BYTES;
+                    uint64_t db = v_desc + (uint32_t)(vs * C::TILE_BYTES >> 4);
+                    uint32_t pa = tmem_base + s * 128;
 #pragma unroll
-                    for (int kk = 0; kk < CK / 16; ++kk)
-                        if (leader) umma_ta(tmem_base + 256 + s * 128, tmem_base + s * 128 + kk * 8, smem_desc(v_addr + kk * 16 * 128, HALF_BYTES), C::IDESC_PV,
-                                            (j > 0 || kk > 0) ? 1u : 0u);
-                    if (leader && s == subs - 1) umma_commit(&empty[vs]);
-                    if (leader && j == pc.n - 1) umma_commit(&o_full[s]);
-                    if (j + 1 < pc.n) {
-                        if (s == 0) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(&k_full[(ch + 1) % NB], ((ch + 1) / NB) & 1, s_abort));
-                            if (!ok) break;
-                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        }
-                        issue_qk(s, ks);
-                        if (leader && s == subs - 1) umma_commit(&empty[ks]);
-                        if (leader && s == subs - 1 && j + 2 == pc.n) umma_commit(q_empty);
+                    for (int hf = 0; hf < 2 && ok; ++hf) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[2 * s + hf], (g + j) & 1, s_abort) &&
+                                                         (s + hf > 0 || mbar_wait(&v_ok[vs], (ch / C::VST) & 1, s_abort)) &&
+                                                         (j + hf > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)));
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                        for (int kk = 0; kk < CK / 32; ++kk, pa += 8, db += 16 * 128 >> 4)
+                            if (leader) umma_ta(tmem_base + 256 + s * 128, pa, db, C::IDESC_PV, (j + hf + kk > 0) ? 1u : 0u);
                     }
+                    if (!ok) break;
+                    if (leader && s == subs - 1) umma_commit(&v_empty[vs]);
+                    if (!more) {
+                        if (leader) umma_commit(&o_full[s]);
+                        continue;
+                    }
+                    if (s == 0) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(&k_full[ks], ((ch + 1) / C::KST) & 1, s_abort));
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    }
+                    issue_qk(s, ks);
+                    if (leader && s == subs - 1) umma_commit(&k_empty[ks]);
+                    if (leader && s == subs - 1 && j + 2 == pc.n) umma_commit(q_empty);
                 }
             }
             g0 += pc.n;
@@ -261,40 +336,51 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
         uint32_t ch = 0, n_it = 0;
         bool ok = true;
-        Cursor c = s_deal.at;
-        for (long long u = begin; u < end && ok; ++n_it) {
+        MergeDesc desc;
+        desc.parts = 0;
+        for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
-            if (lane == 0) s_odd[warp - 2][(n_it + 1) % ODD_RING] = 0;
+            if (pc.slot >= 0 && pc.c0 == c.x.c0) desc = make_desc(a, c, share, pc, blockIdx.x);
+            if (lane == 0) s_odd[(n_it + 1) % ODD_RING] = 0;
             for (int j = 0; j < pc.n; ++j, ++ch) {
-                const int st = (2 * ch + 1) % C::STAGES, p0 = (pc.c0 + j) * CK;
-                if (!__all_sync(0xffffffffu, mbar_wait(&v_full[ch % NB], (ch / NB) & 1, s_abort))) { ok = false; break; }
+                const int st = ch % C::VST, p0 = (pc.c0 + j) * CK;
+                if (!__all_sync(0xffffffffu, mbar_wait(&v_full[st], (ch / C::VST) & 1, s_abort))) { ok = false; break; }
                 if (is_edge(a, c, p0)) {
-                    // a lane takes every other row of 16 bytes; its key follows from the row
+                    uint4* tile = reinterpret_cast<uint4*>(sV + st * C::TILE_BYTES);
+                    uint32_t seen = 0;          // an exponent of all ones carries into its sign bit
+#pragma unroll 8
+                    for (int i = lane; i < C::TILE_BYTES / 16; i += 32) {
+                        const uint4 x = tile[i];
+                        seen |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) | ((x.z & 0x7f807f80u) + 0x00800080u) |
+                                ((x.w & 0x7f807f80u) + 0x00800080u);
+                    }
                     bool odd = false;
-                    for (int i = (warp - 2) * 32 + lane; i < C::TILE_BYTES / 16; i += 64) {
-                        uint4* at = reinterpret_cast<uint4*>(sKV + st * C::TILE_BYTES) + i;
-                        uint4 x = *at;
-                        uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-                        bool here = false;
+                    if (seen & 0x80008000u) {
+                        for (int i = lane; i < C::TILE_BYTES / 16; i += 32) {
+                            uint4 x = tile[i];
+                            uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+                            bool here = false;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; here = true; }
-                            if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0x0000ffffu; here = true; }
-                        }
-                        if (here) {
-                            *at = x;
-                            odd = odd || p0 + ((i >> 3) & 127) < c.s.kv;
+                            for (int e = 0; e < 4; ++e) {
+                                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; here = true; }
+                                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0x0000ffffu; here = true; }
+                            }
+                            if (here) {
+                                tile[i] = x;
+                                odd = odd || p0 + ((i >> 3) & 127) < c.s.kv;
+                            }
                         }
                     }
-                    if (odd) s_odd[warp - 2][n_it % ODD_RING] = 1;
+                    if (odd) s_odd[n_it % ODD_RING] = 1;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                if (lane == 0) mbar_arrive(&v_ok[ch % NB]);
+                if (lane == 0) mbar_arrive(&v_ok[st]);
             }
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);
         }
+        if (lane == 0) a.desc[blockIdx.x] = desc;
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
     } } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -303,8 +389,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         const uint32_t s_addr = tmem_base + ((uint32_t)(q4 * 32) << 16) + sub * 128, o_addr = s_addr + 256;
         uint32_t g = 0, np = 0, n_it = 0;
         bool ok = true;
-        Cursor c = s_deal.at;
-        for (long long u = begin; u < end && ok; ++n_it) {
+        for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int L = c.s.kv - c.s.n;
             if (sub == 0 || c.x.nr > p.sub_rows) {
@@ -325,7 +410,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         const int p0 = (pc.c0 + j) * CK;
                         uint32_t sv[128];
                         tmem_ld128(s_addr, sv);
-                        if (!__all_sync(0xffffffffu, p0 >= mask.lo && p0 + CK <= mask.hi)) {
+                        const bool whole = __all_sync(0xffffffffu, p0 >= mask.lo && p0 + CK <= mask.hi);
+                        if (!whole) {
                             uint32_t w[4];
                             chunk_bits(mask, p0, L, c.s.n, w);
 #pragma unroll
@@ -335,59 +421,43 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
 #pragma unroll
                         for (int i = 0; i < 128; i += 8)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) m4[e] = fmaxf(fmaxf(m4[e], __uint_as_float(sv[i + 2 * e])), __uint_as_float(sv[i + 2 * e + 1]));
-                        const float cmax = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
-                        const bool move = m_run == -INFINITY ? cmax != -INFINITY : cmax - m_run > 8.f;
+                            for (int e = 0; e < 4; ++e) m4[e] = max3_nan(m4[e], __uint_as_float(sv[i + 2 * e]), __uint_as_float(sv[i + 2 * e + 1]));
+                        float cmax = max3_nan(m4[0], m4[1], max3_nan(m4[2], m4[3], m4[3])) * a.scale_log2;
+                        // a logit that is no number or +infinity makes the whole row undefined, and so does a reference that is no number
+                        if (!(cmax < INFINITY)) cmax = __int_as_float(0x7fffffff);
+                        const bool move = m_run == -INFINITY ? cmax != -INFINITY : !(cmax - m_run <= 8.f);
                         const float m_new = move ? cmax : m_run;
                         const float m_use = m_new == -INFINITY ? 0.f : m_new;
                         const float alpha = m_run == m_use ? 1.f : exp2f(m_run - m_use);
-                        const uint64_t scale2 = attn::pack2(a.scale_log2, a.scale_log2), neg_m2 = attn::pack2(-m_use, -m_use);
-                        uint64_t sum2[2] = {0, 0};
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            uint32_t pk[16];
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                float w0, w1;
-                                attn::unpack2(attn::fma2(attn::pack2(__uint_as_float(sv[b * 32 + i]), __uint_as_float(sv[b * 32 + i + 1])), scale2, neg_m2), w0, w1);
-                                w0 = attn::ex2_approx(w0);
-                                w1 = attn::ex2_approx(w1);
-                                sum2[(i >> 1) & 1] = attn::add2(sum2[(i >> 1) & 1], attn::pack2(w0, w1));
-                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
-                                pk[i >> 1] = *reinterpret_cast<const uint32_t*>(&b2);
-                            }
-                            tmem_st16(s_addr + b * 16, pk);
-                        }
-                        float c0, c1;
-                        attn::unpack2(attn::add2(sum2[0], sum2[1]), c0, c1);
-                        l_run = fmaf(l_run, alpha, c0 + c1);
-                        m_run = m_new;
                         if (j > 0 && __any_sync(0xffffffffu, move)) {
-                            // O <- O * 2^(old - new); S arriving said that O is complete.  (Here, where the scores' registers are free again)
+                            // O <- O * 2^(old - new); S arriving said that O is complete
 #pragma unroll
-                            for (int b = 0; b < D / 32; ++b) {
-                                uint32_t o[32];
-                                tmem_ld32(o_addr + b * 32, o);
+                            for (int b = 0; b < D / 16; ++b) {
+                                uint32_t o[16];
+                                tmem_ld16_issue(o_addr + b * 16, o);
+                                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tmem_st32(o_addr + b * 32, o);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st16(o_addr + b * 16, o);
                             }
                         }
-                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                        const float csum = whole ? weights<true>(sv, s_addr, a.scale_log2, m_use, &p_ready[2 * sub]) : weights<false>(sv, s_addr, a.scale_log2, m_use, &p_ready[2 * sub]);
+                        l_run = fmaf(l_run, alpha, csum);
+                        m_run = m_new;
+                    } else {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) { mbar_arrive(&p_ready[2 * sub]); mbar_arrive(&p_ready[2 * sub + 1]); }
                     }
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_ready[sub]);
                 }
                 if (!ok) break;
                 if (!__all_sync(0xffffffffu, mbar_wait(&o_full[sub], np & 1, s_abort))) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 ++np;
                 if (live) {
-                    const bool odd = (*reinterpret_cast<volatile int*>(&s_odd[0][n_it % ODD_RING]) | *reinterpret_cast<volatile int*>(&s_odd[1][n_it % ODD_RING])) != 0;
+                    const bool odd = *reinterpret_cast<volatile int*>(&s_odd[n_it % ODD_RING]) != 0;
                     const int token = c.s.start + c.x.r0 + trow;
                     const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-                    const size_t at = ((size_t)blockIdx.x * 2 + (pc.slot < 0 ? 0 : pc.slot)) * a.pairs + pair;
 #pragma unroll 1
                     for (int b = 0; b < D / 32; ++b) {
                         uint32_t o[32];
@@ -430,10 +500,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         } else if (valid) {
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
-                                *reinterpret_cast<uint4*>(a.part_o + at * D + b * 32 + i * 4) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                                *reinterpret_cast<uint4*>(a.part_o + part_quad(a, blockIdx.x, pc.slot, b * 8 + i, pair)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                         }
                     }
-                    if (valid && pc.slot >= 0) a.part_ml[at] = make_float2(m_run, l_run);
+                    if (valid && pc.slot >= 0) a.part_ml[part_row(a, blockIdx.x, pc.slot, pair)] = make_float2(m_run, l_run);
                     if (valid && pc.slot < 0 && a.lse) a.lse[(size_t)token * a.Hq + head] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * 0.6931471805599453f;
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -515,7 +585,7 @@ int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s) {
     p.out_vec = reinterpret_cast<uintptr_t>(a.out.p) % 16 == 0 && a.out.tok % 8 == 0 && a.out.head % 8 == 0;
     p.a = a;
     const int rc = a.D == 128 ? run_tc<128>(p, s) : run_tc<64>(p, s);
-    return rc ? rc : launch_paged_merge(1, a, CK, 1, s);
+    return rc ? rc : launch_paged_merge(1, a, s);
 }
 
 }  // namespace esp
