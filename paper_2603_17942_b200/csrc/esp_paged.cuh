@@ -251,5 +251,19 @@ __device__ __forceinline__ bool sees(const RowMask& m, int pos, int L, int kv) {
 // where pair p of the tile's (token, head) pairs goes
 __device__ __forceinline__ size_t out_offset(const HeadsView& v, int token, int head) { return (size_t)((long long)token * v.tok + (long long)head * v.head); }
 
+template <typename T>
+__device__ __forceinline__ void store4(T* y, const float4& x, bool vec) {
+    if constexpr (sizeof(T) == 4) {
+        if (vec) { *reinterpret_cast<float4*>(y) = x; return; }
+    } else {
+        if (vec) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
+            *reinterpret_cast<uint2*>(y) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            return;
+        }
+    }
+    y[0] = from_f32<T>(x.x); y[1] = from_f32<T>(x.y); y[2] = from_f32<T>(x.z); y[3] = from_f32<T>(x.w);
+}
+
 }  // namespace paged
 }  // namespace esp

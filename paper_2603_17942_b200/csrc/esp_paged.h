@@ -71,6 +71,10 @@ void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStr
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s);
 bool paged_tc_supported(int dtype, const PagedAttnArgs& a);
 int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s);
+bool paged_tma_pages(const PagedAttnArgs& a, int chunk, int* box_rows);      // boxes of *box_rows slots can be copied
+bool paged_few_supported(int dtype, const PagedAttnArgs& a);
+int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s);
+int launch_paged_merge_few(int dtype, const PagedAttnArgs& a, cudaStream_t s);   // tiles of at most 16 pairs
 int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s);
 
 }  // namespace esp

@@ -268,7 +268,9 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     a.out_vec = by4(a.out.p, a.out.tok, a.out.head, 0);
     a.vec = by4(a.q.p, a.q.tok, a.q.head, 0) && by4(a.pages.k, a.pages.page, a.pages.tok, a.pages.head) && by4(a.pages.v, 0, 0, 0);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const int rc = paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s) : launch_paged_simt(cache->dtype, a, n_sm, s);
+    const int rc = paged_few_supported(cache->dtype, a)  ? launch_paged_few(a, n_sm, s)
+                   : paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s)
+                                                         : launch_paged_simt(cache->dtype, a, n_sm, s);
     if (rc) return ESP_E_CUDA;
     return cuda_ok(cudaGetLastError());
 }

@@ -33,19 +33,6 @@ __device__ __forceinline__ float4 load4(const T* x) {
         return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
     }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T* y, const float4& x, bool vec) {
-    if constexpr (sizeof(T) == 4) {
-        if (vec) { *reinterpret_cast<float4*>(y) = x; return; }
-    } else {
-        if (vec) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
-            *reinterpret_cast<uint2*>(y) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-            return;
-        }
-    }
-    y[0] = from_f32<T>(x.x); y[1] = from_f32<T>(x.y); y[2] = from_f32<T>(x.z); y[3] = from_f32<T>(x.w);
-}
 __device__ __forceinline__ bool finite4(const float4& x) { return isfinite(x.x) && isfinite(x.y) && isfinite(x.z) && isfinite(x.w); }
 
 template <typename T, int D, int MP, bool VEC>
@@ -232,7 +219,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
 
 // The tile whose first piece CTA c has as its last one (c = blockIdx.x), if other CTAs have the rest: the partials are weighed by 2^(m - max m) in the
 // order of the CTAs.  A lane takes four quads of one pair; a warp has LP pairs side by side, as the partials lie.
-constexpr int MERGE_WARPS = 8, MERGE_QUADS = 4;
+constexpr int MERGE_WARPS = 8, MERGE_QUADS = 4, MERGE_PARTS = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge(const __grid_constant__ PagedAttnArgs a) {
@@ -246,28 +233,43 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge(const __grid_c
     if (n == 0 || pr >= n_pairs || q0 >= D / 4) return;
     // CTA c has the tile's first piece in slot 0 if the tile is where it starts; the CTAs behind it have theirs in slot 0
     const float2* ml = a.part_ml + part_row(a, c, 0, pr);
+    // (loads of several parts are under way at once: a part at a time, every one is a round trip)
+    auto slot_of = [&](int k) { return 2 * k + (k == 0 ? first_slot : 0); };
     float m = -INFINITY;
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(ml + (size_t)(2 * k + (k == 0 ? first_slot : 0)) * a.pairs).x);
+    for (int k0 = 0; k0 < n; k0 += 8) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __ldcg(ml + (size_t)slot_of(min(k0 + e, n - 1)) * a.pairs).x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, x[e]);
+    }
     const float m_use = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     float4 o[MERGE_QUADS];
 #pragma unroll
     for (int i = 0; i < MERGE_QUADS; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (int k = 0; k < n; ++k) {
-        const int sl = 2 * k + (k == 0 ? first_slot : 0);
-        const float2 x = __ldcg(ml + (size_t)sl * a.pairs);
-        float4 v[MERGE_QUADS];
+    const size_t part = (size_t)(D / 4) * a.pairs;
+    const float4* po = a.part_o + part_quad(a, c, 0, q0, pr);
+    for (int k0 = 0; k0 < n; k0 += MERGE_PARTS) {
+        float2 x[MERGE_PARTS];
+        float4 v[MERGE_PARTS][MERGE_QUADS];
 #pragma unroll
-        for (int i = 0; i < MERGE_QUADS; ++i)
-            v[i] = q0 + i * LQ < D / 4 ? __ldcg(a.part_o + part_quad(a, c, sl, q0 + i * LQ, pr)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float w = exp2f(x.x - m_use);
-        l = fmaf(x.y, w, l);
+        for (int e = 0; e < MERGE_PARTS; ++e) {
+            const int sl = slot_of(min(k0 + e, n - 1));
+            x[e] = __ldcg(ml + (size_t)sl * a.pairs);
 #pragma unroll
-        for (int i = 0; i < MERGE_QUADS; ++i) {
-            o[i].x = fmaf(v[i].x, w, o[i].x); o[i].y = fmaf(v[i].y, w, o[i].y);
-            o[i].z = fmaf(v[i].z, w, o[i].z); o[i].w = fmaf(v[i].w, w, o[i].w);
+            for (int i = 0; i < MERGE_QUADS; ++i) v[e][i] = __ldcg(po + sl * part + (q0 + i * LQ < D / 4 ? i * LQ : 0) * a.pairs);
+        }
+#pragma unroll
+        for (int e = 0; e < MERGE_PARTS; ++e) {
+            if (k0 + e >= n) break;
+            const float w = exp2f(x[e].x - m_use);
+            l = fmaf(x[e].y, w, l);
+#pragma unroll
+            for (int i = 0; i < MERGE_QUADS; ++i) {
+                o[i].x = fmaf(v[e][i].x, w, o[i].x); o[i].y = fmaf(v[e][i].y, w, o[i].y);
+                o[i].z = fmaf(v[e][i].z, w, o[i].z); o[i].w = fmaf(v[e][i].w, w, o[i].w);
+            }
         }
     }
     const int row = pr / a.group, head = head0 + pr - row * a.group;
@@ -319,8 +321,10 @@ int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {
     a.rows = a.pairs / a.group;
     if (a.rows < 1) return -1;                      // more than 64 query heads share a KV head
     a.n_cta = n_sm * (a.pairs == 16 ? 4 : 2);
+    a.min_units = 2;
     const int rc = dtype == 0 ? run_simt_t<float>(a, s) : run_simt_t<__nv_bfloat16>(a, s);
-    return rc ? rc : launch_paged_merge(dtype, a, s);
+    if (rc) return rc;
+    return a.pairs <= 16 ? launch_paged_merge_few(dtype, a, s) : launch_paged_merge(dtype, a, s);
 }
 
 }  // namespace esp
