@@ -349,41 +349,49 @@ def _need(ok: bool, where: str, what: str):
         raise EspError(-8, f"{where} ({what})")
 
 
-def _device(where: str) -> int:
-    import torch
-    _need(torch.cuda.is_available(), where, "no CUDA device")
-    return torch.cuda.current_device()
+_torch = None
+_DTYPES: Dict[object, int] = {}        # torch dtype -> dtype of the library
+
+
+def _on_current_device(device: int, where: str):
+    """The tensors' device (their get_device()) has to be the current one: the library launches there."""
+    global _torch
+    if _torch is None:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1})
+        _torch = torch
+    if device < 0 or device != _torch.cuda.current_device():
+        raise EspError(-8, f"{where} (tensors on device {device}, which is not the current one)")
 
 
 def esp_rope_table(rope: esp_rope_cfg, table, stream=None):
     """Fills `table` (a CUDA tensor of esp_rope_table_bytes bytes or more), once per configuration."""
-    _need(table.get_device() == _device("esp_rope_table") and table.is_contiguous(), "esp_rope_table", "table: another device, or not dense")
+    _on_current_device(table.get_device(), "esp_rope_table")
+    _need(table.is_contiguous(), "esp_rope_table", "table: not dense")
     _check(load_library().esp_rope_table(ctypes.byref(rope), table.data_ptr(), table.numel() * table.element_size(), _stream(stream)), "esp_rope_table")
 
 
 def _stream(stream):
-    return getattr(stream, "cuda_stream", stream)
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
-_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1}
-
-
-def _heads(x, like, where: str, name: str) -> esp_heads:
-    """x [tokens, heads, head_dim] as esp_heads; `like`: (tokens, head_dim, dtype, device) it has to have."""
+def _heads(x, tokens: int, dim: int, dtype, device: int, where: str, name: str):
+    """x [tokens, heads, head_dim] as a reference to an esp_heads; None stays None.  (A call per layer: nothing here is formatted unless it fails.)"""
+    if x is None:
+        return None
     shape, stride = x.shape, x.stride()
-    if not (len(shape) == 3 and shape[0] == like[0] and shape[2] == like[1] and (stride[2] == 1 or shape[2] == 1) and x.dtype == like[2] and
-            x.get_device() == like[3]):
-        raise EspError(-8, f"{where} ({name}: {tuple(shape)} {x.dtype} on {x.device}, strides {stride}; wanted [{like[0]}, heads, {like[1]}] "
-                           f"{like[2]} on device {like[3]}, last dimension dense)")
-    return esp_heads(x.data_ptr(), stride[0], stride[1], shape[1])
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or x.dtype is not dtype or x.get_device() != device or (stride[2] != 1 and dim != 1):
+        raise EspError(-8, f"{where} ({name}: {tuple(shape)} {x.dtype} on {x.device}, strides {stride}; wanted [{tokens}, heads, {dim}] {dtype} on device {device}, "
+                           f"last dimension dense)")
+    return ctypes.byref(esp_heads(x.data_ptr(), stride[0], stride[1], shape[1]))
 
 
-def _vector(x, n: int, dtype, device: int, where: str, name: str):
+def _vector(x, n: int, dtypes, device: int, where: str, name: str):
     """Address of a dense tensor of n elements (None: NULL)."""
     if x is None:
         return None
-    if not (x.numel() == n and x.is_contiguous() and str(x.dtype) in (dtype if isinstance(dtype, tuple) else (dtype,)) and x.get_device() == device):
-        raise EspError(-8, f"{where} ({name}: {tuple(x.shape)} {x.dtype} on {x.device}; wanted {n} dense elements of {dtype} on device {device})")
+    if x.numel() != n or x.dtype not in dtypes or x.get_device() != device or not x.is_contiguous():
+        raise EspError(-8, f"{where} ({name}: {tuple(x.shape)} {x.dtype} on {x.device}; wanted {n} dense elements of {dtypes} on device {device})")
     return x.data_ptr()
 
 
@@ -395,12 +403,12 @@ class PagedCache:
         where = "PagedCache"
         _need(order in ("head", "token"), where, f"order {order!r}")
         _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device, where, "k and v differ")
-        _need(str(k.dtype) in _DTYPES and (k.stride(3) == 1 or k.shape[3] == 1), where, "type, or last dimension not dense")
+        _need(str(k.dtype) in ("torch.float32", "torch.bfloat16") and (k.stride(3) == 1 or k.shape[3] == 1), where, "type, or last dimension not dense")
         h, s = (1, 2) if order == "head" else (2, 1)
         self.k, self.v, self.order = k, v, order
         self.dtype, self.device, self.head_dim = k.dtype, k.get_device(), k.shape[3]
         self.c = esp_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(s), k.stride(h), k.shape[0], k.shape[s], k.shape[h], k.shape[3],
-                                 _DTYPES[str(k.dtype)])
+                                 0 if str(k.dtype) == "torch.float32" else 1)
         self.ref = ctypes.byref(self.c)
 
 
@@ -429,15 +437,18 @@ def esp_qk_norm_rope(q, k, q_out, k_out, rope: Optional[esp_rope_cfg] = None, ro
                      stream=None):
     """Per-head RMSNorm (where a gain is given) and rotation (where `rope` is) of q and k into q_out and k_out; one pair may be None."""
     where = "esp_qk_norm_rope"
-    x = q if q is not None else k
-    _need(x is not None and x.dim() == 3 and str(x.dtype) in _DTYPES, where, "q or k [tokens, heads, head_dim], fp32 or bf16")
-    like = (x.shape[0], x.shape[2], x.dtype, _device(where))
-    views = [None if t is None else ctypes.byref(_heads(t, like, where, n)) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
-    dt = str(x.dtype)
+    x = k if q is None else q
+    _need(x is not None and x.dim() == 3, where, "q or k [tokens, heads, head_dim]")
+    dev = x.get_device()
+    _on_current_device(dev, where)
+    n, _, d = x.shape
+    dt = x.dtype
+    _need(dt in _DTYPES, where, "fp32 or bf16")
     _check(load_library().esp_qk_norm_rope(
-        _DTYPES[dt], like[0], like[1], views[0], views[1], _vector(q_gain, like[1], dt, like[3], where, "q_gain"),
-        _vector(k_gain, like[1], dt, like[3], where, "k_gain"), eps, None if rope is None else ctypes.byref(rope),
-        _table(rope, rope_table, like[3], where), _vector(positions, like[0], "torch.int32", like[3], where, "positions"), views[2], views[3], _stream(stream)), where)
+        _DTYPES[dt], n, d, _heads(q, n, d, dt, dev, where, "q"), _heads(k, n, d, dt, dev, where, "k"), _vector(q_gain, d, (dt,), dev, where, "q_gain"),
+        _vector(k_gain, d, (dt,), dev, where, "k_gain"), eps, None if rope is None else ctypes.byref(rope), _table(rope, rope_table, dev, where),
+        _vector(positions, n, (_torch.int32,), dev, where, "positions"), _heads(q_out, n, d, dt, dev, where, "q_out"),
+        _heads(k_out, n, d, dt, dev, where, "k_out"), _stream(stream)), where)
 
 
 def _table(rope, table, device: int, where: str):
@@ -451,15 +462,15 @@ def esp_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Optional[
                      q_out=None, q_gain=None, eps: float = 1e-6, stream=None):
     """Appends the new tokens' k (normed and rotated as asked) and v to the pages; with q, norms and rotates the queries into q_out in the same launch."""
     where = "esp_paged_append"
-    dev = _device(where)
-    _need(cache.device == dev and batch.device == dev, where, "cache and batch on the current device")
-    like = (k.shape[0], cache.head_dim, cache.dtype, dev)
-    views = [None if t is None else ctypes.byref(_heads(t, like, where, n)) for t, n in ((k, "k"), (v, "v"), (q, "q"), (q_out, "q_out"))]
-    dt = str(cache.dtype)
+    dev, dt, d = cache.device, cache.dtype, cache.head_dim
+    _on_current_device(dev, where)
+    _need(batch.device == dev, where, "cache and batch on one device")
+    n = k.shape[0]
     _check(load_library().esp_paged_append(
-        like[0], cache.ref, batch.ref, views[0], views[1], views[2], _vector(q_gain, like[1], dt, dev, where, "q_gain"),
-        _vector(k_gain, like[1], dt, dev, where, "k_gain"), eps, None if rope is None else ctypes.byref(rope), _table(rope, rope_table, dev, where),
-        _vector(positions, like[0], "torch.int32", dev, where, "positions"), views[3], _stream(stream)), where)
+        n, cache.ref, batch.ref, _heads(k, n, d, dt, dev, where, "k"), _heads(v, n, d, dt, dev, where, "v"), _heads(q, n, d, dt, dev, where, "q"),
+        _vector(q_gain, d, (dt,), dev, where, "q_gain"), _vector(k_gain, d, (dt,), dev, where, "k_gain"), eps,
+        None if rope is None else ctypes.byref(rope), _table(rope, rope_table, dev, where), _vector(positions, n, (_torch.int32,), dev, where, "positions"),
+        _heads(q_out, n, d, dt, dev, where, "q_out"), _stream(stream)), where)
 
 
 def esp_paged_attention_scratch_bytes(n_q_heads: int, head_dim: int) -> int:
@@ -472,14 +483,15 @@ def esp_paged_attention(cache: PagedCache, batch: PagedBatch, q, out, scratch, s
                         stream=None):
     """Attention of the new tokens over the pages into `out`: causal, with a window, or with the ancestor masks `anc` [tokens, 2] (64-bit words) of draft trees."""
     where = "esp_paged_attention"
-    dev = _device(where)
-    _need(cache.device == dev and batch.device == dev and scratch.get_device() == dev, where, "cache, batch and scratch on the current device")
-    _need(scratch.numel() * scratch.element_size() >= scratch_bytes, where, "scratch_bytes")
-    like = (q.shape[0], cache.head_dim, cache.dtype, dev)
-    hq, ho = _heads(q, like, where, "q"), _heads(out, like, where, "out")
+    dev, dt, d = cache.device, cache.dtype, cache.head_dim
+    _on_current_device(dev, where)
+    _need(batch.device == dev and scratch.get_device() == dev, where, "cache, batch and scratch on one device")
+    _need(scratch.numel() * scratch.element_size() >= scratch_bytes and scratch.is_contiguous(), where, "scratch_bytes")
+    n = q.shape[0]
     _check(load_library().esp_paged_attention(
-        like[0], cache.ref, batch.ref, ctypes.byref(hq), _vector(anc, 2 * like[0], ("torch.int64", "torch.uint64"), dev, where, "anc"), window, scale,
-        ctypes.byref(ho), _vector(lse, like[0] * hq.n_heads, "torch.float32", dev, where, "lse"), scratch.data_ptr(), scratch_bytes, _stream(stream)), where)
+        n, cache.ref, batch.ref, _heads(q, n, d, dt, dev, where, "q"), _vector(anc, 2 * n, (_torch.int64, _torch.uint64), dev, where, "anc"), window, scale,
+        _heads(out, n, d, dt, dev, where, "out"), None if lse is None else _vector(lse, n * q.shape[1], (_torch.float32,), dev, where, "lse"),
+        scratch.data_ptr(), scratch_bytes, _stream(stream)), where)
 
 
 def esp_paged_status(batch: PagedBatch, stream=None) -> int:
