@@ -132,161 +132,192 @@ __global__ void __launch_bounds__(ANY_WARPS * 32) k_norm_rope_any(const __grid_c
     }
 }
 
-// Heads of 32, 64, 128 or 256 elements on 16 bytes (rotated halves of whole groups of eight): a lane has eight neighbouring elements, LH lanes a
-// head, a block a token or some of its heads.  Memory bounds it, so the loads of all of a thread's heads (the same elements of each)
-// are requested first; while they are on their way one warp looks up the token's slot and the others turn its angles, once for all heads.
-constexpr int ROPE_ROUNDS = 4;          // heads of a thread
+// Heads of 32, 64, 128 or 256 elements on 16 bytes (rotated halves of whole groups of four): a lane has four pairs of a head, LH lanes a
+// head, a block a few tokens or some heads of one; a thread has the same pairs of up to ROUNDS heads of its token.  In halves the
+// lane's elements are four neighbours of each half, so that both members of a pair are its own; what is not rotated is halved likewise.
+// Memory bounds it, next to it the instructions (a lane that had eight neighbours and its partners' values by shuffle needed 333 per eight
+// elements and 65 us for 8192 tokens of 40 heads of 128), so the loads of all of a thread's heads are requested first; while they are on
+// their way the tokens' slots are looked up, a warp for each, and their angles turned, once for all heads.
 constexpr int ROPE_THREADS = 384;       // threads of a block at most
+constexpr int ROPE_PAIRS = 1024;        // angles a block keeps
+constexpr int ROPE_TOKENS = 16;         // tokens of a block at most
+template <typename T> constexpr int ROPE_ROUNDS = sizeof(T) == 2 ? 4 : 2;      // heads of a thread: 64 bytes under way
 
-template <typename T> struct Vec8;
-template <> struct Vec8<__nv_bfloat16> {
-    uint4 x;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = x; }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+template <typename T> struct Vec4;
+template <> struct Vec4<__nv_bfloat16> {
+    uint2 x;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint2*>(p) = x; }
+    __device__ __forceinline__ void get(float (&v)[4]) const {
+        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
+        v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
     }
-    __device__ __forceinline__ void set(const float (&v)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&b); }
-        x = make_uint4(w[0], w[1], w[2], w[3]);
+    __device__ __forceinline__ void set(const float (&v)[4]) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+        x = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
     }
 };
-template <> struct Vec8<float> {
-    float4 x, y;
-    __device__ __forceinline__ void load(const float* p) { x = reinterpret_cast<const float4*>(p)[0]; y = reinterpret_cast<const float4*>(p)[1]; }
-    __device__ __forceinline__ void store(float* p) const { reinterpret_cast<float4*>(p)[0] = x; reinterpret_cast<float4*>(p)[1] = y; }
-    __device__ __forceinline__ void get(float (&v)[8]) const { v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w; }
-    __device__ __forceinline__ void set(const float (&v)[8]) { x = make_float4(v[0], v[1], v[2], v[3]); y = make_float4(v[4], v[5], v[6], v[7]); }
+template <> struct Vec4<float> {
+    float4 x;
+    __device__ __forceinline__ void load(const float* p) { x = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = x; }
+    __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
+    __device__ __forceinline__ void set(const float (&v)[4]) { x = make_float4(v[0], v[1], v[2], v[3]); }
 };
 
-template <typename T, int LH, bool APPEND>
-__global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(const __grid_constant__ NormRopeArgs a, int heads_per_block) {
-    __shared__ float2 turn[LH * 4];     // the token's pairs
-    __shared__ Slot s_slot;
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l = tid % LH;
-    const int h0 = blockIdx.y * heads_per_block, n_heads = min(heads_per_block, a.q.n + a.k.n + a.v.n - h0), per_round = blockDim.x / LH;
-    Vec8<T> x[ROPE_ROUNDS];
+template <typename T, int LH, bool APPEND, bool INTER>
+__global__ void __launch_bounds__(ROPE_THREADS, 3) k_norm_rope(const __grid_constant__ NormRopeArgs a, int heads_per_block, int heads_per_round, int tokens_per_block) {
+    constexpr int ROUNDS = ROPE_ROUNDS<T>, D = LH * 8;
+    __shared__ __align__(16) float2 s_turn[ROPE_PAIRS];       // [token of the block][pair]
+    __shared__ Slot s_slot[ROPE_TOKENS];
+    const int t0 = blockIdx.x * tokens_per_block, n_tok = min(tokens_per_block, a.n_tokens - t0);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l = tid % LH;
+    const int h0 = blockIdx.y * heads_per_block, h_end = min(h0 + heads_per_block, a.q.n + a.k.n + a.v.n);
+    const int tk = tid / (heads_per_round * LH), hg = h0 + (tid - tk * heads_per_round * LH) / LH, t = t0 + tk;
+    const bool mine = tk < n_tok;
+    // the lane's two groups of four elements, and whether they are pairs that turn
+    const int j = l * 4;
+    const bool turns = j < a.pairs;
+    const int o1 = INTER ? 2 * j : (turns ? j : a.pairs + j), o2 = INTER ? 2 * j + 4 : (turns ? a.pairs + j : D / 2 + j);
+    const int k0 = a.q.n, v0 = a.q.n + a.k.n;
+    Vec4<T> x1[ROUNDS], x2[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < ROPE_ROUNDS; ++r) {
-        const int i = tid / LH + r * per_round;
-        if (i < n_heads) {
-            int h = h0 + i;
-            const HeadsView& in = h < a.q.n ? a.q : (h < a.q.n + a.k.n ? a.k : a.v);
-            h -= h < a.q.n ? 0 : (h < a.q.n + a.k.n ? a.q.n : a.q.n + a.k.n);
-            x[r].load(reinterpret_cast<const T*>(in.p) + paged::out_offset(in, t, h) + l * 8);
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int h = hg + r * heads_per_round;
+        if (mine && h < h_end) {
+            const HeadsView& in = h < k0 ? a.q : (h < v0 ? a.k : a.v);
+            const T* p = reinterpret_cast<const T*>(in.p) + paged::out_offset(in, t, h - (h < k0 ? 0 : (h < v0 ? k0 : v0)));
+            x1[r].load(p + o1);
+            x2[r].load(p + o2);
         }
     }
-    Slot slot;
-    slot.page = slot.slot = slot.pos = 0;
     if (APPEND) {
-        if (warp == 0) {
-            slot = find_slot(a.seq, a.pages, t, lane);
-            if (lane == 0) s_slot = slot;
+        for (int k = warp; k < n_tok; k += blockDim.x >> 5) {
+            const Slot slot = find_slot(a.seq, a.pages, t0 + k, lane);
+            if (lane == 0) s_slot[k] = slot;
         }
-        if (!a.positions) {              // the angles wait for the slot
-            __syncthreads();
-            slot = s_slot;
-        }
+        if (!a.positions) __syncthreads();       // the angles wait for the slots
     }
-    if (a.pairs) {
-        const int p = a.positions ? __ldg(a.positions + t) : slot.pos;
-        for (int i = tid; i < a.pairs; i += blockDim.x) turn[i] = rope_turn(p, __ldg(a.freq + i), a.amplitude);
+    const int kept = (a.pairs + 3) & ~3;
+    for (int i = tid; i < n_tok * a.pairs; i += blockDim.x) {
+        const int k = i / a.pairs, pair = i - k * a.pairs;
+        s_turn[k * kept + pair] = rope_turn(a.positions ? __ldg(a.positions + t0 + k) : s_slot[k].pos, __ldg(a.freq + pair), a.amplitude);
     }
     __syncthreads();
-    if (APPEND) {
-        slot = s_slot;
-        if (slot.page < 0) return;
+    float c[4], s[4];
+    Slot slot;
+    slot.page = slot.slot = 0;
+    bool valid = mine;
+    if (mine) {
+        if (APPEND) {
+            slot = s_slot[tk];
+            valid = slot.page >= 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 cs = j + e < a.pairs ? s_turn[tk * kept + j + e] : make_float2(1.f, 0.f);
+            c[e] = cs.x;
+            s[e] = cs.y;
+        }
     }
-    // the pairs of this lane's elements: in halves, eight of the first elements or eight of the second ones; else four whole pairs
-    const int shift = a.pairs / 8;       // lanes between a pair's halves
-    const bool first = l < shift, second = !first && l < 2 * shift;
+    if (__all_sync(0xffffffffu, !valid)) return;
+    Vec4<T> gq1, gq2, gk1, gk2;
+    const T *gq = reinterpret_cast<const T*>(a.q_gain), *gk = reinterpret_cast<const T*>(a.k_gain);
+    if (gq) { gq1.load(gq + o1); gq2.load(gq + o2); }
+    if (gk) { gk1.load(gk + o1); gk2.load(gk + o2); }
 #pragma unroll
-    for (int r = 0; r < ROPE_ROUNDS; ++r) {
-        const int i = tid / LH + r * per_round;
-        if (__all_sync(0xffffffffu, i >= n_heads)) break;
-        const bool valid = i < n_heads;
-        int h = valid ? h0 + i : h0;
-        const int kind = h < a.q.n ? 0 : (h < a.q.n + a.k.n ? 1 : 2);
-        h -= kind == 0 ? 0 : (kind == 1 ? a.q.n : a.q.n + a.k.n);
-        float v[8];
-        if (!valid) {
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int h = hg + r * heads_per_round;
+        const bool here = valid && h < h_end;
+        if (__all_sync(0xffffffffu, !here)) break;
+        const bool is_q = h < k0, is_v = h >= v0;
+        float u[4], w[4];
+        x1[r].get(u);
+        x2[r].get(w);
+        if (gq || gk) {
+            float sq = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            for (int e = 0; e < 4; ++e) sq = fmaf(w[e], w[e], fmaf(u[e], u[e], sq));
+#pragma unroll
+            for (int o = LH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            if (is_q ? gq != nullptr : (!is_v && gk)) {
+                const float root = rsqrtf(sq * (1.f / D) + a.eps);
+                float f[4];
+                (is_q ? gq1 : gk1).get(f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = u[e] * root * f[e];
+                (is_q ? gq2 : gk2).get(f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = w[e] * root * f[e];
+            }
+        }
+        if (!here) continue;
+        T* y;
+        if (APPEND && !is_q) {
+            const int head = h - (is_v ? v0 : k0);
+            y = reinterpret_cast<T*>(is_v ? a.pages.v : a.pages.k) + (slot.page * a.pages.page + slot.slot * a.pages.tok + head * a.pages.head);
         } else {
-            x[r].get(v);
+            const HeadsView& to = is_q ? a.q_out : a.k_out;
+            y = reinterpret_cast<T*>(to.p) + paged::out_offset(to, t, h - (is_q ? 0 : k0));
         }
-        const T* gain = reinterpret_cast<const T*>(kind == 0 ? a.q_gain : (kind == 1 ? a.k_gain : nullptr));
-        float sq = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq = fmaf(v[e], v[e], sq);
-#pragma unroll
-        for (int o = LH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        if (gain) {
-            const float root = rsqrtf(sq / (float)(LH * 8) + a.eps);
-            Vec8<T> gv;
-            gv.load(gain + l * 8);
-            float gf[8];
-            gv.get(gf);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = v[e] * root * gf[e];
-        }
-        if (a.pairs && a.interleaved) {
-            if (kind < 2) {
+        if (!is_v) {                             // values go as they are
+            if (INTER) {
+                // pairs (u0, u1), (u2, u3), (w0, w1), (w2, w3)
+                float p[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (l * 4 + e < a.pairs) {
-                        const float2 cs = turn[l * 4 + e];
-                        const float p = v[2 * e], q = v[2 * e + 1];
-                        v[2 * e] = fmaf(p, cs.x, -(q * cs.y));
-                        v[2 * e + 1] = fmaf(q, cs.x, p * cs.y);
-                    }
+                    const float x = p[2 * e], z = p[2 * e + 1];
+                    p[2 * e] = j + e < a.pairs ? fmaf(x, c[e], -(z * s[e])) : x;
+                    p[2 * e + 1] = j + e < a.pairs ? fmaf(z, c[e], x * s[e]) : z;
                 }
-            }
-        } else if (a.pairs) {
-            const int src = first ? l + shift : (second ? l - shift : l);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float other = __shfl_sync(0xffffffffu, v[e], src, LH);
-                if (kind < 2 && (first || second)) {
-                    const float2 cs = turn[(first ? l : l - shift) * 8 + e];
-                    v[e] = first ? fmaf(v[e], cs.x, -(other * cs.y)) : fmaf(v[e], cs.x, other * cs.y);
+                for (int e = 0; e < 4; ++e) { u[e] = p[e]; w[e] = p[4 + e]; }
+            } else if (turns) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = u[e], z = w[e];
+                    u[e] = fmaf(x, c[e], -(z * s[e]));
+                    w[e] = fmaf(z, c[e], x * s[e]);
                 }
             }
+            x1[r].set(u);
+            x2[r].set(w);
         }
-        if (!valid) continue;
-        T* y;
-        if (APPEND && kind) y = reinterpret_cast<T*>(kind == 1 ? a.pages.k : a.pages.v) + (slot.page * a.pages.page + slot.slot * a.pages.tok + h * a.pages.head);
-        else {
-            const HeadsView& to = kind == 0 ? a.q_out : a.k_out;
-            y = reinterpret_cast<T*>(to.p) + paged::out_offset(to, t, h);
-        }
-        if (kind < 2) x[r].set(v);       // values go as they are
-        x[r].store(y + l * 8);
+        x1[r].store(y + o1);
+        x2[r].store(y + o2);
     }
 }
 
 template <typename T, int LH>
 void run_norm_rope(const NormRopeArgs& a, cudaStream_t s) {
-    const int heads = a.q.n + a.k.n + a.v.n;
-    // a call that does not fill the GPU spreads its heads over the SMs, a head per thread group
-    const int small = 128 / LH;
-    int hb, threads;
+    constexpr int ROUNDS = ROPE_ROUNDS<T>;
+    const int heads = a.q.n + a.k.n + a.v.n, small = 128 / LH;
+    int hb, per, tokens = 1;             // heads of a block and of a round, tokens of a block
     if ((long long)a.n_tokens * ((heads + small - 1) / small) <= 4 * 148) {
-        hb = heads < small ? heads : small;
-        threads = (hb * LH + 31) / 32 * 32;
+        // a call that does not fill the GPU spreads its heads over the SMs, a head per thread group
+        hb = per = heads < small ? heads : small;
     } else {
-        const int parts = (heads * LH + ROPE_ROUNDS * ROPE_THREADS - 1) / (ROPE_ROUNDS * ROPE_THREADS);
+        const int most = ROUNDS * (ROPE_THREADS / LH), parts = (heads + most - 1) / most;
         hb = (heads + parts - 1) / parts;
-        const int rounds = (hb * LH + ROPE_THREADS - 1) / ROPE_THREADS;
-        threads = ((hb * LH + rounds - 1) / rounds + 31) / 32 * 32;
+        per = (hb + ROUNDS - 1) / ROUNDS;
+        // as many tokens as a block has threads for, but a block for every SM twice over
+        tokens = ROPE_THREADS / (per * LH);
+        if (tokens > ROPE_TOKENS) tokens = ROPE_TOKENS;
+        const int kept = (a.pairs + 3) & ~3;
+        if (kept && tokens > ROPE_PAIRS / kept) tokens = ROPE_PAIRS / kept;
+        if (tokens > a.n_tokens / (2 * 148)) tokens = a.n_tokens / (2 * 148);
+        if (tokens < 1) tokens = 1;
     }
-    const dim3 grid(a.n_tokens, (heads + hb - 1) / hb);
-    if (a.append) k_norm_rope<T, LH, true><<<grid, threads, 0, s>>>(a, hb);
-    else k_norm_rope<T, LH, false><<<grid, threads, 0, s>>>(a, hb);
+    const int threads = (tokens * per * LH + 31) / 32 * 32;
+    const dim3 grid((a.n_tokens + tokens - 1) / tokens, (heads + hb - 1) / hb);
+    const bool inter = a.pairs && a.interleaved;
+    if (a.append) {
+        if (inter) k_norm_rope<T, LH, true, true><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+        else k_norm_rope<T, LH, true, false><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+    } else {
+        if (inter) k_norm_rope<T, LH, false, true><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+        else k_norm_rope<T, LH, false, false><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+    }
 }
 template <typename T>
 void run_norm_rope_d(const NormRopeArgs& a, cudaStream_t s) {
@@ -297,7 +328,7 @@ void run_norm_rope_d(const NormRopeArgs& a, cudaStream_t s) {
 }
 bool fast_shape(const NormRopeArgs& a, int elem) {
     if (a.D != 32 && a.D != 64 && a.D != 128 && a.D != 256) return false;
-    if (a.pairs && !a.interleaved && a.pairs % 8) return false;
+    if (a.pairs && !a.interleaved && a.pairs % 4) return false;
     const int per16 = 16 / elem;
     auto al = [&](const HeadsView& v) { return !v.p || (reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.tok % per16 == 0 && v.head % per16 == 0); };
     auto al_p = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
