@@ -26,7 +26,7 @@ struct SeqTable {
 };
 
 struct NormRopeArgs {
-    HeadsView q, k, v, q_out, k_out;
+    HeadsView in[3], out[2];     // queries, keys, values
     const void *q_gain, *k_gain;
     const uint64_t* freq;        // [pairs] fractions of a turn per position, 2^64 = one turn
     const int32_t* positions;    // NULL: the slot's position (append)

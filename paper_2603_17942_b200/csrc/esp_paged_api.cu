@@ -179,8 +179,8 @@ int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const es
     memset(&a, 0, sizeof(a));
     if (const int rc = set_rope(a, rope, rope_table, head_dim)) return rc;
     if (n_tokens == 0) return ESP_OK;
-    a.q = view_of(q, n_tokens); a.k = view_of(k, n_tokens); a.v = view_of(nullptr, n_tokens);
-    a.q_out = view_of(q_out, n_tokens); a.k_out = view_of(k_out, n_tokens);
+    a.in[0] = view_of(q, n_tokens); a.in[1] = view_of(k, n_tokens); a.in[2] = view_of(nullptr, n_tokens);
+    a.out[0] = view_of(q_out, n_tokens); a.out[1] = view_of(k_out, n_tokens);
     a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps;
     a.positions = positions;
     a.n_tokens = n_tokens; a.D = head_dim;
@@ -209,8 +209,8 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
     memset(&a, 0, sizeof(a));
     if (const int rc = set_rope(a, rope, rope_table, cache->head_dim)) return rc;
     if (n_tokens == 0 || batch->batch == 0 || batch->max_new == 0) return ESP_OK;
-    a.q = view_of(q, n_tokens); a.k = view_of(k, n_tokens); a.v = view_of(v, n_tokens);
-    a.q_out = view_of(q_out, n_tokens); a.k_out = view_of(nullptr, n_tokens);
+    a.in[0] = view_of(q, n_tokens); a.in[1] = view_of(k, n_tokens); a.in[2] = view_of(v, n_tokens);
+    a.out[0] = view_of(q_out, n_tokens); a.out[1] = view_of(nullptr, n_tokens);
     a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps;
     a.positions = positions;
     a.n_tokens = n_tokens; a.D = cache->head_dim;

@@ -69,15 +69,15 @@ template <typename T>
 __global__ void __launch_bounds__(ANY_WARPS * 32) k_norm_rope_any(const __grid_constant__ NormRopeArgs a) {
     __shared__ float rows[ANY_WARPS][ESP_ROPE_MAX_DIM];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int heads = a.q.n + a.k.n + a.v.n;
+    const int heads = a.in[0].n + a.in[1].n + a.in[2].n;
     const long long task = (long long)blockIdx.x * ANY_WARPS + warp;
     if (task >= (long long)a.n_tokens * heads) return;
     const int t = (int)(task / heads);
     int h = (int)(task - (long long)t * heads);
-    const int kind = h < a.q.n ? 0 : (h < a.q.n + a.k.n ? 1 : 2);
-    const HeadsView& in = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
-    const HeadsView& to = kind == 0 ? a.q_out : a.k_out;
-    h -= kind == 0 ? 0 : (kind == 1 ? a.q.n : a.q.n + a.k.n);
+    const int kind = h < a.in[0].n ? 0 : (h < a.in[0].n + a.in[1].n ? 1 : 2);
+    const HeadsView& in = a.in[kind];
+    const HeadsView& to = a.out[kind == 0 ? 0 : 1];
+    h -= kind == 0 ? 0 : (kind == 1 ? a.in[0].n : a.in[0].n + a.in[1].n);
 
     Slot slot;
     slot.page = slot.slot = slot.pos = 0;
@@ -135,10 +135,11 @@ __global__ void __launch_bounds__(ANY_WARPS * 32) k_norm_rope_any(const __grid_c
 // Heads of 32, 64, 128 or 256 elements on 16 bytes (rotated halves of whole groups of four): a lane has four pairs of a head, LH lanes a
 // head, a block a few tokens or some heads of one; a thread has the same pairs of up to ROUNDS heads of its token.  In halves the
 // lane's elements are four neighbours of each half, so that both members of a pair are its own; what is not rotated is halved likewise.
-// Memory bounds it, next to it the instructions (a lane that had eight neighbours and its partners' values by shuffle needed 333 per eight
-// elements and 65 us for 8192 tokens of 40 heads of 128), so the loads of all of a thread's heads are requested first; while they are on
-// their way the tokens' slots are looked up, a warp for each, and their angles turned, once for all heads.
-constexpr int ROPE_THREADS = 384;       // threads of a block at most
+// Memory bounds it, and next to it the instructions: a block has heads of one kind (queries, keys or values), so that nothing but the numbers differs from
+// head to head, and gain and angle are one set of coefficients per thread.  Blocks with all kinds needed 240 instructions per eight elements and 50 us for
+// 8192 tokens of 40 heads of 128.  The loads of all of a thread's heads are requested first; while they are on their way the tokens'
+// slots are looked up, a warp for each, and their angles turned.
+constexpr int ROPE_THREADS = 128;       // threads of a block at most
 constexpr int ROPE_PAIRS = 1024;        // angles a block keeps
 constexpr int ROPE_TOKENS = 16;         // tokens of a block at most
 template <typename T> constexpr int ROPE_ROUNDS = sizeof(T) == 2 ? 4 : 2;      // heads of a thread: 64 bytes under way
@@ -165,166 +166,201 @@ template <> struct Vec4<float> {
     __device__ __forceinline__ void set(const float (&v)[4]) { x = make_float4(v[0], v[1], v[2], v[3]); }
 };
 
+struct RopePart {          // the blocks of one kind of head
+    int32_t block0, heads, hb, per, tokens, ny;      // first block, heads, heads of a block and of a round, tokens of a block, blocks for the heads of a token
+};
+struct RopePlan {
+    RopePart part[3];
+};
+
 template <typename T, int LH, bool APPEND, bool INTER>
-__global__ void __launch_bounds__(ROPE_THREADS, 3) k_norm_rope(const __grid_constant__ NormRopeArgs a, int heads_per_block, int heads_per_round, int tokens_per_block) {
+__global__ void __launch_bounds__(ROPE_THREADS, 9) k_norm_rope(const __grid_constant__ NormRopeArgs a, const __grid_constant__ RopePlan plan) {
     constexpr int ROUNDS = ROPE_ROUNDS<T>, D = LH * 8;
     __shared__ __align__(16) float2 s_turn[ROPE_PAIRS];       // [token of the block][pair]
     __shared__ Slot s_slot[ROPE_TOKENS];
-    const int t0 = blockIdx.x * tokens_per_block, n_tok = min(tokens_per_block, a.n_tokens - t0);
+    const int kind = (int)blockIdx.x >= plan.part[2].block0 ? 2 : ((int)blockIdx.x >= plan.part[1].block0 ? 1 : 0);
+    const RopePart part = plan.part[kind];
+    const HeadsView in = a.in[kind];
+    const int block = blockIdx.x - part.block0, by = block % part.ny, t0 = block / part.ny * part.tokens, n_tok = min(part.tokens, a.n_tokens - t0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l = tid % LH;
-    const int h0 = blockIdx.y * heads_per_block, h_end = min(h0 + heads_per_block, a.q.n + a.k.n + a.v.n);
-    const int tk = tid / (heads_per_round * LH), hg = h0 + (tid - tk * heads_per_round * LH) / LH, t = t0 + tk;
-    const bool mine = tk < n_tok;
+    const int tk = tid / (part.per * LH), hg = by * part.hb + (tid - tk * part.per * LH) / LH, h_end = min(by * part.hb + part.hb, part.heads), t = t0 + tk;
+    const int n_here = tk < n_tok && hg < h_end ? (h_end - hg + part.per - 1) / part.per : 0;      // heads of this thread
     // the lane's two groups of four elements, and whether they are pairs that turn
     const int j = l * 4;
     const bool turns = j < a.pairs;
     const int o1 = INTER ? 2 * j : (turns ? j : a.pairs + j), o2 = INTER ? 2 * j + 4 : (turns ? a.pairs + j : D / 2 + j);
-    const int k0 = a.q.n, v0 = a.q.n + a.k.n;
     Vec4<T> x1[ROUNDS], x2[ROUNDS];
+    {
+        const T* p = reinterpret_cast<const T*>(in.p) + paged::out_offset(in, t, hg);
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int h = hg + r * heads_per_round;
-        if (mine && h < h_end) {
-            const HeadsView& in = h < k0 ? a.q : (h < v0 ? a.k : a.v);
-            const T* p = reinterpret_cast<const T*>(in.p) + paged::out_offset(in, t, h - (h < k0 ? 0 : (h < v0 ? k0 : v0)));
-            x1[r].load(p + o1);
-            x2[r].load(p + o2);
-        }
+        for (int r = 0; r < ROUNDS; ++r, p += part.per * in.head)
+            if (r < n_here) {
+                x1[r].load(p + o1);
+                x2[r].load(p + o2);
+            }
     }
     if (APPEND) {
         for (int k = warp; k < n_tok; k += blockDim.x >> 5) {
             const Slot slot = find_slot(a.seq, a.pages, t0 + k, lane);
             if (lane == 0) s_slot[k] = slot;
         }
-        if (!a.positions) __syncthreads();       // the angles wait for the slots
+        if (!a.positions || kind == 2) __syncthreads();       // the angles wait for the slots
     }
     const int kept = (a.pairs + 3) & ~3;
-    for (int i = tid; i < n_tok * a.pairs; i += blockDim.x) {
-        const int k = i / a.pairs, pair = i - k * a.pairs;
-        s_turn[k * kept + pair] = rope_turn(a.positions ? __ldg(a.positions + t0 + k) : s_slot[k].pos, __ldg(a.freq + pair), a.amplitude);
+    if (!APPEND || kind < 2) {
+        for (int i = tid; i < n_tok * kept; i += blockDim.x) {
+            const int k = i / kept, pair = i - k * kept;
+            if (pair < a.pairs) s_turn[i] = rope_turn(a.positions ? __ldg(a.positions + t0 + k) : s_slot[k].pos, __ldg(a.freq + pair), a.amplitude);
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    float c[4], s[4];
-    Slot slot;
-    slot.page = slot.slot = 0;
-    bool valid = mine;
-    if (mine) {
-        if (APPEND) {
-            slot = s_slot[tk];
-            valid = slot.page >= 0;
+    if (n_here == 0) return;                 // (whole groups of LH lanes)
+    T* y;
+    long long step;
+    if (APPEND) {
+        const Slot slot = s_slot[tk];
+        if (slot.page < 0) return;
+        if (kind) {
+            y = reinterpret_cast<T*>(kind == 2 ? a.pages.v : a.pages.k) + (slot.page * a.pages.page + slot.slot * a.pages.tok + hg * a.pages.head);
+            step = part.per * a.pages.head;
+        }
+    }
+    if (!APPEND || kind == 0) {
+        const HeadsView to = a.out[APPEND ? 0 : kind];
+        y = reinterpret_cast<T*>(to.p) + paged::out_offset(to, t, hg);
+        step = part.per * to.head;
+    }
+    if (APPEND && kind == 2) {               // values go as they are
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r, y += step)
+            if (r < n_here) {
+                x1[r].store(y + o1);
+                x2[r].store(y + o2);
+            }
+        return;
+    }
+    // gain and angle as one: a pair (u, w) becomes root * (u * uc - w * ws, w * wc + u * us)
+    const T* gain = reinterpret_cast<const T*>(kind ? a.k_gain : a.q_gain);
+    float uc[4], us[4], wc[4], ws[4];
+    {
+        float f1[4] = {1.f, 1.f, 1.f, 1.f}, f2[4] = {1.f, 1.f, 1.f, 1.f};
+        if (gain) {
+            Vec4<T> g;
+            g.load(gain + o1);
+            g.get(f1);
+            g.load(gain + o2);
+            g.get(f2);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float2 cs = j + e < a.pairs ? s_turn[tk * kept + j + e] : make_float2(1.f, 0.f);
-            c[e] = cs.x;
-            s[e] = cs.y;
+            // (interleaved: pair e is elements 2e and 2e + 1 of the eight)
+            const float fu = INTER ? (e < 2 ? f1[2 * e & 3] : f2[2 * e & 3]) : f1[e], fw = INTER ? (e < 2 ? f1[(2 * e + 1) & 3] : f2[(2 * e + 1) & 3]) : f2[e];
+            uc[e] = fu * cs.x; us[e] = fu * cs.y;
+            wc[e] = fw * cs.x; ws[e] = fw * cs.y;
         }
     }
-    if (__all_sync(0xffffffffu, !valid)) return;
-    Vec4<T> gq1, gq2, gk1, gk2;
-    const T *gq = reinterpret_cast<const T*>(a.q_gain), *gk = reinterpret_cast<const T*>(a.k_gain);
-    if (gq) { gq1.load(gq + o1); gq2.load(gq + o2); }
-    if (gk) { gk1.load(gk + o1); gk2.load(gk + o2); }
+    const uint32_t group = LH == 32 ? 0xffffffffu : ((1u << LH) - 1u) << (lane & ~(LH - 1));      // the lanes of a head have the same rounds
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int h = hg + r * heads_per_round;
-        const bool here = valid && h < h_end;
-        if (__all_sync(0xffffffffu, !here)) break;
-        const bool is_q = h < k0, is_v = h >= v0;
+    for (int r = 0; r < ROUNDS; ++r, y += step) {
+        if (r >= n_here) break;
         float u[4], w[4];
         x1[r].get(u);
         x2[r].get(w);
-        if (gq || gk) {
+        float root = 1.f;
+        if (gain) {
             float sq = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) sq = fmaf(w[e], w[e], fmaf(u[e], u[e], sq));
 #pragma unroll
-            for (int o = LH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-            if (is_q ? gq != nullptr : (!is_v && gk)) {
-                const float root = rsqrtf(sq * (1.f / D) + a.eps);
-                float f[4];
-                (is_q ? gq1 : gk1).get(f);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) u[e] = u[e] * root * f[e];
-                (is_q ? gq2 : gk2).get(f);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = w[e] * root * f[e];
-            }
+            for (int o = LH / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(group, sq, o);
+            root = rsqrtf(fmaf(sq, 1.f / D, a.eps));
         }
-        if (!here) continue;
-        T* y;
-        if (APPEND && !is_q) {
-            const int head = h - (is_v ? v0 : k0);
-            y = reinterpret_cast<T*>(is_v ? a.pages.v : a.pages.k) + (slot.page * a.pages.page + slot.slot * a.pages.tok + head * a.pages.head);
+        // what does not turn has a sine of 0, but may be infinite: it is not multiplied by it
+        if (INTER) {
+            const float p[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+            float q[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool turn = j + e < a.pairs;
+                q[2 * e] = turn ? fmaf(p[2 * e], uc[e], -(p[2 * e + 1] * ws[e])) : p[2 * e] * uc[e];
+                q[2 * e + 1] = turn ? fmaf(p[2 * e + 1], wc[e], p[2 * e] * us[e]) : p[2 * e + 1] * wc[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { u[e] = q[e]; w[e] = q[4 + e]; }
+        } else if (turns) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = u[e], z = w[e];
+                u[e] = fmaf(x, uc[e], -(z * ws[e]));
+                w[e] = fmaf(z, wc[e], x * us[e]);
+            }
         } else {
-            const HeadsView& to = is_q ? a.q_out : a.k_out;
-            y = reinterpret_cast<T*>(to.p) + paged::out_offset(to, t, h - (is_q ? 0 : k0));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { u[e] *= uc[e]; w[e] *= wc[e]; }
         }
-        if (!is_v) {                             // values go as they are
-            if (INTER) {
-                // pairs (u0, u1), (u2, u3), (w0, w1), (w2, w3)
-                float p[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+        if (gain) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = p[2 * e], z = p[2 * e + 1];
-                    p[2 * e] = j + e < a.pairs ? fmaf(x, c[e], -(z * s[e])) : x;
-                    p[2 * e + 1] = j + e < a.pairs ? fmaf(z, c[e], x * s[e]) : z;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { u[e] = p[e]; w[e] = p[4 + e]; }
-            } else if (turns) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = u[e], z = w[e];
-                    u[e] = fmaf(x, c[e], -(z * s[e]));
-                    w[e] = fmaf(z, c[e], x * s[e]);
-                }
-            }
-            x1[r].set(u);
-            x2[r].set(w);
+            for (int e = 0; e < 4; ++e) { u[e] *= root; w[e] *= root; }
         }
+        x1[r].set(u);
+        x2[r].set(w);
         x1[r].store(y + o1);
         x2[r].store(y + o2);
     }
 }
 
 template <typename T, int LH>
-void run_norm_rope(const NormRopeArgs& a, cudaStream_t s) {
+int run_norm_rope(const NormRopeArgs& a, cudaStream_t s) {
     constexpr int ROUNDS = ROPE_ROUNDS<T>;
-    const int heads = a.q.n + a.k.n + a.v.n, small = 128 / LH;
-    int hb, per, tokens = 1;             // heads of a block and of a round, tokens of a block
-    if ((long long)a.n_tokens * ((heads + small - 1) / small) <= 4 * 148) {
-        // a call that does not fill the GPU spreads its heads over the SMs, a head per thread group
-        hb = per = heads < small ? heads : small;
-    } else {
-        const int most = ROUNDS * (ROPE_THREADS / LH), parts = (heads + most - 1) / most;
-        hb = (heads + parts - 1) / parts;
-        per = (hb + ROUNDS - 1) / ROUNDS;
-        // as many tokens as a block has threads for, but a block for every SM twice over
-        tokens = ROPE_THREADS / (per * LH);
-        if (tokens > ROPE_TOKENS) tokens = ROPE_TOKENS;
-        const int kept = (a.pairs + 3) & ~3;
-        if (kept && tokens > ROPE_PAIRS / kept) tokens = ROPE_PAIRS / kept;
-        if (tokens > a.n_tokens / (2 * 148)) tokens = a.n_tokens / (2 * 148);
-        if (tokens < 1) tokens = 1;
+    const int all = a.in[0].n + a.in[1].n + a.in[2].n, most = 128 / LH, kept = (a.pairs + 3) & ~3;
+    // a call that does not fill the GPU spreads its heads over the SMs, a head per thread group
+    const bool small = (long long)a.n_tokens * ((all + most - 1) / most) <= 4 * 148;
+    RopePlan plan;
+    long long blocks = 0;
+    int threads = 32;
+    for (int kind = 0; kind < 3; ++kind) {
+        RopePart& p = plan.part[kind];
+        p.block0 = (int)blocks;
+        p.heads = a.in[kind].n;
+        p.hb = p.per = p.tokens = p.ny = 1;
+        if (p.heads == 0) continue;
+        if (small) {
+            p.hb = p.per = p.heads < most ? p.heads : most;
+        } else {
+            const int cap = ROUNDS * (ROPE_THREADS / LH);
+            p.ny = (p.heads + cap - 1) / cap;
+            p.hb = (p.heads + p.ny - 1) / p.ny;
+            p.per = (p.hb + ROUNDS - 1) / ROUNDS;
+            // as many tokens as a block has threads for, but a block for every SM
+            p.tokens = ROPE_THREADS / (p.per * LH);
+            if (p.tokens > ROPE_TOKENS) p.tokens = ROPE_TOKENS;
+            if (kept && p.tokens > ROPE_PAIRS / kept) p.tokens = ROPE_PAIRS / kept;
+            if (p.tokens > a.n_tokens / 148) p.tokens = a.n_tokens / 148;
+            if (p.tokens < 1) p.tokens = 1;
+        }
+        p.ny = (p.heads + p.hb - 1) / p.hb;
+        const int need = (p.tokens * p.per * LH + 31) / 32 * 32;
+        if (need > threads) threads = need;
+        blocks += (long long)((a.n_tokens + p.tokens - 1) / p.tokens) * p.ny;
     }
-    const int threads = (tokens * per * LH + 31) / 32 * 32;
-    const dim3 grid((a.n_tokens + tokens - 1) / tokens, (heads + hb - 1) / hb);
+    for (int kind = 1; kind < 3; ++kind)            // a kind that is not there has no blocks
+        if (plan.part[kind].heads == 0) plan.part[kind].block0 = 0x7fffffff;
+    if (blocks > 0x7ffffffe) return -1;
     const bool inter = a.pairs && a.interleaved;
+    const unsigned grid = (unsigned)blocks;
     if (a.append) {
-        if (inter) k_norm_rope<T, LH, true, true><<<grid, threads, 0, s>>>(a, hb, per, tokens);
-        else k_norm_rope<T, LH, true, false><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+        if (inter) k_norm_rope<T, LH, true, true><<<grid, threads, 0, s>>>(a, plan);
+        else k_norm_rope<T, LH, true, false><<<grid, threads, 0, s>>>(a, plan);
     } else {
-        if (inter) k_norm_rope<T, LH, false, true><<<grid, threads, 0, s>>>(a, hb, per, tokens);
-        else k_norm_rope<T, LH, false, false><<<grid, threads, 0, s>>>(a, hb, per, tokens);
+        if (inter) k_norm_rope<T, LH, false, true><<<grid, threads, 0, s>>>(a, plan);
+        else k_norm_rope<T, LH, false, false><<<grid, threads, 0, s>>>(a, plan);
     }
+    return 0;
 }
 template <typename T>
-void run_norm_rope_d(const NormRopeArgs& a, cudaStream_t s) {
-    if (a.D == 32) run_norm_rope<T, 4>(a, s);
-    else if (a.D == 64) run_norm_rope<T, 8>(a, s);
-    else if (a.D == 128) run_norm_rope<T, 16>(a, s);
-    else run_norm_rope<T, 32>(a, s);
+int run_norm_rope_d(const NormRopeArgs& a, cudaStream_t s) {
+    return a.D == 32 ? run_norm_rope<T, 4>(a, s) : (a.D == 64 ? run_norm_rope<T, 8>(a, s) : (a.D == 128 ? run_norm_rope<T, 16>(a, s) : run_norm_rope<T, 32>(a, s)));
 }
 bool fast_shape(const NormRopeArgs& a, int elem) {
     if (a.D != 32 && a.D != 64 && a.D != 128 && a.D != 256) return false;
@@ -332,7 +368,7 @@ bool fast_shape(const NormRopeArgs& a, int elem) {
     const int per16 = 16 / elem;
     auto al = [&](const HeadsView& v) { return !v.p || (reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.tok % per16 == 0 && v.head % per16 == 0); };
     auto al_p = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    if (!al(a.q) || !al(a.k) || !al(a.v) || !al(a.q_out) || !al(a.k_out) || !al_p(a.q_gain) || !al_p(a.k_gain)) return false;
+    if (!al(a.in[0]) || !al(a.in[1]) || !al(a.in[2]) || !al(a.out[0]) || !al(a.out[1]) || !al_p(a.q_gain) || !al_p(a.k_gain)) return false;
     return !a.append || (al_p(a.pages.k) && al_p(a.pages.v) && a.pages.page % per16 == 0 && a.pages.tok % per16 == 0 && a.pages.head % per16 == 0);
 }
 
@@ -345,12 +381,8 @@ void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStr
 }
 
 int launch_norm_rope(int dtype, const NormRopeArgs& a, cudaStream_t s) {
-    const int heads = a.q.n + a.k.n + a.v.n;
-    if (fast_shape(a, dtype == 0 ? 4 : 2) && heads <= 65535) {
-        if (dtype == 0) run_norm_rope_d<float>(a, s);
-        else run_norm_rope_d<__nv_bfloat16>(a, s);
-        return 0;
-    }
+    const int heads = a.in[0].n + a.in[1].n + a.in[2].n;
+    if (fast_shape(a, dtype == 0 ? 4 : 2)) return dtype == 0 ? run_norm_rope_d<float>(a, s) : run_norm_rope_d<__nv_bfloat16>(a, s);
     const long long tasks = (long long)a.n_tokens * heads;
     const long long blocks = (tasks + ANY_WARPS - 1) / ANY_WARPS;
     if (blocks > 0x7fffffff) return -1;
