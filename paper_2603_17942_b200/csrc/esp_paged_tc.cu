@@ -64,6 +64,9 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int x, int y, int z) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -168,6 +171,7 @@ template <int D>
 __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__ TcParams p) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ int2 s_box[2][16];          // [keys, values] page and slot of a chunk's boxes
     __shared__ int s_odd[ODD_RING];        // a value that some pair sees is no finite number
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR); // [KST] keys of a chunk have landed
@@ -241,12 +245,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 uint64_t* full = (is_v ? v_full : k_full) + st;
                 if (lane == 0) mbar_expect_tx(full, C::TILE_BYTES);
                 unsigned char* dst = (is_v ? sV : sK) + st * C::TILE_BYTES;
+                if (lane < n_boxes) s_box[is_v][lane] = make_int2(page, slot);
+                __syncwarp();
+                if (lane == 0) {
 #pragma unroll 4
-                for (int i = 0; i < n_boxes; ++i) {
-                    const int pg = __shfl_sync(0xffffffffu, page, i), sl = __shfl_sync(0xffffffffu, slot, i);
-                    if (lane == 0) {
+                    for (int i = 0; i < n_boxes; ++i) {
+                        const int2 b = s_box[is_v][i];
 #pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) tma_load_4d(dst + h * HALF_BYTES + i * p.box_rows * 128, map, h * 64, sl, c.kvh, pg, full);
+                        for (int h = 0; h < C::HALVES; ++h) tma_load_4d(dst + h * HALF_BYTES + i * p.box_rows * 128, map, h * 64, b.y, c.kvh, b.x, full);
                     }
                 }
                 if (!is_v && j == 0) {                      // the piece's queries behind its first keys
@@ -257,6 +263,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         for (int s = 0; s < subs; ++s)
                             for (int h = 0; h < C::HALVES; ++h)
                                 tma_load_3d(sQ + s * C::TILE_BYTES + h * HALF_BYTES, &p.map_q, h * 64, c.kvh * a.group, c.s.start + c.x.r0 + s * p.sub_rows, q_full);
+                    }
+                    if (u + pc.n < end) {                   // the next piece's queries come from far away: into L2 by then
+                        Cursor nx = c;
+                        next_tile<CK>(a, nx);
+                        if (lane == 0)
+                            for (int s = 0; s < (nx.x.nr > p.sub_rows ? 2 : 1); ++s)
+                                for (int h = 0; h < C::HALVES; ++h) tma_prefetch_3d(&p.map_q, h * 64, nx.kvh * a.group, nx.s.start + nx.x.r0 + s * p.sub_rows);
                     }
                 }
                 __syncwarp();
@@ -396,8 +409,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 const int pair = sub * p.sub_rows * a.group + row;               // of the tile
                 const bool valid = row < p.sub_rows * a.group && pair < c.x.nr * a.group;
                 const int trow = pair / a.group, head = c.kvh * a.group + pair - trow * a.group;
-                RowMask mask;
-                mask.lo = mask.hi = 0;
+                RowMask mask;                  // (a lane without a pair may see anything: nobody reads its row)
+                mask.lo = 0;
+                mask.hi = KV_LIMIT;
                 mask.b0 = mask.b1 = 0;
                 if (valid) mask = row_mask(a, c.s, c.x.r0 + trow);
                 const bool live = __any_sync(0xffffffffu, valid);
