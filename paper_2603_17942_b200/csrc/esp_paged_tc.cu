@@ -29,6 +29,7 @@ using namespace tc;
 using namespace paged;
 
 constexpr int CK = 128;                   // keys per chunk
+constexpr int STEP = 64;                  // keys per step of the softmax: a chunk's halves one after the other
 constexpr int SUB = 128;                  // pairs per subtile
 constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
 constexpr int THREADS = 384;
@@ -67,72 +68,27 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int x, int y, int z) {
     asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-
 __device__ __forceinline__ float max3_nan(float x, float y, float z) {
     float d;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
     return d;
 }
-// 2^x of a pair on the FMA pipe: x = n + f, |f| <= 1/2, a polynomial of degree 5 in f (fitted for the smallest relative error with p(0) = 1:
-// 1.1e-7), n added to the exponent.  Below -126 the result stays at 2^-126.
-__device__ __forceinline__ void ex2_poly2(float& x0, float& x1) {
-    const uint64_t magic = attn::pack2(12582912.f, 12582912.f), neg_magic = attn::pack2(-12582912.f, -12582912.f), minus_one = attn::pack2(-1.f, -1.f);
-    const uint64_t x = attn::pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const uint64_t t = attn::add2(x, magic);                       // the low bits are n
-    const uint64_t f = attn::fma2(attn::add2(t, neg_magic), minus_one, x);
-    uint64_t r = attn::pack2(0.001326472731307149f, 0.001326472731307149f);
-    r = attn::fma2(r, f, attn::pack2(0.009671512991189957f, 0.009671512991189957f));
-    r = attn::fma2(r, f, attn::pack2(0.05550733581185341f, 0.05550733581185341f));
-    r = attn::fma2(r, f, attn::pack2(0.24022242426872253f, 0.24022242426872253f));
-    r = attn::fma2(r, f, attn::pack2(0.6931470036506653f, 0.6931470036506653f));
-    r = attn::fma2(r, f, attn::pack2(1.f, 1.f));
-    float t0, t1;
-    attn::unpack2(t, t0, t1);
-    attn::unpack2(r, x0, x1);
-    x0 = __int_as_float(__float_as_int(x0) + (__float_as_int(t0) << 23));
-    x1 = __int_as_float(__float_as_int(x1) + (__float_as_int(t1) << 23));
-}
-// The weights of a row's 128 scores, as bf16 over the scores' columns; their sum.  The first 64 are announced on ready[0] as soon as they stand, so that their product
-// with V runs beside the other half's exponentials.
-// WHOLE: every key is seen, and POLY of eight pairs take the FMA pipe instead of the special-function unit, which alone would need as long as the
-// tensor cores do; masked scores (-infinity) have to give exactly 0 and take the special-function unit.
-constexpr uint32_t POLY_PAIRS = 0;      // of the 16 pairs of 32 columns: 3 of 8
-template <bool WHOLE>
-__device__ __forceinline__ float weights(const uint32_t (&sv)[128], uint32_t s_addr, float scale_log2, float m_use, uint64_t* ready) {
+// The weights of a row's scores of one step, as bf16 over the scores' columns; their sum.
+__device__ __forceinline__ float weights(const uint32_t (&sv)[STEP], uint32_t s_addr, float scale_log2, float m_use) {
     const uint64_t scale2 = attn::pack2(scale_log2, scale_log2), neg_m2 = attn::pack2(-m_use, -m_use);
     uint64_t sum2[2] = {0, 0};
+    uint32_t pk[STEP / 2];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        uint32_t pk[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float w0, w1;
-            attn::unpack2(attn::fma2(attn::pack2(__uint_as_float(sv[b * 32 + 2 * i]), __uint_as_float(sv[b * 32 + 2 * i + 1])), scale2, neg_m2), w0, w1);
-            if (WHOLE && ((POLY_PAIRS >> i) & 1u)) {
-                ex2_poly2(w0, w1);
-            } else {
-                w0 = attn::ex2_approx(w0);
-                w1 = attn::ex2_approx(w1);
-            }
-            sum2[i & 1] = attn::add2(sum2[i & 1], attn::pack2(w0, w1));
-            const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
-            pk[i] = *reinterpret_cast<const uint32_t*>(&b2);
-        }
-        tmem_st16(s_addr + b * 16, pk);
-        if (b & 1) {
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) mbar_arrive(&ready[b >> 1]);
-        }
+    for (int i = 0; i < STEP / 2; ++i) {
+        float w0, w1;
+        attn::unpack2(attn::fma2(attn::pack2(__uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1])), scale2, neg_m2), w0, w1);
+        w0 = attn::ex2_approx(w0);
+        w1 = attn::ex2_approx(w1);
+        sum2[i & 1] = attn::add2(sum2[i & 1], attn::pack2(w0, w1));
+        const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
+        pk[i] = *reinterpret_cast<const uint32_t*>(&b2);
     }
+    tmem_st32(s_addr, pk);
     float c0, c1;
     attn::unpack2(attn::add2(sum2[0], sum2[1]), c0, c1);
     return c0 + c1;
@@ -145,26 +101,23 @@ __device__ __forceinline__ bool is_edge(const PagedAttnArgs& a, const Cursor& c,
     const int lo = a.window > 0 ? L + c.x.r0 + c.x.nr - a.window : 0;
     return p0 + CK > hi || p0 < lo;
 }
-// the 128 keys of the chunk at p0 as bits: which of them the pair sees
-__device__ __forceinline__ void chunk_bits(const RowMask& m, int p0, int L, int n, uint32_t (&w)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int lo = max(m.lo - p0 - 32 * i, 0), hi = min(m.hi - p0 - 32 * i, 32);
-        w[i] = hi > lo ? (hi - lo >= 32 ? 0xffffffffu : ((1u << (hi - lo)) - 1u) << lo) : 0u;
-    }
+// the keys of the step at p0 as bits: which of them the pair sees
+__device__ __forceinline__ void step_bits(const RowMask& m, int p0, int L, int n, uint32_t (&w)[2]) {
+    const int lo = max(m.lo - p0, 0), hi = min(m.hi - p0, STEP);
+    unsigned long long bits = hi > lo ? (hi - lo >= 64 ? ~0ull : ((1ull << (hi - lo)) - 1ull) << lo) : 0ull;
     if (m.b0 | m.b1) {
         // block row j stands at position L + j: bit j goes to bit j + L - p0
         unsigned long long b0 = m.b0, b1 = m.b1;
         if (n < 64) { b0 &= (1ull << n) - 1ull; b1 = 0; }
         else if (n < 128) b1 &= (1ull << (n - 64)) - 1ull;
-        const int up = L - p0;
-        if (up >= 64 && up < 128) { b1 = b0 << (up - 64); b0 = 0; }
-        else if (up > 0 && up < 64) { b1 = (b1 << up) | (b0 >> (64 - up)); b0 <<= up; }
-        else if (up < 0 && up > -64) { b0 = (b0 >> -up) | (b1 << (64 + up)); b1 >>= -up; }
-        else if (up <= -64 && up > -128) { b0 = b1 >> (-up - 64); b1 = 0; }
-        else if (up != 0) b0 = b1 = 0;
-        w[0] |= (uint32_t)b0; w[1] |= (uint32_t)(b0 >> 32); w[2] |= (uint32_t)b1; w[3] |= (uint32_t)(b1 >> 32);
+        const int down = p0 - L;
+        if (down == 0) bits |= b0;
+        else if (down > 0 && down < 64) bits |= (b0 >> down) | (b1 << (64 - down));
+        else if (down >= 64 && down < 128) bits |= b1 >> (down - 64);
+        else if (down < 0 && down > -64) bits |= b0 << -down;
     }
+    w[0] = (uint32_t)bits;
+    w[1] = (uint32_t)(bits >> 32);
 }
 
 template <int D>
@@ -180,8 +133,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     uint64_t* v_ok = v_full + C::VST;                                  // [VST] they have been looked after
     uint64_t* v_empty = v_ok + C::VST;                                 // [VST] both subtiles' P V have completed
     uint64_t* s_full = v_empty + C::VST;                               // [2] scores of a subtile's chunk
-    uint64_t* p_ready = s_full + 2;                                    // [2][2] its weights, by halves of the chunk
-    uint64_t* o_full = p_ready + 4;                                    // [2] the piece's last P V has completed
+    uint64_t* p_ready = s_full + 2;                                    // [2][2] weights, by halves of the chunk
+    uint64_t* pv_done = p_ready + 4;                                   // [2] the first half's P V has completed
+    uint64_t* o_full = pv_done + 2;                                    // [2] the piece's last P V has completed
     uint64_t* o_free = o_full + 2;                                     // [2] the accumulator has been read
     uint64_t* q_full = o_free + 2;
     uint64_t* q_empty = q_full + 1;
@@ -196,7 +150,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         prefetch_tensormap(&p.map_q);
         for (int i = 0; i < C::KST; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < C::VST; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_ok[i], 1); mbar_init(&v_empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[2 * i], 4); mbar_init(&p_ready[2 * i + 1], 4); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
+        for (int i = 0; i < 4; ++i) mbar_init(&p_ready[i], 4);
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&pv_done[i], 1); mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 4); }
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         *s_abort = 0;
@@ -219,8 +174,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
     unsigned char* sQ = smem;
     unsigned char *sK = smem + C::OFF_K, *sV = smem + C::OFF_V;
 
-    // registers: 384 x 168 at launch = 128 x 88 + 256 x 208; a softmax thread holds its 128 scores at once
-    if (warp < 4) { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0 || warp == 2) {
         // ---------------- TMA: warp 0 keys and queries, warp 2 values.  The lanes look up a chunk's pages, one lane issues box after box (a copy
         // issued by every lane for itself runs lane by lane, at some 50 cycles each)
@@ -285,13 +238,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         uint32_t ch = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // chunks, pieces, chunks and pieces of each subtile
         bool ok = true;
         auto issue_qk = [&](int s, int st) {
-            uint64_t da = q_desc + (uint32_t)(s * C::TILE_BYTES >> 4), db = k_desc + (uint32_t)(st * C::TILE_BYTES >> 4);
+            const uint64_t da = q_desc + (uint32_t)(s * C::TILE_BYTES >> 4), db = k_desc + (uint32_t)(st * C::TILE_BYTES >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                if (leader) umma(tmem_base + s * 128, da, db, C::IDESC_QK, kk > 0 ? 1u : 0u);
-                const uint32_t step = kk == 3 ? (HALF_BYTES - 96) >> 4 : 32 >> 4;      // the next 32 bytes of the row, or the row in the other half
-                da += step;
-                db += step;
+                const uint32_t off = ((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
+                if (leader) umma(tmem_base + s * 128, da + off, db + off, C::IDESC_QK, kk > 0 ? 1u : 0u);
             }
             if (leader) umma_commit(&s_full[s]);
         };
@@ -307,35 +258,34 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             for (int j = 0; j < pc.n && ok; ++j, ++ch) {
                 const uint32_t vs = ch % C::VST, ks = (ch + 1) % C::KST;     // stages of this chunk's values, of the next one's keys
                 const bool more = j + 1 < pc.n;
-                for (int s = 0; s < subs && ok; ++s) {
+#pragma unroll 1
+                for (int s = 0; s < subs; ++s) {
                     const uint32_t g = s ? g1 : g0, np = s ? pieces1 : pieces0;
-                    uint64_t db = v_desc + (uint32_t)(vs * C::TILE_BYTES >> 4);
-                    uint32_t pa = tmem_base + s * 128;
-#pragma unroll
-                    for (int hf = 0; hf < 2 && ok; ++hf) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(&p_ready[2 * s + hf], (g + j) & 1, s_abort) &&
-                                                         (s + hf > 0 || mbar_wait(&v_ok[vs], (ch / C::VST) & 1, s_abort)) &&
-                                                         (j + hf > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)));
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                        for (int kk = 0; kk < CK / 32; ++kk, pa += 8, db += 16 * 128 >> 4)
-                            if (leader) umma_ta(tmem_base + 256 + s * 128, pa, db, C::IDESC_PV, (j + hf + kk > 0) ? 1u : 0u);
-                    }
+                    const uint64_t db = v_desc + (uint32_t)(vs * C::TILE_BYTES >> 4);
+                    const uint32_t pa = tmem_base + s * 128;
+                    // the first half of the weights, as soon as it stands
+                    ok = __all_sync(0xffffffffu, (s > 0 || mbar_wait(&v_ok[vs], (ch / C::VST) & 1, s_abort)) &&
+                                                     (j > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)) && mbar_wait(&p_ready[2 * s], (g + j) & 1, s_abort));
                     if (!ok) break;
-                    if (leader && s == subs - 1) umma_commit(&v_empty[vs]);
-                    if (!more) {
-                        if (leader) umma_commit(&o_full[s]);
-                        continue;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int kk = 0; kk < STEP / 16; ++kk)
+                        if (leader) umma_ta(pa + 256, pa + kk * 8, db + (kk * 16 * 128 >> 4), C::IDESC_PV, (j + kk > 0) ? 1u : 0u);
+                    if (leader) umma_commit(&pv_done[s]);
+                    ok = __all_sync(0xffffffffu, (s > 0 || !more || mbar_wait(&k_full[ks], ((ch + 1) / C::KST) & 1, s_abort)) &&
+                                                     mbar_wait(&p_ready[2 * s + 1], (g + j) & 1, s_abort));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int kk = STEP / 16; kk < CK / 16; ++kk)
+                        if (leader) umma_ta(pa + 256, pa + STEP / 2 + kk * 8, db + (kk * 16 * 128 >> 4), C::IDESC_PV, 1u);
+                    if (more) issue_qk(s, ks);
+                    else if (leader) umma_commit(&o_full[s]);
+                    if (leader && s == subs - 1) {
+                        umma_commit(&v_empty[vs]);
+                        if (more) umma_commit(&k_empty[ks]);
+                        if (j + 2 == pc.n) umma_commit(q_empty);
                     }
-                    if (s == 0) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(&k_full[ks], ((ch + 1) / C::KST) & 1, s_abort));
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    }
-                    issue_qk(s, ks);
-                    if (leader && s == subs - 1) umma_commit(&k_empty[ks]);
-                    if (leader && s == subs - 1 && j + 2 == pc.n) umma_commit(q_empty);
                 }
             }
             g0 += pc.n;
@@ -345,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             if (u < end) next_tile<CK>(a, c);
         }
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
-    } else {
+    } else if (warp == 3) {
         // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
         uint32_t ch = 0, n_it = 0;
         bool ok = true;
@@ -395,8 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         }
         if (lane == 0) a.desc[blockIdx.x] = desc;
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
-    } } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    } else {
         // ---------------- softmax and output of subtile sub: a thread per pair
         const int sub = (warp - 4) >> 2, q4 = warp & 3, row = q4 * 32 + lane;
         const uint32_t s_addr = tmem_base + ((uint32_t)(q4 * 32) << 16) + sub * 128, o_addr = s_addr + 256;
@@ -416,54 +365,66 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 if (valid) mask = row_mask(a, c.s, c.x.r0 + trow);
                 const bool live = __any_sync(0xffffffffu, valid);
                 float m_run = -INFINITY, l_run = 0.f;
-                for (int j = 0; j < pc.n; ++j, ++g) {
+#pragma unroll 2
+                for (int i = 0; i < 2 * pc.n; ++i) {
+                    const int h = i & 1;                                         // half h of a chunk goes through half h of the columns
+                    const uint32_t gc = g + (i >> 1);                            // chunks of this subtile so far
                     // (a wait that fails takes the whole warp out: the accesses to tensor memory are warp-wide)
-                    if (!__all_sync(0xffffffffu, mbar_wait(&s_full[sub], g & 1, s_abort))) { ok = false; break; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (h == 0) {
+                        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[sub], gc & 1, s_abort))) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    }
                     if (live) {
-                        const int p0 = (pc.c0 + j) * CK;
-                        uint32_t sv[128];
-                        tmem_ld128(s_addr, sv);
-                        const bool whole = __all_sync(0xffffffffu, p0 >= mask.lo && p0 + CK <= mask.hi);
+                        const int p0 = pc.c0 * CK + i * STEP;
+                        uint32_t sv[STEP];
+                        attn::tmem_ld64(s_addr + h * STEP, sv);
+                        const bool whole = __all_sync(0xffffffffu, p0 >= mask.lo && p0 + STEP <= mask.hi);
                         if (!whole) {
-                            uint32_t w[4];
-                            chunk_bits(mask, p0, L, c.s.n, w);
+                            uint32_t w[2];
+                            step_bits(mask, p0, L, c.s.n, w);
 #pragma unroll
-                            for (int i = 0; i < 128; ++i) sv[i] = (w[i >> 5] >> (i & 31)) & 1u ? sv[i] : 0xff800000u;
+                            for (int e = 0; e < STEP; ++e) sv[e] = (w[e >> 5] >> (e & 31)) & 1u ? sv[e] : 0xff800000u;
                         }
                         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int i = 0; i < 128; i += 8)
+                        for (int e = 0; e < STEP; e += 8)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) m4[e] = max3_nan(m4[e], __uint_as_float(sv[i + 2 * e]), __uint_as_float(sv[i + 2 * e + 1]));
+                            for (int f = 0; f < 4; ++f) m4[f] = max3_nan(m4[f], __uint_as_float(sv[e + 2 * f]), __uint_as_float(sv[e + 2 * f + 1]));
                         float cmax = max3_nan(m4[0], m4[1], max3_nan(m4[2], m4[3], m4[3])) * a.scale_log2;
                         // a logit that is no number or +infinity makes the whole row undefined, and so does a reference that is no number
                         if (!(cmax < INFINITY)) cmax = __int_as_float(0x7fffffff);
                         const bool move = m_run == -INFINITY ? cmax != -INFINITY : !(cmax - m_run <= 8.f);
                         const float m_new = move ? cmax : m_run;
                         const float m_use = m_new == -INFINITY ? 0.f : m_new;
-                        const float alpha = m_run == m_use ? 1.f : exp2f(m_run - m_use);
-                        if (j > 0 && __any_sync(0xffffffffu, move)) {
-                            // O <- O * 2^(old - new); S arriving said that O is complete
-#pragma unroll
-                            for (int b = 0; b < D / 16; ++b) {
-                                uint32_t o[16];
-                                tmem_ld16_issue(o_addr + b * 16, o);
-                                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tmem_st16(o_addr + b * 16, o);
-                            }
-                        }
-                        const float csum = whole ? weights<true>(sv, s_addr, a.scale_log2, m_use, &p_ready[2 * sub]) : weights<false>(sv, s_addr, a.scale_log2, m_use, &p_ready[2 * sub]);
+                        float alpha = 1.f;
+                        if (__any_sync(0xffffffffu, move)) alpha = m_run == m_use ? 1.f : exp2f(m_run - m_use);
+                        const float csum = weights(sv, s_addr + h * STEP, a.scale_log2, m_use);
                         l_run = fmaf(l_run, alpha, csum);
                         m_run = m_new;
-                    } else {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) { mbar_arrive(&p_ready[2 * sub]); mbar_arrive(&p_ready[2 * sub + 1]); }
+                        if (i > 0 && __any_sync(0xffffffffu, move)) {
+                            // O <- O * 2^(old - new).  The chunk's scores said that the products of the chunk before have completed; within a chunk the
+                            // first half's has to.  (Its phase before is over for the same reason, and the next one waits for this half's weights: no
+                            // phase can be mistaken for another.)
+                            if (h == 1) {
+                                if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[sub], gc & 1, s_abort))) { ok = false; break; }
+                                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            }
+#pragma unroll 1
+                            for (int b = 0; b < D / 32; ++b) {
+                                uint32_t o[32];
+                                tmem_ld32(o_addr + b * 32, o);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                                tmem_st32(o_addr + b * 32, o);
+                            }
+                        }
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_ready[2 * sub + h]);
                 }
+                g += pc.n;
                 if (!ok) break;
                 if (!__all_sync(0xffffffffu, mbar_wait(&o_full[sub], np & 1, s_abort))) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
