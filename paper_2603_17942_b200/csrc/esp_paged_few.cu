@@ -19,7 +19,7 @@ namespace {
 using namespace tc;
 using namespace paged;
 
-constexpr int WARPS = 4, STAGES = 3, STAGE_BYTES = 16384;
+constexpr int WARPS = 6, STAGES = 2, STAGE_BYTES = 16384;
 constexpr int SMEM = 1024 + WARPS * STAGES * STAGE_BYTES + 256;
 
 struct FewParams {
@@ -402,7 +402,7 @@ int launch_paged_merge_few(int dtype, const PagedAttnArgs& a, cudaStream_t s) {
 bool paged_few_supported(int dtype, const PagedAttnArgs& a) {
     int box = 0;
     // (a lane reads two elements of a query at a time)
-    return dtype == 1 && (a.D == 64 || a.D == 128) && a.group <= 16 && a.seq.max_new == 1 && !a.anc && paged_tma_pages(a, a.D == 128 ? 32 : 64, &box) &&
+    return dtype == 1 && (a.D == 64 || a.D == 128) && a.group <= 16 && a.seq.max_new == 1 && !a.anc && paged_tma_pages(a, STAGE_BYTES / (a.D * 4), &box) &&
            reinterpret_cast<uintptr_t>(a.q.p) % 4 == 0 && a.q.tok % 2 == 0 && a.q.head % 2 == 0;
 }
 
@@ -410,14 +410,14 @@ int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s) {
     FewParams p;
     memset(&p, 0, sizeof(p));
     int box = 0;
-    if (!paged_tma_pages(a, a.D == 128 ? 32 : 64, &box)) return -1;
+    if (!paged_tma_pages(a, STAGE_BYTES / (a.D * 4), &box)) return -1;
     if (page_map5(&p.map_k, a, a.pages.k, box) || page_map5(&p.map_v, a, a.pages.v, box)) return -1;
     while ((1 << p.box_shift) < box) ++p.box_shift;
     a.rows = 1;
     a.pairs = 1;
     while (a.pairs < a.group) a.pairs *= 2;
     a.n_cta = n_sm * WARPS;
-    a.min_units = 4;
+    a.min_units = 2;
     p.a = a;
     const int rc = a.D == 128 ? run_few<128>(p, s) : run_few<64>(p, s);
     return rc ? rc : launch_paged_merge_few(1, a, s);
