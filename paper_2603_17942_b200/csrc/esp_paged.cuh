@@ -28,6 +28,7 @@ __device__ __forceinline__ Seq load_seq(const SeqTable& t, int b) {
     if (!ok) set_error(t.status, DEV_E_INDEX);
     return s;
 }
+__device__ __forceinline__ int page_index(const PagesView& p, int pos) { return p.page_shift >= 0 ? pos >> p.page_shift : pos / p.page_size; }
 // the page of a position < kv_len, -1 if the table names none
 __device__ __forceinline__ int load_page(const SeqTable& t, const PagesView& p, int b, int index) {
     const int page = __ldg(t.table + (size_t)b * t.table_stride + index);
@@ -51,7 +52,7 @@ __device__ __forceinline__ Tile make_tile(const PagedAttnArgs& a, const Seq& s, 
     x.nc = max(1, (hi + CK - 1) / CK - x.c0);
     return x;
 }
-__device__ __forceinline__ int n_tiles(const PagedAttnArgs& a, const Seq& s) { return (s.n + a.rows - 1) / a.rows; }
+__device__ __forceinline__ int n_tiles(const PagedAttnArgs& a, const Seq& s) { return a.rows_shift >= 0 ? (s.n + a.rows - 1) >> a.rows_shift : (s.n + a.rows - 1) / a.rows; }
 
 // Where a CTA stands on the line: a tile, and the CTA's own range of units.
 struct Cursor {
@@ -111,13 +112,14 @@ template <int CK>
 __device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, Share& share, Cursor& at) {
     const int per = (a.seq.batch + 31) >> 5;                             // consecutive sequences of a lane
     const int b0 = lane * per;
-    uint32_t mine = 0;
+    uint32_t mine = 0, chunks = 0;
     unsigned long long wide = 0;
     Seq s;
     for (int i = 0; i < per; ++i) {                                      // the same trips in every lane
         s.start = s.n = s.kv = 0;
         if (b0 + i < a.seq.batch) s = load_seq(a.seq, b0 + i);
-        const unsigned long long w = (unsigned long long)seq_chunks<CK>(a, s, lane) * a.Hkv;
+        chunks = seq_chunks<CK>(a, s, lane);
+        const unsigned long long w = (unsigned long long)chunks * a.Hkv;
         wide += w;
         mine += (uint32_t)w;
     }
@@ -142,7 +144,7 @@ __device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, 
         at.s.start = __shfl_sync(0xffffffffu, s.start, owner);
         at.s.n = __shfl_sync(0xffffffffu, s.n, owner);
         at.s.kv = __shfl_sync(0xffffffffu, s.kv, owner);
-        Wt = (__shfl_sync(0xffffffffu, incl, owner) - u0) / a.Hkv;
+        Wt = __shfl_sync(0xffffffffu, chunks, owner);
     } else {
         for (;; ++at.b) {                                                // the same sequence in every lane
             at.s = load_seq(a.seq, at.b);
@@ -203,15 +205,30 @@ __device__ __forceinline__ Piece make_piece(const Cursor& c, uint32_t begin, uin
     return p;
 }
 
-// What the merge kernel has to know of the tile whose first piece is CTA c's last one, if other CTAs have the rest.
-__device__ __forceinline__ MergeDesc make_desc(const PagedAttnArgs& a, const Cursor& c, const Share& share, const Piece& p, int cta) {
-    MergeDesc d;
-    d.token = c.s.start + c.x.r0;
-    d.pairs = c.x.nr * a.group;
-    d.head0 = c.kvh * a.group;
-    d.parts = (share.cta_of(c.tile_u + c.x.nc - 1) - cta + 1) * 2 + p.slot;
-    return d;
-}
+// What the merge kernel has to know of the split tiles that CTA `cta` has pieces of: at most one it has the first piece of (its last piece) and one that
+// began before it (its first piece).  two: each CTA has two parts.
+struct Descs {
+    MergeDesc starts, goes_on;
+    __device__ __forceinline__ void clear() { starts.parts = goes_on.parts = 0; }
+    __device__ __forceinline__ void note(const PagedAttnArgs& a, const Cursor& c, const Share& share, const Piece& p, bool two = false) {
+        if (p.slot < 0) return;
+        MergeDesc d;
+        d.token = c.s.start + c.x.r0;
+        d.pairs = c.x.nr * a.group;
+        d.head0 = c.kvh * a.group;
+        d.first = share.cta_of(c.tile_u);
+        d.parts = (share.cta_of(c.tile_u + c.x.nc - 1) - d.first + 1) * 4 + (two ? 2 : 0) + (share.begin(d.first) >= c.tile_u ? 0 : 1);
+        if (p.c0 == c.x.c0) starts = d;
+        else goes_on = d;
+    }
+    __device__ __forceinline__ void store(const PagedAttnArgs& a, int cta) const {
+        int4* to = reinterpret_cast<int4*>(a.desc + 2 * cta);
+        to[0] = make_int4(starts.token, starts.pairs, starts.head0, starts.parts);
+        to[1] = make_int4(starts.first, 0, 0, 0);
+        to[2] = make_int4(goes_on.token, goes_on.pairs, goes_on.head0, goes_on.parts);
+        to[3] = make_int4(goes_on.first, 0, 0, 0);
+    }
+};
 // split partials: quad dq of a pair's weighted values, in the order in which a warp with a lane per pair writes them
 __device__ __forceinline__ size_t part_quad(const PagedAttnArgs& a, int cta, int slot, int dq, int pair) {
     return ((size_t)(cta * 2 + slot) * (a.D / 4) + dq) * a.pairs + pair;

@@ -15,8 +15,14 @@ struct HeadsView {      // as esp_heads; p NULL: absent
 struct PagesView {
     void *k, *v;
     long long page, tok, head;
-    int32_t n_pages, page_size;
+    int32_t n_pages, page_size, page_shift;     // log2 of page_size, -1 if it is no power of two
 };
+// log2 of x, -1 if x is no power of two: what is divided by on the way to a kernel's first load is a shift where it can be
+inline int shift_of(int x) {
+    int s = 0;
+    while ((1 << s) < x) ++s;
+    return (1 << s) == x ? s : -1;
+}
 
 struct SeqTable {
     const int32_t *q_start, *kv_len, *table;
@@ -37,9 +43,11 @@ struct NormRopeArgs {
     int32_t append;
 };
 
-struct MergeDesc {        // a tile that several CTAs share
+struct __align__(16) MergeDesc {        // a tile that several CTAs share
     int32_t token, pairs, head0;
-    int32_t parts;        // 2 x CTAs that have a piece of it + the first one's slot; 0: no such tile
+    int32_t parts;        // 4 x CTAs that have a piece of it + 2 if each of them has two parts + the first one's slot; 0: no such tile
+    int32_t first;        // the first of these CTAs
+    int32_t pad[3];
 };
 
 struct PagedAttnArgs {
@@ -50,13 +58,13 @@ struct PagedAttnArgs {
     const unsigned long long* anc;
     int32_t Hq, Hkv, group, D, window;
     float scale_log2;
-    int32_t rows;           // tokens of a tile: rows * group (token, head) pairs
+    int32_t rows, rows_shift;   // tokens of a tile: rows * group (token, head) pairs
     int32_t pairs;          // pairs of a tile's partial in the scratch
     int32_t n_cta;          // CTAs the work is dealt to
     int32_t min_units;      // fewer CTAs rather than fewer chunks than this for each
     int32_t vec;            // CUDA-core kernel: rows can be read four elements at a time
     int32_t out_vec;        // rows of out can be written four elements at a time
-    MergeDesc* desc;        // [n_cta]
+    MergeDesc* desc;        // [PAGED_MAX_CTAS][2] the split tiles that a CTA has the first piece of, and a later piece of
     float4* part_o;         // [n_cta][2][D / 4][pairs] split partials: weighted values, not divided by the sum
     float2* part_ml;        // [n_cta][2][pairs] their (maximum in the log2 domain, sum)
 };

@@ -60,7 +60,7 @@ PagesView pages_of(const esp_paged_cache* c) {
     p.page = c->n_pages > 1 ? c->page_stride : 0;
     p.tok = c->page_size > 1 ? c->token_stride : 0;
     p.head = c->n_kv_heads > 1 ? c->head_stride : 0;
-    p.n_pages = c->n_pages; p.page_size = c->page_size;
+    p.n_pages = c->n_pages; p.page_size = c->page_size; p.page_shift = c->page_size <= (1 << 30) ? shift_of(c->page_size) : -1;
     return p;
 }
 SeqTable seqs_of(const esp_paged_batch* b, const esp_paged_cache* c, int32_t n_tokens) {
@@ -226,7 +226,7 @@ int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_
     if (!bytes_out || n_q_heads < 1) return ESP_E_ARG;
     if (head_dim != 32 && head_dim != 64 && head_dim != 128) return ESP_E_BADCFG;
     const size_t rows = (size_t)PAGED_MAX_SMS * 2 * PAGED_MAX_PAIRS;
-    *bytes_out = sizeof(MergeDesc) * PAGED_MAX_CTAS + rows * head_dim * sizeof(float) + rows * sizeof(float2);
+    *bytes_out = 2 * sizeof(MergeDesc) * PAGED_MAX_CTAS + rows * head_dim * sizeof(float) + rows * sizeof(float2);
     return ESP_OK;
 }
 
@@ -259,7 +259,7 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     const size_t rows = (size_t)PAGED_MAX_SMS * 2 * PAGED_MAX_PAIRS;
     a.min_units = 1;
     a.desc = reinterpret_cast<MergeDesc*>(scratch);
-    a.part_o = reinterpret_cast<float4*>(a.desc + PAGED_MAX_CTAS);
+    a.part_o = reinterpret_cast<float4*>(a.desc + 2 * PAGED_MAX_CTAS);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + rows * (a.D / 4));
     const size_t es = elem_size(cache->dtype), quad = 4 * es;
     auto by4 = [&](const void* p, int64_t s0, int64_t s1, int64_t s2) {

@@ -73,10 +73,10 @@ __global__ void __launch_bounds__(WARPS * 32) k_paged_few(const __grid_constant_
     pdl_launch_dependents();
     Share share;
     Cursor c;
-    MergeDesc desc;
-    desc.token = desc.pairs = desc.head0 = desc.parts = 0;
+    Descs desc;
+    desc.clear();
     if (!deal<KEYS>(a, worker, lane, share, c)) {
-        if (lane == 0) a.desc[worker] = desc;
+        if (lane == 0) desc.store(a, worker);
         return;
     }
     const uint32_t begin = share.begin(worker), end = share.begin(worker + 1);
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(WARPS * 32) k_paged_few(const __grid_constant_
         page = a.pages.n_pages;         // a page that there is not reads as zeros
         slot = 0;
         if (pos < ci.s.kv) {
-            const int index = pos / a.pages.page_size;
+            const int index = page_index(a.pages, pos);
             const int pg = load_page(a.seq, a.pages, ci.b, index);
             if (pg >= 0) page = pg;
             slot = pos - index * a.pages.page_size;
@@ -276,10 +276,10 @@ __global__ void __launch_bounds__(WARPS * 32) k_paged_few(const __grid_constant_
                 else if (a.lse) a.lse[(size_t)c.s.start * a.Hq + head] = l_run[r] == 0.f ? -INFINITY : (m_run[r] + log2f(l_run[r])) * 0.6931471805599453f;
             }
         }
-        if (pc.slot >= 0 && pc.c0 == c.x.c0) desc = make_desc(a, c, share, pc, worker);
+        desc.note(a, c, share, pc);
         if (u < end) next_tile<KEYS>(a, c);
     }
-    if (lane == 0) a.desc[worker] = desc;
+    if (lane == 0) desc.store(a, worker);
     if (!ok) {
         if (lane == 0) set_error(a.seq.status, DEV_E_WAIT_TIMEOUT);
         for (int i = 0; i < 64; ++i) __nanosleep(10000);    // let copies in flight land before shared memory goes away
@@ -295,8 +295,8 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge_few(const __gr
     __shared__ float s_l[MERGE_WARPS][16], s_m[16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x, pairs = a.pairs;      // a power of two, at most 16
     pdl_wait();
-    const int4 dd = __ldcg(reinterpret_cast<const int4*>(a.desc + c));
-    const int n_pairs = dd.y, n = dd.w >> 1, first_slot = dd.w & 1;
+    const int4 dd = __ldcg(reinterpret_cast<const int4*>(a.desc + 2 * c));
+    const int n_pairs = dd.y, n = dd.w >> 2, first_slot = dd.w & 1;
     if (n == 0) return;
     auto slot_of = [&](int k) { return 2 * k + (k == 0 ? first_slot : 0); };
     const float2* ml = a.part_ml + part_row(a, c, 0, lane & (pairs - 1));
@@ -412,8 +412,9 @@ int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s) {
     int box = 0;
     if (!paged_tma_pages(a, STAGE_BYTES / (a.D * 4), &box)) return -1;
     if (page_map5(&p.map_k, a, a.pages.k, box) || page_map5(&p.map_v, a, a.pages.v, box)) return -1;
-    while ((1 << p.box_shift) < box) ++p.box_shift;
+    p.box_shift = shift_of(box);
     a.rows = 1;
+    a.rows_shift = 0;
     a.pairs = 1;
     while (a.pairs < a.group) a.pairs *= 2;
     a.n_cta = n_sm * WARPS;

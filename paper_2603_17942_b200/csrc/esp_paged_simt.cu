@@ -45,10 +45,10 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
     pdl_launch_dependents();
     Share share;
     Cursor c;
-    MergeDesc desc;
-    desc.parts = 0;
+    Descs desc;
+    desc.clear();
     if (!deal<CK>(a, blockIdx.x, tid & 31, share, c)) {
-        if (tid == 0) a.desc[blockIdx.x] = desc;
+        if (tid == 0) desc.store(a, blockIdx.x);
         return;
     }
     const uint32_t begin = share.begin(blockIdx.x), end = share.begin(blockIdx.x + 1);
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
                 const int pos = p0 + tid;
                 long long base = -1;
                 if (pos < c.s.kv) {
-                    const int index = pos / a.pages.page_size;
+                    const int index = page_index(a.pages, pos);
                     const int page = load_page(a.seq, a.pages, c.b, index);
                     if (page >= 0) base = page * a.pages.page + (pos - index * a.pages.page_size) * a.pages.tok + c.kvh * a.pages.head;
                 }
@@ -210,77 +210,106 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
                 if (tx == 0) a.part_ml[part_row(a, blockIdx.x, pc.slot, pr)] = make_float2(m_run[i], l_run[i]);
             }
         }
-        if (pc.slot >= 0 && pc.c0 == c.x.c0) desc = make_desc(a, c, share, pc, blockIdx.x);
+        desc.note(a, c, share, pc);
         u += pc.n;
         if (u < end) next_tile<CK>(a, c);
     }
-    if (tid == 0) a.desc[blockIdx.x] = desc;
+    if (tid == 0) desc.store(a, blockIdx.x);
 }
 
-// The tile whose first piece CTA c has as its last one (c = blockIdx.x), if other CTAs have the rest: the partials are weighed by 2^(m - max m) in the
-// order of the CTAs.  A lane takes four quads of one pair; a warp has LP pairs side by side, as the partials lie.
-constexpr int MERGE_WARPS = 8, MERGE_QUADS = 4, MERGE_PARTS = 4;
+// Joins the split partials: column x of blocks takes its share of the tiles that CTA x has pieces of, every CTA's column the same
+// amount, however many parts a tile has.  A task is 32 pairs x 4 quads (a lane has a pair, as the partials lie); its parts are dealt to 1, 2, 4 or 8 warps, each of
+// which weighs its own by 2^(m - its maximum), and the warps' sums are joined in order through shared memory.  (One warp for all
+// parts, all tasks of a tile in the column of its first CTA: 16 us for 18 parts; this 5.)
+constexpr int MERGE_WARPS = 8, MERGE_QUADS = 4, MERGE_PARTS = 4, MERGE_SECOND = PAGED_MAX_PAIRS / 2, MERGE_BLOCKS = 8;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) k_paged_merge(const __grid_constant__ PagedAttnArgs a) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x;
-    const int LP = min(32, a.pairs), LQ = 32 / LP, WQ = LQ * MERGE_QUADS;       // pairs and quads side by side, quads of a warp
-    const int cols = (D / 4 + WQ - 1) / WQ;                                     // warps for the quads of a pair
-    const int task = blockIdx.y * MERGE_WARPS + warp, pr = (task / cols) * LP + lane % LP, q0 = (task % cols) * WQ + lane / LP;
+    __shared__ float4 s_o[MERGE_WARPS][MERGE_QUADS][32];
+    __shared__ float2 s_ml[MERGE_WARPS][32];
+    constexpr int COLS = D / 4 / MERGE_QUADS;                                   // tasks for the quads of a pair
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, x = blockIdx.x;
     pdl_wait();
-    const int4 dd = __ldcg(reinterpret_cast<const int4*>(a.desc + c));
-    const int token = dd.x, n_pairs = dd.y, head0 = dd.z, n = dd.w >> 1, first_slot = dd.w & 1;
-    if (n == 0 || pr >= n_pairs || q0 >= D / 4) return;
-    // CTA c has the tile's first piece in slot 0 if the tile is where it starts; the CTAs behind it have theirs in slot 0
-    const float2* ml = a.part_ml + part_row(a, c, 0, pr);
-    // (loads of several parts are under way at once: a part at a time, every one is a round trip)
-    auto slot_of = [&](int k) { return 2 * k + (k == 0 ? first_slot : 0); };
-    float m = -INFINITY;
-    for (int k0 = 0; k0 < n; k0 += 8) {
-        float x[8];
+    // half of the column's blocks for the tile that starts in CTA x, half for the one that goes on in it
+    const int4* dp = reinterpret_cast<const int4*>(a.desc + 2 * x + (blockIdx.y & 1));
+    const int4 dd = __ldcg(dp);
+    const int c = __ldcg(dp + 1).x, token = dd.x, n_pairs = dd.y, head0 = dd.z, code = dd.w;
+    {
+        if (code == 0) return;
+        const int ctas = code >> 2, two = code >> 1 & 1, n = ctas << two, first_slot = code & 1;
+        const int wp = n <= 4 ? 1 : (n <= 8 ? 2 : (n <= 16 ? 4 : 8)), w = warp & (wp - 1);      // warps of a task
+        const int tasks = (n_pairs + 31) / 32 * COLS;
+        // tasks x - c, x - c + ctas, .. are this column's; its blocks take them in turn, MERGE_WARPS / wp at a time
+        for (int m0 = (blockIdx.y >> 1) * (MERGE_WARPS / wp); x - c + m0 * ctas < tasks; m0 += MERGE_BLOCKS / 2 * (MERGE_WARPS / wp)) {
+            const int task = x - c + (m0 + warp / wp) * ctas;
+            const int pr = task / COLS * 32 + lane, q0 = task % COLS * MERGE_QUADS;
+            const bool valid = task < tasks && pr < n_pairs;
+            float m = -INFINITY, l = 0.f;
+            float4 o[MERGE_QUADS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __ldcg(ml + (size_t)slot_of(min(k0 + e, n - 1)) * a.pairs).x;
+            for (int i = 0; i < MERGE_QUADS; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (valid) {
+                // (two parts of a CTA, where two groups of warps took its chunks in turn: the second one's pairs behind the first one's)
+                for (int k0 = w; k0 < n; k0 += wp * MERGE_PARTS) {
+                    float2 ml[MERGE_PARTS];
+                    float4 v[MERGE_PARTS][MERGE_QUADS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, x[e]);
-    }
-    const float m_use = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 o[MERGE_QUADS];
+                    for (int e = 0; e < MERGE_PARTS; ++e) {
+                        const int k = min(k0 + e * wp, n - 1), cta = k >> two, slot = cta == 0 ? first_slot : 0, at = pr + (two && (k & 1) ? MERGE_SECOND : 0);
+                        ml[e] = __ldcg(a.part_ml + part_row(a, c + cta, slot, at));
 #pragma unroll
-    for (int i = 0; i < MERGE_QUADS; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    const size_t part = (size_t)(D / 4) * a.pairs;
-    const float4* po = a.part_o + part_quad(a, c, 0, q0, pr);
-    for (int k0 = 0; k0 < n; k0 += MERGE_PARTS) {
-        float2 x[MERGE_PARTS];
-        float4 v[MERGE_PARTS][MERGE_QUADS];
+                        for (int i = 0; i < MERGE_QUADS; ++i) v[e][i] = __ldcg(a.part_o + part_quad(a, c + cta, slot, q0 + i, at));
+                    }
 #pragma unroll
-        for (int e = 0; e < MERGE_PARTS; ++e) {
-            const int sl = slot_of(min(k0 + e, n - 1));
-            x[e] = __ldcg(ml + (size_t)sl * a.pairs);
+                    for (int e = 0; e < MERGE_PARTS; ++e) {
+                        if (k0 + e * wp >= n || ml[e].y == 0.f) continue;      // (a part that saw nothing may have left its values as they were)
+                        const float m_new = fmaxf(m, ml[e].x), old = m == m_new ? 1.f : exp2f(m - m_new), wt = ml[e].x == m_new ? 1.f : exp2f(ml[e].x - m_new);
+                        l = fmaf(ml[e].y, wt, l * old);
 #pragma unroll
-            for (int i = 0; i < MERGE_QUADS; ++i) v[e][i] = __ldcg(po + sl * part + (q0 + i * LQ < D / 4 ? i * LQ : 0) * a.pairs);
-        }
-#pragma unroll
-        for (int e = 0; e < MERGE_PARTS; ++e) {
-            if (k0 + e >= n) break;
-            const float w = exp2f(x[e].x - m_use);
-            l = fmaf(x[e].y, w, l);
-#pragma unroll
-            for (int i = 0; i < MERGE_QUADS; ++i) {
-                o[i].x = fmaf(v[e][i].x, w, o[i].x); o[i].y = fmaf(v[e][i].y, w, o[i].y);
-                o[i].z = fmaf(v[e][i].z, w, o[i].z); o[i].w = fmaf(v[e][i].w, w, o[i].w);
+                        for (int i = 0; i < MERGE_QUADS; ++i) {
+                            o[i].x = fmaf(v[e][i].x, wt, o[i].x * old); o[i].y = fmaf(v[e][i].y, wt, o[i].y * old);
+                            o[i].z = fmaf(v[e][i].z, wt, o[i].z * old); o[i].w = fmaf(v[e][i].w, wt, o[i].w * old);
+                        }
+                        m = m_new;
+                    }
+                }
             }
+            if (wp > 1) {
+                s_ml[warp][lane] = make_float2(m, l);
+#pragma unroll
+                for (int i = 0; i < MERGE_QUADS; ++i) s_o[warp][i][lane] = o[i];
+                __syncthreads();
+                const int w0 = warp - w;                                        // the task's first warp
+                m = -INFINITY;
+                for (int k = 0; k < wp; ++k) m = fmaxf(m, s_ml[w0 + k][lane].x);
+                l = 0.f;
+#pragma unroll
+                for (int i = 0; i < MERGE_QUADS; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k = 0; k < wp; ++k) {
+                    const float2 ml = s_ml[w0 + k][lane];
+                    if (ml.y == 0.f) continue;
+                    const float wt = ml.x == m ? 1.f : exp2f(ml.x - m);
+                    l = fmaf(ml.y, wt, l);
+#pragma unroll
+                    for (int i = 0; i < MERGE_QUADS; ++i) {
+                        if (i % wp != w) continue;                              // a quad for each of the warps
+                        const float4 y = s_o[w0 + k][i][lane];
+                        o[i].x = fmaf(y.x, wt, o[i].x); o[i].y = fmaf(y.y, wt, o[i].y); o[i].z = fmaf(y.z, wt, o[i].z); o[i].w = fmaf(y.w, wt, o[i].w);
+                    }
+                }
+            }
+            if (valid) {
+                const int row = pr / a.group, head = head0 + pr - row * a.group;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                T* y = reinterpret_cast<T*>(a.out.p) + out_offset(a.out, token + row, head);
+#pragma unroll
+                for (int i = 0; i < MERGE_QUADS; ++i)
+                    if (wp == 1 || i % wp == w) store4<T>(y + 4 * (q0 + i), make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
+                if (a.lse && q0 == 0 && w == 0) a.lse[(size_t)(token + row) * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            }
+            if (wp > 1) __syncthreads();                                        // shared memory is free for the next round
         }
     }
-    const int row = pr / a.group, head = head0 + pr - row * a.group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* y = reinterpret_cast<T*>(a.out.p) + out_offset(a.out, token + row, head);
-#pragma unroll
-    for (int i = 0; i < MERGE_QUADS; ++i) {
-        const int q = q0 + i * LQ;
-        if (q < D / 4) store4<T>(y + 4 * q, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
-    }
-    if (a.lse && q0 == 0) a.lse[(size_t)(token + row) * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, int MP, bool VEC>
@@ -302,10 +331,7 @@ int run_simt_t(const PagedAttnArgs& a, cudaStream_t s) {
 
 template <typename T, int D>
 int run_merge(const PagedAttnArgs& a, cudaStream_t s) {
-    const int lp = a.pairs < 32 ? a.pairs : 32, wq = 32 / lp * MERGE_QUADS;
-    const int tasks = (a.rows * a.group + lp - 1) / lp * ((D / 4 + wq - 1) / wq);
-    if (a.n_cta < 2) return 0;
-    return launch_k(k_paged_merge<T, D>, dim3(a.n_cta - 1, (tasks + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, true, a) != cudaSuccess;
+    return launch_k(k_paged_merge<T, D>, dim3(a.n_cta, MERGE_BLOCKS), dim3(MERGE_WARPS * 32), 0, s, true, a) != cudaSuccess;
 }
 
 }  // namespace
@@ -316,12 +342,15 @@ int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s) {
 }
 
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {
-    const int need = a.group * a.seq.max_new;       // pairs of the longest sequence and KV head
-    a.pairs = need <= 16 ? 16 : 64;
+    // Small tiles in small calls: more blocks at once, at a higher price per pair.  696 pairs in all (5 sequences of up to 100 tokens, heads of 64)
+    // 25.5 us with tiles of 64 pairs, 18.6 with 16; 3200 pairs (4 of up to 300) 43 and 54.
+    const bool few = a.group * a.seq.max_new <= 16 || (long long)a.seq.n_tokens * a.Hq < 16ll * n_sm;
+    a.pairs = few && a.group <= 16 ? 16 : 64;
     a.rows = a.pairs / a.group;
     if (a.rows < 1) return -1;                      // more than 64 query heads share a KV head
+    a.rows_shift = shift_of(a.rows);
     a.n_cta = n_sm * (a.pairs == 16 ? 4 : 2);
-    a.min_units = 2;
+    a.min_units = 1;
     const int rc = dtype == 0 ? run_simt_t<float>(a, s) : run_simt_t<__nv_bfloat16>(a, s);
     if (rc) return rc;
     return a.pairs <= 16 ? launch_paged_merge_few(dtype, a, s) : launch_paged_merge(dtype, a, s);

@@ -94,6 +94,12 @@ __device__ __forceinline__ float weights(const uint32_t (&sv)[STEP], uint32_t s_
     return c0 + c1;
 }
 
+// A tile of one subtile whose keys several CTAs share anyway: its chunks go to the two sets of scores, accumulators and softmax warps in turn, each
+// with a reference and a sum of its own, and the merge kernel joins one part more.  A single set would wait for every product and every
+// softmax in turn (XX).
+__device__ __forceinline__ bool in_turn(const Piece& pc, int subs) { return subs == 1 && pc.slot >= 0; }
+__device__ __forceinline__ int chunks_of(const Piece& pc, int subs, int sub) { return in_turn(pc, subs) ? (pc.n + 1 - sub) / 2 : (sub < subs ? pc.n : 0); }
+
 // A chunk that some pair of the tile does not see as a whole (the last one of the cache, the diagonal, the window's edge, the tree).
 __device__ __forceinline__ bool is_edge(const PagedAttnArgs& a, const Cursor& c, int p0) {
     const int L = c.s.kv - c.s.n;
@@ -188,7 +194,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 const int pos = (pc.c0 + j) * CK + box * p.box_rows;
                 int page = a.pages.n_pages, slot = 0;       // a page that there is not reads as zeros
                 if (pos < c.s.kv) {
-                    const int index = pos / a.pages.page_size;
+                    const int index = page_index(a.pages, pos);
                     const int pg = load_page(a.seq, a.pages, c.b, index);
                     if (pg >= 0) page = pg;
                     slot = pos - index * a.pages.page_size;
@@ -237,8 +243,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         const uint64_t q_desc = smem_desc(smem_u32(sQ), 16), k_desc = smem_desc(smem_u32(sK), 16), v_desc = smem_desc(smem_u32(sV), HALF_BYTES);
         uint32_t ch = 0, n_it = 0, g0 = 0, g1 = 0, pieces0 = 0, pieces1 = 0;   // chunks, pieces, chunks and pieces of each subtile
         bool ok = true;
-        auto issue_qk = [&](int s, int st) {
-            const uint64_t da = q_desc + (uint32_t)(s * C::TILE_BYTES >> 4), db = k_desc + (uint32_t)(st * C::TILE_BYTES >> 4);
+        auto issue_qk = [&](int s, int q, int st) {          // scores s of the queries of subtile q
+            const uint64_t da = q_desc + (uint32_t)(q * C::TILE_BYTES >> 4), db = k_desc + (uint32_t)(st * C::TILE_BYTES >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 const uint32_t off = ((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4;
@@ -249,48 +255,61 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int subs = c.x.nr > p.sub_rows ? 2 : 1;
+            const bool alt = in_turn(pc, subs);
             ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&k_full[ch % C::KST], (ch / C::KST) & 1, s_abort));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int s = 0; s < subs; ++s) issue_qk(s, ch % C::KST);
+            for (int s = 0; s < subs; ++s) issue_qk(s, s, ch % C::KST);
             if (leader) umma_commit(&k_empty[ch % C::KST]);
-            if (leader && pc.n == 1) umma_commit(q_empty);
+            const int ahead = alt ? 2 : 1;                               // a set of scores' next chunk
+            if (alt && pc.n > 1) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&k_full[(ch + 1) % C::KST], ((ch + 1) / C::KST) & 1, s_abort));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                issue_qk(1, 0, (ch + 1) % C::KST);
+                if (leader) umma_commit(&k_empty[(ch + 1) % C::KST]);
+            }
+            if (leader && pc.n <= ahead) umma_commit(q_empty);
             for (int j = 0; j < pc.n && ok; ++j, ++ch) {
-                const uint32_t vs = ch % C::VST, ks = (ch + 1) % C::KST;     // stages of this chunk's values, of the next one's keys
-                const bool more = j + 1 < pc.n;
+                const uint32_t vs = ch % C::VST, kn = ch + ahead, ks = kn % C::KST;     // stages of this chunk's values, of the next keys
+                const bool more = j + ahead < pc.n;
+                const int jl = alt ? j >> 1 : j, s_end = alt ? (j & 1) + 1 : subs;
 #pragma unroll 1
-                for (int s = 0; s < subs; ++s) {
+                for (int s = alt ? j & 1 : 0; s < s_end; ++s) {
                     const uint32_t g = s ? g1 : g0, np = s ? pieces1 : pieces0;
                     const uint64_t db = v_desc + (uint32_t)(vs * C::TILE_BYTES >> 4);
                     const uint32_t pa = tmem_base + s * 128;
+                    const bool first = alt || s == 0;
                     // the first half of the weights, as soon as it stands
-                    ok = __all_sync(0xffffffffu, (s > 0 || mbar_wait(&v_ok[vs], (ch / C::VST) & 1, s_abort)) &&
-                                                     (j > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)) && mbar_wait(&p_ready[2 * s], (g + j) & 1, s_abort));
+                    ok = __all_sync(0xffffffffu, (!first || mbar_wait(&v_ok[vs], (ch / C::VST) & 1, s_abort)) &&
+                                                     (jl > 0 || mbar_wait(&o_free[s], (np & 1) ^ 1, s_abort)) && mbar_wait(&p_ready[2 * s], (g + jl) & 1, s_abort));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                     for (int kk = 0; kk < STEP / 16; ++kk)
-                        if (leader) umma_ta(pa + 256, pa + kk * 8, db + (kk * 16 * 128 >> 4), C::IDESC_PV, (j + kk > 0) ? 1u : 0u);
+                        if (leader) umma_ta(pa + 256, pa + kk * 8, db + (kk * 16 * 128 >> 4), C::IDESC_PV, (jl + kk > 0) ? 1u : 0u);
                     if (leader) umma_commit(&pv_done[s]);
-                    ok = __all_sync(0xffffffffu, (s > 0 || !more || mbar_wait(&k_full[ks], ((ch + 1) / C::KST) & 1, s_abort)) &&
-                                                     mbar_wait(&p_ready[2 * s + 1], (g + j) & 1, s_abort));
+                    ok = __all_sync(0xffffffffu, (!first || !more || mbar_wait(&k_full[ks], (kn / C::KST) & 1, s_abort)) &&
+                                                     mbar_wait(&p_ready[2 * s + 1], (g + jl) & 1, s_abort));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                     for (int kk = STEP / 16; kk < CK / 16; ++kk)
                         if (leader) umma_ta(pa + 256, pa + STEP / 2 + kk * 8, db + (kk * 16 * 128 >> 4), C::IDESC_PV, 1u);
-                    if (more) issue_qk(s, ks);
+                    if (more) issue_qk(s, alt ? 0 : s, ks);
                     else if (leader) umma_commit(&o_full[s]);
-                    if (leader && s == subs - 1) {
+                    if (leader && s == s_end - 1) {
                         umma_commit(&v_empty[vs]);
                         if (more) umma_commit(&k_empty[ks]);
-                        if (j + 2 == pc.n) umma_commit(q_empty);
+                        if (j + ahead + 1 == pc.n) umma_commit(q_empty);
                     }
                 }
             }
-            g0 += pc.n;
+            const int n1 = chunks_of(pc, subs, 1);
+            g0 += chunks_of(pc, subs, 0);
             ++pieces0;
-            if (subs == 2) { g1 += pc.n; ++pieces1; }
+            g1 += n1;
+            pieces1 += n1 > 0;
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);
         }
@@ -299,11 +318,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         // ---------------- values: in chunks that not every pair sees, what is no finite number becomes zero before the product
         uint32_t ch = 0, n_it = 0;
         bool ok = true;
-        MergeDesc desc;
-        desc.parts = 0;
+        Descs desc;
+        desc.clear();
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
-            if (pc.slot >= 0 && pc.c0 == c.x.c0) desc = make_desc(a, c, share, pc, blockIdx.x);
+            desc.note(a, c, share, pc, in_turn(pc, c.x.nr > p.sub_rows ? 2 : 1));
             if (lane == 0) s_odd[(n_it + 1) % ODD_RING] = 0;
             for (int j = 0; j < pc.n; ++j, ++ch) {
                 const int st = ch % C::VST, p0 = (pc.c0 + j) * CK;
@@ -343,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);
         }
-        if (lane == 0) a.desc[blockIdx.x] = desc;
+        if (lane == 0) desc.store(a, blockIdx.x);
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
     } else {
         // ---------------- softmax and output of subtile sub: a thread per pair
@@ -354,8 +373,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int L = c.s.kv - c.s.n;
-            if (sub == 0 || c.x.nr > p.sub_rows) {
-                const int pair = sub * p.sub_rows * a.group + row;               // of the tile
+            const int subs = c.x.nr > p.sub_rows ? 2 : 1, n_mine = chunks_of(pc, subs, sub);
+            const bool alt = in_turn(pc, subs);
+            if (n_mine > 0) {
+                const int pair = (alt ? 0 : sub * p.sub_rows * a.group) + row;   // of the tile
+                const int part_pair = alt ? sub * SUB + row : pair;              // where its split partial goes
                 const bool valid = row < p.sub_rows * a.group && pair < c.x.nr * a.group;
                 const int trow = pair / a.group, head = c.kvh * a.group + pair - trow * a.group;
                 RowMask mask;                  // (a lane without a pair may see anything: nobody reads its row)
@@ -366,7 +388,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 const bool live = __any_sync(0xffffffffu, valid);
                 float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll 2
-                for (int i = 0; i < 2 * pc.n; ++i) {
+                for (int i = 0; i < 2 * n_mine; ++i) {
                     const int h = i & 1;                                         // half h of a chunk goes through half h of the columns
                     const uint32_t gc = g + (i >> 1);                            // chunks of this subtile so far
                     // (a wait that fails takes the whole warp out: the accesses to tensor memory are warp-wide)
@@ -375,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     }
                     if (live) {
-                        const int p0 = pc.c0 * CK + i * STEP;
+                        const int p0 = (pc.c0 + (alt ? 2 * (i >> 1) + sub : i >> 1)) * CK + h * STEP;
                         uint32_t sv[STEP];
                         attn::tmem_ld64(s_addr + h * STEP, sv);
                         const bool whole = __all_sync(0xffffffffu, p0 >= mask.lo && p0 + STEP <= mask.hi);
@@ -424,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&p_ready[2 * sub + h]);
                 }
-                g += pc.n;
+                g += n_mine;
                 if (!ok) break;
                 if (!__all_sync(0xffffffffu, mbar_wait(&o_full[sub], np & 1, s_abort))) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -439,12 +461,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         tmem_ld32(o_addr + b * 32, o);
                         if (odd && valid) {
                             // the values that were set to zero, for the pairs that see them
-                            for (int j = 0; j < pc.n; ++j) {
+                            for (int j = alt ? sub : 0; j < pc.n; j += alt ? 2 : 1) {
                                 const int p0 = (pc.c0 + j) * CK;
                                 if (!is_edge(a, c, p0)) continue;
                                 for (int pos = p0; pos < min(p0 + CK, c.s.kv); ++pos) {
                                     if (!sees(mask, pos, L, c.s.kv)) continue;
-                                    const int index = pos / a.pages.page_size;
+                                    const int index = page_index(a.pages, pos);
                                     const int page = load_page(a.seq, a.pages, c.b, index);
                                     if (page < 0) continue;
                                     const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(a.pages.v) + page * a.pages.page +
@@ -475,15 +497,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                         } else if (valid) {
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
-                                *reinterpret_cast<uint4*>(a.part_o + part_quad(a, blockIdx.x, pc.slot, b * 8 + i, pair)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                                *reinterpret_cast<uint4*>(a.part_o + part_quad(a, blockIdx.x, pc.slot, b * 8 + i, part_pair)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                         }
                     }
-                    if (valid && pc.slot >= 0) a.part_ml[part_row(a, blockIdx.x, pc.slot, pair)] = make_float2(m_run, l_run);
+                    if (valid && pc.slot >= 0) a.part_ml[part_row(a, blockIdx.x, pc.slot, part_pair)] = make_float2(m_run, l_run);
                     if (valid && pc.slot < 0 && a.lse) a.lse[(size_t)token * a.Hq + head] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * 0.6931471805599453f;
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&o_free[sub]);
+            } else if (alt) {
+                a.part_ml[part_row(a, blockIdx.x, pc.slot, sub * SUB + row)] = make_float2(-INFINITY, 0.f);       // one chunk only: nothing left for this set
             }
             u += pc.n;
             if (u < end) next_tile<CK>(a, c);
@@ -555,6 +579,7 @@ int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s) {
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return -1;
     }
     a.rows = 2 * p.sub_rows;
+    a.rows_shift = shift_of(a.rows);
     a.pairs = 2 * SUB;
     a.n_cta = n_sm;
     p.out_vec = reinterpret_cast<uintptr_t>(a.out.p) % 16 == 0 && a.out.tok % 8 == 0 && a.out.head % 8 == 0;

@@ -51,7 +51,7 @@ __device__ __forceinline__ Slot find_slot(const SeqTable& q, const PagesView& pa
         b = __shfl_sync(0xffffffffu, b, src);
         r.pos = __shfl_sync(0xffffffffu, first, src) + t;
         if (r.pos >= 0) {
-            const int index = r.pos / pages.page_size;
+            const int index = paged::page_index(pages, r.pos);
             r.page = paged::load_page(q, pages, b, index);
             r.slot = r.pos - index * pages.page_size;
         }
