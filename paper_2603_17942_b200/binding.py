@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -375,15 +376,19 @@ def _stream(stream):
     return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
+_pack_heads = struct.Struct("Pqqi4x").pack        # the bytes of an esp_heads: a quarter of the time that filling the struct takes
+assert struct.calcsize("Pqqi4x") == ctypes.sizeof(esp_heads)
+
+
 def _heads(x, tokens: int, dim: int, dtype, device: int, where: str, name: str):
-    """x [tokens, heads, head_dim] as a reference to an esp_heads; None stays None.  (A call per layer: nothing here is formatted unless it fails.)"""
+    """x [tokens, heads, head_dim] as the bytes of an esp_heads; None stays None.  (A call per layer: nothing here is formatted unless it fails.)"""
     if x is None:
         return None
     shape, stride = x.shape, x.stride()
     if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or x.dtype is not dtype or x.get_device() != device or (stride[2] != 1 and dim != 1):
         raise EspError(-8, f"{where} ({name}: {tuple(shape)} {x.dtype} on {x.device}, strides {stride}; wanted [{tokens}, heads, {dim}] {dtype} on device {device}, "
                            f"last dimension dense)")
-    return ctypes.byref(esp_heads(x.data_ptr(), stride[0], stride[1], shape[1]))
+    return _pack_heads(x.data_ptr(), stride[0], stride[1], shape[1])
 
 
 def _vector(x, n: int, dtypes, device: int, where: str, name: str):

@@ -271,8 +271,8 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     const int rc = paged_few_supported(cache->dtype, a)  ? launch_paged_few(a, n_sm, s)
                    : paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s)
                                                          : launch_paged_simt(cache->dtype, a, n_sm, s);
-    if (rc) return ESP_E_CUDA;
-    return cuda_ok(cudaGetLastError());
+    const cudaError_t e = cudaGetLastError();       // taken in either case: the next call's error is its own
+    return rc ? ESP_E_CUDA : cuda_ok(e);
 }
 
 int esp_paged_status(const int32_t* status, void* cuda_stream, int32_t* device_status_out) {

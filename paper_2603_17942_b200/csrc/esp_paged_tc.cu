@@ -94,11 +94,13 @@ __device__ __forceinline__ float weights(const uint32_t (&sv)[STEP], uint32_t s_
     return c0 + c1;
 }
 
-// A tile of one subtile whose keys several CTAs share anyway: its chunks go to the two sets of scores, accumulators and softmax warps in turn, each
-// with a reference and a sum of its own, and the merge kernel joins one part more.  A single set would wait for every product and every
-// softmax in turn (XX).
-__device__ __forceinline__ bool in_turn(const Piece& pc, int subs) { return subs == 1 && pc.slot >= 0; }
-__device__ __forceinline__ int chunks_of(const Piece& pc, int subs, int sub) { return in_turn(pc, subs) ? (pc.n + 1 - sub) / 2 : (sub < subs ? pc.n : 0); }
+// A tile of one subtile whose keys several CTAs share anyway, in a call with many chunks for each of them: its chunks go to the two sets of scores,
+// accumulators and softmax warps in turn, each with a reference and a sum of its own, and the merge kernel joins one part more per
+// CTA.  One set waits for every product and every softmax in turn; two parts cost the merge.  4 sequences of 16 tokens over 32k
+// positions (54 chunks per CTA) 106 us with one set, 97 with two; 8 of 17 over 8k (28) 64 both; 32 of 4 over 4k (10) 61 and 63; 1 of 32 over 4k
+// (2) 18 and 22.
+__device__ __forceinline__ bool in_turn(const Piece& pc, int subs, const Share& share) { return subs == 1 && pc.slot >= 0 && share.each >= 32; }
+__device__ __forceinline__ int chunks_of(const Piece& pc, int subs, int sub, const Share& share) { return in_turn(pc, subs, share) ? (pc.n + 1 - sub) / 2 : (sub < subs ? pc.n : 0); }
 
 // A chunk that some pair of the tile does not see as a whole (the last one of the cache, the diagonal, the window's edge, the tree).
 __device__ __forceinline__ bool is_edge(const PagedAttnArgs& a, const Cursor& c, int p0) {
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int subs = c.x.nr > p.sub_rows ? 2 : 1;
-            const bool alt = in_turn(pc, subs);
+            const bool alt = in_turn(pc, subs, share);
             ok = __all_sync(0xffffffffu, mbar_wait(q_full, n_it & 1, s_abort) && mbar_wait(&k_full[ch % C::KST], (ch / C::KST) & 1, s_abort));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -305,8 +307,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                     }
                 }
             }
-            const int n1 = chunks_of(pc, subs, 1);
-            g0 += chunks_of(pc, subs, 0);
+            const int n1 = chunks_of(pc, subs, 1, share);
+            g0 += chunks_of(pc, subs, 0, share);
             ++pieces0;
             g1 += n1;
             pieces1 += n1 > 0;
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         desc.clear();
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
-            desc.note(a, c, share, pc, in_turn(pc, c.x.nr > p.sub_rows ? 2 : 1));
+            desc.note(a, c, share, pc, in_turn(pc, c.x.nr > p.sub_rows ? 2 : 1, share));
             if (lane == 0) s_odd[(n_it + 1) % ODD_RING] = 0;
             for (int j = 0; j < pc.n; ++j, ++ch) {
                 const int st = ch % C::VST, p0 = (pc.c0 + j) * CK;
@@ -373,8 +375,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
         for (uint32_t u = begin; u < end && ok; ++n_it) {
             const Piece pc = make_piece(c, begin, u, end);
             const int L = c.s.kv - c.s.n;
-            const int subs = c.x.nr > p.sub_rows ? 2 : 1, n_mine = chunks_of(pc, subs, sub);
-            const bool alt = in_turn(pc, subs);
+            const int subs = c.x.nr > p.sub_rows ? 2 : 1, n_mine = chunks_of(pc, subs, sub, share);
+            const bool alt = in_turn(pc, subs, share);
             if (n_mine > 0) {
                 const int pair = (alt ? 0 : sub * p.sub_rows * a.group) + row;   // of the tile
                 const int part_pair = alt ? sub * SUB + row : pair;              // where its split partial goes

@@ -413,6 +413,38 @@ def test_every_visible_position_counts_once(dtype, Hq, Hkv, D, page, n, kv, wind
     b.ok()
 
 
+@pytest.mark.parametrize("D,page,n,kv", [(128, 64, [16, 9, 1, 3, 30], [32100, 29999, 16000, 1, 30]), (64, 16, [4] * 6, [30000 - 77 * i for i in range(6)])])
+def test_a_few_tokens_over_long_caches(D, page, n, kv):
+    """Tiles of few pairs whose chunks go through both sets of scores in turn (more than 32 chunks for every CTA), beside one of one position: every visible
+    position counts once, the last and the first of every token included, and random values stay within the roundings."""
+    Hq, Hkv = 16, 8
+    b = Batch(n, kv, page, Hkv, D, "bf16", seed=3, fill=0.0)
+    for s in range(len(n)):
+        pg, sl = b.slots(s)
+        b.view(b.v)[pg, sl] = torch.eye(D, device="cuda").repeat(-(-kv[s] // D), 1)[:kv[s], None].expand(-1, Hkv, -1).to(torch.bfloat16)
+    q = torch.zeros(b.tokens, Hq, D, device="cuda", dtype=torch.bfloat16)
+    out, lse = _attention(b, q)
+    at = 0
+    for s, m in enumerate(n):
+        for i in range(m):
+            t = kv[s] - m + i + 1
+            if t <= 0:                      # padding
+                assert bool((out[at + i] == 0).all())
+                continue
+            count = torch.bincount(torch.arange(t) % D, minlength=D).double().cuda() / t
+            # a share is rounded once, 2^-8; a position more or less is D / t of it, 2^-7.9 at the longest
+            assert bool(((out[at + i].double() - count).abs() <= 2.0 ** -8 * 1.01 * count).all())
+            assert bool(((lse[at + i].double() - math.log(t)).abs() <= 2.0 ** -20 * 11).all())
+        at += m
+    b.k.copy_(_randn(_gen(8), *b.k.shape))
+    b.v.copy_(_randn(_gen(9), *b.v.shape))
+    q = _randn(_gen(10), *q.shape, dtype=torch.bfloat16, scale=1.5)
+    out, lse = _attention(b, q)
+    _check_attention(b, q, out, lse)
+    again, _ = _attention(b, q)
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("heads", range(len(HEADS)))
 @pytest.mark.parametrize("kind", ["causal", "window", "tree"])
 def test_what_a_token_does_not_see_does_not_reach_it(heads, kind):
@@ -455,6 +487,60 @@ def test_what_a_token_does_not_see_does_not_reach_it(heads, kind):
     assert torch.equal(torch.nan_to_num(last[blind], nan=123.0), torch.nan_to_num(spoiled[blind], nan=123.0))
     assert bool(torch.isnan(last[~blind]).all())
     b.ok()
+
+
+@pytest.mark.parametrize("heads", range(len(HEADS)))
+@pytest.mark.parametrize("window", [1, 33, 90])
+def test_what_a_single_token_does_not_see_does_not_reach_it(heads, window):
+    """Single tokens with a window: keys and values in front of it and behind kv_len are NaN or infinite, and nothing of that shows."""
+    dtype, Hq, Hkv, D = HEADS[heads]
+    b = Batch([1, 1, 1], [400, 97, 31], 16, Hkv, D, dtype, seed=11)
+    q = _randn(_gen(13), 3, Hq, D, dtype=DT[dtype])
+    clean, l0 = _attention(b, q, window=window)
+    _check_attention(b, q, clean, l0, window=window)
+    keep_k, keep_v = b.k.clone(), b.v.clone()
+    b.k.fill_(NAN)
+    b.v.fill_(math.inf)
+    for s in range(3):
+        pg, sl = (x[max(0, b.kv[s] - window):] for x in b.slots(s))
+        b.view(b.k)[pg, sl], b.view(b.v)[pg, sl] = b.view(keep_k)[pg, sl], b.view(keep_v)[pg, sl]
+    spoiled, l1 = _attention(b, q, window=window)
+    assert torch.equal(clean, spoiled) and torch.equal(l0, l1)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 33, 1, 64), ("bf16", 64, 1, 128), ("bf16", 40, 2, 128), ("fp32", 40, 1, 32), ("bf16", 16, 1, 64), ("bf16", 9, 1, 128)])
+@pytest.mark.parametrize("n,kv", [([1, 1], [300, 5]), ([9, 2], [400, 2])])
+def test_attention_of_many_heads_on_one(dtype, Hq, Hkv, D, n, kv):
+    b = Batch(n, kv, 16, Hkv, D, dtype, seed=5)
+    q = _randn(_gen(1), b.tokens, Hq, D, dtype=DT[dtype])
+    out, lse = _attention(b, q)
+    _check_attention(b, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 2), ("fp32", 1)])
+def test_attention_and_append_of_very_many_sequences(dtype, n):
+    """1300 sequences: more than the threads that deal them have at hand."""
+    Hq, Hkv, D, B = 4, 2, 64, 1300
+    kv = [2 + (7 * i) % 61 for i in range(B)]
+    b = Batch([n] * B, kv, 16, Hkv, D, dtype, seed=5, back=1)
+    x = _randn(_gen(2), b.tokens, Hq + 2 * Hkv, D, dtype=DT[dtype])
+    P.esp_paged_append(b.cache, b.batch, x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:])
+    out, _ = _attention(b, x[:, :Hq])
+    b.ok()
+    k, v = torch.zeros(B, 64, Hkv, D, device="cuda", dtype=DT[dtype]), torch.zeros(B, 64, Hkv, D, device="cuda", dtype=DT[dtype])
+    for s in range(B):
+        k[s, :kv[s]], v[s, :kv[s]] = b.read(b.k, s), b.read(b.v, s)
+    at = torch.tensor(kv, device="cuda")
+    assert torch.equal(k[torch.arange(B, device="cuda"), at - 1], x[n - 1:n * B:n, Hq:Hq + Hkv])
+    q = x[:n * B, :Hq].view(B, n, Hkv, Hq // Hkv, D).double()
+    z = torch.einsum("bihgd,bjhd->bhgij", q, k.double()) * D ** -0.5
+    see = torch.arange(64, device="cuda") < (at[:, None] - n + 1 + torch.arange(n, device="cuda"))[..., None]
+    w = torch.softmax(z.masked_fill(~see[:, None, None], -math.inf), -1)
+    ref = torch.einsum("bhgij,bjhd->bihgd", w, v.double()).reshape(n * B, Hq, D)
+    mag = torch.einsum("bhgij,bjhd->bihgd", w, v.double().abs()).reshape(n * B, Hq, D)
+    # the weight's rounding, twice the logit's error ((D + 8) 2^-24 of about 40 at most, 2^-21) and the output's own rounding
+    tol = ((0 if dtype == "fp32" else HALF["bf16"]) + 2 * (72 * 40 * 2.0 ** -24 + 2.0 ** -20)) * mag * 1.01 + HALF[dtype] * 1.01 * ref.abs()
+    assert bool(((out[:-1].double() - ref).abs() <= tol).all()) and bool((out[-1] == 7.0).all())
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
