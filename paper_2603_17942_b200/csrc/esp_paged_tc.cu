@@ -9,13 +9,21 @@
 //                    The reference of the exponentials follows the maximum lazily: it moves, and O_s is rescaled, only after a growth of 2^8.
 // The tensor cores work on one subtile while the softmax of the other runs; products are issued in the order P_0 V, Q_0 K^T (next chunk),
 // P_1 V, Q_1 K^T, and run in that order, so S_s may be overwritten as soon as the P_s V that reads P_s from it has been issued, and S_s
-// arriving says that O_s is complete.  (A warp for each subtile's products interleaves them, and the tensor cores take longer: chunk of 2048 behind
-// 6144 347 us against 262.)
+// arriving says that O_s is complete.
 // Weights of keys that a pair does not see are zero, but zero times an infinite value is no number: in chunks that not every pair sees
 // as a whole, a warp sets values that are no finite numbers to zero in shared memory before the product, and the pairs that see them get them
 // when the tile is finished.
 // Roles: warps 0 and 2 TMA (keys and queries, values), warp 1 issues the products, warp 3 looks after the values, warps 4-7 and 8-11 softmax and
 // output of a subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
+//
+// What bounds it: 2048 tokens behind 6144, 32/8 heads of 128, take 225 us, 1.07 PFLOP/s.  A chunk takes a subtile about 3500 cycles: 300 to load the
+// scores of a half and find their maximum and 730 for its weights (512 of them the special-function unit's), twice, the last half's product and the next
+// scores 770, and the waits between the warps; the tensor cores have 1024 of them for each of the two subtiles, 55 to 60 %.  Built, correct and slower (us
+// for the same call): scores of 64 keys in two buffers per subtile, so that the softmax never waits for a product (276: products of 64 keys read the
+// queries twice as often, and the issuing warp has twice the hand-overs); a warp of its own for each subtile's products (305: they interleave); a share of
+// the exponentials as a polynomial on the FMA pipe (228 to 243); two threads per pair (265 to 290); waits that spin (237 to 244).  What brought
+// it from 480: registers for 64 scores instead of 128 without spilling, one lane that issues the copies (32 lanes with a copy each run one after
+// the other), loops over the products unrolled.
 #include <string.h>
 
 #include "esp_attn_tc.cuh"
@@ -389,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 if (valid) mask = row_mask(a, c.s, c.x.r0 + trow);
                 const bool live = __any_sync(0xffffffffu, valid);
                 float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll 2
+#pragma unroll 2                                                                 // (the two halves as code of their own: 220 us, as a loop 245)
                 for (int i = 0; i < 2 * n_mine; ++i) {
                     const int h = i & 1;                                         // half h of a chunk goes through half h of the columns
                     const uint32_t gc = g + (i >> 1);                            // chunks of this subtile so far

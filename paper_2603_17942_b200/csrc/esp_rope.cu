@@ -139,7 +139,9 @@ __global__ void __launch_bounds__(ANY_WARPS * 32) k_norm_rope_any(const __grid_c
 // head to head, and gain and angle are one set of coefficients per thread.  Blocks with all kinds needed 240 instructions per eight elements and 50 us for
 // 8192 tokens of 40 heads of 128.  The loads of all of a thread's heads are requested first; while they are on their way the tokens'
 // slots are looked up, a warp for each, and their angles turned.
-constexpr int ROPE_THREADS = 128;       // threads of a block at most
+// Threads of a block at most, and blocks per SM that the registers are held to (us, 8192 tokens of 40 heads / append of 4099 of 48): 384 x 3 39.5 / 26.7, 256 x 4 39.2 /
+// 25.8, 128 x 8 37.0 / 25.3, 128 x 9 35.5 / 24.7, 128 x 10 36.5 / 25.4 (spills).
+constexpr int ROPE_THREADS = 128;
 constexpr int ROPE_PAIRS = 1024;        // angles a block keeps
 constexpr int ROPE_TOKENS = 16;         // tokens of a block at most
 template <typename T> constexpr int ROPE_ROUNDS = sizeof(T) == 2 ? 4 : 2;      // heads of a thread: 64 bytes under way
