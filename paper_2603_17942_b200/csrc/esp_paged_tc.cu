@@ -42,7 +42,7 @@ constexpr int SUB = 128;                  // pairs per subtile
 constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
 constexpr int THREADS = 384;
 constexpr int TMEM_COLS = 512;            // S0, S1, O0, O1: 128 columns each
-constexpr int ODD_RING = 8;               // tiles whose note on odd values is kept: more than the stages can hold values of
+constexpr int ODD_RING = 8;               // pieces whose note on odd values is kept: the one being read, the next one, one for each stage of values, two that warp 3 enters
 
 template <int D>
 struct Cfg {
@@ -316,6 +316,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
                 }
             }
             const int n1 = chunks_of(pc, subs, 1, share);
+            // subtile 1 may rest for any number of pieces: the last one it had has to have been read, or the ring of s_odd could come round
+            if (ok && n1 == 0) ok = __all_sync(0xffffffffu, mbar_wait(&o_free[1], (pieces1 & 1) ^ 1, s_abort));
             g0 += chunks_of(pc, subs, 0, share);
             ++pieces0;
             g1 += n1;
