@@ -339,8 +339,9 @@ typedef struct {
  * p % page_size of page page_table[b][p / page_size].  A position below 0 (kv_len[b] < n) is padding: nothing is cached
  * for it, it sees nothing.  Tokens before q_start[0] and from q_start[batch] on are left alone.
  * The device checks what the host cannot see: a sequence whose q_start leaves 0 .. n_tokens, falls, or spans more than max_new tokens, or
- * whose kv_len is negative or beyond its table's pages, is left out as a whole; a page number outside 0 .. n_pages - 1 where a
- * position needs one makes the sequence's results meaningless (no other memory is touched).  Both are recorded in *status. */
+ * whose kv_len is negative, above 2^30 or beyond its table's pages, is left out as a whole; a page number outside 0 .. n_pages - 1 where a
+ * position needs one makes the sequence's results meaningless (no other memory is touched).  Both are recorded in *status.  A call takes
+ * up to 2^30 tokens. */
 typedef struct {
     int32_t batch;
     int32_t max_new;            /* no sequence has more new tokens than this */
@@ -402,7 +403,8 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
  * token sees every position before its block and the block rows whose bits are set in its mask (max_new <= ESP_MAX_ROWS, window 0; bits of rows
  * that the block does not have are ignored).  A token that sees nothing gets zeros.  scale 0: 1 / sqrt(head_dim).
  * lse [device] or NULL: [n_tokens][n_heads of q] fp32, the logarithm of the sum of exp(scale * q k) over the visible positions,
- * -infinity where there are none.  out must not overlap q.
+ * -infinity where there are none.  out must not overlap q.  At most 64 query heads share a key/value head.  A call whose tiles of tokens have 2^31
+ * chunks of keys or more to walk in all (chunks of 32 to 128 positions; seconds of work) writes nothing and records the capacity code in *status.
  * What a token does not see does not reach its result: slots behind kv_len may hold anything, and an infinite or undefined value reaches
  * only the tokens that see it.  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);
  * the same call gives the same bits.

@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t warp_scan_u32(uint32_t v, int lane) {
     return v;
 }
 
-// Chunks of all tiles of a sequence (one KV head).  All 32 lanes call it together with a sequence each; long ones are counted by the whole warp.
+// Chunks of all tiles of a sequence (one KV head), 2^31 if a lane's share of them is 2^26 or more.  All 32 lanes call it together with a sequence each; long ones are counted by the whole warp.
 template <int CK>
 __device__ __forceinline__ uint32_t seq_chunks(const PagedAttnArgs& a, const Seq& s, int lane) {
     const int T = n_tiles(a, s);
@@ -98,16 +98,17 @@ __device__ __forceinline__ uint32_t seq_chunks(const PagedAttnArgs& a, const Seq
         o.n = __shfl_sync(0xffffffffu, s.n, src);
         o.kv = __shfl_sync(0xffffffffu, s.kv, src);
         const int To = n_tiles(a, o);
-        uint32_t p = 0;
+        unsigned long long p = 0;
         for (int t = lane; t < To; t += 32) p += make_tile<CK>(a, o, t).nc;
-        p = warp_sum_u32(p);
-        if (lane == src) w = p;
+        const bool most = __any_sync(0xffffffffu, p >> 26);              // (32 lanes below 2^26 each stay below 2^31)
+        const uint32_t sum = warp_sum_u32((uint32_t)p);
+        if (lane == src) w = most ? 1u << 31 : sum;
     }
     return w;
 }
 
 // Called by all lanes of a warp, each warp that needs to know for itself (no barrier, nothing shared): counts the batch's units and finds the tile in
-// which CTA `cta` starts.  false: the CTA has no units.  A batch of 2^31 units or more (months of work) is refused on the device.
+// which CTA `cta` starts.  false: the CTA has no units.  A batch of 2^31 units or more is refused on the device.
 template <int CK>
 __device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, Share& share, Cursor& at) {
     const int per = (a.seq.batch + 31) >> 5;                             // consecutive sequences of a lane

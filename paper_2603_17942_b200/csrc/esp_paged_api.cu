@@ -165,7 +165,7 @@ int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const es
                      const esp_heads* k_out, void* cuda_stream) {
     if (dtype != 0 && dtype != 1) return ESP_E_BADCFG;
     if (head_dim < 1 || head_dim > ESP_ROPE_MAX_DIM) return ESP_E_BADCFG;
-    if (n_tokens < 0 || (!q && !k) || !q != !q_out || !k != !k_out || !(eps >= 0.f)) return ESP_E_ARG;
+    if (n_tokens < 0 || n_tokens > paged::KV_LIMIT || (!q && !k) || !q != !q_out || !k != !k_out || !(eps >= 0.f)) return ESP_E_ARG;
     if ((q_gain && !q) || (k_gain && !k) || (rope && !positions && n_tokens > 0)) return ESP_E_ARG;
     for (int i = 0; i < 2; ++i) {
         const esp_heads *x = i ? k : q, *y = i ? k_out : q_out;
@@ -191,7 +191,7 @@ int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const es
 int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* k, const esp_heads* v,
                      const esp_heads* q, const void* q_gain, const void* k_gain, float eps, const esp_rope_cfg* rope, const void* rope_table,
                      const int32_t* positions, const esp_heads* q_out, void* cuda_stream) {
-    if (!cache || !batch || !k || !v || n_tokens < 0 || !q != !q_out || (q_gain && !q) || !(eps >= 0.f)) return ESP_E_ARG;
+    if (!cache || !batch || !k || !v || n_tokens < 0 || n_tokens > paged::KV_LIMIT || !q != !q_out || (q_gain && !q) || !(eps >= 0.f)) return ESP_E_ARG;
     if (const int rc = check_cache(cache)) return rc;
     if (const int rc = check_batch(batch)) return rc;
     const esp_heads* ins[3] = {k, v, q};
@@ -232,7 +232,7 @@ int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_
 
 int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const uint64_t* anc,
                         int32_t window, float scale, const esp_heads* out, float* lse, void* scratch, size_t scratch_bytes, void* cuda_stream) {
-    if (!cache || !batch || !q || !out || !scratch || n_tokens < 0 || window < 0 || !(scale >= 0.f) || !isfinite(scale)) return ESP_E_ARG;
+    if (!cache || !batch || !q || !out || !scratch || n_tokens < 0 || n_tokens > paged::KV_LIMIT || window < 0 || !(scale >= 0.f) || !isfinite(scale)) return ESP_E_ARG;
     if (const int rc = check_cache(cache)) return rc;
     if (const int rc = check_batch(batch)) return rc;
     if (const int rc = check_heads(q, cache->dtype, n_tokens, cache->head_dim, false)) return rc;

@@ -345,7 +345,7 @@ int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s) {
 int launch_paged_simt(int dtype, PagedAttnArgs a, int n_sm, cudaStream_t s) {
     // Small tiles in small calls: more blocks at once, at a higher price per pair.  696 pairs in all (5 sequences of up to 100 tokens, heads of 64)
     // 25.5 us with tiles of 64 pairs, 18.6 with 16; 3200 pairs (4 of up to 300) 43 and 54.
-    const bool few = a.group * a.seq.max_new <= 16 || (long long)a.seq.n_tokens * a.Hq < 16ll * n_sm;
+    const bool few = (long long)a.group * a.seq.max_new <= 16 || (long long)a.seq.n_tokens * a.Hq < 16ll * n_sm;
     a.pairs = few && a.group <= 16 ? 16 : 64;
     a.rows = a.pairs / a.group;
     if (a.rows < 1) return -1;                      // more than 64 query heads share a KV head

@@ -683,6 +683,33 @@ def test_many_calls_behind_one_another(dtype, D, n, kv):
     b.ok()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_bound_on_new_tokens_far_above_them(dtype):
+    """max_new is a bound: 2^31 - 1 is one too."""
+    b = Batch([1, 7], [100, 50], 16, 2, 64, dtype, seed=2)
+    b.batch = P.PagedBatch(b.q_start, b.kv_len, b.table_d, 2 ** 31 - 1, b.status)
+    q = _randn(_gen(7), b.tokens, 8, 64, dtype=DT[dtype])
+    out, lse = _attention(b, q)
+    _check_attention(b, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype,tokens,Hq,Hkv", [("bf16", 2200, 64, 1), ("bf16", 1100, 64, 2), ("fp32", 300, 64, 1)])
+def test_more_work_than_is_counted(dtype, tokens, Hq, Hkv):
+    """A table that names one page for 2^30 positions: more chunks than 32 bits count, or 2^31 and more over the KV heads.  Nothing is walked or written."""
+    k = torch.zeros(1, Hkv, 1024, 64, device="cuda", dtype=DT[dtype])
+    table = torch.zeros(1, 2 ** 20, device="cuda", dtype=torch.int32)
+    status = torch.zeros(1, device="cuda", dtype=torch.int32)
+    q_start = torch.tensor([0, tokens], device="cuda", dtype=torch.int32)
+    kv_len = torch.tensor([2 ** 30], device="cuda", dtype=torch.int32)
+    batch = P.PagedBatch(q_start, kv_len, table, tokens, status)
+    q = torch.zeros(tokens, Hq, 64, device="cuda", dtype=DT[dtype])
+    out = torch.full_like(q, 7.0)
+    sc, nb = _scratch(Hq, 64)
+    P.esp_paged_attention(P.PagedCache(k, k.clone()), batch, q, out, sc, nb)
+    torch.cuda.synchronize()
+    assert int(status) == 4 and bool((out == 7.0).all())
+
+
 def test_nothing_to_do():
     b = Batch([0, 0], [5, 0], 16, 2, 128, "bf16", seed=2, front=2, back=1)
     q = _randn(_gen(7), 3, 8, 128, dtype=torch.bfloat16)

@@ -114,7 +114,7 @@ def test_norm_rope_refusals(lib):
     q, o = _heads(), _heads(data=2 * X)
     rope = P.rope_cfg(128)
     bad = [
-        (ARG, dict()), (ARG, dict(q=q)), (ARG, dict(q_out=o)), (ARG, dict(q=q, k_out=o)), (ARG, dict(q=q, q_out=o, tokens=-1)),
+        (ARG, dict()), (ARG, dict(q=q)), (ARG, dict(q_out=o)), (ARG, dict(q=q, k_out=o)), (ARG, dict(q=q, q_out=o, tokens=-1)), (ARG, dict(q=q, q_out=o, tokens=2 ** 30 + 1)),
         (BADCFG, dict(q=q, q_out=o, dtype=2)), (BADCFG, dict(q=q, q_out=o, dim=0)), (BADCFG, dict(q=q, q_out=o, dim=257)),
         (ARG, dict(q=q, q_out=_heads(n=3, data=2 * X))), (ARG, dict(q=q, q_out=o, k_gain=X)), (ARG, dict(q=q, q_out=o, eps=-1.0)), (ARG, dict(q=q, q_out=o, eps=math.nan)),
         (ARG, dict(q=q, q_out=o, rope=rope, table=X, positions=None)), (ARG, dict(q=q, q_out=o, rope=rope)), (ARG, dict(q=q, q_out=o, rope=rope, table=X + 8)),
@@ -157,7 +157,7 @@ def test_append_refusals(lib):
         assert call(batch=kw) == code, kw
     q, o = _heads(n=4), _heads(n=4, data=4 * X)
     for code, kw in [(ARG, dict(k=None)), (ARG, dict(v=None)), (ARG, dict(k=_heads(n=3))), (ARG, dict(v=_heads(n=1))), (ARG, dict(q=q)), (ARG, dict(q_out=o)),
-                     (ARG, dict(q=q, q_out=_heads(n=2, data=4 * X))), (ARG, dict(q_gain=X)), (ARG, dict(tokens=-1)), (ARG, dict(eps=math.nan)), (ARG, dict(rope=P.rope_cfg(128))),
+                     (ARG, dict(q=q, q_out=_heads(n=2, data=4 * X))), (ARG, dict(q_gain=X)), (ARG, dict(tokens=-1)), (ARG, dict(tokens=2 ** 30 + 1)), (ARG, dict(eps=math.nan)), (ARG, dict(rope=P.rope_cfg(128))),
                      (BADCFG, dict(rope=P.rope_cfg(256), table=X)), (ARG, dict(q=q, q_out=_heads(n=4, tok=300, data=4 * X)))]:
         assert call(**kw) == code, kw
     assert call(tokens=0) == 0 and call(batch=dict(batch=0)) == 0 and call(batch=dict(max_new=0)) == 0
@@ -174,7 +174,7 @@ def test_attention_refusals(lib):
     for code, kw in BAD_BATCHES:
         assert call(batch=kw) == code, kw
     for code, kw in [(ARG, dict(q=None)), (ARG, dict(out=None)), (ARG, dict(scratch=None)), (WORKSPACE, dict(nbytes=need - 1)), (WORKSPACE, dict(scratch=X + 16)),
-                     (ARG, dict(window=-1)), (ARG, dict(scale=-1.0)), (ARG, dict(scale=math.nan)), (ARG, dict(scale=math.inf)), (ARG, dict(tokens=-1)),
+                     (ARG, dict(window=-1)), (ARG, dict(scale=-1.0)), (ARG, dict(scale=math.nan)), (ARG, dict(scale=math.inf)), (ARG, dict(tokens=-1)), (ARG, dict(tokens=2 ** 30 + 1)),
                      (ARG, dict(out=_heads(n=4))), (ARG, dict(out=_heads(n=2, data=4 * X))), (BADCFG, dict(q=_heads(n=5), out=_heads(n=5, data=4 * X))),
                      (BADCFG, dict(q=_heads(n=130), out=_heads(n=130, tok=130 * 128, data=4 * X))),
                      (ARG, dict(anc=X, window=5)), (ARG, dict(anc=X, batch=dict(max_new=129))), (ARG, dict(out=_heads(n=4, tok=64, data=4 * X)))]:
