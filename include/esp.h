@@ -406,7 +406,8 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
  * -infinity where there are none.  out must not overlap q.  At most 64 query heads share a key/value head.  A call whose tiles of tokens have 2^31
  * chunks of keys or more to walk in all (chunks of 32 to 128 positions; seconds of work) writes nothing and records the capacity code in *status.
  * What a token does not see does not reach its result: slots behind kv_len may hold anything, and an infinite or undefined value reaches
- * only the tokens that see it.  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);
+ * only the tokens that see it.  To them an infinite value makes its element of the result infinite (undefined with one of the other sign or one that is no number; where
+ * its weight is below 2^-100 of the row's largest the element is infinite or undefined).  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);
  * the same call gives the same bits.
  * scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
 int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
