@@ -15,18 +15,35 @@ namespace paged {
 constexpr int KV_LIMIT = 1 << 30;
 
 // A sequence as the device reads it, checked; a description that does not hold together leaves the sequence without tokens.
+// top: the furthest end of the sequences before b that hold together by themselves; b must not start in front of it, or two sequences would own a token.  That can only be
+// where some sequence did not hold together, which `odd` tells: callers that start at another sequence than the first pass 0 for top as long as there is none.
 struct Seq {
     int start, n, kv;     // first token, tokens, cached positions with them
 };
-__device__ __forceinline__ Seq load_seq(const SeqTable& t, int b) {
+__device__ __forceinline__ Seq load_seq(const SeqTable& t, int b, int& top, bool& odd) {
     Seq s;
     s.start = __ldg(t.q_start + b);
     const int end = __ldg(t.q_start + b + 1);
     s.kv = __ldg(t.kv_len + b);
-    const bool ok = s.start >= 0 && end >= s.start && end <= t.n_tokens && end - s.start <= t.max_new && s.kv >= 0 && s.kv <= t.kv_cap;
+    const bool alone = s.start >= 0 && end >= s.start && end <= t.n_tokens && end - s.start <= t.max_new && s.kv >= 0 && s.kv <= t.kv_cap;
+    const bool ok = alone && s.start >= top;
+    if (alone) top = max(top, end);
     s.n = ok ? end - s.start : 0;
-    if (!ok) set_error(t.status, DEV_E_INDEX);
+    if (!ok) {
+        odd = true;
+        set_error(t.status, DEV_E_INDEX);
+    }
     return s;
+}
+// the largest value of the lanes before this one, 0 in the first
+__device__ __forceinline__ int warp_max_before(int v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v = max(v, x);
+    }
+    v = __shfl_up_sync(0xffffffffu, v, 1);
+    return lane ? v : 0;
 }
 __device__ __forceinline__ int page_index(const PagesView& p, int pos) { return p.page_shift >= 0 ? pos >> p.page_shift : pos / p.page_size; }
 // the page of a position < kv_len, -1 if the table names none
@@ -58,6 +75,7 @@ __device__ __forceinline__ int n_tiles(const PagedAttnArgs& a, const Seq& s) { r
 struct Cursor {
     uint32_t tile_u;      // first unit of the tile
     int b, kvh, t;
+    int top;              // as load_seq has it, behind sequence b
     Seq s;
     Tile x;
 };
@@ -113,16 +131,25 @@ template <int CK>
 __device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, Share& share, Cursor& at) {
     const int per = (a.seq.batch + 31) >> 5;                             // consecutive sequences of a lane
     const int b0 = lane * per;
-    uint32_t mine = 0, chunks = 0;
-    unsigned long long wide = 0;
+    uint32_t mine, chunks = 0;
+    unsigned long long wide;
     Seq s;
-    for (int i = 0; i < per; ++i) {                                      // the same trips in every lane
-        s.start = s.n = s.kv = 0;
-        if (b0 + i < a.seq.batch) s = load_seq(a.seq, b0 + i);
-        chunks = seq_chunks<CK>(a, s, lane);
-        const unsigned long long w = (unsigned long long)chunks * a.Hkv;
-        wide += w;
-        mine += (uint32_t)w;
+    int top0 = 0, top;                                                   // in front of the lane's sequences, behind them
+    for (bool again = false;; again = true) {
+        bool odd = false;
+        top = top0;
+        mine = 0;
+        wide = 0;
+        for (int i = 0; i < per; ++i) {                                  // the same trips in every lane
+            s.start = s.n = s.kv = 0;
+            if (b0 + i < a.seq.batch) s = load_seq(a.seq, b0 + i, top, odd);
+            chunks = seq_chunks<CK>(a, s, lane);
+            const unsigned long long w = (unsigned long long)chunks * a.Hkv;
+            wide += w;
+            mine += (uint32_t)w;
+        }
+        if (again || !__any_sync(0xffffffffu, odd)) break;
+        top0 = warp_max_before(top, lane);                               // once more, with what stands in front of each lane's sequences
     }
     if (__any_sync(0xffffffffu, wide >> 26)) {                           // (32 lanes below 2^26 each stay below 2^31)
 #pragma unroll
@@ -145,10 +172,13 @@ __device__ __forceinline__ bool deal(const PagedAttnArgs& a, int cta, int lane, 
         at.s.start = __shfl_sync(0xffffffffu, s.start, owner);
         at.s.n = __shfl_sync(0xffffffffu, s.n, owner);
         at.s.kv = __shfl_sync(0xffffffffu, s.kv, owner);
+        at.top = __shfl_sync(0xffffffffu, top, owner);
         Wt = __shfl_sync(0xffffffffu, chunks, owner);
     } else {
+        at.top = __shfl_sync(0xffffffffu, top0, owner);
+        bool odd;
         for (;; ++at.b) {                                                // the same sequence in every lane
-            at.s = load_seq(a.seq, at.b);
+            at.s = load_seq(a.seq, at.b, at.top, odd);
             const int T = n_tiles(a, at.s);
             Wt = 0;
             for (int t = lane; t < T; t += 32) Wt += make_tile<CK>(a, at.s, t).nc;
@@ -183,9 +213,10 @@ __device__ __forceinline__ void next_tile(const PagedAttnArgs& a, Cursor& c) {
         c.t = 0;
         if (++c.kvh >= a.Hkv) {
             c.kvh = 0;
+            bool odd;
             do {
                 if (++c.b >= a.seq.batch) return;                        // the end of the line: nobody looks at the tile
-                c.s = load_seq(a.seq, c.b);
+                c.s = load_seq(a.seq, c.b, c.top, odd);
             } while (c.s.n == 0);
         }
     }

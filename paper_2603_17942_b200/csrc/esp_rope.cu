@@ -27,6 +27,30 @@ __device__ __forceinline__ float2 rope_turn(int p, uint64_t f, float amplitude) 
     return make_float2(amplitude * c, amplitude * s);
 }
 
+// Token t's sequence in a batch where some do not hold together (see load_seq) and the position of its first new token minus that token's number; x < 0: none.
+__device__ __forceinline__ int2 find_among_odd(const SeqTable& q, int t, int lane) {
+    int before = 0;                                    // furthest end of the sequences of earlier rounds
+    for (int b0 = 0; b0 < q.batch; b0 += 32) {
+        const int x = b0 + lane;
+        int end = 0, first = 0;
+        bool odd, here = false;
+        paged::Seq s;
+        s.start = 0;
+        if (x < q.batch) {
+            s = paged::load_seq(q, x, end, odd);
+            here = t >= s.start && t < s.start + s.n;
+            first = s.kv - s.n - s.start;
+        }
+        const int top = max(before, paged::warp_max_before(end, lane));
+        const uint32_t who = __ballot_sync(0xffffffffu, here && s.start >= top);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            return make_int2(b0 + src, __shfl_sync(0xffffffffu, first, src));
+        }
+        before = max(before, __reduce_max_sync(0xffffffffu, end));
+    }
+    return make_int2(-1, 0);
+}
 // Where token t of the call goes: its sequence's slot.  page < 0: nowhere.  Called by whole warps.
 struct Slot {
     int page, slot, pos;
@@ -35,13 +59,15 @@ __device__ __forceinline__ Slot find_slot(const SeqTable& q, const PagesView& pa
     Slot r;
     r.page = -1;
     r.slot = r.pos = 0;
+    bool odd = false;
     for (int b0 = 0; b0 < q.batch; b0 += 128) {
         int b = -1, first = 0;                         // this lane's sequence, position of its first new token minus the token's number
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int x = b0 + 32 * i + lane;
             if (x < q.batch) {
-                const paged::Seq s = paged::load_seq(q, x);
+                int top = 0;
+                const paged::Seq s = paged::load_seq(q, x, top, odd);
                 if (t >= s.start && t < s.start + s.n) { b = x; first = s.kv - s.n - s.start; }
             }
         }
@@ -49,7 +75,14 @@ __device__ __forceinline__ Slot find_slot(const SeqTable& q, const PagesView& pa
         if (!who) continue;
         const int src = __ffs(who) - 1;
         b = __shfl_sync(0xffffffffu, b, src);
-        r.pos = __shfl_sync(0xffffffffu, first, src) + t;
+        first = __shfl_sync(0xffffffffu, first, src);
+        if (__any_sync(0xffffffffu, odd)) {
+            const int2 found = find_among_odd(q, t, lane);
+            b = found.x;
+            first = found.y;
+            if (b < 0) break;
+        }
+        r.pos = first + t;
         if (r.pos >= 0) {
             const int index = paged::page_index(pages, r.pos);
             r.page = paged::load_page(q, pages, b, index);

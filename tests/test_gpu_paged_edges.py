@@ -1,9 +1,11 @@
 """The operators over a paged cache at the edges of what their header promises.  Tolerances as in test_gpu_paged.py."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+import paper_2603_17942_b200 as P
 from tests.test_gpu_paged import DT, NAN, Batch, _attention, _check_attention, _gen, _randn
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +63,78 @@ def test_an_infinite_value_that_every_token_sees_stays_infinite(dtype, Hq, Hkv, 
     assert torch.equal(got.isnan(), want.isnan())
     assert torch.equal(got[~want.isnan()], want[~want.isnan()])
     b.ok()
+
+
+# ================================================================ descriptions that contradict each other
+class One:
+    """Sequence s of a batch on its own, for _check_attention."""
+
+    def __init__(self, b, s, start, n):
+        self.n, self.kv, self.front, self.k, self.v, self.order = [n], [b.kv[s]], start, b.k, b.v, b.order
+        self.read = lambda x, _: b.read(x, s)
+        self.ok = lambda: None
+
+
+def _check_served(b, q, out, lse, starts, served):
+    """Every served sequence has its results, all other rows of out and lse are as they were."""
+    mine = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
+    for s in served:
+        mine[starts[s]:starts[s + 1]] = True
+    assert bool((out[~mine] == 7.0).all()) and bool((lse[~mine] == 7.0).all())
+    for s in served:
+        keep = torch.full_like(out, 7.0)
+        keep[starts[s]:starts[s + 1]] = out[starts[s]:starts[s + 1]]
+        _check_attention(One(b, s, starts[s], starts[s + 1] - starts[s]), q, keep, lse)
+
+
+def _check_appended(b, k, v, k0, v0, starts, served):
+    """The slots of the served sequences hold their tokens, every other one its bits."""
+    for s in served:
+        n = starts[s + 1] - starts[s]
+        pg, sl = (x[b.kv[s] - n:] for x in b.slots(s))
+        b.view(k0)[pg, sl], b.view(v0)[pg, sl] = k[starts[s]:starts[s + 1]], v[starts[s]:starts[s + 1]]
+    assert torch.equal(b.k, k0) and torch.equal(b.v, v0)
+
+
+def _recorded(b):
+    with pytest.raises(P.EspError) as e:
+        P.esp_paged_status(b.batch)
+    assert e.value.code == -5
+    b.status.zero_()
+
+
+OVERLAPS = {
+    "later sequence inside an earlier one": ([0, 100, 50, 120, 130], [0, 3]),
+    "starts before it fell": ([60, 20, 80, 100, 130], [1, 2, 3]),
+    "one inside two": ([0, 40, 90, 30, 70, 130], [0, 1]),
+    "falls behind the last": ([0, 60, 130, 20], [0, 1]),
+    "single tokens": (list(range(100)) + list(range(60, 130)), list(range(99)) + list(range(139, 169))),
+    "very many": (list(range(400)) + list(range(300, 500)), list(range(399)) + list(range(499, 599))),
+}
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 8, 2, 128), ("fp32", 4, 2, 64)])
+@pytest.mark.parametrize("what", list(OVERLAPS))
+@pytest.mark.parametrize("spare", [0, 6])               # a bound above 1: the kernel of several tokens
+def test_no_token_has_two_owners(dtype, Hq, Hkv, D, what, spare):
+    """Where q_start falls, a later sequence may claim tokens that an earlier one has: the earlier one has them, the later one is left out as a whole, in the attention and in
+    the append; who does not overlap is served; the same call gives the same bits."""
+    starts, served = OVERLAPS[what]
+    B, tokens = len(starts) - 1, max(starts) + 3
+    most = max(starts[s + 1] - starts[s] for s in range(B))
+    kv = [130 + 7 * s % 50 for s in range(B)]
+    b = Batch([1] * B, kv, 16, Hkv, D, dtype, seed=B)
+    b.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+    b.batch = P.PagedBatch(b.q_start, b.kv_len, b.table_d, most + spare, b.status)
+    x = _randn(_gen(24), tokens, Hq + 2 * Hkv, D, dtype=DT[dtype])
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    k0, v0 = b.k.clone(), b.v.clone()
+    P.esp_paged_append(b.cache, b.batch, k, v)
+    _recorded(b)
+    _check_appended(b, k, v, k0, v0, starts, served)
+    out, lse = _attention(b, q)
+    _recorded(b)
+    _check_served(b, q, out, lse, starts, served)
+    again, _ = _attention(b, q)
+    _recorded(b)
+    assert torch.equal(out, again)
