@@ -340,8 +340,9 @@ typedef struct {
  * for it, it sees nothing.  Tokens before q_start[0] and from q_start[batch] on are left alone.
  * The device checks what the host cannot see: a sequence whose q_start leaves 0 .. n_tokens, falls, or spans more than max_new tokens, or
  * whose kv_len is negative, above 2^30 or beyond its table's pages, is left out as a whole, and so is one that begins in front of the end of an earlier
- * sequence without such a fault (q_start has fallen in between): no token has two owners; a page number outside 0 .. n_pages - 1 where a
- * position needs one makes the sequence's results meaningless (no other memory is touched).  Both are recorded in *status.  A call takes
+ * sequence without such a fault (q_start has fallen in between): no token has two owners.  A page number outside 0 .. n_pages - 1 where a
+ * position needs one makes the sequence's results meaningless (no other memory is touched): in the append the positions of the new tokens, in the
+ * attention those that a token of the sequence sees (entries of pages that lie behind every window may hold anything).  Both are recorded in *status.  A call takes
  * up to 2^30 tokens. */
 typedef struct {
     int32_t batch;

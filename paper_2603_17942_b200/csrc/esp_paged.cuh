@@ -57,6 +57,8 @@ __device__ __forceinline__ int load_page(const SeqTable& t, const PagesView& p, 
 struct Tile {
     int r0, nr, c0, nc;   // tokens [r0, r0 + nr), chunks [c0, c0 + nc), nc >= 1 (a tile that sees nothing has one chunk without visible keys)
 };
+// What the tile whose first token is r0 sees first (0 or less: everything).  The positions before it in its first chunk are not looked up: a server may have given their pages back.
+__device__ __forceinline__ int first_seen(const PagedAttnArgs& a, const Seq& s, int r0) { return a.window > 0 ? s.kv - s.n + r0 - a.window + 1 : 0; }
 template <int CK>
 __device__ __forceinline__ Tile make_tile(const PagedAttnArgs& a, const Seq& s, int t) {
     Tile x;
@@ -64,7 +66,7 @@ __device__ __forceinline__ Tile make_tile(const PagedAttnArgs& a, const Seq& s, 
     x.nr = min(a.rows, s.n - x.r0);
     const int L = s.kv - s.n;
     const int hi = max(0, a.anc ? s.kv : L + x.r0 + x.nr);
-    const int lo = a.window > 0 ? max(0, L + x.r0 - a.window + 1) : 0;
+    const int lo = max(0, first_seen(a, s, x.r0));
     x.c0 = lo / CK;
     x.nc = max(1, (hi + CK - 1) / CK - x.c0);
     return x;

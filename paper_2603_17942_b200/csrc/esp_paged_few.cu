@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_paged_few(const __grid_consta
         const int pos = (ci.x.c0 + (int)(ui - ci.tile_u)) * KEYS + ((lane & (n_boxes - 1)) << p.box_shift);
         page = a.pages.n_pages;         // a page that there is not reads as zeros
         slot = 0;
-        if (pos < ci.s.kv) {
+        if (pos < ci.s.kv && pos + (1 << p.box_shift) > first_seen(a, ci.s, 0)) {
             const int index = page_index(a.pages, pos);
             const int pg = load_page(a.seq, a.pages, ci.b, index);
             if (pg >= 0) page = pg;

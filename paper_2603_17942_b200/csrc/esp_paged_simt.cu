@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_simt(const __grid_constant__ 
             if (tid < CK) {
                 const int pos = p0 + tid;
                 long long base = -1;
-                if (pos < c.s.kv) {
+                if (pos < c.s.kv && pos >= first_seen(a, c.s, c.x.r0)) {
                     const int index = page_index(a.pages, pos);
                     const int page = load_page(a.seq, a.pages, c.b, index);
                     if (page >= 0) base = page * a.pages.page + (pos - index * a.pages.page_size) * a.pages.tok + c.kvh * a.pages.head;

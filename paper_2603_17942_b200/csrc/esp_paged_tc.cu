@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_paged_tc(const __grid_constant__
             for (int j = 0; j < pc.n; ++j, ++ch) {
                 const int pos = (pc.c0 + j) * CK + box * p.box_rows;
                 int page = a.pages.n_pages, slot = 0;       // a page that there is not reads as zeros
-                if (pos < c.s.kv) {
+                if (pos < c.s.kv && pos + p.box_rows > first_seen(a, c.s, c.x.r0)) {
                     const int index = page_index(a.pages, pos);
                     const int pg = load_page(a.seq, a.pages, c.b, index);
                     if (pg >= 0) page = pg;

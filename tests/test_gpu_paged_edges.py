@@ -65,6 +65,28 @@ def test_an_infinite_value_that_every_token_sees_stays_infinite(dtype, Hq, Hkv, 
     b.ok()
 
 
+# ================================================================ page tables with holes
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 8, 2, 128), ("bf16", 16, 1, 64), ("fp32", 4, 2, 64), ("bf16", 3, 1, 32)])
+@pytest.mark.parametrize("page", [16, 64, 24, 5])
+@pytest.mark.parametrize("n,kv", [([1, 1, 1], [400, 97, 1031]), ([50, 1, 300], [400, 97, 1031])])
+@pytest.mark.parametrize("window", [1, 90, 130])
+def test_pages_behind_every_window_need_no_entry(dtype, Hq, Hkv, D, page, n, kv, window):
+    """A server that gives the pages behind the window back leaves no page number there: positions that no token sees are not looked up, and nothing is recorded."""
+    b = Batch(n, kv, page, Hkv, D, dtype, seed=page + window)
+    q = _randn(_gen(22), b.tokens, Hq, D, dtype=DT[dtype])
+    full, l0 = _attention(b, q, window=window)
+    _check_attention(b, q, full, l0, window=window)
+    for s in range(len(n)):
+        first = max(0, kv[s] - n[s] - window + 1)                 # what the sequence's first token sees first
+        b.table_d[s, :first // page] = -1
+        if first // page > 1:
+            b.table_d[s, 1] = 2 ** 31 - 1
+    assert bool((b.table_d[0] == -1).any())
+    got, l1 = _attention(b, q, window=window)
+    assert torch.equal(got, full) and torch.equal(l0, l1)
+    b.ok()
+
+
 # ================================================================ descriptions that contradict each other
 class One:
     """Sequence s of a batch on its own, for _check_attention."""
