@@ -316,7 +316,7 @@ def esp_gemm_bf16(impl: int, rows: int, n_out: int, k_in: int, x, w, y, scratch,
 
 # ---------------------------------------------------------------- operators over a paged key/value cache
 # These take the tensors themselves ([tokens, heads, head_dim], the last dimension dense) and read shapes, strides and types off them; what does not
-# fit together raises EspError(ESP_E_ARG) before the library is called.
+# fit together raises EspError(ESP_E_ARG) before the library is called.  They run on `stream` (a torch stream or its address), by default on torch's current one.
 ESP_ROPE_MAX_DIM = 256
 ROPE_SCALINGS = ("none", "linear", "base", "rotations", "index")
 
@@ -373,7 +373,10 @@ def esp_rope_table(rope: esp_rope_cfg, table, stream=None):
 
 
 def _stream(stream):
-    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
+    """Address of a stream; None: the current one, on which the call's tensors are used."""
+    if stream is None:
+        stream = _torch.cuda.current_stream()
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 _pack_heads = struct.Struct("Pqqi4x").pack        # the bytes of an esp_heads: a quarter of the time that filling the struct takes
@@ -502,6 +505,7 @@ def esp_paged_attention(cache: PagedCache, batch: PagedBatch, q, out, scratch, s
 def esp_paged_status(batch: PagedBatch, stream=None) -> int:
     """The batch's status word (0); raises EspError(ESP_E_DEVICE) if a kernel has set it."""
     _need(batch.status is not None, "esp_paged_status", "the batch has no status word")
+    _on_current_device(batch.device, "esp_paged_status")           # (whose current stream is waited for)
     st = ctypes.c_int32(0)
     _check(load_library().esp_paged_status(batch.status.data_ptr(), _stream(stream), ctypes.byref(st)), "esp_paged_status")
     return st.value

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2603_17942_b200 as P
-from tests.test_gpu_paged import DT, NAN, Batch, _attention, _check_attention, _gen, _randn
+from tests.test_gpu_paged import DT, NAN, Batch, _attention, _check_attention, _check_norm_rope, _gen, _layer, _randn, _rope_table
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,50 @@ def test_no_token_has_two_owners(dtype, Hq, Hkv, D, what, spare):
     again, _ = _attention(b, q)
     _recorded(b)
     assert torch.equal(out, again)
+
+
+# ================================================================ streams
+def test_calls_without_a_stream_are_ordered_with_their_tensors():
+    """Under torch.cuda.stream() a call that names no stream runs behind the work that makes its inputs and before the work that reads its outputs."""
+    Hq, Hkv, D = 8, 2, 128
+    b = Batch([1, 40], [300, 200], 16, Hkv, D, "bf16", seed=1)
+    cfg = P.rope_cfg(D)
+    good = _randn(_gen(25), b.tokens, Hq + 2 * Hkv, D, dtype=torch.bfloat16)
+    x = torch.zeros_like(good)
+    pos = torch.arange(b.tokens, dtype=torch.int32, device="cuda")
+    k_out = torch.zeros(b.tokens, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        table = _rope_table(cfg)
+        torch.cuda._sleep(100_000_000)                    # about 50 ms
+        x.copy_(good)
+        P.esp_qk_norm_rope(None, x[:, Hq:Hq + Hkv], None, k_out, cfg, table, pos)
+        q, out = _layer(b, x, cfg, table, [None, None])
+        kept = q.clone(), out.clone(), k_out.clone()
+        b.ok()                                            # waits for this stream
+        done = side.query()
+    assert done
+    torch.cuda.synchronize()
+    _check_attention(b, kept[0], kept[1], None)
+    _check_norm_rope(kept[2], good[:, Hq:Hq + Hkv], pos.cpu().numpy(), cfg, None, 0, "bf16")
+
+
+def test_captured_without_naming_the_stream():
+    Hq, Hkv, D = 8, 2, 64
+    b = Batch([1, 1], [300, 200], 16, Hkv, D, "bf16", seed=1)
+    cfg = P.rope_cfg(D)
+    table = _rope_table(cfg)
+    x = _randn(_gen(26), b.tokens, Hq + 2 * Hkv, D, dtype=torch.bfloat16)
+    q, out = torch.empty(b.tokens, Hq, D, device="cuda", dtype=torch.bfloat16), torch.empty(b.tokens, Hq, D, device="cuda", dtype=torch.bfloat16)
+    nb = P.esp_paged_attention_scratch_bytes(Hq, D)
+    scratch = torch.empty(nb, dtype=torch.uint8, device="cuda"), nb
+    _layer(b, x, cfg, table, [None, None], q_out=q, out=out, scratch=scratch)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _layer(b, x, cfg, table, [None, None], q_out=q, out=out, scratch=scratch)
+    x.copy_(_randn(_gen(27), *x.shape))
+    out.fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    _check_attention(b, q, out, None)

@@ -1,0 +1,25 @@
+"""What the binding and the C entry points of the operators over a paged cache hand over and refuse (no GPU: nothing is launched)."""
+import types
+
+import pytest
+import torch
+
+import paper_2603_17942_b200 as P
+from paper_2603_17942_b200 import binding
+
+
+def test_a_call_without_a_stream_runs_on_the_current_one(monkeypatch):
+    """Tensors are used on torch's current stream: a call without one of its own is ordered with them."""
+    stream = types.SimpleNamespace(cuda_stream=0x1234)
+    monkeypatch.setattr(binding, "_torch", types.SimpleNamespace(cuda=types.SimpleNamespace(current_stream=lambda: stream)))
+    assert binding._stream(None) == 0x1234
+    assert binding._stream(types.SimpleNamespace(cuda_stream=0x99)) == 0x99 and binding._stream(0) == 0
+
+
+def test_the_status_of_another_device_is_not_read():
+    """The stream that is waited for is the current device's: a batch that is elsewhere is refused as in the other calls."""
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    batch = P.PagedBatch(i(3), i(2), i(2, 4), 1, i(1))
+    with pytest.raises(P.EspError) as e:
+        P.esp_paged_status(batch)
+    assert e.value.code == -8
