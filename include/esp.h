@@ -316,7 +316,7 @@ int esp_gemm_bf16(int32_t impl, int32_t rows, int32_t n_out, int32_t k_in, const
  * lengths, tables and tensors as they are then. */
 
 /* `n_heads` vectors of head_dim adjacent elements for each token: head h of token t starts at data + t * token_stride +
- * h * head_stride (elements).  Strides of tensors that are read may be zero. */
+ * h * head_stride (elements).  Strides of tensors that are read may be zero; up to 2^40 elements, and up to 2^20 heads. */
 typedef struct {
     void* data;        /* [device] */
     int64_t token_stride, head_stride;

@@ -11,17 +11,18 @@ namespace {
 int cuda_ok(cudaError_t e) { return e == cudaSuccess ? ESP_OK : ESP_E_CUDA; }
 size_t elem_size(int32_t dtype) { return dtype == 0 ? 4 : 2; }
 
+constexpr int32_t MAX_HEADS = 1 << 20;
 // A token-major tensor of n_tokens tokens: 0 or an error.  written: its rows must not share elements.
 int check_heads(const esp_heads* x, int32_t dtype, int32_t n_tokens, int32_t head_dim, bool written) {
-    if ((!x->data && n_tokens > 0) || x->n_heads < 1 || x->token_stride < 0 || x->head_stride < 0) return ESP_E_ARG;
+    if ((!x->data && n_tokens > 0) || x->n_heads < 1 || x->n_heads > MAX_HEADS || x->token_stride < 0 || x->head_stride < 0) return ESP_E_ARG;
     if (reinterpret_cast<uintptr_t>(x->data) % elem_size(dtype)) return ESP_E_ARG;
     if (x->token_stride > ((int64_t)1 << 40) || x->head_stride > ((int64_t)1 << 40)) return ESP_E_ARG;
     if (written) {
         if (x->n_heads > 1 && x->head_stride < head_dim) return ESP_E_ARG;
         if (n_tokens > 1 && x->token_stride < head_dim) return ESP_E_ARG;
         // either the heads of a token lie inside its stride or the tokens of a head inside the head's
-        const bool by_token = x->token_stride >= (x->n_heads - 1) * x->head_stride + head_dim;
-        const bool by_head = x->head_stride >= (n_tokens - 1) * x->token_stride + head_dim;
+        const bool by_token = x->token_stride >= (__int128)(x->n_heads - 1) * x->head_stride + head_dim;
+        const bool by_head = x->head_stride >= (__int128)(n_tokens - 1) * x->token_stride + head_dim;
         if (x->n_heads > 1 && n_tokens > 1 && !by_token && !by_head) return ESP_E_ARG;
     }
     return ESP_OK;

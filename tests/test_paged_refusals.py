@@ -6,6 +6,7 @@ import torch
 
 import paper_2603_17942_b200 as P
 from paper_2603_17942_b200 import binding
+from tests.test_paged_host import ARG, X, _batch, _cache, _heads, _norm_rope, lib  # noqa: F401
 
 
 def test_a_call_without_a_stream_runs_on_the_current_one(monkeypatch):
@@ -23,3 +24,16 @@ def test_the_status_of_another_device_is_not_read():
     with pytest.raises(P.EspError) as e:
         P.esp_paged_status(batch)
     assert e.value.code == -8
+
+
+def test_rows_that_share_elements_are_refused_at_every_size(lib):  # noqa: F811
+    """Heads or tokens whose span is 2^64 elements: it does not wrap around to nothing."""
+    # token 2^20 of a head stands where token 0 of the next head does
+    far = dict(n=2 ** 24 + 1, tok=2 ** 20, head=2 ** 40)
+    assert _norm_rope(lib, q=_heads(**far), q_out=_heads(data=2 * X, **far), tokens=2 ** 20 + 1) == ARG
+    # head 2^19 of a token stands where head 0 of the next token does
+    far = dict(n=2 ** 20, tok=2 ** 40, head=2 ** 21)
+    assert _norm_rope(lib, q=_heads(**far), q_out=_heads(data=2 * X, **far), tokens=2 ** 24 + 1) == ARG
+    # more heads than a call takes (their sum over queries, keys and values is counted in 32 bits)
+    many = dict(n=2 ** 20 + 1, tok=(2 ** 20 + 1) * 128, head=128)
+    assert _norm_rope(lib, q=_heads(**many), q_out=_heads(data=2 * X, **many)) == ARG
