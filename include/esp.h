@@ -343,7 +343,7 @@ typedef struct {
  * sequence without such a fault (q_start has fallen in between): no token has two owners.  A page number outside 0 .. n_pages - 1 where a
  * position needs one makes the sequence's results meaningless (no other memory is touched): in the append the positions of the new tokens, in the
  * attention those that a token of the sequence sees (entries of pages that lie behind every window may hold anything).  Both are recorded in *status.  A call takes
- * up to 2^30 tokens. */
+ * up to 2^30 tokens and sequences. */
 typedef struct {
     int32_t batch;
     int32_t max_new;            /* no sequence has more new tokens than this */

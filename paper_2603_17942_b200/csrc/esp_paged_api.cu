@@ -11,7 +11,7 @@ namespace {
 int cuda_ok(cudaError_t e) { return e == cudaSuccess ? ESP_OK : ESP_E_CUDA; }
 size_t elem_size(int32_t dtype) { return dtype == 0 ? 4 : 2; }
 
-constexpr int32_t MAX_HEADS = 1 << 20;
+constexpr int32_t MAX_HEADS = 1 << 20, MAX_BATCH = 1 << 30;
 // A token-major tensor of n_tokens tokens: 0 or an error.  written: its rows must not share elements.
 int check_heads(const esp_heads* x, int32_t dtype, int32_t n_tokens, int32_t head_dim, bool written) {
     if ((!x->data && n_tokens > 0) || x->n_heads < 1 || x->n_heads > MAX_HEADS || x->token_stride < 0 || x->head_stride < 0) return ESP_E_ARG;
@@ -50,7 +50,7 @@ int check_cache(const esp_paged_cache* c) {
     return ESP_OK;
 }
 int check_batch(const esp_paged_batch* b) {
-    if (b->batch < 0 || b->max_new < 0) return ESP_E_ARG;
+    if (b->batch < 0 || b->batch > MAX_BATCH || b->max_new < 0) return ESP_E_ARG;
     if (b->batch > 0 && (!b->q_start || !b->kv_len || !b->page_table || b->table_pages < 1)) return ESP_E_ARG;
     if (b->batch > 1 && b->table_stride < b->table_pages) return ESP_E_ARG;
     return ESP_OK;

@@ -1,4 +1,5 @@
 """What the binding and the C entry points of the operators over a paged cache hand over and refuse (no GPU: nothing is launched)."""
+import ctypes
 import types
 
 import pytest
@@ -37,3 +38,22 @@ def test_rows_that_share_elements_are_refused_at_every_size(lib):  # noqa: F811
     # more heads than a call takes (their sum over queries, keys and values is counted in 32 bits)
     many = dict(n=2 ** 20 + 1, tok=(2 ** 20 + 1) * 128, head=128)
     assert _norm_rope(lib, q=_heads(**many), q_out=_heads(data=2 * X, **many)) == ARG
+
+
+def _append(lib, cache=None, batch=None, k=None, v=None, q=None, q_gain=None, k_gain=None, positions=None, q_out=None, tokens=4):  # noqa: F811
+    r = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    return lib.esp_paged_append(tokens, r(cache or _cache()), r(batch or _batch()), r(k or _heads()), r(v or _heads(data=3 * X)), r(q), q_gain, k_gain, 1e-6, None, None, positions,
+                                r(q_out), None)
+
+
+def _attend(lib, cache=None, batch=None, anc=None, lse=None, tokens=4):  # noqa: F811
+    r = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    return lib.esp_paged_attention(tokens, r(cache or _cache()), r(batch or _batch()), r(_heads(n=4)), anc, 0, 0.0, r(_heads(n=4, data=4 * X)), lse, X,
+                                   P.esp_paged_attention_scratch_bytes(4, 128), None)
+
+
+def test_more_sequences_than_the_kernels_count(lib):  # noqa: F811
+    """The kernels deal 32 lanes their shares of the sequences in 32 bits: above 2^30 of them nothing would be walked, and nobody told."""
+    batch = _batch(batch=2 ** 30 + 1)
+    assert _append(lib, batch=batch) == ARG and _attend(lib, batch=batch) == ARG
+    assert _append(lib, batch=_batch(batch=2 ** 30), tokens=0) == 0 and _attend(lib, batch=_batch(batch=2 ** 30), tokens=0) == 0
