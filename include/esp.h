@@ -313,7 +313,7 @@ int esp_gemm_bf16(int32_t impl, int32_t rows, int32_t n_out, int32_t k_in, const
  * projection, for decode steps, draft trees and chunks of prompts, in one ragged batch.  Token-major tensors hold the new tokens
  * of all sequences one behind the other.  Everything is asynchronous on cuda_stream and on the current device, whose memory every
  * [device] pointer is.  The calls allocate nothing and keep nothing, so they can be captured into a CUDA graph; a replay reads
- * lengths, tables and tensors as they are then. */
+ * lengths, tables and tensors as they are then.  Addresses lie on their types' boundaries (ESP_E_ARG otherwise). */
 
 /* `n_heads` vectors of head_dim adjacent elements for each token: head h of token t starts at data + t * token_stride +
  * h * head_stride (elements).  Strides of tensors that are read may be zero; up to 2^40 elements, and up to 2^20 heads. */

@@ -10,12 +10,13 @@ namespace {
 
 int cuda_ok(cudaError_t e) { return e == cudaSuccess ? ESP_OK : ESP_E_CUDA; }
 size_t elem_size(int32_t dtype) { return dtype == 0 ? 4 : 2; }
+bool off(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }      // (NULL is on every boundary)
 
 constexpr int32_t MAX_HEADS = 1 << 20, MAX_BATCH = 1 << 30;
 // A token-major tensor of n_tokens tokens: 0 or an error.  written: its rows must not share elements.
 int check_heads(const esp_heads* x, int32_t dtype, int32_t n_tokens, int32_t head_dim, bool written) {
     if ((!x->data && n_tokens > 0) || x->n_heads < 1 || x->n_heads > MAX_HEADS || x->token_stride < 0 || x->head_stride < 0) return ESP_E_ARG;
-    if (reinterpret_cast<uintptr_t>(x->data) % elem_size(dtype)) return ESP_E_ARG;
+    if (off(x->data, elem_size(dtype))) return ESP_E_ARG;
     if (x->token_stride > ((int64_t)1 << 40) || x->head_stride > ((int64_t)1 << 40)) return ESP_E_ARG;
     if (written) {
         if (x->n_heads > 1 && x->head_stride < head_dim) return ESP_E_ARG;
@@ -41,7 +42,7 @@ int check_cache(const esp_paged_cache* c) {
     if (!c->k || !c->v || c->n_pages < 1 || c->page_size < 1 || c->n_kv_heads < 1) return ESP_E_ARG;
     if (c->dtype != 0 && c->dtype != 1) return ESP_E_BADCFG;
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return ESP_E_BADCFG;
-    if (reinterpret_cast<uintptr_t>(c->k) % elem_size(c->dtype) || reinterpret_cast<uintptr_t>(c->v) % elem_size(c->dtype)) return ESP_E_ARG;
+    if (off(c->k, elem_size(c->dtype)) || off(c->v, elem_size(c->dtype))) return ESP_E_ARG;
     if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return ESP_E_ARG;
     if (c->page_stride > ((int64_t)1 << 40) || c->token_stride > ((int64_t)1 << 40) || c->head_stride > ((int64_t)1 << 40)) return ESP_E_ARG;
     // slots do not share elements (the pages of k may lie between those of v)
@@ -53,6 +54,7 @@ int check_batch(const esp_paged_batch* b) {
     if (b->batch < 0 || b->batch > MAX_BATCH || b->max_new < 0) return ESP_E_ARG;
     if (b->batch > 0 && (!b->q_start || !b->kv_len || !b->page_table || b->table_pages < 1)) return ESP_E_ARG;
     if (b->batch > 1 && b->table_stride < b->table_pages) return ESP_E_ARG;
+    if (off(b->q_start, 4) || off(b->kv_len, 4) || off(b->page_table, 4) || off(b->status, 4)) return ESP_E_ARG;
     return ESP_OK;
 }
 PagesView pages_of(const esp_paged_cache* c) {
@@ -117,7 +119,7 @@ int set_rope(NormRopeArgs& a, const esp_rope_cfg* rope, const void* table, int32
     if (!rope) return ESP_OK;
     if (const int rc = check_rope(rope)) return rc;
     if (rope->rotary_dim > head_dim) return ESP_E_BADCFG;
-    if (!table || reinterpret_cast<uintptr_t>(table) % 16) return ESP_E_ARG;
+    if (!table || off(table, 16)) return ESP_E_ARG;
     a.freq = reinterpret_cast<const uint64_t*>(table);
     a.pairs = rope->rotary_dim / 2;
     a.interleaved = rope->interleaved;
@@ -148,7 +150,7 @@ int esp_rope_table_bytes(const esp_rope_cfg* rope, size_t* bytes_out) {
 int esp_rope_table(const esp_rope_cfg* rope, void* table, size_t table_bytes, void* cuda_stream) {
     size_t need = 0;
     if (const int rc = esp_rope_table_bytes(rope, &need)) return rc;
-    if (!table || reinterpret_cast<uintptr_t>(table) % 16) return ESP_E_ARG;
+    if (!table || off(table, 16)) return ESP_E_ARG;
     if (table_bytes < need) return ESP_E_WORKSPACE;
     long double f[ESP_ROPE_MAX_DIM / 2];
     uint64_t turns[ESP_ROPE_MAX_DIM / 2];
@@ -168,6 +170,7 @@ int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const es
     if (head_dim < 1 || head_dim > ESP_ROPE_MAX_DIM) return ESP_E_BADCFG;
     if (n_tokens < 0 || n_tokens > paged::KV_LIMIT || (!q && !k) || !q != !q_out || !k != !k_out || !(eps >= 0.f)) return ESP_E_ARG;
     if ((q_gain && !q) || (k_gain && !k) || (rope && !positions && n_tokens > 0)) return ESP_E_ARG;
+    if (off(q_gain, elem_size(dtype)) || off(k_gain, elem_size(dtype)) || off(positions, 4)) return ESP_E_ARG;
     for (int i = 0; i < 2; ++i) {
         const esp_heads *x = i ? k : q, *y = i ? k_out : q_out;
         if (!x) continue;
@@ -195,6 +198,7 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
     if (!cache || !batch || !k || !v || n_tokens < 0 || n_tokens > paged::KV_LIMIT || !q != !q_out || (q_gain && !q) || !(eps >= 0.f)) return ESP_E_ARG;
     if (const int rc = check_cache(cache)) return rc;
     if (const int rc = check_batch(batch)) return rc;
+    if (off(q_gain, elem_size(cache->dtype)) || off(k_gain, elem_size(cache->dtype)) || off(positions, 4)) return ESP_E_ARG;
     const esp_heads* ins[3] = {k, v, q};
     for (int i = 0; i < 3; ++i) {
         if (!ins[i]) continue;
@@ -241,9 +245,10 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
     if (q->n_heads != out->n_heads || (n_tokens > 0 && q->data == out->data)) return ESP_E_ARG;
     if (q->n_heads % cache->n_kv_heads || q->n_heads / cache->n_kv_heads > 64) return ESP_E_BADCFG;
     if (anc && (batch->max_new > RT || window)) return ESP_E_ARG;
+    if (off(anc, 8) || off(lse, 4)) return ESP_E_ARG;
     size_t need = 0;
     if (const int rc = esp_paged_attention_scratch_bytes(q->n_heads, cache->head_dim, &need)) return rc;
-    if (scratch_bytes < need || reinterpret_cast<uintptr_t>(scratch) % 256) return ESP_E_WORKSPACE;
+    if (scratch_bytes < need || off(scratch, 256)) return ESP_E_WORKSPACE;
     if (n_tokens == 0 || batch->batch == 0 || batch->max_new == 0) return ESP_OK;
     int n_sm = current_sm_count();
     if (n_sm < 1) return ESP_E_CUDA;
@@ -277,7 +282,7 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
 }
 
 int esp_paged_status(const int32_t* status, void* cuda_stream, int32_t* device_status_out) {
-    if (!status) return ESP_E_ARG;
+    if (!status || off(status, 4)) return ESP_E_ARG;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
     int32_t e = 0;
     if (cudaMemcpyAsync(&e, status, sizeof(e), cudaMemcpyDeviceToHost, s) != cudaSuccess) return ESP_E_CUDA;

@@ -57,3 +57,20 @@ def test_more_sequences_than_the_kernels_count(lib):  # noqa: F811
     batch = _batch(batch=2 ** 30 + 1)
     assert _append(lib, batch=batch) == ARG and _attend(lib, batch=batch) == ARG
     assert _append(lib, batch=_batch(batch=2 ** 30), tokens=0) == 0 and _attend(lib, batch=_batch(batch=2 ** 30), tokens=0) == 0
+
+
+def test_addresses_off_their_types_alignment(lib):  # noqa: F811
+    """A kernel that reads a gain, a length or a mask off its type's alignment would fault: the host says so first."""
+    q, o = _heads(), _heads(data=2 * X)
+    for gain in ("q_gain", "k_gain"):
+        both = dict(q=q, q_out=o, k=_heads(data=3 * X), k_out=_heads(data=4 * X))
+        assert _norm_rope(lib, **both, **{gain: X + 1}) == ARG and _norm_rope(lib, **both, dtype=0, **{gain: X + 2}) == ARG
+        assert _append(lib, q=_heads(n=4), q_out=_heads(n=4, data=4 * X), **{gain: X + 1}) == ARG
+        assert _norm_rope(lib, **both, **{gain: X + 2}, tokens=0) == 0
+    assert _norm_rope(lib, q=q, q_out=o, positions=X + 2) == ARG and _append(lib, positions=X + 1) == ARG
+    for name in ("q_start", "kv_len", "page_table", "status"):
+        batch = _batch(**{name: X + 2})
+        assert _append(lib, batch=batch) == ARG and _attend(lib, batch=batch) == ARG, name
+    assert _attend(lib, anc=X + 4) == ARG and _attend(lib, lse=X + 2) == ARG
+    assert _attend(lib, anc=X + 8, lse=X + 4, tokens=0) == 0
+    assert lib.esp_paged_status(X + 1, None, None) == ARG
