@@ -551,9 +551,9 @@ int run_tc(TcParams& p, cudaStream_t s) {
 }  // namespace
 
 bool paged_tma_pages(const PagedAttnArgs& a, int chunk, int* box_rows) {
-    // boxes of whole swizzle groups of eight rows; every stride a multiple of 16 bytes
+    // boxes of whole swizzle groups of eight rows; every stride a multiple of 16 bytes below 2^40
     *box_rows = gcd(a.pages.page_size, chunk);
-    auto al = [](long long x) { return x % 8 == 0; };
+    auto al = [](long long x) { return x % 8 == 0 && x < (1ll << 39); };
     return *box_rows % 8 == 0 && reinterpret_cast<uintptr_t>(a.pages.k) % 16 == 0 && reinterpret_cast<uintptr_t>(a.pages.v) % 16 == 0 && al(a.pages.page) &&
            al(a.pages.tok) && al(a.pages.head) && a.pages.page_size <= (1 << 30);
 }
@@ -572,7 +572,7 @@ int paged_page_map(CUtensorMap* map, const PagedAttnArgs& a, const void* base, i
 bool paged_tc_supported(int dtype, const PagedAttnArgs& a) {
     int box = 0;
     return dtype == 1 && (a.D == 64 || a.D == 128) && a.group <= SUB && paged_tma_pages(a, CK, &box) && reinterpret_cast<uintptr_t>(a.q.p) % 16 == 0 &&
-           a.q.tok % 8 == 0 && a.q.head % 8 == 0 && (a.q.tok > 0 || a.seq.n_tokens == 1) && (a.q.head > 0 || a.Hq == 1);
+           a.q.tok % 8 == 0 && a.q.head % 8 == 0 && a.q.tok < (1ll << 39) && a.q.head < (1ll << 39) && (a.q.tok > 0 || a.seq.n_tokens == 1) && (a.q.head > 0 || a.Hq == 1);
 }
 
 int launch_paged_tc(PagedAttnArgs a, int n_sm, cudaStream_t s) {

@@ -87,6 +87,26 @@ def test_pages_behind_every_window_need_no_entry(dtype, Hq, Hkv, D, page, n, kv,
     b.ok()
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("stride", [1 << 39, 1 << 40])
+def test_page_strides_that_a_tensor_map_cannot_hold(n, stride):
+    """Pages 2^40 bytes and more apart, of which the table names the first alone: such a cache goes the way of those that no tensor map fits."""
+    b = Batch([n, 1], [60, 48], 64, 2, 128, "bf16", seed=3)
+    x = _randn(_gen(28), b.tokens, 12, 128, dtype=torch.bfloat16)
+    b.n, b.kv = [n, 0], [60, 0]
+    b.table[0, 0], b.unused = 0, None
+    b.table_d[0, 0] = 0
+    b.q_start.copy_(torch.tensor([0, n, n], dtype=torch.int32))
+    b.kv_len.copy_(torch.tensor([60, 0], dtype=torch.int32))
+    P.esp_paged_append(b.cache, b.batch, x[:, 8:10], x[:, 10:])
+    want, l0 = _attention(b, x[:, :8])
+    b.cache.c.page_stride = stride
+    P.esp_paged_append(b.cache, b.batch, x[:, 8:10], x[:, 10:])
+    got, l1 = _attention(b, x[:, :8])
+    _check_attention(b, x[:, :8], want, l0)
+    _check_attention(b, x[:, :8], got, l1)
+
+
 # ================================================================ descriptions that contradict each other
 class One:
     """Sequence s of a batch on its own, for _check_attention."""
