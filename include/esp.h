@@ -394,7 +394,8 @@ int esp_qk_norm_rope(int32_t dtype, int32_t n_tokens, int32_t head_dim, const es
 /* Appends the new tokens' keys and values to the pages: k normed (k_gain) and rotated as above, v as it is.  With q (may be NULL,
  * with q_out) the queries are normed and rotated in the same launch; rows of q_out that belong to no position are left alone.
  * positions [device] [n_tokens] gives the rotation's positions where they are not the slots' (the rows of a draft tree share
- * positions); NULL: the slot's position.  Two tokens of a call must not share a slot. */
+ * positions); NULL: the slot's position.  Two tokens of a call must not share a slot, and
+ * slots no elements (of pages, tokens and heads each stride spans all that lies inside it, in any order of nesting; ESP_E_ARG otherwise). */
 int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* k, const esp_heads* v,
                      const esp_heads* q, const void* q_gain, const void* k_gain, float eps, const esp_rope_cfg* rope, const void* rope_table,
                      const int32_t* positions, const esp_heads* q_out, void* cuda_stream);

@@ -45,9 +45,25 @@ int check_cache(const esp_paged_cache* c) {
     if (off(c->k, elem_size(c->dtype)) || off(c->v, elem_size(c->dtype))) return ESP_E_ARG;
     if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return ESP_E_ARG;
     if (c->page_stride > ((int64_t)1 << 40) || c->token_stride > ((int64_t)1 << 40) || c->head_stride > ((int64_t)1 << 40)) return ESP_E_ARG;
-    // slots do not share elements (the pages of k may lie between those of v)
+    // no two pages, tokens or heads share elements (the pages of k may lie between those of v)
     if ((c->n_pages > 1 && c->page_stride < c->head_dim) || (c->page_size > 1 && c->token_stride < c->head_dim) ||
         (c->n_kv_heads > 1 && c->head_stride < c->head_dim)) return ESP_E_ARG;
+    return ESP_OK;
+}
+// Slots that are written: no two of them share elements, whichever of pages, tokens and heads lie inside which.
+int check_slots(const esp_paged_cache* c) {
+    struct { int64_t stride, count; } dim[3] = {{c->page_stride, c->n_pages}, {c->token_stride, c->page_size}, {c->head_stride, c->n_kv_heads}};
+    __int128 span = c->head_dim;
+    for (int done = 0; done < 3; ++done) {                  // the smallest stride of those left: it has to span what lies inside
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (dim[i].count > 0 && (at < 0 || dim[i].stride < dim[at].stride)) at = i;
+        if (dim[at].count > 1) {
+            if (dim[at].stride < span) return ESP_E_ARG;
+            span += (__int128)(dim[at].count - 1) * dim[at].stride;
+        }
+        dim[at].count = 0;
+    }
     return ESP_OK;
 }
 int check_batch(const esp_paged_batch* b) {
@@ -197,6 +213,7 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
                      const int32_t* positions, const esp_heads* q_out, void* cuda_stream) {
     if (!cache || !batch || !k || !v || n_tokens < 0 || n_tokens > paged::KV_LIMIT || !q != !q_out || (q_gain && !q) || !(eps >= 0.f)) return ESP_E_ARG;
     if (const int rc = check_cache(cache)) return rc;
+    if (const int rc = check_slots(cache)) return rc;
     if (const int rc = check_batch(batch)) return rc;
     if (off(q_gain, elem_size(cache->dtype)) || off(k_gain, elem_size(cache->dtype)) || off(positions, 4)) return ESP_E_ARG;
     const esp_heads* ins[3] = {k, v, q};

@@ -74,3 +74,14 @@ def test_addresses_off_their_types_alignment(lib):  # noqa: F811
     assert _attend(lib, anc=X + 4) == ARG and _attend(lib, lse=X + 2) == ARG
     assert _attend(lib, anc=X + 8, lse=X + 4, tokens=0) == 0
     assert lib.esp_paged_status(X + 1, None, None) == ARG
+
+
+def test_append_into_slots_that_share_elements(lib):  # noqa: F811
+    """Every stride spans a head, but two tokens' slots are one: nothing is written there.  Slots in any order of nesting are fine, and so is reading them."""
+    for strides in (dict(head_stride=1024), dict(page_stride=2048), dict(page_stride=128, token_stride=256, head_stride=4096), dict(page_stride=2 ** 40, token_stride=128, head_stride=2 ** 40),
+                    dict(token_stride=192, head_stride=256)):
+        assert _append(lib, cache=_cache(**strides)) == ARG, strides
+        assert _append(lib, cache=_cache(**strides), tokens=0) == ARG and _attend(lib, cache=_cache(**strides), tokens=0) == 0
+    for strides in (dict(), dict(page_stride=128, token_stride=1024, head_stride=16384), dict(token_stride=256, head_stride=128), dict(page_stride=128, token_stride=2048, head_stride=1024)):
+        assert _append(lib, cache=_cache(**strides), tokens=0) == 0, strides
+    assert _append(lib, cache=_cache(page_size=1, token_stride=0, head_stride=128, page_stride=256), tokens=0) == 0
