@@ -321,6 +321,14 @@ ESP_ROPE_MAX_DIM = 256
 ROPE_SCALINGS = ("none", "linear", "base", "rotations", "index")
 
 
+def _i32(x, where: str, name: str) -> int:
+    """x where the library takes 32 bits (ctypes would cut the rest off)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise EspError(-8, f"{where} ({name}: {x} is more than 32 bits hold)")
+    return x
+
+
 def rope_cfg(rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, original_len: int = 8192,
              low: float = 1.0, high: Optional[float] = None, amplitude: float = 1.0) -> esp_rope_cfg:
     """esp_rope_cfg.  scaling: none, linear, base, rotations or index (see esp.h); high: turns above which a pair is kept, by default 4 for
@@ -329,7 +337,8 @@ def rope_cfg(rotary_dim: int, base: float = 10000.0, interleaved: bool = False, 
         raise EspError(-1, f"rope_cfg(scaling={scaling!r})")
     if high is None:
         high = 32.0 if scaling == "index" else 4.0
-    return esp_rope_cfg(int(rotary_dim), int(bool(interleaved)), ROPE_SCALINGS.index(scaling), int(original_len), base, factor, low, high, amplitude)
+    return esp_rope_cfg(_i32(rotary_dim, "rope_cfg", "rotary_dim"), int(bool(interleaved)), ROPE_SCALINGS.index(scaling), _i32(original_len, "rope_cfg", "original_len"), base, factor,
+                        low, high, amplitude)
 
 
 def esp_rope_frequencies(rope: esp_rope_cfg) -> np.ndarray:
@@ -415,7 +424,8 @@ class PagedCache:
         h, s = (1, 2) if order == "head" else (2, 1)
         self.k, self.v, self.order = k, v, order
         self.dtype, self.device, self.head_dim = k.dtype, k.get_device(), k.shape[3]
-        self.c = esp_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(s), k.stride(h), k.shape[0], k.shape[s], k.shape[h], k.shape[3],
+        sizes = [_i32(k.shape[i], where, "pages, page_size, kv_heads, head_dim") for i in (0, s, h, 3)]
+        self.c = esp_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(s), k.stride(h), *sizes,
                                  0 if str(k.dtype) == "torch.float32" else 1)
         self.ref = ctypes.byref(self.c)
 
@@ -435,8 +445,9 @@ class PagedBatch:
         _need(status is None or status.numel() >= 1, where, "status")
         self.q_start, self.kv_len, self.page_table, self.status = q_start, kv_len, page_table, status
         self.device = page_table.get_device()
-        self.c = esp_paged_batch(n, int(max_new), q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
-                                 page_table.stride(0) if n > 1 else page_table.shape[1],
+        row = _i32(page_table.shape[1], where, "page_table")
+        self.c = esp_paged_batch(_i32(n, where, "batch"), _i32(max_new, where, "max_new"), q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), row,
+                                 _i32(page_table.stride(0), where, "page_table") if n > 1 else row,
                                  None if status is None else status.data_ptr())
         self.ref = ctypes.byref(self.c)
 
@@ -447,9 +458,10 @@ def esp_qk_norm_rope(q, k, q_out, k_out, rope: Optional[esp_rope_cfg] = None, ro
     where = "esp_qk_norm_rope"
     x = k if q is None else q
     _need(x is not None and x.dim() == 3, where, "q or k [tokens, heads, head_dim]")
+    n, _, d = x.shape
+    n, d = _i32(n, where, "tokens"), _i32(d, where, "head_dim")
     dev = x.get_device()
     _on_current_device(dev, where)
-    n, _, d = x.shape
     dt = x.dtype
     _need(dt in _DTYPES, where, "fp32 or bf16")
     _check(load_library().esp_qk_norm_rope(
@@ -470,10 +482,10 @@ def esp_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Optional[
                      q_out=None, q_gain=None, eps: float = 1e-6, stream=None):
     """Appends the new tokens' k (normed and rotated as asked) and v to the pages; with q, norms and rotates the queries into q_out in the same launch."""
     where = "esp_paged_append"
+    n = _i32(k.shape[0], where, "tokens")
     dev, dt, d = cache.device, cache.dtype, cache.head_dim
     _on_current_device(dev, where)
     _need(batch.device == dev, where, "cache and batch on one device")
-    n = k.shape[0]
     _check(load_library().esp_paged_append(
         n, cache.ref, batch.ref, _heads(k, n, d, dt, dev, where, "k"), _heads(v, n, d, dt, dev, where, "v"), _heads(q, n, d, dt, dev, where, "q"),
         _vector(q_gain, d, (dt,), dev, where, "q_gain"), _vector(k_gain, d, (dt,), dev, where, "k_gain"), eps,
@@ -483,7 +495,8 @@ def esp_paged_append(cache: PagedCache, batch: PagedBatch, k, v, rope: Optional[
 
 def esp_paged_attention_scratch_bytes(n_q_heads: int, head_dim: int) -> int:
     out = ctypes.c_size_t(0)
-    _check(load_library().esp_paged_attention_scratch_bytes(n_q_heads, head_dim, ctypes.byref(out)), "esp_paged_attention_scratch_bytes")
+    where = "esp_paged_attention_scratch_bytes"
+    _check(load_library().esp_paged_attention_scratch_bytes(_i32(n_q_heads, where, "n_q_heads"), _i32(head_dim, where, "head_dim"), ctypes.byref(out)), where)
     return out.value
 
 
@@ -491,11 +504,11 @@ def esp_paged_attention(cache: PagedCache, batch: PagedBatch, q, out, scratch, s
                         stream=None):
     """Attention of the new tokens over the pages into `out`: causal, with a window, or with the ancestor masks `anc` [tokens, 2] (64-bit words) of draft trees."""
     where = "esp_paged_attention"
+    n, window = _i32(q.shape[0], where, "tokens"), _i32(window, where, "window")
     dev, dt, d = cache.device, cache.dtype, cache.head_dim
     _on_current_device(dev, where)
     _need(batch.device == dev and scratch.get_device() == dev, where, "cache, batch and scratch on one device")
     _need(scratch.numel() * scratch.element_size() >= scratch_bytes and scratch.is_contiguous(), where, "scratch_bytes")
-    n = q.shape[0]
     _check(load_library().esp_paged_attention(
         n, cache.ref, batch.ref, _heads(q, n, d, dt, dev, where, "q"), _vector(anc, 2 * n, (_torch.int64, _torch.uint64), dev, where, "anc"), window, scale,
         _heads(out, n, d, dt, dev, where, "out"), None if lse is None else _vector(lse, n * q.shape[1], (_torch.float32,), dev, where, "lse"),

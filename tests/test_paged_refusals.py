@@ -85,3 +85,30 @@ def test_append_into_slots_that_share_elements(lib):  # noqa: F811
     for strides in (dict(), dict(page_stride=128, token_stride=1024, head_stride=16384), dict(token_stride=256, head_stride=128), dict(page_stride=128, token_stride=2048, head_stride=1024)):
         assert _append(lib, cache=_cache(**strides), tokens=0) == 0, strides
     assert _append(lib, cache=_cache(page_size=1, token_stride=0, head_stride=128, page_stride=256), tokens=0) == 0
+
+
+def test_numbers_that_do_not_fit_are_not_cut_off(lib):  # noqa: F811
+    """2^32 + 5 is not 5: numbers that the library takes in 32 bits are checked before they are handed over."""
+    far = 2 ** 32
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    k = torch.zeros(4, 2, 16, 64)
+    cache, batch, x = P.PagedCache(k, k.clone()), P.PagedBatch(i(3), i(2), i(2, 4), 1), torch.zeros(2, 2, 64)
+    many = torch.zeros(1, 1, 64).expand(far + 2, 2, 64)
+    calls = {
+        "max_new": lambda: P.PagedBatch(i(3), i(2), i(2, 4), far + 1),
+        "page_table": lambda: P.PagedBatch(i(3).to("meta"), i(2).to("meta"), torch.empty(2, far, dtype=torch.int32, device="meta")[:, :4], 1),
+        "rotary_dim": lambda: P.rope_cfg(far + 64),
+        "original_len": lambda: P.rope_cfg(64, scaling="linear", factor=2.0, original_len=far + 8192),
+        "n_q_heads": lambda: P.esp_paged_attention_scratch_bytes(far + 4, 64),
+        "head_dim": lambda: P.esp_paged_attention_scratch_bytes(4, far + 64),
+        "window": lambda: P.esp_paged_attention(cache, batch, x, x.clone(), torch.zeros(8), 32, window=far + 5),
+        "tokens": lambda: P.esp_paged_attention(cache, batch, many, many, torch.zeros(8), 32),
+        "tokens ": lambda: P.esp_paged_append(cache, batch, many, many),
+        "tokens  ": lambda: P.esp_qk_norm_rope(many, None, many, None),
+    }
+    for what, call in calls.items():
+        with pytest.raises(P.EspError, match=what.strip()):
+            call()
+    with pytest.raises(P.EspError):
+        P.PagedCache(k[:1].expand(far + 1, 2, 16, 64), k[:1].expand(far + 1, 2, 16, 64))
+    assert P.PagedBatch(i(3), i(2), i(2, 4), 2 ** 31 - 1).c.max_new == 2 ** 31 - 1
