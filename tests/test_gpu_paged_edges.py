@@ -182,6 +182,77 @@ def test_no_token_has_two_owners(dtype, Hq, Hkv, D, what, spare):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("n", [1, 50])
+def test_who_holds_together_has_its_results(n):
+    """Beside a sequence whose numbers contradict each other, or whose table names a page that there is not, the others have the results of their own keys and values, and
+    the append writes their slots alone."""
+    x = _randn(_gen(30), 3 * n, 12, 128, dtype=torch.bfloat16)
+    q, k, v = x[:, :8], x[:, 8:10], x[:, 10:]
+    whole = [0, n, 2 * n, 3 * n]
+    changes = [
+        (lambda b: b.kv_len[1:2].fill_(b.table.shape[1] * 16 + 1), whole, [0, 2]),
+        (lambda b: b.kv_len[1:2].fill_(-1), whole, [0, 2]),
+        (lambda b: b.kv_len[0:1].fill_(2 ** 31 - 1), whole, [1, 2]),
+        (lambda b: b.q_start[3:].fill_(3 * n + 1), whole[:3] + [3 * n + 1], [0, 1]),
+        (lambda b: b.q_start[1:2].fill_(2 * n + 1), [0, 2 * n + 1, 2 * n, 3 * n], [2]),       # the first has too many tokens, the second falls
+        (lambda b: b.q_start[:1].fill_(-1), [-1, n, 2 * n, 3 * n], [1, 2]),
+    ]
+    for change, starts, served in changes:
+        b = Batch([n, n, n], [100, 200, 300], 16, 2, 128, "bf16", seed=2)
+        change(b)
+        k0, v0 = b.k.clone(), b.v.clone()
+        P.esp_paged_append(b.cache, b.batch, k, v)
+        _recorded(b)
+        _check_appended(b, k, v, k0, v0, starts, served)
+        out, lse = _attention(b, q)
+        _recorded(b)
+        _check_served(b, q, out, lse, starts, served)
+    for page in (-1, b.k.shape[0], 2 ** 31 - 1):                          # the page of the second sequence's positions 192 .. 199
+        b = Batch([n, n, n], [100, 200, 300], 16, 2, 128, "bf16", seed=2)
+        lost = int(b.table[1, 12])
+        b.table_d[1, 12] = page
+        k0, v0 = b.k.clone(), b.v.clone()
+        P.esp_paged_append(b.cache, b.batch, k, v)
+        _recorded(b)
+        pages = b.k[lost].clone(), b.v[lost].clone()
+        assert torch.equal(pages[0], k0[lost]) and torch.equal(pages[1], v0[lost])
+        if n == 1:                                                        # (the only new token of the second sequence has no slot)
+            _check_appended(b, k, v, k0, v0, whole, [0, 2])
+        out, lse = _attention(b, q)
+        _recorded(b)
+        out[n:2 * n], lse[n:2 * n] = 7.0, 7.0                             # no promise about its own rows
+        _check_served(b, q, out, lse, whole, [0, 2])
+
+
+# ================================================================ every position, one by one
+@pytest.mark.parametrize("Hq,Hkv,D,page,n,kv", [(16, 8, 128, 64, [16, 9, 1, 3, 30], [32100, 29999, 16000, 1, 30]), (16, 8, 64, 16, [4] * 6, [30000 - 77 * i for i in range(6)]),
+                                               (8, 2, 128, 16, [130, 70], [5000, 3333]), (8, 2, 64, 24, [1] * 5, [9000, 31, 4099, 1, 20000])])
+def test_every_position_has_its_own_share(Hq, Hkv, D, page, n, kv):
+    """Queries of zero weigh the t visible keys alike.  Values are 1 in dim p - first for the D positions from `first` on and zero elsewhere, one call for each `first`: an output is
+    1 / t for each of those positions that is seen, 0 for the others, so that a position lost or counted twice is an error of the whole value.  Tiles of few pairs
+    whose chunks go through both sets of scores in turn, tiles of two subtiles, single tokens.  Roundings: weights and 1 are exact, the output is rounded once."""
+    b = Batch(n, kv, page, Hkv, D, "bf16", seed=3, fill=0.0)
+    q = torch.zeros(b.tokens, Hq, D, device="cuda", dtype=torch.bfloat16)
+    seen = torch.cat([torch.arange(t - m + 1, t + 1) for m, t in zip(n, kv)]).clamp(min=0).cuda()     # t of every token; 0: padding
+    eye = torch.eye(D, device="cuda", dtype=torch.bfloat16)[:, None].expand(-1, Hkv, -1)
+    slots = [b.slots(s) for s in range(len(n))]
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for first in range(0, max(kv), D):
+        for (pg, sl), t in zip(slots, kv):
+            last = min(first + D, t)
+            if first < last:
+                b.view(b.v)[pg[first:last], sl[first:last]] = eye[:last - first]
+        out, _ = _attention(b, q, lse=False)
+        want = torch.where(first + torch.arange(D, device="cuda") < seen[:, None], 1.0 / seen.clamp(min=1)[:, None].double(), 0.0)[:, None]
+        wrong += ((out.double() - want).abs() > 2.0 ** -8 * 1.01 * want).sum()
+        for (pg, sl), t in zip(slots, kv):
+            last = min(first + D, t)
+            if first < last:
+                b.view(b.v)[pg[first:last], sl[first:last]] = 0.0
+    assert int(wrong) == 0
+    b.ok()
+
+
 # ================================================================ streams
 def test_calls_without_a_stream_are_ordered_with_their_tensors():
     """Under torch.cuda.stream() a call that names no stream runs behind the work that makes its inputs and before the work that reads its outputs."""
