@@ -377,8 +377,8 @@ typedef struct {
 /* f_i in radians per position: out [host] [rotary_dim / 2].  No GPU is needed. */
 int esp_rope_frequencies(const esp_rope_cfg* rope, double* out);
 
-/* Writes the table that the rotating operators read: the frequencies as 64-bit fractions of a turn, so that the angle of any 32-bit
- * position is exact to 2^-31 of a turn.  table [device], 16-byte aligned, esp_rope_table_bytes bytes; made once per configuration. */
+/* Writes the table that the rotating operators read: the frequencies as 64-bit fractions of a turn, so that position times frequency is exact to
+ * 2^-31 of a turn for any 32-bit position; the sine is taken of that angle rounded to fp32, within half a turn 2^-26 of a turn at most.  table [device], 16-byte aligned, esp_rope_table_bytes bytes; made once per configuration. */
 int esp_rope_table_bytes(const esp_rope_cfg* rope, size_t* bytes_out);
 int esp_rope_table(const esp_rope_cfg* rope, void* table, size_t table_bytes, void* cuda_stream);
 
@@ -407,7 +407,8 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
  * that the block does not have are ignored).  A token that sees nothing gets zeros.  scale 0: 1 / sqrt(head_dim).
  * lse [device] or NULL: [n_tokens][n_heads of q] fp32, the logarithm of the sum of exp(scale * q k) over the visible positions,
  * -infinity where there are none.  out must not overlap q.  At most 64 query heads share a key/value head.  A call whose tiles of tokens have 2^31
- * chunks of keys or more to walk in all (chunks of 32 to 128 positions; seconds of work) writes nothing and records the capacity code in *status.
+ * chunks of keys or more to walk in all (chunks of 32 to 128 positions; seconds of work) writes nothing and records the capacity code in *status; one
+ * sequence over 2^30 positions may be refused so from 2^30 chunks on.
  * What a token does not see does not reach its result: slots behind kv_len may hold anything, and an infinite or undefined value reaches
  * only the tokens that see it.  To them an infinite value makes its element of the result infinite (undefined with one of the other sign or one that is no number; where
  * its weight is below 2^-100 of the row's largest the element is infinite or undefined).  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);

@@ -3,8 +3,9 @@
 //   y = x * gain / sqrt(mean(x^2) + eps);   pair (y_a, y_b) -> A (y_a c - y_b s, y_b c + y_a s),  c + i s = e^(i p f)
 //
 // The angle p f is taken modulo one turn in whole numbers: the table holds f / 2 pi as a 64-bit fraction of a turn, p times it
-// wraps around by itself, and the upper 32 bits are the angle to 2^-32 of a turn for every 32-bit position.  (p * f in fp32
-// would be off by 0.06 rad at p = 10^6 for the fastest pair.)
+// wraps around by itself, and the upper 32 bits are the angle to 2^-31 of a turn for every 32-bit position.  (p * f in fp32
+// would be off by 0.06 rad at p = 10^6 for the fastest pair.)  The sine takes it in fp32: 24 bits of at most half a turn, off by 2^-26 of a turn or 9.4e-8 rad at
+// most, about the rounding that an fp32 result has anyway.
 #include "esp_paged.cuh"
 
 namespace esp {
@@ -19,7 +20,7 @@ __global__ void k_rope_table_paged(const __grid_constant__ RopeFreqs r, int pair
     if (i < pairs) table[i] = r.f[i];
 }
 
-// (A cos, A sin) of position p's angle.  (int32) of the upper word is the angle in 2^-31 half turns, in [-1, 1).
+// (A cos, A sin) of position p's angle.  (int32) of the upper word is the angle in 2^-31 half turns, in [-1, 1); the float keeps 24 bits of it.
 __device__ __forceinline__ float2 rope_turn(int p, uint64_t f, float amplitude) {
     const uint64_t turns = (uint64_t)(int64_t)p * f;
     float s, c;

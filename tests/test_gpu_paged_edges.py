@@ -298,3 +298,24 @@ def test_captured_without_naming_the_stream():
     graph.replay()
     torch.cuda.synchronize()
     _check_attention(b, q, out, None)
+
+# ================================================================ the angle of a position
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D", [64, 36])                   # wide accesses, and one element at a time
+def test_the_angle_is_off_by_its_rounding_to_fp32_at_most(D, interleaved):
+    """Pairs (1, 0) come out as (cos, sin): off by the angle's rounding (2^-26 of a turn), the table's (2^-31), and two roundings of the sine; the reference's frequency
+    in fp64 adds position * 2^-53 rad."""
+    cfg = P.rope_cfg(D, 500000.0, interleaved=interleaved)
+    pos = torch.randint(-2 ** 24, 2 ** 24, (4000,), generator=_gen(29), device="cuda", dtype=torch.int32)
+    x = torch.zeros(4000, 1, D, device="cuda")
+    first = torch.arange(0, D, 2) if interleaved else torch.arange(D // 2)
+    second = first + (1 if interleaved else D // 2)
+    x[..., first] = 1.0
+    out = torch.empty_like(x)
+    P.esp_qk_norm_rope(x, None, out, None, cfg, _rope_table(cfg), pos)
+    p = pos.cpu().numpy().astype(np.longdouble)
+    angle = p[:, None] * P.esp_rope_frequencies(cfg).astype(np.longdouble)
+    tol = 2 * np.pi * (2.0 ** -26 + 2.0 ** -31) + 2 * 2.0 ** -24 + np.abs(p.astype(np.float64))[:, None] * 2.0 ** -53
+    got = out[:, 0].double().cpu().numpy()
+    for at, f in ((first, np.cos), (second, np.sin)):
+        assert bool((np.abs(got[:, at.numpy()] - f(angle).astype(np.float64)) <= tol).all())
