@@ -7,7 +7,6 @@
 // for the whole tile, keys and values as ldmatrix gives them.  Weights go as two bf16 numbers, hi + lo (up to 8 heads: hi in rows 0-7 and lo in rows
 // 8-15 of one operand), so that they lose nothing against the output's own rounding; the tensor cores have the time.
 // The one new token sees the same positions in all rows: what it does not see is cut off the ends, its values are set to zero in registers.
-// An infinite value times hi + lo is no number (lo may be zero, or negative), so sums that are not finite are made good when a piece is finished.
 #include <string.h>
 
 #include "esp_attn_tc.cuh"
@@ -48,58 +47,18 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
     const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
     return *reinterpret_cast<const uint32_t*>(&b);
 }
-// hi + lo = the weights x, y to 16 bits
+// hi + lo = the weights x, y to 16 bits.  hi is cut off and lo taken of a weight one fp32 step larger, so that both are positive down to weights of 2^-103: an infinite value times
+// hi plus the same times lo is infinite.  (With hi rounded lo was zero or negative for many weights, a single key's 1 among them, and the sum no number.)
 __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
-    hi = pack(x, y);
-    lo = pack(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+    constexpr float UP = 1.f + 0x1p-23f;
+    hi = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+    lo = pack(fmaf(x, UP, -__uint_as_float(hi << 16)), fmaf(y, UP, -__uint_as_float(hi & 0xffff0000u)));
 }
 
-// Sums of a piece that are not finite: a dimension of the positions [p0, p1) that holds infinite values or values that are no numbers gets their sum, for all rows
-// (the token sees them in all; a row whose weights are no numbers keeps that in its sum of weights).  Lanes with the same c4 have the same dimensions and deal
-// the positions among themselves.  Nothing is read unless there is such a sum.
+// Registers for one block per SM, which is what shared memory allows; heads of 128 are left to the compiler (us, 64 sequences of 1k to 8k, bounded / not: 4 KV heads of 64
+// with 64 query heads 55.7 / 59.8, where it spilled for a second block; 8 of 128 with 32 149.7 / 147.9, 8 sequences of 32k 179 / 173).
 template <int D, bool G8>
-__device__ __forceinline__ void odd_values(const PagedAttnArgs& a, const Cursor& c, int p0, int p1, int lane, float (&o)[D / 8][4]) {
-    float all = 0.f;                                    // (row g shows it: every row sees the same positions)
-#pragma unroll
-    for (int n = 0; n < D / 8; ++n) all = fmaf(o[n][0], 0.f, fmaf(o[n][1], 0.f, all));
-    if (!__any_sync(0xffffffffu, all != 0.f)) return;
-    constexpr int NB = 8;                               // eight groups of dimensions at a time: the registers are full of sums
-#pragma unroll
-    for (int n0 = 0; n0 < D / 8; n0 += NB) {
-        float odd[NB][2];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) odd[n][0] = odd[n][1] = 0.f;
-#pragma unroll 1
-        for (int pos = p0 + (lane >> 2); pos < p1; pos += 8) {
-            const int index = page_index(a.pages, pos);
-            const int page = load_page(a.seq, a.pages, c.b, index);
-            if (page < 0) continue;
-            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(a.pages.v) + page * a.pages.page + (pos - index * a.pages.page_size) * a.pages.tok +
-                                     c.kvh * a.pages.head + (lane & 3) * 2 + n0 * 8;
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(v + n * 8));
-                if ((w & 0x7f80u) == 0x7f80u) odd[n][0] += __uint_as_float(w << 16);
-                if ((w & 0x7f800000u) == 0x7f800000u) odd[n][1] += __uint_as_float(w & 0xffff0000u);
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float x = odd[n][e];
-#pragma unroll
-                for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
-                if (x != 0.f) {
-                    o[n0 + n][e] = x;
-                    o[n0 + n][e + 2] = G8 ? 0.f : x;    // (the sums of lo, or those of row g + 8)
-                }
-            }
-    }
-}
-
-template <int D, bool G8>
-__global__ void __launch_bounds__(WARPS * 32, 1) k_paged_few(const __grid_constant__ FewParams p) {
+__global__ void __launch_bounds__(WARPS * 32, D == 64 ? 1 : 0) k_paged_few(const __grid_constant__ FewParams p) {
     constexpr int HALVES = D / 64, KEYS = STAGE_BYTES / (D * 4), NT = KEYS / 8, HALF_STAGE = STAGE_BYTES / 2;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -295,7 +254,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_paged_few(const __grid_consta
             if (ui < end) request();
         }
         if (!ok) break;
-        odd_values<D, G8>(a, c, max(lo, pc.c0 * KEYS), min(c.s.kv, (pc.c0 + pc.n) * KEYS), lane, o);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
