@@ -424,7 +424,9 @@ int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s) {
     a.pairs = 1;
     while (a.pairs < a.group) a.pairs *= 2;
     a.n_cta = n_sm * WARPS;
-    a.min_units = 2;        // one sequence of 4096 positions: 18 us with 1, 14.6 with 2, 16.5 with 4, 22 with 8
+    // Chunks of a worker at least (us in a graph with 1 / 2 / 4 / 8, 32/8 heads of 128): one sequence of 512 9.7 / 10.6 / 12.8 / 17.5, of 4096 16.4 / 13.1 / 14.1 / 18.4, of 16384
+    // 27.4 / 27.5 / 26.8 / 23.2; 4 of 1024 12.4 / 11.3 / 13.6 / 18.3; 16 of 512 16.0 / 15.9 / 13.9 / 18.6.  Fewer parts to join against fewer chunks behind one another.
+    a.min_units = 2;
     p.a = a;
     const int rc = a.D == 128 ? run_few<128>(p, s) : run_few<64>(p, s);
     return rc ? rc : launch_paged_merge_few(1, a, s);

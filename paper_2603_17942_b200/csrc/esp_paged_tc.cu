@@ -16,7 +16,8 @@
 // Roles: warps 0 and 2 TMA (keys and queries, values), warp 1 issues the products, warp 3 looks after the values, warps 4-7 and 8-11 softmax and
 // output of a subtile.  Every wait is bounded; one that runs out is recorded, the tensor memory is given back and the kernel returns.
 //
-// What bounds it: 2048 tokens behind 6144, 32/8 heads of 128, take 225 us, 1.07 PFLOP/s.  A chunk takes a subtile about 3500 cycles: 300 to load the
+// What bounds it: 2048 tokens behind 6144, 32/8 heads of 128, take 228 us over the first hundred calls at 1965 MHz, 1.05 PFLOP/s, and 250 to 259 in long rows, where the
+// power cap lowers the clock to 1.7 GHz.  A chunk takes a subtile about 3500 cycles: 300 to load the
 // scores of a half and find their maximum and 730 for its weights (512 of them the special-function unit's), twice, the last half's product and the next
 // scores 770, and the waits between the warps; the tensor cores have 1024 of them for each of the two subtiles, 55 to 60 %.  Built, correct and slower (us
 // for the same call): scores of 64 keys in two buffers per subtile, so that the softmax never waits for a product (276: products of 64 keys read the
@@ -81,7 +82,9 @@ __device__ __forceinline__ float max3_nan(float x, float y, float z) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
     return d;
 }
-// The weights of a row's scores of one step, as bf16 over the scores' columns; their sum.
+// The weights of a row's scores of one step, as bf16 over the scores' columns; their sum, of the weights before rounding.  bf16 is what one product with bf16 values takes: a
+// weight is off by 2^-8 of itself at most, an output by 0.0023 of the norm instead of the 0.0017 that its own rounding costs.  Two products with hi + lo, as single tokens
+// have them where memory is the bound, would be half as much tensor work again.
 __device__ __forceinline__ float weights(const uint32_t (&sv)[STEP], uint32_t s_addr, float scale_log2, float m_use) {
     const uint64_t scale2 = attn::pack2(scale_log2, scale_log2), neg_m2 = attn::pack2(-m_use, -m_use);
     uint64_t sum2[2] = {0, 0};
