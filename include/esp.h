@@ -378,7 +378,8 @@ typedef struct {
 int esp_rope_frequencies(const esp_rope_cfg* rope, double* out);
 
 /* Writes the table that the rotating operators read: the frequencies as 64-bit fractions of a turn, so that position times frequency is exact to
- * 2^-31 of a turn for any 32-bit position; the sine is taken of that angle rounded to fp32, within half a turn 2^-26 of a turn at most.  table [device], 16-byte aligned, esp_rope_table_bytes bytes; made once per configuration. */
+ * 2^-31 of a turn for any 32-bit position; the sine is taken of that angle rounded to fp32, within half a turn 2^-26 of a turn at most.
+ * table [device], 16-byte aligned, esp_rope_table_bytes bytes; made once per configuration. */
 int esp_rope_table_bytes(const esp_rope_cfg* rope, size_t* bytes_out);
 int esp_rope_table(const esp_rope_cfg* rope, void* table, size_t table_bytes, void* cuda_stream);
 
@@ -410,9 +411,9 @@ int esp_paged_append(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
  * chunks of keys or more to walk in all (chunks of 32 to 128 positions; seconds of work) writes nothing and records the capacity code in *status; one
  * sequence over 2^30 positions may be refused so from 2^30 chunks on.
  * What a token does not see does not reach its result: slots behind kv_len may hold anything, and an infinite or undefined value reaches
- * only the tokens that see it.  To them an infinite value makes its element of the result infinite (undefined with one of the other sign or one that is no number; where
- * its weight is below 2^-100 of the row's largest the element is infinite or undefined).  A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly);
- * the same call gives the same bits.
+ * only the tokens that see it.  To them an infinite value makes its element of the result infinite (undefined with one of the other sign or one
+ * that is no number; where its weight is below 2^-100 of the row's largest the element is infinite or undefined).
+ * A token's bits depend on the whole call (the keys are cut where the work of the batch divides evenly); the same call gives the same bits.
  * scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
 int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
 int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const uint64_t* anc,

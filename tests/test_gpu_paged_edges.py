@@ -65,6 +65,31 @@ def test_an_infinite_value_that_every_token_sees_stays_infinite(dtype, Hq, Hkv, 
     b.ok()
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 8, 2, 64), ("bf16", 32, 2, 64), ("bf16", 8, 2, 128), ("bf16", 16, 1, 128), ("bf16", 8, 2, 32), ("fp32", 8, 2, 64)])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("kv", [[300], [3000], [200] * 60])
+def test_an_infinite_value_of_a_small_weight(dtype, Hq, Hkv, D, n, kv):
+    """Keys whose logits are 90 below the others' in powers of two (the header's bound is 100): queries are 4, their keys -c with 4 c D scale log2(e) = 90 up to the rounding of
+    c, all other keys zero; before, between and behind the others."""
+    b = Batch([n] * len(kv), kv, 16, Hkv, D, dtype, seed=D, fill=0.0)
+    c = 90 / (4 * D ** 0.5 * math.log2(math.e))
+    want = torch.zeros(b.tokens, Hq, D, dtype=DT[dtype], device="cuda")
+    for s, t in enumerate(kv):
+        pg, sl = b.slots(s)
+        for d, p in enumerate((0, 1, 130, t // 2, t - n)):            # (every token sees them)
+            b.view(b.k)[pg[p], sl[p]] = -c
+            b.view(b.v)[pg[p], sl[p], :, d] = math.inf if d % 2 else -math.inf
+            want[s * n:(s + 1) * n, :, d] = math.inf if d % 2 else -math.inf
+        if n == 1:                                                     # (t - n is the token itself: left finite)
+            b.view(b.k)[pg[t - 1], sl[t - 1]] = 0.0
+            b.view(b.v)[pg[t - 1], sl[t - 1]] = 0.0
+            want[s, :, 4] = 0.0
+    q = torch.full((b.tokens, Hq, D), 4.0, dtype=DT[dtype], device="cuda")
+    out, _ = _attention(b, q)
+    assert torch.equal(out, want)
+    b.ok()
+
+
 # ================================================================ page tables with holes
 @pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 8, 2, 128), ("bf16", 16, 1, 64), ("fp32", 4, 2, 64), ("bf16", 3, 1, 32)])
 @pytest.mark.parametrize("page", [16, 64, 24, 5])
