@@ -419,6 +419,76 @@ int esp_paged_attention_scratch_bytes(int32_t n_q_heads, int32_t head_dim, size_
 int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const uint64_t* anc,
                         int32_t window, float scale, const esp_heads* out, float* lse, void* scratch, size_t scratch_bytes, void* cuda_stream);
 
+/* ---- what is left of a step over pages: who keeps its place in the cache, which tokens come next ---- */
+
+/* One 32-bit number for every slot and KV head of a cache: token s of page p of head h at p * page_stride + s * token_stride + h * head_stride (elements). */
+typedef struct {
+    void* data;        /* [device] */
+    int64_t page_stride, token_stride, head_stride;
+} esp_paged_slots;
+
+/* The attention that every cached position receives, summed over queries and over the query heads of a KV head h:
+ *   scores[j][h] = keep * scores[j][h] + sum over observed tokens i that see position j and heads e of h of exp(scale * q_ie k_jh - lse_ie)
+ * lse [device] [n_tokens][n_heads of q] fp32 is what esp_paged_attention gives for the same q, masks and scale, so that a token's weights add up to 1 per query
+ * head.  Observed are the last `last` new tokens of each sequence (0: all of them).  Masks (anc, window) as in esp_paged_attention.  scores fp32, in
+ * [0 .. kv_len) of each sequence that has new tokens: positions of the new tokens begin at zero whatever they hold, and with keep 0 nothing is read.  What a token does
+ * not see does not reach a score; an lse that is no number reaches what its token sees.
+ * The same call gives the same bits.  scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
+int esp_paged_key_weights_scratch_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
+int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const float* lse, const uint64_t* anc,
+                          int32_t window, float scale, int32_t last, float keep, const esp_paged_slots* scores, void* scratch, size_t scratch_bytes,
+                          void* cuda_stream);
+
+/* Cuts caches to their budgets.  A sequence with kv_len[b] > budget[b] keeps, in every KV head on its own, budget[b] of its slots: those of the latest `recent`
+ * positions and then those of the largest scores (a NaN counts as -infinity; of equal scores the lower slot stays; a score of +infinity holds a slot as well as being recent does).
+ * Kept slots at budget[b] and behind move, in order, into the dropped slots in front of it, also in order: keys, values, scores and positions.  Everything in front
+ * of kv_len_out[b] = min(kv_len[b], budget[b]) is then the cache; heads differ in which position a slot holds, which attention to a cache in front of all its
+ * queries does not ask for.  Slots from budget[b] on keep what they hold.
+ * positions (int32, may be NULL) tells which position of the sequence a slot holds, for the slots in front of settled[b]; a slot s behind them holds position
+ * seen[b] - kv_len[b] + s, as appended tokens do.  A call that cuts a sequence writes positions of all its slots and sets settled[b] to its budget, so a server starts with
+ * settled 0 and seen = tokens so far.  recent: positions from seen[b] - recent on.  positions NULL (then settled and seen are NULL): slots hold
+ * their own numbers as positions, which is so until a first cut.
+ * budget, settled, seen, kv_len_out [device] [batch]; kv_len_out may be batch->kv_len.  q_start and max_new are not read.  A sequence is left as it is, its kv_len copied and the
+ * batch's status set, if its kv_len is out of range, its budget negative or below `recent` while kv_len is above it, or it is above its budget with more positions
+ * than the scratch was made for (max_kv).  Cut sequences must not share pages.  scratch [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap. */
+int esp_paged_evict_scratch_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_kv, size_t* bytes_out);
+int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_paged_slots* scores, const esp_paged_slots* positions, const int32_t* seen,
+                    int32_t* settled, int32_t recent, const int32_t* budget, int32_t* kv_len_out, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
+/* Draws a token for each row of logits [n_rows][vocab] (dtype as in esp_model_cfg, rows row_stride elements apart) with the row's own settings, arrays [device]
+ * [n_rows], each of which may be NULL:
+ *   weights w_i = exp((logit_i - largest) / temperature); order: larger logits first, of equal ones the lower index;
+ *   kept are the first top_k of the order (top_k < 1: all); of those the shortest front whose weights reach top_p of what they all have (w_i stays while
+ *   the weights in front of it are below top_p times their sum; top_p >= 1: all; the first always stays); and of those the ones with w_i >= min_p (above 1: as 1);
+ *   token = the lowest index at which the kept weights, summed in the order of indices, exceed uniform times their sum.
+ * temperature 0 (NULL: 1): the first of the order.  uniform [device] [n_rows] is the row's random number, in [0, 1); larger ones draw the last kept token.
+ * tokens [device] [n_rows]; logprob [device] [n_rows] or NULL: the logarithm of the token's share of the kept weights.
+ * A logit that is no number counts as -infinity.  With an infinite largest logit only those equal to it have weight.  A row without a finite or +infinite logit, or with a
+ * setting that is no number, a temperature that is negative or infinite, or a uniform that is no number or negative, gets token -1 and a logprob that is no number.
+ * Sums and weights are taken in 64 bits: the draw is that of the formulas unless uniform or top_p meets a border to 1e-12.  The same row gives the same token whatever
+ * other rows there are.  scratch as esp_sample_scratch_bytes says, [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap. */
+typedef struct {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+} esp_sampling;
+int esp_sample_scratch_bytes(int32_t n_rows, int32_t vocab, size_t* bytes_out);
+int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits, int64_t row_stride, const esp_sampling* sampling, const float* uniform,
+               int32_t* tokens, float* logprob, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
+/* Verification of draft trees whose keys and values were appended to pages.  The new tokens of a sequence are the rows of its tree (at most ESP_MAX_ROWS): row 0 the root,
+ * parents[i] in 0 .. i - 1 the row that row i hangs on (any other value: on none, as the rows of probes), drafted[i] its token, chosen[i] the
+ * token that the model put behind it (esp_sample, or the largest logit; below 0: none).  From the root on, the next row is the lowest one that hangs on the present row and
+ * carries its chosen token.  The path's r rows become the cache: the keys and values of its i-th row move to position kv_len[b] - n + i, and
+ *   kv_len_out[b] = kv_len[b] - n + r,  n_out[b] = r (one less if the last row chose none),
+ *   tokens_out[b] = the tokens chosen along the path, rows_out[b] (or NULL) = its rows, rows of out_stride numbers, -1 behind the last.
+ * parents, drafted, chosen [device] [n_tokens]; the others [device] [batch] and [batch][out_stride], out_stride >= max_new.  A sequence without new tokens
+ * keeps its kv_len.  One that does not hold together, or has kv_len < n, keeps it too, with n_out 0, and is recorded in the batch's status.  A page that
+ * the table does not name where a row has to move is recorded, and the row's keys and values are lost.  kv_len_out must not be batch->kv_len. */
+int esp_paged_accept(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const int32_t* parents, const int32_t* drafted, const int32_t* chosen,
+                     int32_t* tokens_out, int32_t* rows_out, int32_t out_stride, int32_t* n_out, int32_t* kv_len_out, void* cuda_stream);
+
 /* The status word of a batch: waits for cuda_stream, copies *status [device] to *device_status_out [host] (may be NULL) and returns ESP_OK
  * if it is 0, ESP_E_DEVICE otherwise. */
 int esp_paged_status(const int32_t* status, void* cuda_stream, int32_t* device_status_out);

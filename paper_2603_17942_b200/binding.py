@@ -32,10 +32,12 @@ EXPORTS = ["esp_workspace_bytes", "esp_init", "esp_prefill", "esp_step", "esp_st
            "esp_tree_attention_scratch_bytes", "esp_tree_attention", "esp_tree_attention_status", "esp_tree_attention_static", "esp_gemm_scratch_bytes",
            "esp_gemm_bf16",
            "esp_rope_frequencies", "esp_rope_table_bytes", "esp_rope_table", "esp_qk_norm_rope", "esp_paged_append",
-           "esp_paged_attention_scratch_bytes", "esp_paged_attention", "esp_paged_status"]
+           "esp_paged_attention_scratch_bytes", "esp_paged_attention", "esp_paged_status",
+           "esp_paged_key_weights_scratch_bytes", "esp_paged_key_weights", "esp_paged_evict_scratch_bytes", "esp_paged_evict", "esp_sample_scratch_bytes", "esp_sample",
+           "esp_paged_accept"]
 
 __all__ = ["EspError", "esp_model_cfg", "esp_spec_cfg", "esp_weights", "esp_stats", "load_library", "model_cfg",
-           "spec_cfg", "Handle", "esp_heads", "esp_paged_cache", "esp_paged_batch", "esp_rope_cfg", "rope_cfg", "PagedCache", "PagedBatch", "ESP_ROPE_MAX_DIM", "ESP_MAX_ROWS", "ESP_MAX_PROBES", "ESP_MAX_KPRIME", "ESP_PREFILL_CHUNK", "ESP_MAX_UNREAD_STEPS", "ESP_STATIC_SCRATCH_BYTES", "EXPORTS", "LIB_PATH", "KINDS"] + EXPORTS
+           "spec_cfg", "Handle", "esp_heads", "esp_paged_cache", "esp_paged_batch", "esp_rope_cfg", "rope_cfg", "PagedCache", "PagedBatch", "PagedSlots", "esp_paged_slots", "esp_sampling", "ESP_ROPE_MAX_DIM", "ESP_MAX_ROWS", "ESP_MAX_PROBES", "ESP_MAX_KPRIME", "ESP_PREFILL_CHUNK", "ESP_MAX_UNREAD_STEPS", "ESP_STATIC_SCRATCH_BYTES", "EXPORTS", "LIB_PATH", "KINDS"] + EXPORTS
 
 
 class EspError(RuntimeError):
@@ -91,6 +93,14 @@ class esp_rope_cfg(ctypes.Structure):
                [(n, ctypes.c_float) for n in ("base", "factor", "low", "high", "amplitude")]
 
 
+class esp_paged_slots(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("page_stride", "token_stride", "head_stride")]
+
+
+class esp_sampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
 _lib = None
 _P, _I, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
 # (with the types declared once, a call hands over plain numbers: a call per layer has no time for wrapping each argument)
@@ -103,6 +113,13 @@ _ARGTYPES = {
     "esp_paged_attention_scratch_bytes": [_I, _I, _P],
     "esp_paged_attention": [_I, _P, _P, _P, _P, _I, _F, _P, _P, _P, ctypes.c_size_t, _P],
     "esp_paged_status": [_P, _P, _P],
+    "esp_paged_key_weights_scratch_bytes": [_I, _I, _I, _P],
+    "esp_paged_key_weights": [_I, _P, _P, _P, _P, _P, _I, _F, _I, _F, _P, _P, ctypes.c_size_t, _P],
+    "esp_paged_evict_scratch_bytes": [_I, _I, _I, _P],
+    "esp_paged_evict": [_P, _P, _P, _P, _P, _P, _I, _P, _P, _P, ctypes.c_size_t, _P],
+    "esp_sample_scratch_bytes": [_I, _I, _P],
+    "esp_sample": [_I, _I, _I, _P, ctypes.c_int64, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "esp_paged_accept": [_I, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P],
 }
 
 
@@ -522,6 +539,131 @@ def esp_paged_status(batch: PagedBatch, stream=None) -> int:
     st = ctypes.c_int32(0)
     _check(load_library().esp_paged_status(batch.status.data_ptr(), _stream(stream), ctypes.byref(st)), "esp_paged_status")
     return st.value
+
+
+# ---------------------------------------------------------------- what is left of a step over pages
+class PagedSlots:
+    """One number for every slot and KV head of a cache: scores (fp32) or positions (int32), [pages, kv_heads, page_size] (order "head") or
+    [pages, page_size, kv_heads] (order "token"), any strides.  Keeps the tensor alive."""
+
+    def __init__(self, data, order: str = "head"):
+        where = "PagedSlots"
+        _need(order in ("head", "token"), where, f"order {order!r}")
+        _need(data.dim() == 3 and str(data.dtype) in ("torch.float32", "torch.int32"), where, "[pages, kv_heads, page_size] fp32 or int32")
+        h, s = (1, 2) if order == "head" else (2, 1)
+        self.data, self.order = data, order
+        self.dtype, self.device = data.dtype, data.get_device()
+        self.sizes = (data.shape[0], data.shape[s], data.shape[h])
+        self.c = esp_paged_slots(data.data_ptr(), data.stride(0), data.stride(s), data.stride(h))
+        self.ref = ctypes.byref(self.c)
+
+
+def _slots(x, cache: PagedCache, dtype, where: str, name: str):
+    """esp_paged_slots of numbers that belong to the cache's slots; None: NULL."""
+    if x is None:
+        return None
+    c = cache.c
+    if x.dtype is not dtype or x.device != cache.device or x.sizes != (c.n_pages, c.page_size, c.n_kv_heads):
+        raise EspError(-8, f"{where} ({name}: {x.dtype} on device {x.device} for {x.sizes}; wanted {dtype} on device {cache.device} for "
+                           f"{(c.n_pages, c.page_size, c.n_kv_heads)} pages, slots, heads)")
+    return x.ref
+
+
+def _scratch(scratch, scratch_bytes: int, device: int, where: str) -> int:
+    if scratch.get_device() != device or scratch.numel() * scratch.element_size() < scratch_bytes or not scratch.is_contiguous():
+        raise EspError(-8, f"{where} (scratch: {scratch_bytes} dense bytes on device {device})")
+    return scratch.data_ptr()
+
+
+def esp_paged_key_weights_scratch_bytes(n_tokens: int, n_q_heads: int, head_dim: int) -> int:
+    out = ctypes.c_size_t(0)
+    where = "esp_paged_key_weights_scratch_bytes"
+    _check(load_library().esp_paged_key_weights_scratch_bytes(_i32(n_tokens, where, "n_tokens"), _i32(n_q_heads, where, "n_q_heads"), _i32(head_dim, where, "head_dim"),
+                                                              ctypes.byref(out)), where)
+    return out.value
+
+
+def esp_paged_key_weights(cache: PagedCache, batch: PagedBatch, q, lse, scores: PagedSlots, scratch, scratch_bytes: int, anc=None, window: int = 0, scale: float = 0.0,
+                          last: int = 0, keep: float = 1.0, stream=None):
+    """scores = keep * scores + the attention weights of the new tokens (the last `last` of each sequence; 0: all) at every cached position, summed over tokens and
+    query heads.  lse [tokens, heads] is what esp_paged_attention gave for the same q, masks and scale."""
+    where = "esp_paged_key_weights"
+    n, window, last = _i32(q.shape[0], where, "tokens"), _i32(window, where, "window"), _i32(last, where, "last")
+    dev, dt, d = cache.device, cache.dtype, cache.head_dim
+    _on_current_device(dev, where)
+    _need(batch.device == dev, where, "cache and batch on one device")
+    _check(load_library().esp_paged_key_weights(
+        n, cache.ref, batch.ref, _heads(q, n, d, dt, dev, where, "q"), _vector(lse, n * q.shape[1], (_torch.float32,), dev, where, "lse"),
+        _vector(anc, 2 * n, (_torch.int64, _torch.uint64), dev, where, "anc"), window, scale, last, keep, _slots(scores, cache, _torch.float32, where, "scores"),
+        _scratch(scratch, scratch_bytes, dev, where), scratch_bytes, _stream(stream)), where)
+
+
+def esp_paged_evict_scratch_bytes(batch: int, n_kv_heads: int, max_kv: int) -> int:
+    out = ctypes.c_size_t(0)
+    where = "esp_paged_evict_scratch_bytes"
+    _check(load_library().esp_paged_evict_scratch_bytes(_i32(batch, where, "batch"), _i32(n_kv_heads, where, "n_kv_heads"), _i32(max_kv, where, "max_kv"), ctypes.byref(out)),
+           where)
+    return out.value
+
+
+def esp_paged_evict(cache: PagedCache, batch: PagedBatch, scores: PagedSlots, budget, kv_len_out, scratch, scratch_bytes: int, recent: int = 0,
+                    positions: Optional[PagedSlots] = None, settled=None, seen=None, stream=None):
+    """Cuts every sequence that has more positions than its budget [batch] to it: the latest `recent` positions and those of the largest scores stay, moved together to the front.
+    positions, settled [batch] and seen [batch] go together (see esp.h): without them a slot's number is its position."""
+    where = "esp_paged_evict"
+    dev, b, recent = cache.device, batch.c.batch, _i32(recent, where, "recent")
+    _on_current_device(dev, where)
+    _need(batch.device == dev, where, "cache and batch on one device")
+    i32 = (_torch.int32,)
+    _check(load_library().esp_paged_evict(
+        cache.ref, batch.ref, _slots(scores, cache, _torch.float32, where, "scores"), _slots(positions, cache, _torch.int32, where, "positions"),
+        _vector(seen, b, i32, dev, where, "seen"), _vector(settled, b, i32, dev, where, "settled"), recent, _vector(budget, b, i32, dev, where, "budget"),
+        _vector(kv_len_out, b, i32, dev, where, "kv_len_out"), _scratch(scratch, scratch_bytes, dev, where), scratch_bytes, _stream(stream)), where)
+
+
+def esp_paged_accept(cache: PagedCache, batch: PagedBatch, parents, drafted, chosen, tokens_out, n_out, kv_len_out, rows=None, stream=None):
+    """Walks every sequence's draft tree along the chosen tokens and moves the path's keys and values to their positions.  parents, drafted, chosen [tokens];
+    tokens_out and rows [batch, at least max_new], n_out and kv_len_out [batch], all int32."""
+    where = "esp_paged_accept"
+    n, b, dev = _i32(parents.numel(), where, "tokens"), batch.c.batch, cache.device
+    _on_current_device(dev, where)
+    _need(batch.device == dev, where, "cache and batch on one device")
+    _need(tokens_out.dim() == 2 and tokens_out.shape[0] == b and (rows is None or rows.shape == tokens_out.shape), where, "tokens_out and rows [batch, rows]")
+    i32, width = (_torch.int32,), _i32(tokens_out.shape[1], where, "tokens_out")
+    _check(load_library().esp_paged_accept(
+        n, cache.ref, batch.ref, _vector(parents, n, i32, dev, where, "parents"), _vector(drafted, n, i32, dev, where, "drafted"),
+        _vector(chosen, n, i32, dev, where, "chosen"), _vector(tokens_out, b * width, i32, dev, where, "tokens_out"),
+        _vector(rows, b * width, i32, dev, where, "rows"), width, _vector(n_out, b, i32, dev, where, "n_out"),
+        _vector(kv_len_out, b, i32, dev, where, "kv_len_out"), _stream(stream)), where)
+
+
+_pack_sampling = struct.Struct("PPPP").pack        # the bytes of an esp_sampling
+assert struct.calcsize("PPPP") == ctypes.sizeof(esp_sampling)
+
+
+def esp_sample_scratch_bytes(n_rows: int, vocab: int) -> int:
+    out = ctypes.c_size_t(0)
+    where = "esp_sample_scratch_bytes"
+    _check(load_library().esp_sample_scratch_bytes(_i32(n_rows, where, "n_rows"), _i32(vocab, where, "vocab"), ctypes.byref(out)), where)
+    return out.value
+
+
+def esp_sample(logits, uniform, tokens, scratch, scratch_bytes: int, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None):
+    """Draws tokens [rows] (int32) from logits [rows, vocab] (fp32 or bf16, rows dense) with the random numbers uniform [rows].  temperature, top_p, min_p (fp32) and
+    top_k (int32) [rows], each of which may be None; logprob [rows] fp32 or None."""
+    where = "esp_sample"
+    dev = logits.get_device()
+    _on_current_device(dev, where)
+    _need(logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1), where, "logits [rows, vocab] fp32 or bf16, rows dense")
+    n, vocab = _i32(logits.shape[0], where, "rows"), _i32(logits.shape[1], where, "vocab")
+    f32 = (_torch.float32,)
+    # (a stride that nothing is reached by may be anything)
+    _check(load_library().esp_sample(
+        _DTYPES[logits.dtype], n, vocab, logits.data_ptr(), logits.stride(0) if n > 1 else 0,
+        _pack_sampling(_vector(temperature, n, f32, dev, where, "temperature") or 0, _vector(top_k, n, (_torch.int32,), dev, where, "top_k") or 0,
+                       _vector(top_p, n, f32, dev, where, "top_p") or 0, _vector(min_p, n, f32, dev, where, "min_p") or 0),
+        _vector(uniform, n, f32, dev, where, "uniform"), _vector(tokens, n, (_torch.int32,), dev, where, "tokens"), _vector(logprob, n, f32, dev, where, "logprob"),
+        _scratch(scratch, scratch_bytes, dev, where), scratch_bytes, _stream(stream)), where)
 
 
 # ---------------------------------------------------------------- convenience: a handle that keeps its tensors alive

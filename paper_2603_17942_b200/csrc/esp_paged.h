@@ -69,10 +69,60 @@ struct PagedAttnArgs {
     float2* part_ml;        // [n_cta][2][pairs] their (maximum in the log2 domain, sum)
 };
 
+// Where the 32-bit number of token s of page p of head h is: p * page + s * tok + h * head elements behind p; NULL: absent
+struct SlotsView {
+    void* p;
+    long long page, tok, head;
+};
+
+// Weights of cached positions (esp_paged_key_weights).  a: queries, pages, sequences, masks and the deal, as in the attention; rows = tokens of a tile.
+struct KeyWeightArgs {
+    PagedAttnArgs a;
+    const float* lse;       // [n_tokens][Hq]
+    SlotsView scores;
+    int32_t last;           // observed tokens of a sequence at most (0: all)
+    float keep;
+    float* part;            // [n_cta][2][keys of a chunk] sums of the pieces of chunks that several CTAs share
+};
+
+struct EvictArgs {
+    PagesView pages;
+    SlotsView scores, positions;
+    SeqTable seq;           // (q_start is not read)
+    const int32_t *seen, *budget;
+    int32_t *settled, *kv_out;
+    int32_t recent, Hkv, D;
+    int32_t list_cap;       // moves of a list at most
+    int32_t vec;            // elements of a row that can be moved at a time
+    int32_t* count;         // [batch * Hkv] moves
+    int32_t* len;           // [batch] kv_len from now on
+    int2* list;             // [batch * Hkv][list_cap] (from, to)
+};
+
+struct AcceptArgs {
+    PagesView pages;
+    SeqTable seq;
+    const int32_t *parents, *drafted, *chosen;
+    int32_t *tokens_out, *rows_out, *n_out, *kv_out;
+    int32_t out_stride, Hkv, D, vec;
+};
+
+struct SampleArgs {
+    const void* logits;
+    long long row_stride;
+    int32_t n_rows, vocab;
+    const float *temperature, *top_p, *min_p, *uniform;
+    const int32_t* top_k;
+    int32_t* tokens;
+    float* logprob;
+    int32_t chunk;          // logits of a row that each block of its cluster has
+};
+
 // Partials a launch may need at most: two tiles of 256 pairs for each of 148 SMs, or as much in smaller tiles.
 constexpr int PAGED_MAX_PAIRS = 256;
 constexpr int PAGED_MAX_SMS = 148;
 constexpr int PAGED_MAX_CTAS = PAGED_MAX_SMS * 8;
+constexpr int KEY_WEIGHT_KEYS = 256;      // keys of a chunk of the weights' kernels at most
 
 int launch_norm_rope(int dtype, const NormRopeArgs& a, cudaStream_t s);
 void launch_rope_table(const uint64_t* freq, int pairs, uint64_t* table, cudaStream_t s);
@@ -84,5 +134,9 @@ bool paged_few_supported(int dtype, const PagedAttnArgs& a);
 int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s);
 int launch_paged_merge_few(int dtype, const PagedAttnArgs& a, cudaStream_t s);   // tiles of at most 16 pairs
 int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s);
+int launch_key_weights_simt(int dtype, KeyWeightArgs w, int n_sm, cudaStream_t s);
+int launch_evict(int dtype, const EvictArgs& a, int n_sm, cudaStream_t s);
+int launch_accept(int dtype, const AcceptArgs& a, cudaStream_t s);
+int launch_sample(int dtype, SampleArgs a, int n_sm, cudaStream_t s);
 
 }  // namespace esp

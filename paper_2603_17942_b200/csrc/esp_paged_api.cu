@@ -82,6 +82,32 @@ PagesView pages_of(const esp_paged_cache* c) {
     p.n_pages = c->n_pages; p.page_size = c->page_size; p.page_shift = c->page_size <= (1 << 30) ? shift_of(c->page_size) : -1;
     return p;
 }
+// One number for each slot and head, two of them never in one place.
+int check_numbers(const esp_paged_slots* x, const esp_paged_cache* c) {
+    if (!x->data || off(x->data, 4) || x->page_stride < 0 || x->token_stride < 0 || x->head_stride < 0) return ESP_E_ARG;
+    if (x->page_stride > ((int64_t)1 << 40) || x->token_stride > ((int64_t)1 << 40) || x->head_stride > ((int64_t)1 << 40)) return ESP_E_ARG;
+    esp_paged_cache as = *c;
+    as.page_stride = x->page_stride; as.token_stride = x->token_stride; as.head_stride = x->head_stride;
+    as.head_dim = 1;
+    return check_slots(&as);
+}
+SlotsView numbers_of(const esp_paged_slots* x, const esp_paged_cache* c) {
+    SlotsView v;
+    v.p = x->data;
+    v.page = c->n_pages > 1 ? x->page_stride : 0;
+    v.tok = c->page_size > 1 ? x->token_stride : 0;
+    v.head = c->n_kv_heads > 1 ? x->head_stride : 0;
+    return v;
+}
+// Elements that a head's row can be moved by at a time: 16 bytes where every row lies on that, less where it does not.
+int row_vec(const esp_paged_cache* c) {
+    const int size = (int)elem_size(c->dtype);
+    int vec = 16 / size;
+    auto fits = [&](int64_t stride, int32_t n) { return n <= 1 || stride % vec == 0; };
+    while (vec > 1 && !(fits(c->page_stride, c->n_pages) && fits(c->token_stride, c->page_size) && fits(c->head_stride, c->n_kv_heads) && !off(c->k, vec * size) &&
+                        !off(c->v, vec * size))) vec /= 2;
+    return vec;
+}
 SeqTable seqs_of(const esp_paged_batch* b, const esp_paged_cache* c, int32_t n_tokens) {
     SeqTable t;
     t.q_start = b->q_start; t.kv_len = b->kv_len; t.table = b->page_table;
@@ -295,6 +321,133 @@ int esp_paged_attention(int32_t n_tokens, const esp_paged_cache* cache, const es
                    : paged_tc_supported(cache->dtype, a) ? launch_paged_tc(a, n_sm, s)
                                                          : launch_paged_simt(cache->dtype, a, n_sm, s);
     const cudaError_t e = cudaGetLastError();       // taken in either case: the next call's error is its own
+    return rc ? ESP_E_CUDA : cuda_ok(e);
+}
+
+// scratch layout: [CTAs][2][keys of a chunk] fp32
+int esp_paged_key_weights_scratch_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t head_dim, size_t* bytes_out) {
+    if (!bytes_out || n_q_heads < 1 || n_tokens < 0) return ESP_E_ARG;
+    if (head_dim != 32 && head_dim != 64 && head_dim != 128) return ESP_E_BADCFG;
+    *bytes_out = sizeof(float) * PAGED_MAX_SMS * 2 * KEY_WEIGHT_KEYS;
+    return ESP_OK;
+}
+
+int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const float* lse, const uint64_t* anc,
+                          int32_t window, float scale, int32_t last, float keep, const esp_paged_slots* scores, void* scratch, size_t scratch_bytes,
+                          void* cuda_stream) {
+    if (!cache || !batch || !q || !scores || !scratch || n_tokens < 0 || n_tokens > paged::KV_LIMIT || window < 0 || last < 0) return ESP_E_ARG;
+    if (!(scale >= 0.f) || !isfinite(scale) || !(keep >= 0.f) || !isfinite(keep) || (!lse && n_tokens > 0)) return ESP_E_ARG;
+    if (const int rc = check_cache(cache)) return rc;
+    if (const int rc = check_batch(batch)) return rc;
+    if (const int rc = check_heads(q, cache->dtype, n_tokens, cache->head_dim, false)) return rc;
+    if (const int rc = check_numbers(scores, cache)) return rc;
+    if (q->n_heads % cache->n_kv_heads || q->n_heads / cache->n_kv_heads > 64) return ESP_E_BADCFG;
+    if (anc && (batch->max_new > RT || window)) return ESP_E_ARG;
+    if (off(anc, 8) || off(lse, 4)) return ESP_E_ARG;
+    size_t need = 0;
+    if (const int rc = esp_paged_key_weights_scratch_bytes(n_tokens, q->n_heads, cache->head_dim, &need)) return rc;
+    if (scratch_bytes < need || off(scratch, 256)) return ESP_E_WORKSPACE;
+    if (n_tokens == 0 || batch->batch == 0 || batch->max_new == 0) return ESP_OK;
+    int n_sm = current_sm_count();
+    if (n_sm < 1) return ESP_E_CUDA;
+    if (n_sm > PAGED_MAX_SMS) n_sm = PAGED_MAX_SMS;
+    KeyWeightArgs w;
+    memset(&w, 0, sizeof(w));
+    PagedAttnArgs& a = w.a;
+    a.q = view_of(q, n_tokens);
+    a.pages = pages_of(cache);
+    a.seq = seqs_of(batch, cache, n_tokens);
+    a.anc = reinterpret_cast<const unsigned long long*>(anc);
+    a.Hq = q->n_heads; a.Hkv = cache->n_kv_heads; a.group = a.Hq / a.Hkv; a.D = cache->head_dim;
+    a.window = window > paged::KV_LIMIT ? 0 : window;
+    a.scale_log2 = (float)(1.4426950408889634 * (scale != 0.f ? (double)scale : 1.0 / sqrt((double)a.D)));
+    const size_t quad = 4 * elem_size(cache->dtype);
+    auto by4 = [&](const void* p, int64_t s0, int64_t s1, int64_t s2) {
+        return reinterpret_cast<uintptr_t>(p) % quad == 0 && s0 % 4 == 0 && s1 % 4 == 0 && s2 % 4 == 0;
+    };
+    a.vec = by4(a.q.p, a.q.tok, a.q.head, 0) && by4(a.pages.k, a.pages.page, a.pages.tok, a.pages.head);
+    w.lse = lse;
+    w.scores = numbers_of(scores, cache);
+    w.last = last;
+    w.keep = keep;
+    w.part = reinterpret_cast<float*>(scratch);
+    const int rc = launch_key_weights_simt(cache->dtype, w, n_sm, reinterpret_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = cudaGetLastError();
+    return rc ? ESP_E_CUDA : cuda_ok(e);
+}
+
+// scratch layout: [batch * heads] moves of a list, [batch] lengths, [batch * heads][max_kv / 2] moves
+namespace {
+size_t evict_front(int64_t batch, int64_t heads) { return ((size_t)(batch * heads + batch) * sizeof(int32_t) + 255) / 256 * 256; }
+}
+int esp_paged_evict_scratch_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_kv, size_t* bytes_out) {
+    if (!bytes_out || batch < 0 || batch > MAX_BATCH || n_kv_heads < 1 || n_kv_heads > MAX_HEADS || max_kv < 0 || max_kv > paged::KV_LIMIT) return ESP_E_ARG;
+    const __int128 bytes = (__int128)evict_front(batch, n_kv_heads) + (__int128)batch * n_kv_heads * ((max_kv + 1) / 2) * (int)sizeof(int2);
+    if (bytes >> 62) return ESP_E_ARG;
+    *bytes_out = (size_t)bytes;
+    return ESP_OK;
+}
+
+int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_paged_slots* scores, const esp_paged_slots* positions, const int32_t* seen,
+                    int32_t* settled, int32_t recent, const int32_t* budget, int32_t* kv_len_out, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+    if (!cache || !batch || !scores || recent < 0 || !positions != !seen || !positions != !settled) return ESP_E_ARG;
+    if (const int rc = check_cache(cache)) return rc;
+    if (const int rc = check_slots(cache)) return rc;
+    if (const int rc = check_batch(batch)) return rc;
+    if (const int rc = check_numbers(scores, cache)) return rc;
+    if (positions)
+        if (const int rc = check_numbers(positions, cache)) return rc;
+    if (off(seen, 4) || off(settled, 4) || off(budget, 4) || off(kv_len_out, 4)) return ESP_E_ARG;
+    if (batch->batch == 0) return ESP_OK;
+    if (!budget || !kv_len_out) return ESP_E_ARG;
+    const int64_t lists = (int64_t)batch->batch * cache->n_kv_heads;
+    if (lists > MAX_BATCH) return ESP_E_ARG;
+    const size_t front = evict_front(batch->batch, cache->n_kv_heads);
+    if (!scratch || scratch_bytes < front || off(scratch, 256)) return ESP_E_WORKSPACE;
+    const int n_sm = current_sm_count();
+    if (n_sm < 1) return ESP_E_CUDA;
+    EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    a.pages = pages_of(cache);
+    a.scores = numbers_of(scores, cache);
+    if (positions) a.positions = numbers_of(positions, cache);
+    a.seq = seqs_of(batch, cache, 0);
+    a.seen = seen; a.settled = settled; a.budget = budget; a.kv_out = kv_len_out;
+    a.recent = recent; a.Hkv = cache->n_kv_heads; a.D = cache->head_dim;
+    const size_t cap = (scratch_bytes - front) / sizeof(int2) / (size_t)lists;
+    a.list_cap = cap < (size_t)paged::KV_LIMIT ? (int32_t)cap : paged::KV_LIMIT;
+    a.vec = row_vec(cache);
+    a.count = reinterpret_cast<int32_t*>(scratch);
+    a.len = a.count + lists;
+    a.list = reinterpret_cast<int2*>(reinterpret_cast<char*>(scratch) + front);
+    const int rc = launch_evict(cache->dtype, a, n_sm, reinterpret_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = cudaGetLastError();
+    return rc ? ESP_E_CUDA : cuda_ok(e);
+}
+
+int esp_paged_accept(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const int32_t* parents, const int32_t* drafted, const int32_t* chosen,
+                     int32_t* tokens_out, int32_t* rows_out, int32_t out_stride, int32_t* n_out, int32_t* kv_len_out, void* cuda_stream) {
+    if (!cache || !batch || n_tokens < 0 || n_tokens > paged::KV_LIMIT) return ESP_E_ARG;
+    if (const int rc = check_cache(cache)) return rc;
+    if (const int rc = check_slots(cache)) return rc;
+    if (const int rc = check_batch(batch)) return rc;
+    if (batch->max_new > RT || out_stride < batch->max_new) return ESP_E_ARG;
+    if (off(parents, 4) || off(drafted, 4) || off(chosen, 4) || off(tokens_out, 4) || off(rows_out, 4) || off(n_out, 4) || off(kv_len_out, 4)) return ESP_E_ARG;
+    if (batch->batch == 0) return ESP_OK;
+    if ((n_tokens > 0 && (!parents || !drafted || !chosen)) || !tokens_out || !n_out || !kv_len_out) return ESP_E_ARG;
+    // (a block looks at the lengths of all sequences in front of its own)
+    const uintptr_t x = reinterpret_cast<uintptr_t>(kv_len_out), y = reinterpret_cast<uintptr_t>(batch->kv_len), bytes = (uintptr_t)batch->batch * 4;
+    if (x < y + bytes && y < x + bytes) return ESP_E_ARG;
+    AcceptArgs a;
+    memset(&a, 0, sizeof(a));
+    a.pages = pages_of(cache);
+    a.seq = seqs_of(batch, cache, n_tokens);
+    a.parents = parents; a.drafted = drafted; a.chosen = chosen;
+    a.tokens_out = tokens_out; a.rows_out = rows_out; a.n_out = n_out; a.kv_out = kv_len_out;
+    a.out_stride = out_stride; a.Hkv = cache->n_kv_heads; a.D = cache->head_dim;
+    a.vec = row_vec(cache);
+    const int rc = launch_accept(cache->dtype, a, reinterpret_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = cudaGetLastError();
     return rc ? ESP_E_CUDA : cuda_ok(e);
 }
 
