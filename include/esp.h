@@ -431,7 +431,8 @@ typedef struct {
  *   scores[j][h] = keep * scores[j][h] + sum over observed tokens i that see position j and heads e of h of exp(scale * q_ie k_jh - lse_ie)
  * lse [device] [n_tokens][n_heads of q] fp32 is what esp_paged_attention gives for the same q, masks and scale, so that a token's weights add up to 1 per query
  * head.  Observed are the last `last` new tokens of each sequence (0: all of them).  Masks (anc, window) as in esp_paged_attention.  scores fp32, in
- * [0 .. kv_len) of each sequence that has new tokens: positions of the new tokens begin at zero whatever they hold, and with keep 0 nothing is read.  What a token does
+ * [0, kv_len) of each sequence that has new tokens, the positions that no observed token sees among them; where the table names no page for these, they are passed over, and their
+ * keys are not read.  Positions of the new tokens begin at zero whatever they hold, and with keep 0 nothing is read.  What a token does
  * not see does not reach a score; an lse that is no number reaches what its token sees.
  * The same call gives the same bits.  scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
 int esp_paged_key_weights_scratch_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);

@@ -1,0 +1,244 @@
+// Weights of cached positions from a handful of (token, query head) pairs: bf16, heads of 64 or 128, up to 32 observed pairs of a sequence and KV head.
+//
+// Every cached key is read once, so memory bounds it, as in the attention of single tokens, and it is built the same way: each warp is a worker
+// with a share of the line of chunks, a ring of stages of its own that TMA fills, and no partner to wait for.  The products are m16n8k16 with the
+// keys as rows, so that what belongs to a key ends in four lanes of a quad: queries in registers for the whole sequence and head, weights and their sum over the
+// columns in registers, two shuffles, one number written for each key.  All tokens fit one tile, so no chunk has several owners and nothing is joined.
+#include <string.h>
+
+#include "esp_attn_tc.cuh"
+#include "esp_key_weights.cuh"
+
+namespace esp {
+
+namespace {
+
+using namespace tc;
+using namespace paged;
+
+constexpr int WARPS = 6, STAGES = 2, STAGE_BYTES = 16384;
+constexpr int SMEM = 1024 + WARPS * STAGES * STAGE_BYTES + 256;
+
+struct FewParams {
+    CUtensorMap map_k;    // [pages][heads][halves][slots][64], box 64 x box_rows x halves
+    KeyWeightArgs w;
+    int32_t box_shift;    // log2 of the slots of a box
+};
+
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int y, int w, int v, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %3, %5, %6}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(0), "r"(y), "r"(w), "r"(v)
+        : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+// NB: columns of the products in eights.
+template <int D, int NB>
+__global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_constant__ FewParams p) {
+    constexpr int HALVES = D / 64, KEYS = STAGE_BYTES / (D * 2), MT = KEYS / 16, MINE = MT / 4;      // a lane writes the keys of every fourth row of products
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned char* ring = smem + warp * STAGES * STAGE_BYTES;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + WARPS * STAGES * STAGE_BYTES) + warp * STAGES;
+    volatile int* s_abort = reinterpret_cast<volatile int*>(smem + WARPS * STAGES * STAGE_BYTES + WARPS * STAGES * 8) + warp;
+    const KeyWeightArgs& w = p.w;
+    const PagedAttnArgs& a = w.a;
+    const int worker = warp * gridDim.x + blockIdx.x;       // the first workers on SMs of their own
+    if (lane == 0) {
+        prefetch_tensormap(&p.map_k);
+        for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1);
+        *s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    pdl_launch_dependents();
+    Share share;
+    WCursor c;
+    if (!deal_keys<KEYS>(w, worker, lane, share, c)) return;
+    const uint32_t begin = share.begin(worker), end = share.begin(worker + 1);
+
+    // ---- requests, up to STAGES units ahead of the products
+    WCursor ci = c;
+    uint32_t ui = begin;
+    const int n_boxes = KEYS >> p.box_shift, box_bytes = (128 * HALVES) << p.box_shift;
+    int page = 0, slot = 0;
+    auto look_up = [&]() {              // the pages of unit ui, a lane per box
+        const int pos = ci.c * KEYS + ((lane & (n_boxes - 1)) << p.box_shift);
+        page = a.pages.n_pages;         // a page that there is not reads as zeros
+        slot = 0;
+        if (pos < ci.x.s.kv && pos + (1 << p.box_shift) > first_observed(w, ci.x)) {
+            const int index = page_index(a.pages, pos);
+            const int pg = load_page(a.seq, a.pages, ci.b, index);
+            if (pg >= 0) page = pg;
+            slot = pos - index * a.pages.page_size;
+        }
+    };
+    auto request = [&]() {
+        const uint32_t st = (ui - begin) % STAGES;
+        unsigned char* dst = ring + st * STAGE_BYTES;
+        if (lane == 0) mbar_expect_tx(&full[st], STAGE_BYTES);
+        for (int i = 0; i < n_boxes; ++i) {
+            const int pg = __shfl_sync(0xffffffffu, page, i), sl = __shfl_sync(0xffffffffu, slot, i);
+            if (lane == 0) tma_load_5d(dst + i * box_bytes, &p.map_k, sl, ci.kvh, pg, &full[st]);
+        }
+        __syncwarp();
+        if (++ui < end) {
+            next_chunk<KEYS>(w, ci);
+            look_up();
+        }
+    };
+    look_up();
+    for (int i = 0; i < STAGES && ui < end; ++i) request();
+
+    // ---- products
+    const int g = lane >> 2, c4 = lane & 3;
+    auto row_off = [&](int r) { return (uint32_t)((r >> p.box_shift) * box_bytes + (r & ((1 << p.box_shift) - 1)) * 128); };
+    auto chunk_off = [&](int ch) { return (uint32_t)(((ch >> 3) << (p.box_shift + 7)) + (((ch & 7) ^ (lane & 7)) << 4)); };
+    bool ok = true;
+    int b_of = -1, h_of = -1;            // whose queries the registers hold
+    uint32_t qb[D / 16][NB][2];
+    float minus[NB][2];                  // -lse in the log2 domain
+    uint32_t valid = 0;
+    for (uint32_t u = begin; u < end; ++u) {
+        const Seq& s = c.x.s;
+        const int L = s.kv - s.n, p0 = c.c * KEYS, pairs = (s.n - c.x.i0) * a.group;
+        if (c.b != b_of || c.kvh != h_of) {
+            b_of = c.b;
+            h_of = c.kvh;
+            valid = 0;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int pr = nb * 8 + g, row = pr / a.group;
+                const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + out_offset(a.q, s.start + c.x.i0 + row, c.kvh * a.group + pr - row * a.group) + c4 * 2;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    qb[kk][nb][0] = qb[kk][nb][1] = 0;
+                    if (pr < pairs) {
+                        qb[kk][nb][0] = __ldg(reinterpret_cast<const uint32_t*>(q + kk * 16));
+                        qb[kk][nb][1] = __ldg(reinterpret_cast<const uint32_t*>(q + kk * 16 + 8));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int col = nb * 8 + c4 * 2 + e, r = col / a.group;
+                    minus[nb][e] = 0.f;
+                    if (col < pairs) {
+                        minus[nb][e] = __ldg(w.lse + (size_t)(s.start + c.x.i0 + r) * a.Hq + c.kvh * a.group + col - r * a.group) * -1.4426950408889634f;
+                        valid |= 1u << (2 * nb + e);
+                    }
+                }
+            }
+        }
+        // the places of this lane's scores, and what they hold, while the keys are on their way
+        float *to[MINE][2], old[MINE][2];
+#pragma unroll
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int pos = p0 + (m * 4 + c4) * 16 + r * 8 + g;
+                to[m][r] = pos < s.kv ? score_at(w, c, pos) : nullptr;
+                old[m][r] = to[m][r] && has_old(w, s, pos) ? w.keep * *to[m][r] : 0.f;
+            }
+        const uint32_t st = (u - begin) % STAGES;
+        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], ((u - begin) / STAGES) & 1, s_abort))) { ok = false; break; }
+        const uint32_t k_addr = smem_u32(ring + st * STAGE_BYTES);
+        // a chunk that some token does not see as a whole
+        const bool edge = p0 + KEYS > (a.anc ? L : L + c.x.i0 + 1) || (a.window > 0 && p0 < L + s.n - a.window);
+        float sum[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float x[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) x[nb][0] = x[nb][1] = x[nb][2] = x[nb][3] = 0.f;
+            const uint32_t row = k_addr + row_off(mt * 16 + (lane & 15));
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                uint32_t k[4];
+                ldsm4(k, row + chunk_off(kk * 2 + (lane >> 4)));
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) attn::mma16816(x[nb], k[0], k[1], k[2], k[3], qb[kk][nb][0], qb[kk][nb][1]);
+            }
+            sum[mt][0] = sum[mt][1] = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bool in = (valid >> (2 * nb + (e & 1))) & 1;
+                    if (edge && in) {
+                        const int col = nb * 8 + c4 * 2 + (e & 1), i = c.x.i0 + col / a.group;
+                        in = sees(row_mask(a, s, i), p0 + mt * 16 + (e >> 1) * 8 + g, L, s.kv);
+                    }
+                    const float y = attn::ex2_approx(fmaf(x[nb][e], a.scale_log2, minus[nb][e & 1]));
+                    sum[mt][e >> 1] += in ? y : 0.f;
+                }
+        }
+        __syncwarp();                   // every lane has read the stage
+        if (ui < end) request();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                sum[mt][r] += __shfl_xor_sync(0xffffffffu, sum[mt][r], 1);
+                sum[mt][r] += __shfl_xor_sync(0xffffffffu, sum[mt][r], 2);
+            }
+#pragma unroll
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float x = sum[m * 4][r];
+#pragma unroll
+                for (int q = 1; q < 4; ++q) x = c4 == q ? sum[m * 4 + q][r] : x;
+                if (to[m][r]) *to[m][r] = old[m][r] + x;
+            }
+        if (u + 1 < end) next_chunk<KEYS>(w, c);
+    }
+    if (!ok) {
+        if (lane == 0) set_error(a.seq.status, DEV_E_WAIT_TIMEOUT);
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);    // let copies in flight land before shared memory goes away
+    }
+}
+
+int observed_pairs(const KeyWeightArgs& w) {
+    const long long tokens = w.last > 0 && w.last < w.a.seq.max_new ? w.last : w.a.seq.max_new, pairs = tokens * w.a.group;
+    return pairs > 1024 ? 1024 : (int)pairs;
+}
+
+template <int D, int NB>
+int run(const FewParams& p, cudaStream_t s) {
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_key_weights_few<D, NB>), SMEM)) return -1;
+    k_key_weights_few<D, NB><<<p.w.a.n_cta / WARPS, WARPS * 32, SMEM, s>>>(p);
+    return 0;
+}
+
+}  // namespace
+
+bool key_weights_few_supported(int dtype, const KeyWeightArgs& w) {
+    int box = 0;
+    const PagedAttnArgs& a = w.a;
+    // (a lane reads two elements of a query at a time)
+    return dtype == 1 && (a.D == 64 || a.D == 128) && observed_pairs(w) <= 32 && paged_tma_pages(a, STAGE_BYTES / (a.D * 2), &box) &&
+           reinterpret_cast<uintptr_t>(a.q.p) % 4 == 0 && a.q.tok % 2 == 0 && a.q.head % 2 == 0;
+}
+
+int launch_key_weights_few(KeyWeightArgs w, int n_sm, cudaStream_t s) {
+    FewParams p;
+    memset(&p, 0, sizeof(p));
+    PagedAttnArgs& a = w.a;
+    int box = 0;
+    if (!paged_tma_pages(a, STAGE_BYTES / (a.D * 2), &box) || paged_page_map5(&p.map_k, a, a.pages.k, box)) return -1;
+    p.box_shift = shift_of(box);
+    const int pairs = observed_pairs(w);
+    a.rows = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;       // one tile
+    a.rows_shift = shift_of(a.rows);
+    a.n_cta = n_sm * WARPS;
+    a.min_units = 1;
+    p.w = w;
+    if (a.D == 128) return pairs <= 8 ? run<128, 1>(p, s) : (pairs <= 16 ? run<128, 2>(p, s) : run<128, 4>(p, s));
+    return pairs <= 8 ? run<64, 1>(p, s) : (pairs <= 16 ? run<64, 2>(p, s) : run<64, 4>(p, s));
+}
+
+}  // namespace esp

@@ -174,8 +174,13 @@ int launch_key_weights_simt(int dtype, KeyWeightArgs w, int n_sm, cudaStream_t s
     int rc;
     if (dtype == 0) rc = a.D == 32 ? run<float, 32>(w, s) : (a.D == 64 ? run<float, 64>(w, s) : run<float, 128>(w, s));
     else rc = a.D == 32 ? run<__nv_bfloat16, 32>(w, s) : (a.D == 64 ? run<__nv_bfloat16, 64>(w, s) : run<__nv_bfloat16, 128>(w, s));
-    if (rc || a.n_cta < 2) return rc;
-    return launch_k(k_key_weights_join<CK>, dim3(a.n_cta - 1), dim3(CK), 0, s, true, w) != cudaSuccess;
+    return rc ? rc : launch_key_weights_join(w, CK, s);
+}
+
+int launch_key_weights_join(const KeyWeightArgs& w, int keys, cudaStream_t s) {
+    if (w.a.n_cta < 2) return 0;
+    const dim3 grid(w.a.n_cta - 1), block(keys);
+    return (keys == CK ? launch_k(k_key_weights_join<CK>, grid, block, 0, s, true, w) : launch_k(k_key_weights_join<KEY_WEIGHT_KEYS>, grid, block, 0, s, true, w)) != cudaSuccess;
 }
 
 }  // namespace esp

@@ -1,6 +1,8 @@
 // Operators over a paged key/value cache: what their kernels are given, and the launches behind the C entry points.
 #pragma once
 
+#include <cuda.h>
+
 #include "esp_common.cuh"
 
 namespace esp {
@@ -134,6 +136,13 @@ bool paged_few_supported(int dtype, const PagedAttnArgs& a);
 int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s);
 int launch_paged_merge_few(int dtype, const PagedAttnArgs& a, cudaStream_t s);   // tiles of at most 16 pairs
 int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s);
+int paged_page_map5(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows);      // [pages][heads][halves][slots][64], box 64 x box_rows x halves
+int paged_page_map(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows);       // [pages][heads][slots][D], box 64 x box_rows
+int launch_key_weights_join(const KeyWeightArgs& w, int keys, cudaStream_t s);
+bool key_weights_few_supported(int dtype, const KeyWeightArgs& w);
+int launch_key_weights_few(KeyWeightArgs w, int n_sm, cudaStream_t s);
+bool key_weights_tc_supported(int dtype, const KeyWeightArgs& w);
+int launch_key_weights_tc(KeyWeightArgs w, int n_sm, cudaStream_t s);
 int launch_key_weights_simt(int dtype, KeyWeightArgs w, int n_sm, cudaStream_t s);
 int launch_evict(int dtype, const EvictArgs& a, int n_sm, cudaStream_t s);
 int launch_accept(int dtype, const AcceptArgs& a, cudaStream_t s);

@@ -385,7 +385,9 @@ int run_merge_few(const PagedAttnArgs& a, cudaStream_t s) {
     return launch_k(k_paged_merge_few<T, D>, dim3(a.n_cta - 1, (a.pairs * (D / 4) + MERGE_ITEMS - 1) / MERGE_ITEMS), dim3(MERGE_WARPS * 32), 0, s, true, a) != cudaSuccess;
 }
 
-int page_map5(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows) {
+}  // namespace
+
+int paged_page_map5(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows) {
     EncodeFn enc = get_encode();
     if (!enc) return -1;
     auto bytes = [&](long long stride) { return (cuuint64_t)(stride > 0 ? stride * 2 : a.D * 2); };      // (a dimension of one element: any stride)
@@ -396,8 +398,6 @@ int page_map5(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int bo
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? 0 : -1;
 }
-
-}  // namespace
 
 int launch_paged_merge_few(int dtype, const PagedAttnArgs& a, cudaStream_t s) {
     if (a.n_cta < 2) return 0;
@@ -417,7 +417,7 @@ int launch_paged_few(PagedAttnArgs a, int n_sm, cudaStream_t s) {
     memset(&p, 0, sizeof(p));
     int box = 0;
     if (!paged_tma_pages(a, STAGE_BYTES / (a.D * 4), &box)) return -1;
-    if (page_map5(&p.map_k, a, a.pages.k, box) || page_map5(&p.map_v, a, a.pages.v, box)) return -1;
+    if (paged_page_map5(&p.map_k, a, a.pages.k, box) || paged_page_map5(&p.map_v, a, a.pages.v, box)) return -1;
     p.box_shift = shift_of(box);
     a.rows = 1;
     a.rows_shift = 0;
