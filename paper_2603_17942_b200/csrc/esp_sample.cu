@@ -4,11 +4,13 @@
 //   order      larger logits first, of equal ones the lower index: a 32-bit key of the logit (its bits in the order of the values) and the index.  top-k, top-p and min-p each
 //              keep a front of that order.
 //   weights    exp in 64 bits, summed in 64 bits in a fixed order, wherever a sum decides.
-//   list       A histogram of (largest - logit) / temperature in steps of 1/24 octave (elements, or their weights to 2e-4) says behind which bin the front ends at the latest.  What
-//              lies in front of that, a few dozen to a few hundred elements, goes to the first block, the others are done.  It sorts them, takes exact sums along the order,
-//              cuts, and finds the token by searching the index at which the kept weights exceed uniform times their sum.
-//   otherwise  (fronts of thousands of elements, and rows without a limit): the last element of each front by histograms that close in on it, then sums of
-//              the kept weights by stretches in the order of indices, the stretch in which uniform * total lies, the element.
+//   list       A value that the front does not reach below is found first.  For top-k, of the largest logits of each thread the k-th one: k elements are not below it, and of elements
+//              that lie anywhere hardly more.  For top-p, from a histogram of the weights along (largest - logit) / temperature, in steps of 1/24 octave.  For min-p it
+//              is given.  What lies above, a few dozen to a few hundred elements, goes to the first block, the others are done.  It sorts them, takes exact sums along the
+//              order, cuts, and finds the lowest index at which the kept weights exceed uniform times their sum.
+//   long front of top-p: exact sums up to the bin that holds its end, that bin's elements sorted by the first block for the end itself, and the draw
+//              by sums of the kept weights over stretches in the order of indices, the stretch in which uniform * total lies, the element.
+//   the rest   (long fronts of top-k, thousands of equal logits): the last element of a front by histograms that close in on it; then the draw as above.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -24,7 +26,8 @@ using paged::warp_scan_u32;
 
 constexpr int NT = 512, NW = NT / 32;
 constexpr int BINS = NT;                  // of a histogram, a thread for each
-constexpr float STEPS = 24.f;             // bins of an octave of weights: 21 octaves
+constexpr float STEPS = 24.f;             // fine bins of an octave of weights: 21 octaves
+constexpr int FINE = 256, COARSE = 8;     // wide bins: that many fine ones, then as wide as eight of them: 95 octaves
 constexpr int MAX_CL = 8;                 // blocks of a cluster at most
 constexpr int LIST = 2048;                // elements that are sorted at most
 constexpr int SMEM_ROW = 160 * 1024;      // bytes of a row that a block keeps at most
@@ -64,11 +67,15 @@ struct Shared {
     unsigned long long list[LIST];        // the first block's
     double list_w[LIST];
     uint32_t n_list;
-    double warp_sum[NW], warp_sum2[NW];
+    uint32_t n_of[MAX_CL];                // elements of each block's list
+    double warp_sum[NW], warp_sum2[NW], kept_sum;
+    int kept;
     float warp_f[NW];
     unsigned warp_count[NW];
+    uint32_t warp_lo[NW], warp_hi[NW];
     unsigned long long answer;
-    int bin;
+    int verdict;
+    int bin, end_bin;
     unsigned above;
 };
 
@@ -100,8 +107,15 @@ __device__ __forceinline__ double weight(const Row& r, const double* tab, float 
     const double w = __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
     return t > -60.0 * TAB && x != -INFINITY ? w : 0.0;
 }
-// Bins from the largest logit down; BINS - 1: somewhere behind.
+// Fine bins from the largest logit down; BINS - 1: somewhere behind.
 __device__ __forceinline__ float depth_of(const Row& r, float x) { return x == r.M ? 0.f : fminf((r.M - x) * r.steps, (float)(BINS - 1)); }
+
+// The same with a range four times as far
+__device__ __forceinline__ int wide_bin(const Row& r, float x) {
+    const float d = x == r.M ? 0.f : fminf((r.M - x) * r.steps, (float)(BINS * COARSE));
+    return d < (float)FINE ? (int)d : min(FINE + (int)((d - (float)FINE) * (1.f / COARSE)), BINS - 1);
+}
+__device__ __forceinline__ float wide_end(int bin) { return bin < FINE ? (float)(bin + 1) : (float)(FINE + (bin + 1 - FINE) * COARSE); }
 
 template <typename T> struct Raw;
 template <> struct Raw<float> {
@@ -125,6 +139,224 @@ template <> struct Raw<__nv_bfloat16> {
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
+
+// Sorts the block's list along the order and puts the elements' weights beside it.  Called by all threads.
+__device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __syncthreads();
+    if (count <= 128) {
+        // each element counts the ones in front of it
+        unsigned long long v = ~0ull;
+        int rank = 0;
+        if (tid < count) {
+            v = sm.list[tid];
+#pragma unroll 4
+            for (int j = 0; j < count; ++j) rank += sm.list[j] < v;
+        }
+        __syncthreads();
+        if (tid < count) {
+            sm.list[rank] = v;
+            sm.list_w[rank] = weight(r, sm.tab, rank_value(v));
+        }
+        __syncthreads();
+        return;
+    }
+    // by bins of keys, then each element counts the ones in front of it in its bin
+    constexpr int PER = LIST / NT;
+    unsigned long long v[PER];
+    uint32_t lo = ~0u, hi = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (e * NT + tid < count) {
+            v[e] = sm.list[e * NT + tid];
+            const uint32_t k = (uint32_t)(v[e] >> 32);
+            lo = min(lo, k);
+            hi = max(hi, k);
+        }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) { sm.warp_lo[warp] = lo; sm.warp_hi[warp] = hi; }
+    sm.hist[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) { lo = min(lo, sm.warp_lo[w]); hi = max(hi, sm.warp_hi[w]); }
+    int width = 0;
+    while (((hi - lo) >> width) >= BINS) ++width;
+    auto bin = [&](unsigned long long x) { return ((uint32_t)(x >> 32) - lo) >> width; };
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (e * NT + tid < count) atomicAdd(&sm.hist[bin(v[e])], 1u);
+    __syncthreads();
+    const unsigned mine = sm.hist[tid], in = warp_scan_u32(mine, lane), most = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 31) { sm.warp_count[warp] = in; sm.warp_hi[warp] = most; }
+    __syncthreads();
+    unsigned begin = in - mine, largest = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        begin += w < warp ? sm.warp_count[w] : 0u;
+        largest = max(largest, sm.warp_hi[w]);
+    }
+    sm.all[tid] = begin;
+    sm.hist[tid] = begin;
+    __syncthreads();
+    if (largest <= 512) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (e * NT + tid < count) sm.list[atomicAdd(&sm.hist[bin(v[e])], 1u)] = v[e];
+        __syncthreads();
+        int rank[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (e * NT + tid < count) {
+                const int j0 = sm.all[bin(v[e])], j1 = sm.hist[bin(v[e])];
+                int at = j0;
+#pragma unroll 4
+                for (int j = j0; j < j1; ++j) at += sm.list[j] < v[e];
+                rank[e] = at;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (e * NT + tid < count) {
+                sm.list[rank[e]] = v[e];
+                sm.list_w[rank[e]] = weight(r, sm.tab, rank_value(v[e]));
+            }
+    } else {
+        int size = 256;
+        while (size < count) size *= 2;
+        for (int i = count + tid; i < size; i += NT) sm.list[i] = ~0ull;
+        __syncthreads();
+        for (int s = 2; s <= size; s *= 2)
+            for (int d = s / 2; d > 0; d /= 2) {
+                for (int i = tid; i < size / 2; i += NT) {
+                    const int x = 2 * i - (i & (d - 1)), y = x + d;
+                    const unsigned long long p = sm.list[x], q = sm.list[y];
+                    if ((p > q) == ((x & s) == 0)) { sm.list[x] = q; sm.list[y] = p; }
+                }
+                __syncthreads();
+            }
+        for (int i = tid; i < count; i += NT) sm.list_w[i] = weight(r, sm.tab, rank_value(sm.list[i]));
+    }
+    __syncthreads();
+}
+
+// What the first block does with a list of `count` elements that holds the front: sorts it, cuts it and draws.  S: the weights of the whole row that top_p goes by (below 0: those of
+// the first top_k).
+__device__ __forceinline__ void from_list(const Row& r, Shared& sm, const SampleArgs& a, int row, int count, int top_k, float top_p, double S, float uniform) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    sort_list(r, sm, count);
+
+    // ---- exact sums along it, four neighbours a lane, and where the front ends
+    const int n_k = min(count, top_k);
+    const bool one_warp = n_k <= 128;
+    if (!one_warp || warp == 0) {
+        double w[4], run = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = tid * 4 + e;
+            w[e] = i < n_k ? sm.list_w[i] : 0.0;
+            run += w[e];
+        }
+        const double in = warp_scan_f64(run, lane);
+        double upto = in - run, all = __shfl_sync(0xffffffffu, in, 31);
+        if (!one_warp) {
+            if (lane == 31) sm.warp_sum2[warp] = in;
+            __syncthreads();
+            all = 0.0;
+            double before = 0.0;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                if (k == warp) before = all;
+                all += sm.warp_sum2[k];
+            }
+            upto += before;
+        }
+        const double theta = top_p < 1.f ? (double)top_p * (S < 0.0 ? all : S) : INFINITY;
+        int stay = 0;
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = tid * 4 + e;
+            const bool in_front = i < n_k && (i == 0 || (upto < theta && w[e] >= r.min_p));
+            stay += in_front;
+            upto += w[e];
+            if (in_front) sum += w[e];
+        }
+        stay = __reduce_add_sync(0xffffffffu, stay);
+        sum = warp_sum_f64(sum);
+        if (one_warp) {
+            if (lane == 0) { sm.kept = stay; sm.kept_sum = sum; }
+        } else if (lane == 0) { sm.warp_count[warp] = stay; sm.warp_sum[warp] = sum; }
+    }
+    __syncthreads();
+    int kept = 0;
+    double W = 0.0;
+    if (one_warp) {
+        kept = sm.kept;
+        W = sm.kept_sum;
+    } else {
+#pragma unroll
+        for (int k = 0; k < NW; ++k) { kept += sm.warp_count[k]; W += sm.warp_sum[k]; }
+    }
+    const double target = (double)uniform * W;
+
+    // ---- the smallest index at which the kept weights in the order of indices exceed the target; with a target that nothing exceeds, the last kept one with weight
+    if (kept <= 128) {
+        // each element adds up those that its index has in front of it.  (0xffffffff: no candidate)
+        if (warp >= 4) return;
+        if (warp == 0 || warp * 32 < kept) {
+            const int mine = tid < kept ? (int)(uint32_t)sm.list[tid] : -1;
+            double upto = 0.0;
+#pragma unroll 4
+            for (int j = 0; j < kept; ++j)
+                if ((int)(uint32_t)sm.list[j] <= mine) upto += sm.list_w[j];
+            const bool has = tid < kept && sm.list_w[tid] > 0.0;
+            const unsigned over = __reduce_min_sync(0xffffffffu, has && upto > target ? (unsigned)mine : ~0u);
+            const unsigned last = __reduce_max_sync(0xffffffffu, has ? (unsigned)mine + 1u : 0u);
+            if (lane == 0) { sm.all[warp] = over; sm.all[4 + warp] = last; }
+        } else if (lane == 0) { sm.all[warp] = ~0u; sm.all[4 + warp] = 0u; }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        unsigned over = ~0u, last = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { over = min(over, sm.all[k]); last = max(last, sm.all[4 + k]); }
+        const unsigned token = over != ~0u ? over : last - 1u;
+        if (tid < kept && (uint32_t)sm.list[tid] == token) {
+            a.tokens[row] = (int)token;
+            if (a.logprob) a.logprob[row] = (float)log(sm.list_w[tid] / W);
+        }
+        return;
+    }
+    // the range of indices in NW parts at a time: a warp sums up to each border
+    int lo = -1, hi = a.vocab - 1;                                  // the sum up to lo does not exceed the target; up to hi it does, or nothing does
+    while (hi - lo > 1) {
+        const int part = (hi - lo - 1) / NW + 1, at = min(hi, lo + (warp + 1) * part);
+        double t = 0.0;
+        for (int i = lane; i < kept; i += 32)
+            if ((int)(uint32_t)sm.list[i] <= at) t += sm.list_w[i];
+        const bool over = at >= hi || warp_sum_f64(t) > target;
+        __syncthreads();
+        if (lane == 0) sm.warp_count[warp] = over;
+        __syncthreads();
+        const uint32_t overs = __ballot_sync(0xffffffffu, lane < NW && sm.warp_count[lane & (NW - 1)]);
+        const int f = __ffs(overs) - 1;                             // (the last border is always over)
+        const int new_hi = min(hi, lo + (f + 1) * part);
+        lo = min(hi - 1, lo + f * part);
+        hi = new_hi;
+    }
+    if (warp == 0) {
+        if (!(W > target)) {
+            unsigned last = 0;
+            for (int i = lane; i < kept; i += 32)
+                if (sm.list_w[i] > 0.0) last = max(last, (uint32_t)sm.list[i]);
+            hi = (int)__reduce_max_sync(0xffffffffu, last);
+        }
+        for (int i = lane; i < kept; i += 32)
+            if ((int)(uint32_t)sm.list[i] == hi) {
+                a.tokens[row] = hi;
+                if (a.logprob) a.logprob[row] = (float)log(sm.list_w[i] / W);
+            }
+    }
+}
 
 template <typename T, bool RESIDENT>
 __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArgs a) {
@@ -162,12 +394,14 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
     const bool bad = !(temperature >= 0.f) || isinf(temperature) || !(uniform >= 0.f) || top_p != top_p || min_p != min_p;
     const bool use_k = top_k >= 1 && top_k < a.vocab, use_p = top_p < 1.f, use_m = min_p > 0.f;
 
+    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
+    if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
+    sm.hist[tid] = 0;
+    cluster.barrier_arrive();             // (before anybody looks into another block's shared memory, all have to have started)
+
     // ---- the largest
     unsigned long long best = ~0ull;
-#pragma unroll 4
-    for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-        float x[VEC];
-        fetch(i, x);
+    auto take = [&](int i, float (&x)[VEC]) {
         if (RESIDENT) kept_row[i / VEC] = Raw<T>::pack(x);
         float m = x[0];
 #pragma unroll
@@ -178,19 +412,40 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
             for (int e = VEC - 2; e >= 0; --e) at = x[e] == m ? e : at;
             best = rank_of(m, first + i + at);
         }
+    };
+    constexpr int AHEAD = 8;              // loads of a lane under way
+    int i_load = w0 + lane * VEC;
+    if (aligned)
+        for (; i_load + (AHEAD - 1) * STRIDE + VEC <= w1; i_load += AHEAD * STRIDE) {
+            uint4 u[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) u[j] = __ldg(reinterpret_cast<const uint4*>(logits + first + i_load + j * STRIDE));
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                float x[VEC];
+                Raw<T>::unpack(u[j], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[e] = number(x[e]);
+                take(i_load + j * STRIDE, x);
+            }
+        }
+    for (; i_load < w1; i_load += STRIDE) {
+        float x[VEC];
+        fetch(i_load, x);
+        take(i_load, x);
     }
+    const unsigned long long own_best = best;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
-    if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
-    sm.hist[tid] = 0;
     __syncthreads();
     if (lane == 0) atomicMin(&sm.answer, best);
     __syncthreads();
+    cluster.barrier_wait();
     if (tid < CL) cluster.map_shared_rank(sm.best, tid)[me] = sm.answer;
     cluster.sync();
     best = sm.best[0];
-    for (int c = 1; c < CL; ++c) best = min(best, sm.best[c]);
+#pragma unroll
+    for (int c = 1; c < MAX_CL; ++c) best = min(best, c < CL ? sm.best[c] : ~0ull);
     r.M = rank_value(best);
     if (bad || r.M == -INFINITY) {                                // the same in the whole cluster
         if (me == 0 && tid == 0) {
@@ -223,46 +478,92 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
         __syncthreads();
         if (tid < CL) {
             double t = 0.0;
+#pragma unroll
             for (int w = 0; w < NW; ++w) t += sm.warp_sum[w];
             cluster.map_shared_rank(sm.sum[flip], tid)[me] = t;
         }
     };
     auto total = [&]() {
         double t = 0.0;
-        for (int c = 0; c < CL; ++c) t += sm.sum[flip][c];
+#pragma unroll
+        for (int c = 0; c < MAX_CL; ++c) t += c < CL ? sm.sum[flip][c] : 0.0;
         return t;
     };
 
-    double S = 0.0;                       // weights of the whole row, where they count
-    bool have_s = false;
-    // ---- the list
+    // what the list's parts of the blocks come to, and where each begins; LIST + 1: too many
+    int count = 0, from[MAX_CL];
+    auto count_parts = [&]() {                // after a barrier of the block; has one of the cluster
+        if (tid < CL) cluster.map_shared_rank(sm.n_of, tid)[me] = sm.n_list;
+        cluster.sync();
+        count = 0;
+#pragma unroll
+        for (int c = 0; c < MAX_CL; ++c) {
+            from[c] = count;
+            count = min(count + (int)(c < CL ? sm.n_of[c] : 0u), LIST + 1);
+        }
+    };
+    auto fetch_parts = [&]() {                // the first block takes the others' parts behind its own
+        for (int i = (int)sm.n_list + tid; i < count; i += NT) {
+            int c = 1, start = from[1];
+#pragma unroll
+            for (int k = 2; k < MAX_CL; ++k)
+                if (k < CL && i >= from[k]) { c = k; start = from[k]; }
+            sm.list[i] = cluster.map_shared_rank(sm.list, c)[i - start];
+        }
+    };
+
+    double S = 0.0, front_w = 0.0;        // weights of the whole row; of this thread's elements in front of the bin that a front ends in
+    bool have_s = false, have_front = false;
+    int end_bin = 0;
     if (use_k || use_p || use_m) {
-        int last_bin = BINS - 1;          // bins in front of it and it go to the list; BINS - 1: too many
-        if (use_k || use_p) {
-            const bool weigh = !use_k;
+        const bool weigh = use_p && !use_k;
+        int last_bin = -1;                // wide bins up to here go to the list; -1: too many
+        if (a.vocab <= LIST) last_bin = BINS - 1;
+        if (weigh) {
+            // the whole row's weights, and a histogram of them
             double s = 0.0;
+            // what lies at this or below is in no bin (a little lower, so that rounding does not matter)
+            const float cut = r.M - ((float)BINS / r.steps) * 1.00001f;
 #pragma unroll 2
             for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
                 float x[VEC];
                 load(i, x);
+                float top = x[0];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = depth_of(r, x[e]);
-                    const int b = (int)d;
-                    if (weigh) s += weight(r, sm.tab, x[e]);
-                    // (2^(-1/24) = 0.97153; linear in between, off by 1.1e-4 at most)
-                    if (b < BINS - 1) atomicAdd(&sm.hist[b], weigh ? (unsigned)UNIT - (unsigned)((d - (float)b) * (UNIT * (1.f - 0.97153194f))) : 1u);
+                for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s += weight(r, sm.tab, x[e]);
+                if (!(top < cut)) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float d = depth_of(r, x[e]);
+                        const int b = (int)d;
+                        // (2^(-1/24) = 0.97153; linear in between, off by 1.1e-4 at most)
+                        if (b < BINS - 1) atomicAdd(&sm.hist[b], (unsigned)UNIT - (unsigned)((d - (float)b) * (UNIT * (1.f - 0.97153194f))));
+                    }
                 }
             }
-            if (weigh) publish(s);
+            publish(s);
+        } else if (use_k && last_bin < 0) {
+            // the threads' largest logits (equal shares of the row for each, or one element more)
+            if (own_best != ~0ull) {
+                const int b = wide_bin(r, rank_value(own_best));
+                if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
+            }
+        }
+        if (weigh || (use_k && last_bin < 0)) {
             cluster.sync();
+            unsigned part[MAX_CL];
+#pragma unroll
+            for (int c = 0; c < MAX_CL; ++c) part[c] = c < CL ? cluster.map_shared_rank(sm.hist, c)[tid] : 0u;
             unsigned long long mine = 0;
-            for (int c = 0; c < CL; ++c) mine += cluster.map_shared_rank(sm.hist, c)[tid];
+#pragma unroll
+            for (int c = 0; c < MAX_CL; ++c) mine += part[c];
             if (weigh) {
                 S = total();
                 have_s = true;
             }
-            // sums along the bins: elements, or weights (a bin's in front of another's grow smaller by 2^(1/24))
+            // sums along the bins: elements, or weights (a fine bin's smaller by 2^(1/24) than those of the one in front of it)
             const float v = weigh ? (float)mine * (1.f / UNIT) * exp2f((float)tid * (-1.f / STEPS)) : (float)mine;
             float in = v;
 #pragma unroll
@@ -272,148 +573,140 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
             }
             const unsigned cnt = warp_scan_u32(weigh ? (unsigned)ceilf((float)mine * (1.03f / UNIT)) : (unsigned)mine, lane);
             if (lane == 31) { sm.warp_f[warp] = in; sm.warp_count[warp] = cnt; }
-            if (tid == 0) sm.bin = BINS - 1;
+            if (tid == 0) { sm.bin = BINS; sm.end_bin = BINS; }
             __syncthreads();
             float before = 0.f;
             unsigned n_before = 0;
-            for (int w = 0; w < warp; ++w) { before += sm.warp_f[w]; n_before += sm.warp_count[w]; }
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (w < warp) { before += sm.warp_f[w]; n_before += sm.warp_count[w]; }
             // the border is in front of here at the latest: sums in steps of 2^-24 of themselves, the histogram's own error below 2e-4
-            const float goal = weigh ? (float)((double)top_p * S) * 1.001f : (float)top_k;
-            if (before + in >= goal && n_before + cnt <= LIST) atomicMin(&sm.bin, tid);
+            const float goal = weigh ? (float)((double)top_p * S) : (float)top_k;
+            if (before + in >= goal * (weigh ? 1.001f : 1.f) && n_before + cnt <= LIST) atomicMin(&sm.bin, tid);
+            if (weigh && before + in >= goal) atomicMin(&sm.end_bin, tid);
             __syncthreads();
             // (a bin that reaches the goal behind one that holds too much is no answer: sums only grow)
-            last_bin = sm.bin;
-        } else {
-            const double d = -log((double)r.min_p) * 1.4426950408889634 * STEPS;
-            last_bin = (int)fmin(ceil(d * 1.00001) + 1.0, (double)(BINS - 1));
+            end_bin = sm.end_bin;
+            if (last_bin < 0 && sm.bin < BINS - 1) last_bin = weigh && sm.bin >= FINE ? min(FINE + (sm.bin - FINE) / COARSE, BINS - 1) : sm.bin;
+        } else if (last_bin < 0) {
+            const double d = -log((double)r.min_p) * 1.4426950408889634 * STEPS * 1.00001 + 1.0;
+            if (d < FINE) last_bin = (int)d;
         }
-        if (last_bin < BINS - 1) {
+        if (last_bin >= 0) {
+            // each block's own part of it first
+            const float cut = a.vocab <= LIST ? -INFINITY : r.M - wide_end(last_bin) / r.steps * 1.00001f;
+#pragma unroll 4
+            for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
+                float x[VEC];
+                load(i, x);
+                float top = x[0];
+#pragma unroll
+                for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
+                if (!(top < cut)) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (wide_bin(r, x[e]) <= last_bin && i + e < n) {
+                            const unsigned p = atomicAdd(&sm.n_list, 1u);
+                            if (p < LIST) sm.list[p] = rank_of(x[e], first + i + e);
+                        }
+                }
+            }
+            __syncthreads();
+            count_parts();
+            if (count <= LIST) {
+                if (me != 0) {
+                    cluster.sync();                                // (the first block has fetched the parts)
+                    return;
+                }
+                fetch_parts();
+                cluster.barrier_arrive();
+                from_list(r, sm, a, row, count, use_k ? top_k : count, use_p ? top_p : 2.f, use_k ? -1.0 : S, uniform);
+                cluster.barrier_wait();
+                return;
+            }
+        }
+        // ---- a long front of top-p that ends in a fine bin
+        const double theta = (double)top_p * S;
+        for (int tries = 0; weigh && end_bin < BINS - 1 && tries < 4; ++tries) {
+            __syncthreads();
+            if (tid == 0) sm.n_list = 0;
+            cluster.sync();                                        // (histograms, counts and lists have been read)
+            front_w = 0.0;
+            const float cut = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
 #pragma unroll 2
             for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
                 float x[VEC];
                 load(i, x);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if ((int)depth_of(r, x[e]) <= last_bin) {
-                        const unsigned p = atomicAdd(cluster.map_shared_rank(&sm.n_list, 0), 1u);
-                        if (p < LIST) cluster.map_shared_rank(sm.list, 0)[p] = rank_of(x[e], first + i + e);
+                for (int e = 0; e < VEC; ++e) {
+                    if (x[e] < cut) continue;
+                    const int b = (int)depth_of(r, x[e]);
+                    if (b < end_bin) front_w += weight(r, sm.tab, x[e]);
+                    else if (b == end_bin) {
+                        const unsigned p = atomicAdd(&sm.n_list, 1u);
+                        if (p < LIST) sm.list[p] = rank_of(x[e], first + i + e);
                     }
-            }
-            cluster.sync();
-            const int count = (int)*cluster.map_shared_rank(&sm.n_list, 0);
-            if (count <= LIST) {
-                cluster.sync();                                    // (everybody has read the count)
-                if (me != 0) return;
-                // sorted along the order
-                if (count <= 128) {
-                    unsigned long long v = ~0ull;
-                    int rank = 0;
-                    if (tid < count) {
-                        v = sm.list[tid];
-                        for (int j = 0; j < count; ++j) rank += sm.list[j] < v;
-                    }
-                    __syncthreads();
-                    if (tid < count) sm.list[rank] = v;
-                    __syncthreads();
-                } else {
-                    int size = 256;
-                    while (size < count) size *= 2;
-                    for (int i = count + tid; i < size; i += NT) sm.list[i] = ~0ull;
-                    __syncthreads();
-                    for (int s = 2; s <= size; s *= 2)
-                        for (int d = s / 2; d > 0; d /= 2) {
-                            for (int i = tid; i < size / 2; i += NT) {
-                                const int x = 2 * i - (i & (d - 1)), y = x + d;
-                                const unsigned long long p = sm.list[x], q = sm.list[y];
-                                if ((p > q) == ((x & s) == 0)) { sm.list[x] = q; sm.list[y] = p; }
-                            }
-                            __syncthreads();
-                        }
                 }
-                // exact sums along it, a thread for four neighbours: sums up to each of them, and where the front ends
-                const int n_k = use_k ? min(count, top_k) : count;
-                double w[4], run = 0.0;
+            }
+            publish(front_w);
+            count_parts();
+            const double before = total();
+            if (count > LIST || count == 0) break;
+            if (me == 0) {
+                fetch_parts();
+                sort_list(r, sm, count);
+                // sums along it, four neighbours a thread: the first element at which they reach theta
+                double w[LIST / NT], run = 0.0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = tid * 4 + e;
-                    w[e] = i < n_k ? weight(r, sm.tab, rank_value(sm.list[i])) : 0.0;
-                    if (i < count) sm.list_w[i] = w[e];
+                for (int e = 0; e < LIST / NT; ++e) {
+                    w[e] = tid * (LIST / NT) + e < count ? sm.list_w[tid * (LIST / NT) + e] : 0.0;
                     run += w[e];
                 }
                 const double in = warp_scan_f64(run, lane);
                 if (lane == 31) sm.warp_sum2[warp] = in;
+                if (tid == 0) sm.bin = BINS * LIST;
                 __syncthreads();
-                double upto = in - run, all = 0.0;
-                {
-                    double before = 0.0;
-                    for (int k = 0; k < NW; ++k) {
-                        if (k == warp) before = all;
-                        all += sm.warp_sum2[k];
-                    }
-                    upto += before;
-                }
-                const double theta = use_p ? (double)top_p * (use_k ? all : S) : INFINITY;
-                int stay = 0;
+                double upto = before + in - run, all = before;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = tid * 4 + e;
-                    stay += i < n_k && (i == 0 || (upto < theta && w[e] >= r.min_p));
+                for (int k = 0; k < NW; ++k) {
+                    if (k < warp) upto += sm.warp_sum2[k];
+                    all += sm.warp_sum2[k];
+                }
+                int end = BINS * LIST;
+#pragma unroll
+                for (int e = 0; e < LIST / NT; ++e) {
                     upto += w[e];
+                    if (end == BINS * LIST && tid * (LIST / NT) + e < count && upto >= theta) end = tid * (LIST / NT) + e;
                 }
-                stay = __reduce_add_sync(0xffffffffu, stay);
-                if (lane == 0) sm.warp_count[warp] = stay;
+                end = __reduce_min_sync(0xffffffffu, end);
+                if (lane == 0) atomicMin(&sm.bin, end);
                 __syncthreads();
-                int kept = 0;
-                for (int k = 0; k < NW; ++k) kept += sm.warp_count[k];
-                __syncthreads();
-                // The smallest index at which the kept weights in the order of indices exceed uniform times their sum: NW + 1 parts of the range at a time, a warp sums up to each border
-                auto sum_to = [&](int index) {                      // a whole warp
-                    double t = 0.0;
-                    for (int i = lane; i < kept; i += 32)
-                        if ((int)(uint32_t)sm.list[i] <= index) t += sm.list_w[i];
-                    return warp_sum_f64(t);
-                };
-                const double W = sum_to(a.vocab), target = (double)uniform * W;
-                int lo = -1, hi = a.vocab - 1;                      // the sum up to lo does not exceed the target; up to hi it does, or nothing does
-                while (hi - lo > 1) {
-                    const int part = (hi - lo - 1) / NW + 1, at = min(hi, lo + (warp + 1) * part);
-                    const bool over = at >= hi || sum_to(at) > target;
-                    if (lane == 0) sm.warp_count[warp] = over;
-                    __syncthreads();
-                    int f = 0;
-                    while (f < NW && !sm.warp_count[f]) ++f;
-                    const int new_hi = f < NW ? min(hi, lo + (f + 1) * part) : hi;
-                    lo = min(hi - 1, lo + f * part);
-                    hi = new_hi;
-                    __syncthreads();
+                if (tid < CL) {
+                    // (the histogram's sums may be off at a border of bins: the next one then)
+                    const int verdict = before >= theta && end_bin > 0 ? -1 : (sm.bin >= count && all < theta * (1.0 - 1e-13) ? 1 : 0);
+                    *cluster.map_shared_rank(&sm.verdict, tid) = verdict;
+                    *cluster.map_shared_rank(&sm.answer, tid) = sm.list[min(sm.bin, count - 1)];
                 }
-                // the element at hi; with a target that nothing exceeds, the last kept one with weight
-                if (warp == 0) {
-                    const bool none = !(W > target);
-                    int found = -1;
-                    if (none) {
-                        for (int i = lane; i < kept; i += 32)
-                            if (sm.list_w[i] > 0.0) found = max(found, (int)(uint32_t)sm.list[i]);
-                        hi = __reduce_max_sync(0xffffffffu, found);
-                    }
-                    for (int i = lane; i < kept; i += 32)
-                        if ((int)(uint32_t)sm.list[i] == hi) {
-                            a.tokens[row] = hi;
-                            if (a.logprob) a.logprob[row] = (float)log(sm.list_w[i] / W);
-                        }
-                }
-                return;
             }
+            cluster.sync();
+            if (sm.verdict == 0) {
+                r.bound = sm.answer;
+                have_front = true;
+                break;
+            }
+            end_bin += sm.verdict;
         }
-        cluster.sync();                                            // histograms and count have been read
-        if (tid == 0) sm.n_list = 0;
+        if (!have_front) {
+            cluster.sync();
+            if (tid == 0) sm.n_list = 0;
+        }
     }
 
     // ---- fronts too long for the list: what = 0 top-k, 1 top-p
     auto inside = [&](uint32_t k, uint32_t lo, uint32_t hi, int index) {
         return k >= lo && k <= hi && (((unsigned long long)~k << 32) | (unsigned)index) <= r.bound;
     };
-    for (int what = 0; what < 2; ++what) {
+    for (int what = 0; what < 2 && !have_front; ++what) {
         if (what == 0 ? !use_k : !use_p) continue;
         double theta = 0.0;               // top-p: the weights that have to be reached
         if (what == 1) {
@@ -655,12 +948,26 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
         return w >= r.min_p ? w : 0.0;
     };
     double s = 0.0;
-#pragma unroll 2
-    for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-        float x[VEC];
-        load(i, x);
+    if (have_front && !use_m) {
+        // what is in front of the last bin has been added up
+        const float from_x = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
+        s = front_w;
+#pragma unroll 4
+        for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
+            float x[VEC];
+            load(i, x);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s += kept_weight(x[e], first + i + e);
+            for (int e = 0; e < VEC; ++e)
+                if (!(x[e] < from_x) && (int)depth_of(r, x[e]) == end_bin && rank_of(x[e], first + i + e) <= r.bound) s += weight(r, sm.tab, x[e]);
+        }
+    } else {
+#pragma unroll 2
+        for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
+            float x[VEC];
+            load(i, x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += kept_weight(x[e], first + i + e);
+        }
     }
     publish(s);
     cluster.sync();
