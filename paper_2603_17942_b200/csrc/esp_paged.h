@@ -97,7 +97,7 @@ struct EvictArgs {
     int32_t list_cap;       // moves of a list at most
     int32_t vec;            // elements of a row that can be moved at a time
     int32_t* count;         // [batch * Hkv] moves
-    int32_t* len;           // [batch] kv_len from now on
+    int4* info;             // [batch] (kv_len from now on, -1: as it was; settled slots and their positions' base as the call found them)
     int2* list;             // [batch * Hkv][list_cap] (from, to)
 };
 

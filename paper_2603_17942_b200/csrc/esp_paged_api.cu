@@ -379,9 +379,9 @@ int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const 
     return rc ? ESP_E_CUDA : cuda_ok(e);
 }
 
-// scratch layout: [batch * heads] moves of a list, [batch] lengths, [batch * heads][max_kv / 2] moves
+// scratch layout: [batch] lengths and positions, [batch * heads] moves of a list, [batch * heads][max_kv / 2] moves
 namespace {
-size_t evict_front(int64_t batch, int64_t heads) { return ((size_t)(batch * heads + batch) * sizeof(int32_t) + 255) / 256 * 256; }
+size_t evict_front(int64_t batch, int64_t heads) { return ((size_t)batch * sizeof(int4) + (size_t)(batch * heads) * sizeof(int32_t) + 255) / 256 * 256; }
 }
 int esp_paged_evict_scratch_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_kv, size_t* bytes_out) {
     if (!bytes_out || batch < 0 || batch > MAX_BATCH || n_kv_heads < 1 || n_kv_heads > MAX_HEADS || max_kv < 0 || max_kv > paged::KV_LIMIT) return ESP_E_ARG;
@@ -404,7 +404,7 @@ int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, 
     if (batch->batch == 0) return ESP_OK;
     if (!budget || !kv_len_out) return ESP_E_ARG;
     const int64_t lists = (int64_t)batch->batch * cache->n_kv_heads;
-    if (lists > MAX_BATCH) return ESP_E_ARG;
+    if (lists > (1 << 27)) return ESP_E_ARG;
     const size_t front = evict_front(batch->batch, cache->n_kv_heads);
     if (!scratch || scratch_bytes < front || off(scratch, 256)) return ESP_E_WORKSPACE;
     const int n_sm = current_sm_count();
@@ -420,8 +420,8 @@ int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, 
     const size_t cap = (scratch_bytes - front) / sizeof(int2) / (size_t)lists;
     a.list_cap = cap < (size_t)paged::KV_LIMIT ? (int32_t)cap : paged::KV_LIMIT;
     a.vec = row_vec(cache);
-    a.count = reinterpret_cast<int32_t*>(scratch);
-    a.len = a.count + lists;
+    a.info = reinterpret_cast<int4*>(scratch);
+    a.count = reinterpret_cast<int32_t*>(a.info + batch->batch);
     a.list = reinterpret_cast<int2*>(reinterpret_cast<char*>(scratch) + front);
     const int rc = launch_evict(cache->dtype, a, n_sm, reinterpret_cast<cudaStream_t>(cuda_stream));
     const cudaError_t e = cudaGetLastError();

@@ -1,10 +1,15 @@
 // Cutting caches to their budgets, and the acceptance of draft trees: the two operators that move slots of a paged cache.
 //
 // Eviction: a list of a sequence and KV head is a choice of its `budget` largest keys (score, recency), 32-bit numbers in the order of
-// the scores.  k_evict_select finds the smallest key that stays by its digits, 11 + 11 + 10 bits, with histograms in shared memory, then deals the
-// kept slots behind the budget to the dropped ones in front of it, both in order, so the answer depends on nothing but the numbers.
-// k_evict_move moves the rows of all lists, spread over the whole GPU.
+// the scores.  k_evict_select, a block or a cluster of blocks for each list, finds the smallest key that stays by its digits, four times eight bits, with histograms in shared memory,
+// then deals the kept slots behind the budget to the dropped ones in front of it, both in order, so the answer depends on nothing but the numbers.
+// k_evict_move moves the lists' rows, scores and positions, spread over the whole GPU.  Both are chains of short steps: what counts is that the loads of a step are all under
+// way before the first is waited for, and that the code is short (loops unrolled over 32 keys in registers took longer to fetch than to run).
+#include <cooperative_groups.h>
+
 #include "esp_paged.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace esp {
 
@@ -19,6 +24,10 @@ __device__ __forceinline__ size_t row_offset(const PagesView& v, int page, int s
     return (size_t)((long long)page * v.page + (long long)slot * v.tok + (long long)head * v.head);
 }
 
+// The table's entry, whatever it says, and the page it names or -1: several loads can be under way before the first is looked at (load_page branches on each)
+__device__ __forceinline__ int table_entry(const SeqTable& t, int b, int index) { return __ldg(t.table + (size_t)b * t.table_stride + index); }
+__device__ __forceinline__ int named(const PagesView& p, int entry) { return entry >= 0 && entry < p.n_pages ? entry : -1; }
+
 // Larger numbers for larger scores, equal ones for equal scores (-0 = 0); a NaN as -infinity.
 __device__ __forceinline__ uint32_t order_key(float x) {
     if (x != x) x = -INFINITY;
@@ -27,19 +36,19 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 constexpr uint32_t KEY_INF = 0xff800000u;      // order_key(INFINITY)
 
-constexpr int SELECT_THREADS = 1024, SELECT_WARPS = SELECT_THREADS / 32;
-constexpr int KEYS_IN_SMEM = 48 * 1024;        // keys of longer lists are made anew in every pass
-constexpr int BINS = 2048;
+constexpr int BINS = 256, MAX_CL = 8, NEAR = 255;
+constexpr int KEYS = 8192;            // keys that a block keeps; those of a longer stretch are made anew in every pass
 
 struct SeqCut {
-    int kv, budget, seen, settled;
+    int kv, budget;
+    int settled, base;    // slots in front of `settled` have a position of their own, slot s behind them has base + s
     bool cut;
 };
 __device__ __forceinline__ SeqCut load_cut(const EvictArgs& a, int b) {
     SeqCut c;
     c.kv = __ldg(a.seq.kv_len + b);
     c.budget = __ldg(a.budget + b);
-    c.seen = a.positions.p ? __ldg(a.seen + b) : c.kv;
+    c.base = a.positions.p ? __ldg(a.seen + b) - c.kv : 0;
     c.settled = a.positions.p ? a.settled[b] : 0;
     c.cut = false;
     if (c.kv < 0 || c.kv > a.seq.kv_cap || c.budget < 0) set_error(a.seq.status, DEV_E_INDEX);
@@ -50,172 +59,364 @@ __device__ __forceinline__ SeqCut load_cut(const EvictArgs& a, int b) {
     }
     return c;
 }
-__device__ __forceinline__ int position_of(const EvictArgs& a, const SeqCut& c, int s, int page, int slot, int head) {
-    if (a.positions.p && s < c.settled) return page < 0 ? -1 : reinterpret_cast<const int32_t*>(a.positions.p)[slot_offset(a.positions, page, slot, head)];
-    return c.seen - c.kv + s;
-}
-
-__global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_constant__ EvictArgs a) {
-    extern __shared__ uint32_t s_key[];                 // [min(kv, KEYS_IN_SMEM)]
-    __shared__ uint32_t s_hist[BINS];
-    __shared__ int s_warp[SELECT_WARPS + 1], s_warp2[SELECT_WARPS + 1];
-    __shared__ int s_bin, s_above;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int b = blockIdx.x / a.Hkv, h = blockIdx.x - b * a.Hkv;
-    pdl_launch_dependents();
-    const SeqCut c = load_cut(a, b);
-    if (!c.cut) {
-        if (threadIdx.x == 0) {
-            a.count[blockIdx.x] = 0;
-            if (h == 0) a.len[b] = -1;
-        }
-        return;
-    }
-    const bool kept_in_smem = c.kv <= KEYS_IN_SMEM;
-    auto make_key = [&](int s) {
-        const int index = page_index(a.pages, s), slot = s - index * a.pages.page_size;
-        const int page = load_page(a.seq, a.pages, b, index);
-        const float x = page < 0 ? -INFINITY : reinterpret_cast<const float*>(a.scores.p)[slot_offset(a.scores, page, slot, h)];
-        // (positions differ, so they are told apart in 64 bits)
-        if ((long long)position_of(a, c, s, page, slot, h) >= (long long)c.seen - a.recent) return KEY_INF;
-        return order_key(x);
-    };
-    auto key = [&](int s) { return kept_in_smem ? s_key[s] : make_key(s); };
-    if (kept_in_smem)
-        for (int s = threadIdx.x; s < c.kv; s += SELECT_THREADS) s_key[s] = make_key(s);
-
-    // ---- the smallest key that stays, `top`, and how many keys are above it
-    uint32_t top = 0, mask = 0;
-    int above = 0;
-    constexpr int SHIFT[3] = {21, 10, 0}, WIDTH[3] = {11, 11, 10};
-#pragma unroll 1
-    for (int d = 0; d < 3; ++d) {
-        for (int i = threadIdx.x; i < BINS; i += SELECT_THREADS) s_hist[i] = 0;
-        __syncthreads();
-        const uint32_t digit = (1u << WIDTH[d]) - 1u;
-        for (int s = threadIdx.x; s < c.kv; s += SELECT_THREADS) {
-            const uint32_t k = key(s);
-            if ((k & mask) == top) atomicAdd(&s_hist[(k >> SHIFT[d]) & digit], 1u);
-        }
-        __syncthreads();
-        // bins from the top: thread t has bins BINS - 1 - 2t and the one below
-        const int hi = BINS - 1 - 2 * threadIdx.x;
-        const int n0 = (int)s_hist[hi], n1 = (int)s_hist[hi - 1];
-        const int incl = (int)warp_scan_u32(n0 + n1, lane);
-        if (lane == 31) s_warp[warp] = incl;
-        __syncthreads();
-        if (warp == 0) {
-            const int x = s_warp[lane], y = (int)warp_scan_u32(x, lane);
-            s_warp[lane] = y - x;
-        }
-        __syncthreads();
-        const int before = above + s_warp[warp] + incl - n0 - n1;
-        if (before < c.budget && c.budget <= before + n0) { s_bin = hi; s_above = before; }
-        else if (before + n0 < c.budget && c.budget <= before + n0 + n1) { s_bin = hi - 1; s_above = before + n0; }
-        if (c.budget == 0 && threadIdx.x == 0) { s_bin = BINS - 1; s_above = 0; }
-        __syncthreads();
-        above = s_above;
-        top |= ((uint32_t)s_bin & digit) << SHIFT[d];
-        mask |= digit << SHIFT[d];
-    }
-    const int ties = c.budget - above;                  // slots with the key `top` that stay: the first ones
-
-    // ---- each warp has a stretch of slots: ties in front of it, then kept ones behind the budget and dropped ones before it
-    const int each = (c.kv + SELECT_THREADS - 1) / SELECT_THREADS * 32, s0 = min(c.kv, warp * each), s1 = min(c.kv, s0 + each);
-    auto block_before = [&](int* of, int mine) {        // the sum over the warps in front (mine: the same in every lane)
-        if (lane == 0) of[warp] = mine;
-        __syncthreads();
-        int before = 0;
-        for (int w = 0; w < warp; ++w) before += of[w];
-        return before;
-    };
-    int n = 0;
-    for (int i = s0; i < s1; i += 32) n += __popc(__ballot_sync(0xffffffffu, i + lane < s1 && key(min(i + lane, s1 - 1)) == top));
-    const int tie0 = block_before(s_warp, n);
-    __syncthreads();
-    int moves = 0, holes = 0, tie = tie0;
-    auto kept = [&](int s, uint32_t k, bool in) {       // all lanes
-        const uint32_t same = __ballot_sync(0xffffffffu, in && k == top);
-        const bool stays = in && (k > top || (k == top && tie + __popc(same & ((1u << lane) - 1u)) < ties));
-        tie += __popc(same);
-        return stays;
-    };
-    for (int i = s0; i < s1; i += 32) {
-        const int s = i + lane;
-        const bool in = s < s1, stays = kept(s, in ? key(s) : 0u, in);
-        moves += __popc(__ballot_sync(0xffffffffu, stays && s >= c.budget));
-        holes += __popc(__ballot_sync(0xffffffffu, in && !stays && s < c.budget));
-    }
-    int m = block_before(s_warp, moves), e = block_before(s_warp2, holes);
-    int2* list = a.list + (size_t)blockIdx.x * a.list_cap;
-    tie = tie0;
-    for (int i = s0; i < s1; i += 32) {
-        const int s = i + lane;
-        const bool in = s < s1, stays = kept(s, in ? key(s) : 0u, in);
-        const uint32_t go = __ballot_sync(0xffffffffu, stays && s >= c.budget), to = __ballot_sync(0xffffffffu, in && !stays && s < c.budget);
-        const uint32_t low = (1u << lane) - 1u;
-        if ((go >> lane) & 1) list[m + __popc(go & low)].x = s;
-        if ((to >> lane) & 1) list[e + __popc(to & low)].y = s;
-        m += __popc(go);
-        e += __popc(to);
-    }
-    if (threadIdx.x == SELECT_THREADS - 1) {            // (the last warp has them all in front of it)
-        a.count[blockIdx.x] = m;
-        if (h == 0) a.len[b] = c.budget;
-        s_bin = m;
-    }
-    __syncthreads();
-    // ---- scores and positions
-    const int total = s_bin;
-    if (a.positions.p)
-        for (int s = max(c.settled, 0) + (int)threadIdx.x; s < c.budget; s += SELECT_THREADS) {
-            const int index = page_index(a.pages, s), page = load_page(a.seq, a.pages, b, index);
-            if (page >= 0) reinterpret_cast<int32_t*>(a.positions.p)[slot_offset(a.positions, page, s - index * a.pages.page_size, h)] = c.seen - c.kv + s;
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < total; i += SELECT_THREADS) {
-        const int2 x = list[i];
-        const int fi = page_index(a.pages, x.x), ti = page_index(a.pages, x.y), fs = x.x - fi * a.pages.page_size, ts = x.y - ti * a.pages.page_size;
-        const int fp = load_page(a.seq, a.pages, b, fi), tp = load_page(a.seq, a.pages, b, ti);
-        if (tp < 0) continue;
-        reinterpret_cast<float*>(a.scores.p)[slot_offset(a.scores, tp, ts, h)] =
-            fp < 0 ? -INFINITY : reinterpret_cast<const float*>(a.scores.p)[slot_offset(a.scores, fp, fs, h)];
-        if (a.positions.p) reinterpret_cast<int32_t*>(a.positions.p)[slot_offset(a.positions, tp, ts, h)] = position_of(a, c, x.x, fp, fs, h);
-    }
-}
-
-// Row of `bytes` bytes, VEC of them to a lane; lanes of a group that covers the row
+// Row of `bytes` bytes, VEC of them to a lane
 template <int VEC> struct Unit;
 template <> struct Unit<16> { typedef uint4 T; };
 template <> struct Unit<8> { typedef uint2 T; };
 template <> struct Unit<4> { typedef uint32_t T; };
 template <> struct Unit<2> { typedef uint16_t T; };
 
-constexpr int MOVE_THREADS = 256;
+// One move by a warp: keys, values, score and position.  settled, base: what slots hold as positions, as in SeqCut.
 template <int VEC>
-__global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(const __grid_constant__ EvictArgs a, int elem, int blocks) {
+__device__ __forceinline__ void move_one(const EvictArgs& a, int elem, int b, int h, const SeqCut& c, int2 x, int lane) {
+    typedef typename Unit<VEC>::T U;
+    const int row = a.D * elem / VEC, fi = page_index(a.pages, x.x), ti = page_index(a.pages, x.y), fs = x.x - fi * a.pages.page_size, ts = x.y - ti * a.pages.page_size;
+    int fp = table_entry(a.seq, b, fi), tp = table_entry(a.seq, b, ti);
+    fp = named(a.pages, fp);
+    tp = named(a.pages, tp);
+    if (fp < 0 || tp < 0) {
+        set_error(a.seq.status, DEV_E_INDEX);
+        return;
+    }
+    for (int u = lane; u < 2 * row; u += 32) {
+        char* base = reinterpret_cast<char*>(u < row ? a.pages.k : a.pages.v) + (size_t)(u < row ? u : u - row) * VEC;
+        *reinterpret_cast<U*>(base + row_offset(a.pages, tp, ts, h) * elem) = *reinterpret_cast<const U*>(base + row_offset(a.pages, fp, fs, h) * elem);
+    }
+    if (lane == 0) {
+        reinterpret_cast<float*>(a.scores.p)[slot_offset(a.scores, tp, ts, h)] = reinterpret_cast<const float*>(a.scores.p)[slot_offset(a.scores, fp, fs, h)];
+        if (a.positions.p)
+            reinterpret_cast<int32_t*>(a.positions.p)[slot_offset(a.positions, tp, ts, h)] =
+                x.x < c.settled ? reinterpret_cast<const int32_t*>(a.positions.p)[slot_offset(a.positions, fp, fs, h)] : c.base + x.x;
+    }
+}
+
+// The keys of slots first + step * j below `end`, j < N, 0 for the others (no key of a slot is 0): all pages first, then all scores and positions, so that the loads wait for each other
+// twice and not 2 N times.
+template <int N>
+__device__ __forceinline__ void load_keys(const EvictArgs& a, const SeqCut& c, int b, int h, int first, int step, int end, uint32_t (&k)[N]) {
+    int page[N], slot[N];
+    float x[N];
+    bool bad = false;
+    const float* scores = reinterpret_cast<const float*>(a.scores.p) + (long long)h * a.scores.head;
+    const int32_t* positions = reinterpret_cast<const int32_t*>(a.positions.p) + (a.positions.p ? (long long)h * a.positions.head : 0);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int s = min(first + step * j, c.kv - 1), index = page_index(a.pages, s);
+        page[j] = table_entry(a.seq, b, index);
+        slot[j] = s - index * a.pages.page_size;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        page[j] = named(a.pages, page[j]);
+        bad = bad || (page[j] < 0 && first + step * j < end);
+    }
+    if (bad) set_error(a.seq.status, DEV_E_INDEX);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        x[j] = page[j] < 0 ? -INFINITY : scores[page[j] * a.scores.page + slot[j] * a.scores.tok];
+    int pos[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) pos[j] = c.base + first + step * j;
+    if (a.positions.p && a.recent > 0) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (first + step * j < c.settled) pos[j] = page[j] < 0 ? -1 : positions[page[j] * a.positions.page + slot[j] * a.positions.tok];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        k[j] = order_key(x[j]);
+        // (positions differ, so they are told apart in 64 bits)
+        if (a.recent > 0 && (long long)pos[j] >= (long long)c.base + c.kv - a.recent) k[j] = KEY_INF;
+        if (first + step * j >= end) k[j] = 0;
+    }
+}
+
+constexpr int SELECT_THREADS = 512;
+template <int VEC>
+__global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_constant__ EvictArgs a, int elem) {
+    constexpr int THREADS = SELECT_THREADS, WARPS = THREADS / 32;
+    __shared__ uint32_t s_key[KEYS];
+    __shared__ uint32_t s_hist[2][BINS];                // (a block of the cluster may be a digit ahead of another)
+    __shared__ int s_all[BINS];
+    __shared__ int s_warp[WARPS], s_warp2[WARPS], s_word[4];
+    __shared__ int2 s_count[MAX_CL];                    // [block] (kept ones behind the budget, dropped ones in front of it)
+    __shared__ int s_ties[MAX_CL];
+    __shared__ uint32_t s_near[MAX_CL][NEAR + 1];       // [block] the keys that share the digits found so far; the last one: how many
+    __shared__ int s_near_n;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int CL = cluster.num_blocks(), me = cluster.block_rank(), list_no = blockIdx.x / CL;
+    const int b = list_no / a.Hkv, h = list_no - b * a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t low = (1u << lane) - 1u;
+    pdl_launch_dependents();
+    const SeqCut c = load_cut(a, b);
+    if (!c.cut) {                                       // the same in the whole cluster
+        if (me == 0 && threadIdx.x == 0) {
+            a.count[list_no] = 0;
+            if (h == 0) a.info[b] = make_int4(-1, 0, 0, 0);
+        }
+        return;
+    }
+    if (CL > 1) cluster.barrier_arrive();               // (before anybody looks into another block's shared memory, all have to have started)
+    // the block's stretch of slots, and each warp's of it
+    const int per = (c.kv + CL * 32 - 1) / (CL * 32) * 32, f0 = min(c.kv, me * per), f1 = min(c.kv, f0 + per);
+    const int each = (per + THREADS - 1) / THREADS * 32, s0 = min(f1, f0 + warp * each), s1 = min(f1, s0 + each);
+    const bool kept = per <= KEYS;
+    if (kept) {
+        constexpr int N = 4;
+#pragma unroll 1
+        for (int i = f0 + (int)threadIdx.x; i < f1; i += N * THREADS) {
+            uint32_t k[N];
+            load_keys<N>(a, c, b, h, i, THREADS, f1, k);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (i + j * THREADS < f1) s_key[i + j * THREADS - f0] = k[j];
+        }
+    }
+    // f(slot of this lane, its key) over the warp's stretch, by all lanes together
+    auto walk = [&](auto f) {
+        if (kept) {
+#pragma unroll 2
+            for (int i = s0 + lane; i - lane < s1; i += 32) f(i, i < s1 ? s_key[i - f0] : 0u);
+        } else {
+            constexpr int N = 4;
+            for (int i = s0 + lane; i - lane < s1; i += 32 * N) {
+                uint32_t k[N];
+                load_keys<N>(a, c, b, h, i, 32, s1, k);
+#pragma unroll
+                for (int j = 0; j < N; ++j) f(i + 32 * j, k[j]);
+            }
+        }
+    };
+    auto before = [&](const int* of) { return (int)__reduce_add_sync(0xffffffffu, lane < warp && lane < WARPS ? of[lane] : 0); };     // the sum over the warps in front
+    if (CL > 1) cluster.barrier_wait();
+
+    // ---- the smallest key that stays, `top`, how many keys are above it, and how many equal it
+    uint32_t top = 0, mask = 0;
+    int above = 0, same = 0;
+#pragma unroll 1
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (shift == 8 && c.budget > 0) {
+            // few keys share two digits, as a rule: everybody gets all of them, and each counts those above it
+            if (threadIdx.x == 0) s_near_n = 0;
+            __syncthreads();
+            walk([&](int, uint32_t k) {
+                if (k != 0 && (k & mask) == top) {
+                    const int i = atomicAdd(&s_near_n, 1);
+                    if (i < NEAR)
+                        for (int r = 0; r < CL; ++r) cluster.map_shared_rank(&s_near[0][0], r)[me * (NEAR + 1) + i] = k;
+                }
+            });
+            __syncthreads();
+            if ((int)threadIdx.x < CL) cluster.map_shared_rank(&s_near[0][0], threadIdx.x)[me * (NEAR + 1) + NEAR] = (uint32_t)s_near_n;
+            if (CL > 1) cluster.sync();
+            else __syncthreads();
+            bool fits = true;
+#pragma unroll
+            for (int r = 0; r < MAX_CL; ++r) fits = fits && (r >= CL || s_near[r][NEAR] <= NEAR);
+            if (fits) {
+                for (int i = threadIdx.x; i < CL * NEAR; i += THREADS) {
+                    const int r = i / NEAR, e = i % NEAR;
+                    if (e >= (int)s_near[r][NEAR]) continue;
+                    const uint32_t k = s_near[r][e];
+                    int over = above, eq = 0;
+                    for (int q = 0; q < CL; ++q) {
+                        const int n = (int)s_near[q][NEAR];
+#pragma unroll 4
+                        for (int j = 0; j < n; ++j) {
+                            over += s_near[q][j] > k;
+                            eq += s_near[q][j] == k;
+                        }
+                    }
+                    if (over < c.budget && c.budget <= over + eq) {      // (equal ones all write the same)
+                        s_word[0] = (int)k;
+                        s_word[1] = over;
+                        s_word[2] = eq;
+                    }
+                }
+                __syncthreads();
+                top = (uint32_t)s_word[0];
+                above = s_word[1];
+                same = s_word[2];
+                break;
+            }
+        }
+        uint32_t* hist = s_hist[(shift >> 3) & 1];
+        for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
+        __syncthreads();
+        walk([&](int, uint32_t k) {
+            if (k != 0 && (k & mask) == top) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        });
+        if (CL > 1) cluster.sync();
+        else __syncthreads();
+        if (threadIdx.x < BINS) {
+            int n = 0;
+            if (CL == 1) n = (int)hist[threadIdx.x];
+            else {
+                uint32_t part[MAX_CL];
+#pragma unroll
+                for (int r = 0; r < MAX_CL; ++r) part[r] = r < CL ? cluster.map_shared_rank(hist, r)[threadIdx.x] : 0u;
+#pragma unroll
+                for (int r = 0; r < MAX_CL; ++r) n += (int)part[r];
+            }
+            s_all[threadIdx.x] = n;
+        }
+        __syncthreads();
+        if (warp == 0) {                                // bins from the top, eight of them to a lane
+            int n[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] = s_all[BINS - 1 - 8 * lane - i];
+                sum += n[i];
+            }
+            int front = above + (int)warp_scan_u32(sum, lane) - sum;
+            if (lane == 0 && c.budget == 0) { s_word[0] = BINS - 1; s_word[1] = s_word[2] = 0; }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (front < c.budget && c.budget <= front + n[i]) {
+                    s_word[0] = BINS - 1 - 8 * lane - i;
+                    s_word[1] = front;
+                    s_word[2] = n[i];
+                }
+                front += n[i];
+            }
+        }
+        __syncthreads();
+        above = s_word[1];
+        same = s_word[2];
+        top |= (uint32_t)s_word[0] << shift;
+        mask |= 255u << shift;
+    }
+    const int ties = c.budget - above;                  // slots with the key `top` that stay: the first ones of `same`
+
+    // ---- kept ones behind the budget and dropped ones in front of it, in order
+    const bool some = ties < same;                      // which of the equal ones is a matter of order
+    int tie = 0;
+    if (some) {
+        int n = 0;
+        walk([&](int, uint32_t k) { n += __popc(__ballot_sync(0xffffffffu, k == top)); });
+        if (lane == 0) s_warp[warp] = n;
+        __syncthreads();
+        tie = before(s_warp);
+        if (CL > 1) {
+            if (warp == WARPS - 1 && lane < CL) cluster.map_shared_rank(s_ties, lane)[me] = tie + n;
+            cluster.sync();
+            for (int r = 0; r < me; ++r) tie += s_ties[r];
+        }
+        __syncthreads();
+    }
+    const int tie0 = tie;
+    auto stays = [&](uint32_t k) {                      // all lanes
+        if (!some) return k >= top && k != 0;
+        const uint32_t eq = __ballot_sync(0xffffffffu, k == top);
+        const bool s = k > top || (k == top && tie + __popc(eq & low) < ties);
+        tie += __popc(eq);
+        return s;
+    };
+    int go = 0, to = 0;
+    walk([&](int s, uint32_t k) {
+        const bool st = stays(k);
+        go += __popc(__ballot_sync(0xffffffffu, st && s >= c.budget));
+        to += __popc(__ballot_sync(0xffffffffu, k != 0 && !st && s < c.budget));
+    });
+    if (lane == 0) { s_warp[warp] = go; s_warp2[warp] = to; }
+    __syncthreads();
+    int m = before(s_warp), e = before(s_warp2), total;
+    if (CL > 1) {
+        if (warp == WARPS - 1 && lane < CL) cluster.map_shared_rank(s_count, lane)[me] = make_int2(m + go, e + to);
+        cluster.sync();
+        total = 0;
+        for (int r = 0; r < CL; ++r) {
+            const int2 x = s_count[r];
+            if (r < me) { m += x.x; e += x.y; }
+            total += x.x;
+        }
+    } else {
+        total = (int)__reduce_add_sync(0xffffffffu, lane < WARPS ? s_warp[lane] : 0);
+    }
+    int2* list = a.list + (size_t)list_no * a.list_cap;
+    tie = tie0;
+    if (total > 0)
+        walk([&](int s, uint32_t k) {
+            const bool st = stays(k);
+            const uint32_t gm = __ballot_sync(0xffffffffu, st && s >= c.budget), tm = __ballot_sync(0xffffffffu, k != 0 && !st && s < c.budget);
+            if ((gm >> lane) & 1) list[m + __popc(gm & low)].x = s;
+            if ((tm >> lane) & 1) list[e + __popc(tm & low)].y = s;
+            m += __popc(gm);
+            e += __popc(tm);
+        });
+    // few moves of a list that one block has are made here
+    const bool few = CL == 1 && total <= WARPS;
+    if (me == 0 && threadIdx.x == 0) {
+        a.count[list_no] = few ? 0 : total;
+        if (h == 0) a.info[b] = make_int4(c.budget, c.settled, c.base, 0);
+    }
+    // positions of slots that had none
+    if (a.positions.p)
+        for (int s = max(c.settled, f0) + (int)threadIdx.x; s < min(c.budget, f1); s += THREADS) {
+            const int index = page_index(a.pages, s), page = named(a.pages, table_entry(a.seq, b, index));
+            if (page >= 0) reinterpret_cast<int32_t*>(a.positions.p)[slot_offset(a.positions, page, s - index * a.pages.page_size, h)] = c.base + s;
+        }
+    if (few) {
+        __syncthreads();
+        if (warp < total) move_one<VEC>(a, elem, b, h, c, list[warp], lane);
+    }
+    if (CL > 1) cluster.sync();                         // nobody leaves while others may look into its shared memory
+}
+
+// A warp takes up to 32 moves of a list at a time: each lane looks up one of them and moves its score and position, then all lanes move the rows together, four loads of each under way.
+constexpr int MOVE_THREADS = 256, MOVE_AHEAD = 4;
+template <int VEC>
+__global__ void __launch_bounds__(MOVE_THREADS, 5) k_evict_move(const __grid_constant__ EvictArgs a, int elem, int blocks, int row_shift) {
     typedef typename Unit<VEC>::T U;
     const int list = blockIdx.x / blocks, part = blockIdx.x - list * blocks;
-    const int b = list / a.Hkv, h = list - b * a.Hkv;
+    const int b = list / a.Hkv, h = list - b * a.Hkv, lane = threadIdx.x & 31;
     pdl_wait();
-    if (part == 0 && h == 0 && threadIdx.x == 0) {
-        const int len = a.len[b];
-        a.kv_out[b] = len < 0 ? a.seq.kv_len[b] : len;
-        if (a.settled && len >= 0) a.settled[b] = len;
+    const int n = a.count[list];
+    const bool tells = part == 0 && h == 0 && threadIdx.x == 0;
+    if (n == 0 && !tells) return;
+    const int4 info = a.info[b];
+    if (tells) {
+        a.kv_out[b] = info.x < 0 ? a.seq.kv_len[b] : info.x;
+        if (a.settled && info.x >= 0) a.settled[b] = info.x;
     }
-    const int n = a.count[list], row = a.D * elem / VEC;            // units of a row
+    const int warps = blocks * (MOVE_THREADS / 32), each = min(32, (n + warps - 1) / warps);
     const int2* moves = a.list + (size_t)list * a.list_cap;
-    const long long items = (long long)n * row * 2;                 // units of keys, then of values, move after move
-    for (long long i = (long long)part * MOVE_THREADS + threadIdx.x; i < items; i += (long long)blocks * MOVE_THREADS) {
-        const int mv = (int)(i / (2 * row)), r = (int)(i - (long long)mv * 2 * row);
-        const int2 x = moves[mv];
-        const int fi = page_index(a.pages, x.x), ti = page_index(a.pages, x.y);
-        const int fp = load_page(a.seq, a.pages, b, fi), tp = load_page(a.seq, a.pages, b, ti);
-        if (fp < 0 || tp < 0) continue;
-        char* base = reinterpret_cast<char*>(r < row ? a.pages.k : a.pages.v);
-        const int u = r < row ? r : r - row;
-        const U v = *reinterpret_cast<const U*>(base + row_offset(a.pages, fp, x.x - fi * a.pages.page_size, h) * elem + (size_t)u * VEC);
-        *reinterpret_cast<U*>(base + row_offset(a.pages, tp, x.y - ti * a.pages.page_size, h) * elem + (size_t)u * VEC) = v;
+    for (long long m0 = (long long)(part * (MOVE_THREADS / 32) + (int)(threadIdx.x >> 5)) * each; m0 < n; m0 += (long long)warps * each) {
+        const int have = (int)min((long long)each, n - m0);
+        long long from = 0, to = -1;                // bytes behind k and behind v
+        if (lane < have) {
+            const int2 x = moves[m0 + lane];
+            const int fi = page_index(a.pages, x.x), ti = page_index(a.pages, x.y), fs = x.x - fi * a.pages.page_size, ts = x.y - ti * a.pages.page_size;
+            int fp = table_entry(a.seq, b, fi), tp = table_entry(a.seq, b, ti);
+            fp = named(a.pages, fp);
+            tp = named(a.pages, tp);
+            if (fp < 0 || tp < 0) set_error(a.seq.status, DEV_E_INDEX);
+            else {
+                from = (long long)row_offset(a.pages, fp, fs, h) * elem;
+                to = (long long)row_offset(a.pages, tp, ts, h) * elem;
+                const float score = reinterpret_cast<const float*>(a.scores.p)[slot_offset(a.scores, fp, fs, h)];
+                int pos = info.z + x.x;
+                if (a.positions.p && x.x < info.y) pos = reinterpret_cast<const int32_t*>(a.positions.p)[slot_offset(a.positions, fp, fs, h)];
+                reinterpret_cast<float*>(a.scores.p)[slot_offset(a.scores, tp, ts, h)] = score;
+                if (a.positions.p) reinterpret_cast<int32_t*>(a.positions.p)[slot_offset(a.positions, tp, ts, h)] = pos;
+            }
+        }
+        const int units = 2 << row_shift, items = have * units;     // units of keys, then of values, move after move
+        for (int i0 = 0; i0 < items; i0 += 32 * MOVE_AHEAD) {
+            U v[MOVE_AHEAD];
+            char* dst[MOVE_AHEAD];
+#pragma unroll
+            for (int j = 0; j < MOVE_AHEAD; ++j) {
+                const int i = i0 + j * 32 + lane, mv = (i >> (row_shift + 1)) & 31, u = i & (units - 1);
+                const long long f = __shfl_sync(0xffffffffu, from, mv), t = __shfl_sync(0xffffffffu, to, mv);
+                char* base = reinterpret_cast<char*>(u >> row_shift ? a.pages.v : a.pages.k) + (size_t)(u & ((1 << row_shift) - 1)) * VEC;
+                dst[j] = i < items && t >= 0 ? base + t : nullptr;
+                if (dst[j]) v[j] = *reinterpret_cast<const U*>(base + f);
+            }
+#pragma unroll
+            for (int j = 0; j < MOVE_AHEAD; ++j)
+                if (dst[j]) *reinterpret_cast<U*>(dst[j]) = v[j];
+        }
     }
 }
 
@@ -305,24 +506,42 @@ __global__ void __launch_bounds__(ACCEPT_THREADS) k_paged_accept(const __grid_co
     }
 }
 
+
+template <int VEC>
+cudaError_t run_select(const EvictArgs& a, int elem, int cl, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.seq.batch * a.Hkv) * cl);
+    cfg.blockDim = dim3(SELECT_THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cl;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_evict_select<VEC>, a, elem);
+}
+template <int VEC>
+int run_evict(const EvictArgs& a, int elem, int n_sm, cudaStream_t s) {
+    const int lists = a.seq.batch * a.Hkv;
+    int cl = 1;
+    while (cl < MAX_CL && a.seq.kv_cap > cl * KEYS) cl *= 2;
+    if (run_select<VEC>(a, elem, cl, s) != cudaSuccess) return -1;
+    const long long want = (long long)n_sm * 8 / lists;
+    const int blocks = want < 1 ? 1 : (int)want;
+    return launch_k(k_evict_move<VEC>, dim3((unsigned)lists * blocks), dim3(MOVE_THREADS), 0, s, true, a, elem, blocks, shift_of(a.D * elem / VEC)) != cudaSuccess;
+}
+
 }  // namespace
 
 int launch_evict(int dtype, const EvictArgs& a, int n_sm, cudaStream_t s) {
-    const int lists = a.seq.batch * a.Hkv, elem = dtype == 0 ? 4 : 2;
-    const int keys = a.seq.kv_cap < KEYS_IN_SMEM ? a.seq.kv_cap : KEYS_IN_SMEM;
-    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_evict_select), KEYS_IN_SMEM * 4)) return -1;
-    k_evict_select<<<lists, SELECT_THREADS, keys * 4, s>>>(a);
-    const long long want = (long long)n_sm * 8 / lists;
-    const int blocks = want < 1 ? 1 : (int)want;
-    const dim3 grid((unsigned)lists * blocks), block(MOVE_THREADS);
-    cudaError_t e;
+    const int elem = dtype == 0 ? 4 : 2;
     switch (a.vec * elem) {
-        case 16: e = launch_k(k_evict_move<16>, grid, block, 0, s, true, a, elem, blocks); break;
-        case 8: e = launch_k(k_evict_move<8>, grid, block, 0, s, true, a, elem, blocks); break;
-        case 4: e = launch_k(k_evict_move<4>, grid, block, 0, s, true, a, elem, blocks); break;
-        default: e = launch_k(k_evict_move<2>, grid, block, 0, s, true, a, elem, blocks);
+        case 16: return run_evict<16>(a, elem, n_sm, s);
+        case 8: return run_evict<8>(a, elem, n_sm, s);
+        case 4: return run_evict<4>(a, elem, n_sm, s);
+        default: return run_evict<2>(a, elem, n_sm, s);
     }
-    return e != cudaSuccess;
 }
 
 int launch_accept(int dtype, const AcceptArgs& a, cudaStream_t s) {
