@@ -180,16 +180,19 @@ __device__ __forceinline__ void next_chunk(const KeyWeightArgs& w, WCursor& k) {
 
 // The first position that an observed token sees: in front of it a table may name pages that there are no longer, which is no error.
 __device__ __forceinline__ int first_observed(const KeyWeightArgs& w, const WSeq& x) { return w.a.window > 0 ? x.s.kv - x.s.n + x.i0 - w.a.window + 1 : 0; }
-// Where the score of position pos (< kv) of the cursor's sequence is; NULL if the table names no page.
-__device__ __forceinline__ float* score_at(const KeyWeightArgs& w, const WCursor& k, int pos) {
-    const int index = page_index(w.a.pages, pos), page = __ldg(w.a.seq.table + (size_t)k.b * w.a.seq.table_stride + index);
+// The table's entry for position pos (< kv), whatever it says, and where the position's score is; NULL if the entry names no page.
+__device__ __forceinline__ int score_entry(const KeyWeightArgs& w, const WCursor& k, int pos) {
+    return __ldg(w.a.seq.table + (size_t)k.b * w.a.seq.table_stride + page_index(w.a.pages, pos));
+}
+__device__ __forceinline__ float* score_of(const KeyWeightArgs& w, const WCursor& k, int pos, int page) {
     if (page < 0 || page >= w.a.pages.n_pages) {
         if (pos >= first_observed(w, k.x)) set_error(w.a.seq.status, DEV_E_INDEX);
         return nullptr;
     }
-    return reinterpret_cast<float*>(w.scores.p) + (long long)page * w.scores.page + (long long)(pos - index * w.a.pages.page_size) * w.scores.tok +
+    return reinterpret_cast<float*>(w.scores.p) + (long long)page * w.scores.page + (long long)(pos - page_index(w.a.pages, pos) * w.a.pages.page_size) * w.scores.tok +
            (long long)k.kvh * w.scores.head;
 }
+__device__ __forceinline__ float* score_at(const KeyWeightArgs& w, const WCursor& k, int pos) { return score_of(w, k, pos, score_entry(w, k, pos)); }
 // whether position pos of the sequence has a score already: new tokens begin at zero
 __device__ __forceinline__ bool has_old(const KeyWeightArgs& w, const Seq& s, int pos) { return w.keep != 0.f && pos < s.kv - s.n; }
 // What becomes of position pos, given the sum of its weights.

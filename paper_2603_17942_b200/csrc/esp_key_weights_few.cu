@@ -1,7 +1,7 @@
 // Weights of cached positions from a handful of (token, query head) pairs: bf16, heads of 64 or 128, up to 32 observed pairs of a sequence and KV head.
 //
 // Every cached key is read once, so memory bounds it, as in the attention of single tokens, and it is built the same way: each warp is a worker
-// with a share of the line of chunks, a ring of stages of its own that TMA fills, and no partner to wait for.  The products are m16n8k16 with the
+// with a share of the line of chunks, a stage of its own that TMA fills, and no partner to wait for.  The products are m16n8k16 with the
 // keys as rows, so that what belongs to a key ends in four lanes of a quad: queries in registers for the whole sequence and head, weights and their sum over the
 // columns in registers, two shuffles, one number written for each key.  All tokens fit one tile, so no chunk has several owners and nothing is joined.
 #include <string.h>
@@ -16,8 +16,12 @@ namespace {
 using namespace tc;
 using namespace paged;
 
-constexpr int WARPS = 6, STAGES = 2, STAGE_BYTES = 16384;
-constexpr int SMEM = 1024 + WARPS * STAGES * STAGE_BYTES + 256;
+// Warps, stages of a warp and their KB (us, 64 sequences of 1k to 8k positions, 32/8 heads of 128): 4 x 3 x 16 178, 6 x 2 x 16 135, 8 x 3 x 8 133, 12 x 2 x 8 104, 10 x 1 x 16 99,
+// 16 x 1 x 8 93, 12 x 1 x 16 90, 20 x 1 x 8 and 24 x 1 x 8 88; one sequence of 4k 6.3 with 16 KB, 5.7 with 8.  A warp's own chain through a stage is long beside
+// the stage's bytes, so many warps with one stage each do better than few that run ahead.  With more columns the queries' registers leave room for 12.
+constexpr int STAGE_BYTES = 8192;
+template <int NB> constexpr int WARPS = NB <= 2 ? 20 : 12;
+template <int NB> constexpr int SMEM = 1024 + WARPS<NB> * STAGE_BYTES + 512;
 
 struct FewParams {
     CUtensorMap map_k;    // [pages][heads][halves][slots][64], box 64 x box_rows x halves
@@ -37,20 +41,20 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
 
 // NB: columns of the products in eights.
 template <int D, int NB>
-__global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_constant__ FewParams p) {
-    constexpr int HALVES = D / 64, KEYS = STAGE_BYTES / (D * 2), MT = KEYS / 16, MINE = MT / 4;      // a lane writes the keys of every fourth row of products
+__global__ void __launch_bounds__(WARPS<NB> * 32, 1) k_key_weights_few(const __grid_constant__ FewParams p) {
+    constexpr int HALVES = D / 64, KEYS = STAGE_BYTES / (D * 2), MT = KEYS / 16, MINE = (MT + 3) / 4;      // a lane writes the keys of every fourth row of products
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    unsigned char* ring = smem + warp * STAGES * STAGE_BYTES;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + WARPS * STAGES * STAGE_BYTES) + warp * STAGES;
-    volatile int* s_abort = reinterpret_cast<volatile int*>(smem + WARPS * STAGES * STAGE_BYTES + WARPS * STAGES * 8) + warp;
+    unsigned char* stage = smem + warp * STAGE_BYTES;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + WARPS<NB> * STAGE_BYTES) + warp;
+    volatile int* s_abort = reinterpret_cast<volatile int*>(smem + WARPS<NB> * STAGE_BYTES + WARPS<NB> * 8) + warp;
     const KeyWeightArgs& w = p.w;
     const PagedAttnArgs& a = w.a;
     const int worker = warp * gridDim.x + blockIdx.x;       // the first workers on SMs of their own
     if (lane == 0) {
         prefetch_tensormap(&p.map_k);
-        for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1);
+        mbar_init(full, 1);
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -61,7 +65,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_
     if (!deal_keys<KEYS>(w, worker, lane, share, c)) return;
     const uint32_t begin = share.begin(worker), end = share.begin(worker + 1);
 
-    // ---- requests, up to STAGES units ahead of the products
+    // ---- requests, one unit ahead of the products
     WCursor ci = c;
     uint32_t ui = begin;
     const int n_boxes = KEYS >> p.box_shift, box_bytes = (128 * HALVES) << p.box_shift;
@@ -78,12 +82,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_
         }
     };
     auto request = [&]() {
-        const uint32_t st = (ui - begin) % STAGES;
-        unsigned char* dst = ring + st * STAGE_BYTES;
-        if (lane == 0) mbar_expect_tx(&full[st], STAGE_BYTES);
+        if (lane == 0) mbar_expect_tx(full, STAGE_BYTES);
         for (int i = 0; i < n_boxes; ++i) {
             const int pg = __shfl_sync(0xffffffffu, page, i), sl = __shfl_sync(0xffffffffu, slot, i);
-            if (lane == 0) tma_load_5d(dst + i * box_bytes, &p.map_k, sl, ci.kvh, pg, &full[st]);
+            if (lane == 0) tma_load_5d(stage + i * box_bytes, &p.map_k, sl, ci.kvh, pg, full);
         }
         __syncwarp();
         if (++ui < end) {
@@ -92,12 +94,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_
         }
     };
     look_up();
-    for (int i = 0; i < STAGES && ui < end; ++i) request();
+    request();
 
     // ---- products
     const int g = lane >> 2, c4 = lane & 3;
     auto row_off = [&](int r) { return (uint32_t)((r >> p.box_shift) * box_bytes + (r & ((1 << p.box_shift) - 1)) * 128); };
     auto chunk_off = [&](int ch) { return (uint32_t)(((ch >> 3) << (p.box_shift + 7)) + (((ch & 7) ^ (lane & 7)) << 4)); };
+    int entry[MINE][2];                  // the page table's for the positions whose scores this lane writes
+    auto entries = [&](const WCursor& k) {
+#pragma unroll
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) entry[m][r] = score_entry(w, k, min(k.c * KEYS + (m * 4 + c4) * 16 + r * 8 + g, k.x.s.kv - 1));
+    };
+    entries(c);
     bool ok = true;
     int b_of = -1, h_of = -1;            // whose queries the registers hold
     uint32_t qb[D / 16][NB][2];
@@ -133,19 +143,22 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_
                 }
             }
         }
-        // the places of this lane's scores, and what they hold, while the keys are on their way
+        // the places of this lane's scores, and what they hold, while the keys are on their way; the next chunk's table entries for its turn
         float *to[MINE][2], old[MINE][2];
 #pragma unroll
         for (int m = 0; m < MINE; ++m)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int pos = p0 + (m * 4 + c4) * 16 + r * 8 + g;
-                to[m][r] = pos < s.kv ? score_at(w, c, pos) : nullptr;
-                old[m][r] = to[m][r] && has_old(w, s, pos) ? w.keep * *to[m][r] : 0.f;
+                to[m][r] = pos < s.kv && m * 4 + c4 < MT ? score_of(w, c, pos, entry[m][r]) : nullptr;
+                old[m][r] = 0.f;
+                if (to[m][r] && has_old(w, s, pos)) old[m][r] = *to[m][r];
             }
-        const uint32_t st = (u - begin) % STAGES;
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], ((u - begin) / STAGES) & 1, s_abort))) { ok = false; break; }
-        const uint32_t k_addr = smem_u32(ring + st * STAGE_BYTES);
+        WCursor cn = c;
+        if (u + 1 < end) next_chunk<KEYS>(w, cn);
+        entries(cn);
+        if (!__all_sync(0xffffffffu, mbar_wait(full, (u - begin) & 1, s_abort))) { ok = false; break; }
+        const uint32_t k_addr = smem_u32(stage);
         // a chunk that some token does not see as a whole
         const bool edge = p0 + KEYS > (a.anc ? L : L + c.x.i0 + 1) || (a.window > 0 && p0 < L + s.n - a.window);
         float sum[MT][2];
@@ -191,10 +204,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_key_weights_few(const __grid_
             for (int r = 0; r < 2; ++r) {
                 float x = sum[m * 4][r];
 #pragma unroll
-                for (int q = 1; q < 4; ++q) x = c4 == q ? sum[m * 4 + q][r] : x;
-                if (to[m][r]) *to[m][r] = old[m][r] + x;
+                for (int q = 1; q < 4 && m * 4 + q < MT; ++q) x = c4 == q ? sum[m * 4 + q][r] : x;
+                if (to[m][r]) *to[m][r] = fmaf(w.keep, old[m][r], x);
             }
-        if (u + 1 < end) next_chunk<KEYS>(w, c);
+        c = cn;
     }
     if (!ok) {
         if (lane == 0) set_error(a.seq.status, DEV_E_WAIT_TIMEOUT);
@@ -208,9 +221,10 @@ int observed_pairs(const KeyWeightArgs& w) {
 }
 
 template <int D, int NB>
-int run(const FewParams& p, cudaStream_t s) {
-    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_key_weights_few<D, NB>), SMEM)) return -1;
-    k_key_weights_few<D, NB><<<p.w.a.n_cta / WARPS, WARPS * 32, SMEM, s>>>(p);
+int run(FewParams& p, int n_sm, cudaStream_t s) {
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_key_weights_few<D, NB>), SMEM<NB>)) return -1;
+    p.w.a.n_cta = n_sm * WARPS<NB>;
+    k_key_weights_few<D, NB><<<n_sm, WARPS<NB> * 32, SMEM<NB>, s>>>(p);
     return 0;
 }
 
@@ -234,11 +248,10 @@ int launch_key_weights_few(KeyWeightArgs w, int n_sm, cudaStream_t s) {
     const int pairs = observed_pairs(w);
     a.rows = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;       // one tile
     a.rows_shift = shift_of(a.rows);
-    a.n_cta = n_sm * WARPS;
     a.min_units = 1;
     p.w = w;
-    if (a.D == 128) return pairs <= 8 ? run<128, 1>(p, s) : (pairs <= 16 ? run<128, 2>(p, s) : run<128, 4>(p, s));
-    return pairs <= 8 ? run<64, 1>(p, s) : (pairs <= 16 ? run<64, 2>(p, s) : run<64, 4>(p, s));
+    if (a.D == 128) return pairs <= 8 ? run<128, 1>(p, n_sm, s) : (pairs <= 16 ? run<128, 2>(p, n_sm, s) : run<128, 4>(p, n_sm, s));
+    return pairs <= 8 ? run<64, 1>(p, n_sm, s) : (pairs <= 16 ? run<64, 2>(p, n_sm, s) : run<64, 4>(p, n_sm, s));
 }
 
 }  // namespace esp

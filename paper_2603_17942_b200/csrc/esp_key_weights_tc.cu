@@ -2,9 +2,9 @@
 //
 // A CTA holds a chunk of 256 keys in shared memory, as two subtiles of 128, and walks the tiles of up to 128 (token, query head) pairs that see it:
 //   S_s = K_s Q^T    tcgen05.mma with the keys as rows, both operands K-major in shared memory, 128 x 128 fp32 in tensor memory, two sets of both subtiles;
-//   weights          one thread per key (= tensor-memory lane): exp(scale s - lse) of each column, added up in a register; a mask is a range of columns.
+//   weights          two threads per key (= tensor-memory lane), for a half of the columns each: exp(scale s - lse), added up in a register; a mask is a range of columns.
 // So a key's sum never leaves its thread while the chunk stays, keys are read once and queries once for every 256 keys.
-// Roles: warp 0 TMA (keys and queries), warp 1 issues the products, warp 2 brings the tiles' lse, warps 4-7 and 8-11 the weights of a subtile.  Every wait is bounded; one
+// Roles: warp 0 TMA (keys and queries), warp 1 issues the products, warp 2 brings the tiles' lse, warps 4-19 have the weights.  Every wait is bounded; one
 // that runs out is recorded, the tensor memory is given back and the kernel returns.
 #include <string.h>
 
@@ -20,15 +20,15 @@ using namespace paged;
 
 constexpr int CK = KEY_WEIGHT_KEYS, SUB = 128, PAIRS = 128;
 constexpr int HALF_BYTES = 128 * 128;     // 128 rows x 64 elements, 128-byte swizzle
-constexpr int THREADS = 384, SUM_WARPS = 8;
+constexpr int SUM_WARPS = 16, THREADS = 128 + SUM_WARPS * 32;
 constexpr int TMEM_COLS = 512;            // [set][subtile][128]
 
 template <int D>
 struct Cfg {
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;         // 128 rows of a head
-    static constexpr int KST = D == 128 ? 2 : 3, QST = D == 128 ? 2 : 4;
-    static constexpr int OFF_Q = KST * 2 * TILE_BYTES, OFF_LSE = OFF_Q + QST * TILE_BYTES, OFF_BAR = OFF_LSE + QST * PAIRS * 4;
+    static constexpr int KST = D == 128 ? 2 : 3, QST = D == 128 ? 2 : 4, LST = 4;
+    static constexpr int OFF_Q = KST * 2 * TILE_BYTES, OFF_LSE = OFF_Q + QST * TILE_BYTES, OFF_HALF = OFF_LSE + LST * PAIRS * 4, OFF_BAR = OFF_HALF + CK * 4;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     // kind::f16 instruction descriptor: D = f32, A = B = bf16, M = 128, N = 128
     static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -48,6 +48,12 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
         : "memory");
 }
 
+// acc + 2^x of a pair, by the special-function unit
+__device__ __forceinline__ uint64_t mufu_add(uint64_t x, uint64_t acc) {
+    float x0, x1;
+    attn::unpack2(x, x0, x1);
+    return attn::add2(acc, attn::pack2(attn::ex2_approx(x0), attn::ex2_approx(x1)));
+}
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_constant__ TcParams p) {
     using C = Cfg<D>;
@@ -55,15 +61,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
     __shared__ int2 s_box[32];             // page and slot of a chunk's boxes
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *sK = smem, *sQ = smem + C::OFF_Q;
-    float* s_lse = reinterpret_cast<float*>(smem + C::OFF_LSE);        // [QST][PAIRS] -lse in the log2 domain
+    float* s_lse = reinterpret_cast<float*>(smem + C::OFF_LSE);        // [LST][PAIRS] -lse in the log2 domain
+    float* s_half = reinterpret_cast<float*>(smem + C::OFF_HALF);      // [CK] sums over the second half of the columns
     uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR); // [KST] keys of a chunk have landed
     uint64_t* k_empty = k_full + C::KST;                               // [KST] their last product has completed
     uint64_t* q_full = k_empty + C::KST;                               // [QST] queries of a tile have landed
-    uint64_t* l_full = q_full + C::QST;                                // [QST] its lse stand
-    uint64_t* q_empty = l_full + C::QST;                               // [QST] the products and the eight warps are done with both
-    uint64_t* s_full = q_empty + C::QST;                               // [2] scores of a set
+    uint64_t* q_empty = q_full + C::QST;                               // [QST] its products have completed
+    uint64_t* l_full = q_empty + C::QST;                               // [LST] a tile's lse stand (a ring of their own: the queries' places are free a tile earlier)
+    uint64_t* l_empty = l_full + C::LST;                               // [LST] they have been read
+    uint64_t* s_full = l_empty + C::LST;                               // [2] scores of a set
     uint64_t* s_free = s_full + 2;                                     // [2] they have been read
-    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_free + 2);
+    uint64_t* h_full = s_free + 2;                                     // [8] the second half's sums of 32 keys stand
+    uint64_t* h_free = h_full + 8;                                     // [8] they have been taken
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(h_free + 8);
     volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
     const KeyWeightArgs& w = p.w;
@@ -73,8 +83,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
         prefetch_tensormap(&p.map_k);
         prefetch_tensormap(&p.map_q);
         for (int i = 0; i < C::KST; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
-        for (int i = 0; i < C::QST; ++i) { mbar_init(&q_full[i], 1); mbar_init(&l_full[i], 1); mbar_init(&q_empty[i], 1 + SUM_WARPS); }
+        for (int i = 0; i < C::QST; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
+        for (int i = 0; i < C::LST; ++i) { mbar_init(&l_full[i], 1); mbar_init(&l_empty[i], SUM_WARPS); }
         for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_free[i], SUM_WARPS); }
+        for (int i = 0; i < 8; ++i) { mbar_init(&h_full[i], 1); mbar_init(&h_free[i], 1); }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -192,30 +204,37 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                     const int col = j * 32 + lane, row = (col * p.group_inv) >> 16;
                     x[j] = col < pairs ? __ldg(w.lse + (size_t)(c.x.s.start + r0 + row) * a.Hq + c.kvh * a.group + col - row * a.group) * -1.4426950408889634f : 0.f;
                 }
-                const uint32_t sq = n % C::QST;
-                if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[sq], ((n / C::QST) & 1) ^ 1, s_abort))) { ok = false; break; }
+                const uint32_t sl = n % C::LST;
+                if (!__all_sync(0xffffffffu, mbar_wait(&l_empty[sl], ((n / C::LST) & 1) ^ 1, s_abort))) { ok = false; break; }
 #pragma unroll
-                for (int j = 0; j < PAIRS / 32; ++j) s_lse[sq * PAIRS + j * 32 + lane] = x[j];
+                for (int j = 0; j < PAIRS / 32; ++j) s_lse[sl * PAIRS + j * 32 + lane] = x[j];
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&l_full[sq]);
+                if (lane == 0) mbar_arrive(&l_full[sl]);
             }
             u += max(pc.n, 1);
             if (u < end) next_chunk<CK>(w, c);
         }
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
     } else if (warp >= 4) {
-        // ---------------- weights: a thread per key
-        const int sub = (warp - 4) >> 2, key = sub * SUB + (warp & 3) * 32 + lane;
-        const uint32_t s_addr = tmem_base + sub * 128 + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t n = 0;
+        // ---------------- weights: warps 4-7 and 8-11 the first half of the columns of a subtile, 12-15 and 16-19 the second
+        const int sub = ((warp - 4) >> 2) & 1, half = (warp - 4) >> 3, pair = sub * 4 + (warp & 3), key = pair * 32 + lane;
+        const uint32_t s_addr = tmem_base + sub * 128 + half * 64 + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t n = 0, n_p = 0;
         bool ok = true;
-        for (uint32_t u = begin; u < end && ok;) {
+        for (uint32_t u = begin; u < end && ok; ++n_p) {
             const WPiece pc = make_piece(c, begin, u, end);
             const Seq s = c.x.s;
             const int L = s.kv - s.n, p0 = c.c * CK, pos = p0 + key;
-            float sum0 = 0.f, sum1 = 0.f;
+            // the place of the score, and what it holds, before the weights are there
+            float *to = nullptr, old = 0.f;
+            if (half == 0 && pc.slot < 0 && pos < s.kv) {
+                to = score_at(w, c, pos);
+                if (to && has_old(w, s, pos)) old = *to;
+            }
+            float sum0 = 0.f;
+            uint64_t acc_a = 0, acc_b = 0;
             for (int t = pc.t0; t < pc.t0 + pc.n; ++t, ++n) {
-                const uint32_t sq = n % C::QST, set = n & 1;
+                const uint32_t sl = n % C::LST, set = n & 1;
                 const int r0 = c.x.i0 + t * a.rows, nr = min(a.rows, s.n - r0);
                 // columns that see this key: all pairs of the tile, or a range of its tokens, or, inside the block of a tree, as their masks say
                 int lo = 0, hi = nr * a.group;
@@ -231,47 +250,45 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                         if (a.window > 0) hi = (int)min(max((long long)pos - L + a.window - r0, 0ll), (long long)nr) * a.group;
                     }
                 }
-                ok = __all_sync(0xffffffffu, mbar_wait(&l_full[sq], (n / C::QST) & 1, s_abort) && mbar_wait(&s_full[set], (n >> 1) & 1, s_abort));
+                ok = __all_sync(0xffffffffu, mbar_wait(&l_full[sl], (n / C::LST) & 1, s_abort) && mbar_wait(&s_full[set], (n >> 1) & 1, s_abort));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const float4* nl = reinterpret_cast<const float4*>(s_lse + sq * PAIRS);
-                uint32_t x[2][32];
-                tmem_ld32_issue(s_addr + set * 256, x[0]);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (b < 3) tmem_ld32_issue(s_addr + set * 256 + (b + 1) * 32, x[(b + 1) & 1]);
-                    const uint32_t(&y)[32] = x[b & 1];
+                const float4* nl = reinterpret_cast<const float4*>(s_lse + sl * PAIRS + half * 64);
+#pragma unroll 1
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t y[32];
+                    tmem_ld32(s_addr + set * 256 + b * 32, y);
                     if (!edge) {
+                        const uint64_t scale2 = attn::pack2(a.scale_log2, a.scale_log2);
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
                             const float4 m = nl[b * 8 + j / 4];
-                            sum0 += attn::ex2_approx(fmaf(__uint_as_float(y[j]), a.scale_log2, m.x));
-                            sum1 += attn::ex2_approx(fmaf(__uint_as_float(y[j + 1]), a.scale_log2, m.y));
-                            sum0 += attn::ex2_approx(fmaf(__uint_as_float(y[j + 2]), a.scale_log2, m.z));
-                            sum1 += attn::ex2_approx(fmaf(__uint_as_float(y[j + 3]), a.scale_log2, m.w));
+                            const uint64_t e0 = attn::fma2(attn::pack2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), scale2, attn::pack2(m.x, m.y));
+                            const uint64_t e1 = attn::fma2(attn::pack2(__uint_as_float(y[j + 2]), __uint_as_float(y[j + 3])), scale2, attn::pack2(m.z, m.w));
+                            acc_a = mufu_add(e0, acc_a);
+                            acc_b = mufu_add(e1, acc_b);
                         }
                     } else if (!__any_sync(0xffffffffu, tree)) {
+                        const int l = lo - half * 64 - b * 32, r = hi - half * 64 - b * 32;
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
                             const float4 m = nl[b * 8 + j / 4];
                             const float mm[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const int col = b * 32 + j + e;
                                 const float v = attn::ex2_approx(fmaf(__uint_as_float(y[j + e]), a.scale_log2, mm[e]));
-                                sum0 += col >= lo && col < hi ? v : 0.f;
+                                sum0 += j + e >= l && j + e < r ? v : 0.f;
                             }
                         }
                     } else {
                         const int bit = min(max(pos - L, 0), 127);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
-                            const int col = b * 32 + j, i = r0 + ((col * p.group_inv) >> 16);
+                            const int col = half * 64 + b * 32 + j, i = r0 + ((col * p.group_inv) >> 16);
                             bool in = col >= lo && col < hi;
                             if (tree && in)
                                 in = L + i >= 0 && pos - L < 128 && ((__ldg(a.anc + 2 * (size_t)(s.start + i) + (bit >> 6)) >> (bit & 63)) & 1);
-                            const float v = attn::ex2_approx(fmaf(__uint_as_float(y[j]), a.scale_log2, reinterpret_cast<const float*>(nl)[col]));
+                            const float v = attn::ex2_approx(fmaf(__uint_as_float(y[j]), a.scale_log2, reinterpret_cast<const float*>(nl)[b * 32 + j]));
                             sum0 += in ? v : 0.f;
                         }
                     }
@@ -280,13 +297,29 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&s_free[set]);
-                    mbar_arrive(&q_empty[sq]);
+                    mbar_arrive(&l_empty[sl]);
                 }
             }
             if (!ok) break;
-            if (pos < s.kv) {
-                if (pc.slot < 0) store_score(w, c, pos, sum0 + sum1);
-                else w.part[((size_t)blockIdx.x * 2 + pc.slot) * KEY_WEIGHT_KEYS + key] = sum0 + sum1;
+            // the halves' sums together
+            float sum, sa0, sa1, sb0, sb1;
+            attn::unpack2(acc_a, sa0, sa1);
+            attn::unpack2(acc_b, sb0, sb1);
+            sum = sum0 + ((sa0 + sa1) + (sb0 + sb1));
+            if (half == 1) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&h_free[pair], (n_p & 1) ^ 1, s_abort));
+                if (!ok) break;
+                s_half[key] = sum;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&h_full[pair]);
+            } else {
+                ok = __all_sync(0xffffffffu, mbar_wait(&h_full[pair], n_p & 1, s_abort));
+                if (!ok) break;
+                sum += s_half[key];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&h_free[pair]);
+                if (pc.slot >= 0) w.part[((size_t)blockIdx.x * 2 + pc.slot) * KEY_WEIGHT_KEYS + key] = sum;
+                else if (to) *to = has_old(w, s, pos) ? fmaf(w.keep, old, sum) : sum;
             }
             u += max(pc.n, 1);
             if (u < end) next_chunk<CK>(w, c);
@@ -343,7 +376,9 @@ int launch_key_weights_tc(KeyWeightArgs w, int n_sm, cudaStream_t s) {
     a.min_units = 1;
     p.w = w;
     const int rc = a.D == 128 ? run<128>(p, s) : run<64>(p, s);
-    return rc ? rc : launch_key_weights_join(w, CK, s);
+    // (where a sequence's observed tokens fit one tile no chunk has two owners)
+    const long long observed = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;
+    return rc || observed <= a.rows ? rc : launch_key_weights_join(w, CK, s);
 }
 
 }  // namespace esp
