@@ -4,7 +4,7 @@
 //   S_s = K_s Q^T    tcgen05.mma with the keys as rows, both operands K-major in shared memory, 128 x 128 fp32 in tensor memory, two sets of both subtiles;
 //   weights          two threads per key (= tensor-memory lane), for a half of the columns each: exp(scale s - lse), added up in a register; a mask is a range of columns.
 // So a key's sum never leaves its thread while the chunk stays, keys are read once and queries once for every 256 keys.
-// Roles: warp 0 TMA (keys and queries), warp 1 issues the products, warp 2 brings the tiles' lse, warps 4-19 have the weights.  Every wait is bounded; one
+// Roles: warps 0 and 3 TMA (a subtile's keys each, warp 0 the queries too), warp 1 issues the products, warp 2 brings the tiles' lse, warps 4-19 have the weights.  Every wait is bounded; one
 // that runs out is recorded, the tensor memory is given back and the kernel returns.
 #include <string.h>
 
@@ -27,7 +27,7 @@ template <int D>
 struct Cfg {
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;         // 128 rows of a head
-    static constexpr int KST = D == 128 ? 2 : 3, QST = D == 128 ? 2 : 4, LST = 4;
+    static constexpr int KST = D == 128 ? 2 : 3, QST = D == 128 ? 2 : 4, LST = 4;      // (even: a tile of every other chunk has its own places)
     static constexpr int OFF_Q = KST * 2 * TILE_BYTES, OFF_LSE = OFF_Q + QST * TILE_BYTES, OFF_HALF = OFF_LSE + LST * PAIRS * 4, OFF_BAR = OFF_HALF + CK * 4;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     // kind::f16 instruction descriptor: D = f32, A = B = bf16, M = 128, N = 128
@@ -48,17 +48,18 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
         : "memory");
 }
 
-// acc + 2^x of a pair, by the special-function unit
-__device__ __forceinline__ uint64_t mufu_add(uint64_t x, uint64_t acc) {
+// acc + 2^x of a pair
+__device__ __forceinline__ uint64_t exp_add(uint64_t x, uint64_t acc) {
     float x0, x1;
     attn::unpack2(x, x0, x1);
     return attn::add2(acc, attn::pack2(attn::ex2_approx(x0), attn::ex2_approx(x1)));
 }
-template <int D>
+// ONE: no sequence has more observed tokens than a tile.
+template <int D, bool ONE>
 __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_constant__ TcParams p) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ int2 s_box[32];             // page and slot of a chunk's boxes
+    __shared__ int2 s_box[2][16];          // [subtile] page and slot of a chunk's boxes
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *sK = smem, *sQ = smem + C::OFF_Q;
     float* s_lse = reinterpret_cast<float*>(smem + C::OFF_LSE);        // [LST][PAIRS] -lse in the log2 domain
@@ -82,10 +83,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
     if (threadIdx.x == 0) {
         prefetch_tensormap(&p.map_k);
         prefetch_tensormap(&p.map_q);
-        for (int i = 0; i < C::KST; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < C::KST; ++i) { mbar_init(&k_full[i], 2); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < C::QST; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
-        for (int i = 0; i < C::LST; ++i) { mbar_init(&l_full[i], 1); mbar_init(&l_empty[i], SUM_WARPS); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_free[i], SUM_WARPS); }
+        for (int i = 0; i < C::LST; ++i) { mbar_init(&l_full[i], 1); mbar_init(&l_empty[i], ONE ? SUM_WARPS / 2 : SUM_WARPS); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_free[i], ONE ? SUM_WARPS / 2 : SUM_WARPS); }
         for (int i = 0; i < 8; ++i) { mbar_init(&h_full[i], 1); mbar_init(&h_free[i], 1); }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -104,15 +105,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *s_tmem;
 
-    if (warp == 0) {
-        // ---------------- TMA: the lanes look up a chunk's pages, one lane issues box after box
-        const int n_boxes = CK / p.box_rows;        // a power of two, 32 at most
+    if (warp == 0 || warp == 3) {
+        // ---------------- TMA: the lanes look up a chunk's pages, one lane issues box after box; warp 0 has the first subtile's and the queries, warp 3 the second's
+        const int sub = warp == 3, n_boxes = SUB / p.box_rows;       // a power of two, 16 at most
         uint32_t n_k = 0, n_q = 0;                  // chunks and tiles so far
         bool ok = true;
         for (uint32_t u = begin; u < end && ok;) {
             const WPiece pc = make_piece(c, begin, u, end);
             if (pc.n > 0) {
-                const int pos = c.c * CK + (lane & (n_boxes - 1)) * p.box_rows;
+                const int pos = c.c * CK + sub * SUB + (lane & (n_boxes - 1)) * p.box_rows;
                 int page = a.pages.n_pages, slot = 0;       // a page that there is not reads as zeros
                 if (pos < c.x.s.kv && pos + p.box_rows > first_observed(w, c.x)) {
                     const int index = page_index(a.pages, pos);
@@ -122,21 +123,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                 }
                 const uint32_t st = n_k % C::KST;
                 if (!__all_sync(0xffffffffu, mbar_wait(&k_empty[st], ((n_k / C::KST) & 1) ^ 1, s_abort))) { ok = false; break; }
-                if (lane < n_boxes) s_box[lane] = make_int2(page, slot);
+                if (lane < n_boxes) s_box[sub][lane] = make_int2(page, slot);
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_expect_tx(&k_full[st], 2 * C::TILE_BYTES);
+                    mbar_expect_tx(&k_full[st], C::TILE_BYTES);
+                    unsigned char* dst = sK + (st * 2 + sub) * C::TILE_BYTES;
                     for (int i = 0; i < n_boxes; ++i) {
-                        const int2 b = s_box[i];
-                        const int r = i * p.box_rows;
-                        unsigned char* dst = sK + (st * 2 + r / SUB) * C::TILE_BYTES + (r % SUB) * 128;
+                        const int2 b = s_box[sub][i];
 #pragma unroll
-                        for (int h = 0; h < C::HALVES; ++h) tma_load_4d(dst + h * HALF_BYTES, &p.map_k, h * 64, b.y, c.kvh, b.x, &k_full[st]);
+                        for (int h = 0; h < C::HALVES; ++h) tma_load_4d(dst + i * p.box_rows * 128 + h * HALF_BYTES, &p.map_k, h * 64, b.y, c.kvh, b.x, &k_full[st]);
                     }
                 }
                 __syncwarp();
                 ++n_k;
-                for (int t = pc.t0; t < pc.t0 + pc.n; ++t, ++n_q) {
+                for (int t = pc.t0; t < pc.t0 + pc.n && sub == 0; ++t, ++n_q) {
                     const uint32_t sq = n_q % C::QST;
                     if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[sq], ((n_q / C::QST) & 1) ^ 1, s_abort))) { ok = false; break; }
                     if (lane == 0) {
@@ -216,24 +216,29 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
         }
         if (!ok && lane == 0) { set_error(a.seq.status, DEV_E_WAIT_TIMEOUT); *s_abort = 1; }
     } else if (warp >= 4) {
-        // ---------------- weights: warps 4-7 and 8-11 the first half of the columns of a subtile, 12-15 and 16-19 the second
+        // ---------------- weights.  warps 4-7 and 8-11 (the first of two halves) have the subtiles' first 64 columns, 12-15 and 16-19 the others; where no chunk meets more
+        // than one tile (ONE), the first half of the warps has every other chunk as a whole: nothing is put together, and one chunk's loads and stores fall into the other's exponentials
         const int sub = ((warp - 4) >> 2) & 1, half = (warp - 4) >> 3, pair = sub * 4 + (warp & 3), key = pair * 32 + lane;
-        const uint32_t s_addr = tmem_base + sub * 128 + half * 64 + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_addr = tmem_base + sub * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+        const int col0 = ONE ? 0 : half * 64;
         uint32_t n = 0, n_p = 0;
         bool ok = true;
         for (uint32_t u = begin; u < end && ok; ++n_p) {
             const WPiece pc = make_piece(c, begin, u, end);
             const Seq s = c.x.s;
             const int L = s.kv - s.n, p0 = c.c * CK, pos = p0 + key;
+            const bool mine = !ONE || (pc.n > 0 ? (int)(n & 1) == half : half == 0);
+            const bool writes = ONE ? mine : half == 0;
             // the place of the score, and what it holds, before the weights are there
             float *to = nullptr, old = 0.f;
-            if (half == 0 && pc.slot < 0 && pos < s.kv) {
+            if (writes && pc.slot < 0 && pos < s.kv) {
                 to = score_at(w, c, pos);
                 if (to && has_old(w, s, pos)) old = *to;
             }
             float sum0 = 0.f;
             uint64_t acc_a = 0, acc_b = 0;
             for (int t = pc.t0; t < pc.t0 + pc.n; ++t, ++n) {
+                if (!mine) continue;
                 const uint32_t sl = n % C::LST, set = n & 1;
                 const int r0 = c.x.i0 + t * a.rows, nr = min(a.rows, s.n - r0);
                 // columns that see this key: all pairs of the tile, or a range of its tokens, or, inside the block of a tree, as their masks say
@@ -253,23 +258,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                 ok = __all_sync(0xffffffffu, mbar_wait(&l_full[sl], (n / C::LST) & 1, s_abort) && mbar_wait(&s_full[set], (n >> 1) & 1, s_abort));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const float4* nl = reinterpret_cast<const float4*>(s_lse + sl * PAIRS + half * 64);
+                const float4* nl = reinterpret_cast<const float4*>(s_lse + sl * PAIRS + col0);
 #pragma unroll 1
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < (ONE ? 4 : 2); ++b) {
                     uint32_t y[32];
-                    tmem_ld32(s_addr + set * 256 + b * 32, y);
+                    tmem_ld32(s_addr + set * 256 + col0 + b * 32, y);
                     if (!edge) {
                         const uint64_t scale2 = attn::pack2(a.scale_log2, a.scale_log2);
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
                             const float4 m = nl[b * 8 + j / 4];
-                            const uint64_t e0 = attn::fma2(attn::pack2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), scale2, attn::pack2(m.x, m.y));
-                            const uint64_t e1 = attn::fma2(attn::pack2(__uint_as_float(y[j + 2]), __uint_as_float(y[j + 3])), scale2, attn::pack2(m.z, m.w));
-                            acc_a = mufu_add(e0, acc_a);
-                            acc_b = mufu_add(e1, acc_b);
+                            acc_a = exp_add(attn::fma2(attn::pack2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), scale2, attn::pack2(m.x, m.y)), acc_a);
+                            acc_b = exp_add(attn::fma2(attn::pack2(__uint_as_float(y[j + 2]), __uint_as_float(y[j + 3])), scale2, attn::pack2(m.z, m.w)), acc_b);
                         }
                     } else if (!__any_sync(0xffffffffu, tree)) {
-                        const int l = lo - half * 64 - b * 32, r = hi - half * 64 - b * 32;
+                        const int l = lo - col0 - b * 32, r = hi - col0 - b * 32;
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
                             const float4 m = nl[b * 8 + j / 4];
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                         const int bit = min(max(pos - L, 0), 127);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
-                            const int col = half * 64 + b * 32 + j, i = r0 + ((col * p.group_inv) >> 16);
+                            const int col = col0 + b * 32 + j, i = r0 + ((col * p.group_inv) >> 16);
                             bool in = col >= lo && col < hi;
                             if (tree && in)
                                 in = L + i >= 0 && pos - L < 128 && ((__ldg(a.anc + 2 * (size_t)(s.start + i) + (bit >> 6)) >> (bit & 63)) & 1);
@@ -301,26 +304,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
                 }
             }
             if (!ok) break;
-            // the halves' sums together
-            float sum, sa0, sa1, sb0, sb1;
+            float sa0, sa1, sb0, sb1;
             attn::unpack2(acc_a, sa0, sa1);
             attn::unpack2(acc_b, sb0, sb1);
-            sum = sum0 + ((sa0 + sa1) + (sb0 + sb1));
-            if (half == 1) {
-                ok = __all_sync(0xffffffffu, mbar_wait(&h_free[pair], (n_p & 1) ^ 1, s_abort));
-                if (!ok) break;
-                s_half[key] = sum;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&h_full[pair]);
-            } else {
-                ok = __all_sync(0xffffffffu, mbar_wait(&h_full[pair], n_p & 1, s_abort));
-                if (!ok) break;
-                sum += s_half[key];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&h_free[pair]);
-                if (pc.slot >= 0) w.part[((size_t)blockIdx.x * 2 + pc.slot) * KEY_WEIGHT_KEYS + key] = sum;
-                else if (to) *to = has_old(w, s, pos) ? fmaf(w.keep, old, sum) : sum;
+            float sum = sum0 + ((sa0 + sa1) + (sb0 + sb1));
+            if (!ONE) {                                          // the halves' sums together
+                if (half == 1) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&h_free[pair], (n_p & 1) ^ 1, s_abort));
+                    if (!ok) break;
+                    s_half[key] = sum;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&h_full[pair]);
+                } else {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&h_full[pair], n_p & 1, s_abort));
+                    if (!ok) break;
+                    sum += s_half[key];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&h_free[pair]);
+                    if (pc.slot >= 0) w.part[((size_t)blockIdx.x * 2 + pc.slot) * KEY_WEIGHT_KEYS + key] = sum;
+                }
             }
+            if (to) *to = has_old(w, s, pos) ? fmaf(w.keep, old, sum) : sum;
             u += max(pc.n, 1);
             if (u < end) next_chunk<CK>(w, c);
         }
@@ -339,10 +343,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_key_weights_tc(const __grid_cons
     }
 }
 
-template <int D>
+template <int D, bool ONE>
 int run(const TcParams& p, cudaStream_t s) {
-    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_key_weights_tc<D>), Cfg<D>::SMEM)) return -1;
-    k_key_weights_tc<D><<<p.w.a.n_cta, THREADS, Cfg<D>::SMEM, s>>>(p);
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_key_weights_tc<D, ONE>), Cfg<D>::SMEM)) return -1;
+    k_key_weights_tc<D, ONE><<<p.w.a.n_cta, THREADS, Cfg<D>::SMEM, s>>>(p);
     return 0;
 }
 
@@ -375,10 +379,11 @@ int launch_key_weights_tc(KeyWeightArgs w, int n_sm, cudaStream_t s) {
     a.n_cta = n_sm;
     a.min_units = 1;
     p.w = w;
-    const int rc = a.D == 128 ? run<128>(p, s) : run<64>(p, s);
-    // (where a sequence's observed tokens fit one tile no chunk has two owners)
     const long long observed = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;
-    return rc || observed <= a.rows ? rc : launch_key_weights_join(w, CK, s);
+    // (then no chunk has two owners either)
+    if (observed <= a.rows) return a.D == 128 ? run<128, true>(p, s) : run<64, true>(p, s);
+    const int rc = a.D == 128 ? run<128, false>(p, s) : run<64, false>(p, s);
+    return rc ? rc : launch_key_weights_join(w, CK, s);
 }
 
 }  // namespace esp
