@@ -456,7 +456,7 @@ int esp_paged_evict_scratch_bytes(int32_t batch, int32_t n_kv_heads, int32_t max
 int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_paged_slots* scores, const esp_paged_slots* positions, const int32_t* seen,
                     int32_t* settled, int32_t recent, const int32_t* budget, int32_t* kv_len_out, void* scratch, size_t scratch_bytes, void* cuda_stream);
 
-/* Draws a token for each row of logits [n_rows][vocab] (dtype as in esp_model_cfg, rows row_stride elements apart, vocab up to 2^21, n_rows up to 2^27) with the row's own settings, arrays [device]
+/* Draws a token for each row of logits [n_rows][vocab] (dtype as in esp_model_cfg, rows row_stride elements apart, vocab up to 2^21, n_rows up to 2^24 and with 8192 logits of each up to 2^31 - 1 in all) with the row's own settings, arrays [device]
  * [n_rows], each of which may be NULL:
  *   weights w_i = exp((logit_i - largest) / temperature); order: larger logits first, of equal ones the lower index;
  *   kept are the first top_k of the order (top_k < 1: all); of those the shortest front whose weights reach top_p of what they all have (w_i stays while

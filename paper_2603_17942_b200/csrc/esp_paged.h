@@ -109,6 +109,13 @@ struct AcceptArgs {
     int32_t out_stride, Hkv, D, vec;
 };
 
+constexpr int SAMPLE_SLICE = 8192, SAMPLE_CAP = 160, SAMPLE_MAX_SLICES = 256;
+struct SampleSlice {        // what the first pass leaves of a slice of a row
+    unsigned long long best;          // its first element in the order
+    float cut;                        // its elements that are not below this are in its list (infinity: it has none)
+    int32_t n;                        // elements of the list
+    double stretch[8];                // sums of weights of its eighths, in terms of its own largest
+};
 struct SampleArgs {
     const void* logits;
     long long row_stride;
@@ -117,7 +124,11 @@ struct SampleArgs {
     const int32_t* top_k;
     int32_t* tokens;
     float* logprob;
-    int32_t chunk;          // logits of a row that each block of its cluster has
+    int32_t chunk;          // logits of a row that each block of its cluster has (the rest)
+    int32_t slices;         // of a row
+    SampleSlice* slice;     // [n_rows][slices]
+    unsigned long long* entries;      // [n_rows][slices][SAMPLE_CAP]
+    int32_t *rest, *n_rest; // rows that the lists do not settle
 };
 
 // Partials a launch may need at most: two tiles of 256 pairs for each of 148 SMs, or as much in smaller tiles.

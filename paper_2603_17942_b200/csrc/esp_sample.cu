@@ -33,7 +33,8 @@ constexpr int LIST = 2048;                // elements that are sorted at most
 constexpr int SMEM_ROW = 160 * 1024;      // bytes of a row that a block keeps at most
 constexpr int TAB = 256;                  // 2^(j / TAB)
 constexpr float UNIT = 8192.f;            // a histogram of weights counts in 1 / UNIT of a bin's largest: 2^19 elements of a block fit 32 bits
-constexpr int MAX_VOCAB = 1 << 21;
+constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
+constexpr int WANT = 110;                 // elements of a slice that go to its list, more or less
 
 __device__ __forceinline__ uint32_t order_key(float x) {        // no NaN comes here
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -96,7 +97,7 @@ __device__ __forceinline__ double widen(float x) {
     return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + (896u << 20))), (int)(b << 29));
 }
 // exp((x - M) / temperature): 2^n * 2^(j / 256) from a table * a polynomial of degree 3 on what is left, |r| <= 1/512 octave: (ln 2 / 512)^4 / 24 = 1.4e-13 of the
-// weight.  Weights below 2^-60 of the largest count as nothing.
+// weight.  Weights below 2^-120 of the largest count as nothing.
 __device__ __forceinline__ double weight(const Row& r, const double* tab, float x) {
     constexpr double C1 = 0.6931471805599453 / TAB, C2 = C1 * C1 / 2, C3 = C1 * C1 * C1 / 6, MAGIC = 6755399441055744.0;
     const double t = (widen(x) - r.Md) * r.A;
@@ -105,7 +106,7 @@ __device__ __forceinline__ double weight(const Row& r, const double* tab, float 
     const double d = t - (y - MAGIC);
     const double p = fma(d, fma(d, fma(d, C3, C2), C1), 1.0) * tab[n & (TAB - 1)];
     const double w = __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
-    return t > -60.0 * TAB && x != -INFINITY ? w : 0.0;
+    return t > -120.0 * TAB && x != -INFINITY ? w : 0.0;
 }
 // Fine bins from the largest logit down; BINS - 1: somewhere behind.
 __device__ __forceinline__ float depth_of(const Row& r, float x) { return x == r.M ? 0.f : fminf((r.M - x) * r.steps, (float)(BINS - 1)); }
@@ -358,13 +359,41 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
     }
 }
 
+// A row's settings.
+struct Limits {
+    float temperature, uniform, top_p, min_p;
+    int top_k;
+    bool bad, use_k, use_p, use_m, one;       // one: only the first element stays
+};
+__device__ __forceinline__ Limits limits_of(const SampleArgs& a, int row) {
+    Limits l;
+    l.temperature = a.temperature ? __ldg(a.temperature + row) : 1.f;
+    l.uniform = __ldg(a.uniform + row);
+    l.top_k = a.top_k ? __ldg(a.top_k + row) : 0;
+    l.top_p = a.top_p ? __ldg(a.top_p + row) : 1.f;
+    l.min_p = a.min_p ? __ldg(a.min_p + row) : 0.f;
+    l.bad = !(l.temperature >= 0.f) || isinf(l.temperature) || !(l.uniform >= 0.f) || l.top_p != l.top_p || l.min_p != l.min_p;
+    l.use_k = l.top_k >= 1 && l.top_k < a.vocab;
+    l.use_p = l.top_p < 1.f;
+    l.use_m = l.min_p > 0.f;
+    l.one = l.temperature == 0.f || l.top_k == 1 || l.top_p <= 0.f;
+    return l;
+}
+__device__ __forceinline__ void set_row(Row& r, const Limits& l, float M) {
+    const double inv_t = isinf(M) ? 1e300 : 1.0 / (double)l.temperature;      // (next to an infinite logit no other has weight)
+    r.M = M;
+    r.Md = widen(M);
+    r.A = inv_t * (TAB * 1.4426950408889634);
+    r.steps = (float)fmin(inv_t * ((double)STEPS * 1.4426950408889634), 3e38);
+    r.bound = ~0ull;
+    r.min_p = fmin((double)l.min_p, 1.0);
+}
+
 template <typename T, bool RESIDENT>
-__global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArgs a) {
+__device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_raw, int row) {
     constexpr int VEC = Raw<T>::VEC, STRIDE = 32 * VEC;
-    extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ Shared sm;
     cg::cluster_group cluster = cg::this_cluster();
-    const int CL = cluster.num_blocks(), me = cluster.block_rank(), row = blockIdx.x / CL;
+    const int CL = cluster.num_blocks(), me = cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
     const int first = min(a.vocab, me * a.chunk), n = min(a.vocab, first + a.chunk) - first;   // (chunk * CL fits 32 bits)
@@ -388,11 +417,10 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
     };
 
     Row r;
-    const float temperature = a.temperature ? __ldg(a.temperature + row) : 1.f, uniform = __ldg(a.uniform + row);
-    const int top_k = a.top_k ? __ldg(a.top_k + row) : 0;
-    const float top_p = a.top_p ? __ldg(a.top_p + row) : 1.f, min_p = a.min_p ? __ldg(a.min_p + row) : 0.f;
-    const bool bad = !(temperature >= 0.f) || isinf(temperature) || !(uniform >= 0.f) || top_p != top_p || min_p != min_p;
-    const bool use_k = top_k >= 1 && top_k < a.vocab, use_p = top_p < 1.f, use_m = min_p > 0.f;
+    const Limits l = limits_of(a, row);
+    const float uniform = l.uniform, top_p = l.top_p, min_p = l.min_p;
+    const int top_k = l.top_k;
+    const bool use_k = l.use_k, use_p = l.use_p, use_m = l.use_m;
 
     if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
     if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
@@ -447,26 +475,7 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
 #pragma unroll
     for (int c = 1; c < MAX_CL; ++c) best = min(best, c < CL ? sm.best[c] : ~0ull);
     r.M = rank_value(best);
-    if (bad || r.M == -INFINITY) {                                // the same in the whole cluster
-        if (me == 0 && tid == 0) {
-            a.tokens[row] = -1;
-            if (a.logprob) a.logprob[row] = __int_as_float(0x7fffffff);
-        }
-        return;
-    }
-    if (temperature == 0.f || top_k == 1 || top_p <= 0.f) {       // one element stays: the first
-        if (me == 0 && tid == 0) {
-            a.tokens[row] = (int)(uint32_t)best;
-            if (a.logprob) a.logprob[row] = 0.f;
-        }
-        return;
-    }
-    const double inv_t = isinf(r.M) ? 1e300 : 1.0 / (double)temperature;      // (next to an infinite logit no other has weight)
-    r.Md = widen(r.M);
-    r.A = inv_t * (TAB * 1.4426950408889634);
-    r.steps = (float)fmin(inv_t * ((double)STEPS * 1.4426950408889634), 3e38);
-    r.bound = ~0ull;
-    r.min_p = fmin((double)min_p, 1.0);
+    set_row(r, l, r.M);
 
     int flip = 0;
     // a number of each thread, summed over the cluster in a fixed order; each block's share stays in sm.sum[flip], each warp's in sm.warp_sum.  Starts with publish(), and
@@ -1028,37 +1037,406 @@ __global__ void __launch_bounds__(NT) k_sample(const __grid_constant__ SampleArg
     }
 }
 
+template <typename T, bool RESIDENT>
+__global__ void __launch_bounds__(NT) k_sample_rest(const __grid_constant__ SampleArgs a) {
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ Shared sm;
+    pdl_wait();
+    const int CL = cg::this_cluster().num_blocks(), count = __ldcg(a.n_rest);
+    for (int i = blockIdx.x / CL; i < count; i += gridDim.x / CL) {
+        sample_row<T, RESIDENT>(a, sm, smem_raw, __ldcg(a.rest + i));
+        __syncthreads();                  // (a warp may still have been reading the row)
+    }
+}
+
+// ---- first pass: a block has a slice of a row in its registers, reads it once and leaves what the second pass needs
+constexpr int SCAN_THREADS = 256, SCAN_WARPS = SCAN_THREADS / 32, SLICE = SAMPLE_SLICE, CAP = SAMPLE_CAP, STRETCH = SLICE / SCAN_WARPS;
 template <typename T>
-int run(SampleArgs a, cudaStream_t s) {
+__global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_constant__ SampleArgs a) {
+    constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
+    __shared__ double s_tab[TAB], s_sum[SCAN_WARPS];
+    __shared__ uint32_t s_hist[BINS], s_key[SCAN_WARPS], s_index, s_n;
+    __shared__ unsigned s_count[SCAN_WARPS];
+    __shared__ int s_bin;
+    const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_launch_dependents();
+    const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
+    const int first = slice * SLICE, n = min(SLICE, a.vocab - first), i0 = warp * STRETCH + lane * VEC;       // a warp has a stretch, lanes side by side
+    uint4 raw[PER];
+    if (n == SLICE && reinterpret_cast<uintptr_t>(logits + first) % 16 == 0) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) raw[j] = __ldg(reinterpret_cast<const uint4*>(logits + first + i0 + j * 32 * VEC));
+    } else {
+        const bool aligned = reinterpret_cast<uintptr_t>(logits + first) % 16 == 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = i0 + j * 32 * VEC;
+            if (aligned && i + VEC <= n) raw[j] = __ldg(reinterpret_cast<const uint4*>(logits + first + i));
+            else {
+                float x[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[e] = i + e < n ? to_f32(logits[first + i + e]) : -INFINITY;
+                raw[j] = Raw<T>::pack(x);
+            }
+        }
+    }
+    const Limits l = limits_of(a, row);
+    if (tid < TAB) s_tab[tid] = exp2((double)tid / TAB);
+    for (int i = tid; i < BINS; i += SCAN_THREADS) s_hist[i] = 0;
+    if (tid == 0) {
+        s_index = ~0u;
+        s_n = 0;
+        if (blockIdx.x == 0) *a.n_rest = 0;
+    }
+    auto unpack = [&](int j, float (&x)[VEC]) {
+        Raw<T>::unpack(raw[j], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = number(x[e]);
+    };
+    // ---- the largest
+    float mine = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        float x[VEC];
+        unpack(j, x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, x[e]);
+    }
+    const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(mine));
+    if (lane == 0) s_key[warp] = key;
+    __syncthreads();
+    uint32_t top = 0;
+#pragma unroll
+    for (int w = 0; w < SCAN_WARPS; ++w) top = max(top, s_key[w]);
+    const float M = key_value(top);
+    if (order_key(mine) == top) {
+        int at = SLICE;
+#pragma unroll
+        for (int j = PER - 1; j >= 0; --j) {
+            float x[VEC];
+            unpack(j, x);
+#pragma unroll
+            for (int e = VEC - 1; e >= 0; --e)
+                if (x[e] == M) at = i0 + j * 32 * VEC + e;
+        }
+        atomicMin(&s_index, (uint32_t)(first + at));
+    }
+    SampleSlice* out = a.slice + (size_t)row * a.slices + slice;
+    Row r;
+    set_row(r, l, M);
+    const bool skip = l.bad || l.one || M == -INFINITY;
+    // ---- its weights, as far as sums over the row are asked for
+    const bool weigh = !skip && !l.use_k && (l.use_p || !l.use_m);
+    if (weigh) {
+        double s = 0.0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            float x[VEC];
+            unpack(j, x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += weight(r, s_tab, x[e]);
+        }
+        s = warp_sum_f64(s);
+        if (lane == 0) s_sum[warp] = s;
+    }
+    // ---- its largest elements: the ones not below a value that so many of the threads' largest reach that `want` elements do, more or less
+    float cut = INFINITY;
+    if (!skip && (l.use_k || l.use_p || l.use_m)) {
+        if (n <= CAP) cut = -INFINITY;
+        else {
+            const float share = (float)l.top_k * ((float)n / (float)a.vocab), most = fminf((float)WANT, (float)LIST / (float)a.slices);
+            const float want = l.use_k ? share + 6.f * sqrtf(share) + 8.f : most;           // of the first top_k hardly ever more lie in one slice
+            if (want <= (l.use_k ? 125.f : most)) {
+                const int threads = n / STRETCH * 32 + min(32, (n % STRETCH + VEC - 1) / VEC);
+                const unsigned of = (unsigned)fmaxf(1.f, (float)threads * (1.f - __expf(-want / (float)threads)));
+                const int b = wide_bin(r, mine);
+                if (b < BINS - 1) atomicAdd(&s_hist[b], 1u);
+                if (tid == 0) s_bin = BINS - 1;
+                __syncthreads();
+                const unsigned n0 = s_hist[2 * tid], n1 = s_hist[2 * tid + 1], in = warp_scan_u32(n0 + n1, lane);
+                if (lane == 31) s_count[warp] = in;
+                __syncthreads();
+                unsigned before = in - n0 - n1;
+#pragma unroll
+                for (int w = 0; w < SCAN_WARPS; ++w) before += w < warp ? s_count[w] : 0u;
+                if (before < of && of <= before + n0) s_bin = 2 * tid;
+                else if (before + n0 < of && of <= before + n0 + n1) s_bin = 2 * tid + 1;
+                __syncthreads();
+                int bin = s_bin;
+                if (l.use_m && !(l.use_k && l.use_p)) {
+                    // what min_p takes away from the largest here it takes away from the row's
+                    const double d = -log(r.min_p) * (1.4426950408889634 * STEPS) * 1.00001 + 1.0;
+                    bin = min(bin, d < FINE ? (int)d : min(FINE + (int)((fmin(d, 1e6) - FINE) / COARSE), BINS - 1));
+                }
+                if (bin < BINS - 1) cut = M - wide_end(bin) / r.steps;
+            }
+        }
+        unsigned long long* list = a.entries + ((size_t)row * a.slices + slice) * CAP;
+        if (cut < INFINITY) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                float x[VEC], most = -INFINITY;
+                unpack(j, x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) most = fmaxf(most, x[e]);
+                if (most < cut) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int i = i0 + j * 32 * VEC + e;
+                    if (x[e] >= cut && i < n) {
+                        const unsigned at = atomicAdd(&s_n, 1u);
+                        if (at < CAP) list[at] = rank_of(x[e], first + i);
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        out->best = ((unsigned long long)~top << 32) | s_index;
+        const int count = (int)s_n;
+        out->n = min(count, CAP);
+        out->cut = count <= CAP ? cut : INFINITY;
+    }
+    if (tid < SCAN_WARPS) out->stretch[tid] = weigh ? s_sum[tid] : 0.0;
+}
+
+// ---- second pass: a block for each row; what cannot be settled from the slices' lists goes to the rest
+template <typename T>
+__global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ SampleArgs a) {
+    __shared__ Shared sm;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_launch_dependents();
+    if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
+    sm.hist[tid] = 0;
+    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; sm.bin = BINS; sm.lo[0] = 0; }
+    const Limits l = limits_of(a, row);
+    __syncthreads();
+    pdl_wait();
+    const SampleSlice* slice = a.slice + (size_t)row * a.slices;
+    // (slices <= NT: a thread for each)
+    unsigned long long best = ~0ull;
+    float cut = -INFINITY;
+    int n = 0;
+    if (tid < a.slices) {
+        best = __ldcg(&slice[tid].best);
+        cut = __ldcg(&slice[tid].cut);
+        n = __ldcg(&slice[tid].n);
+        sm.all[tid] = n;
+    }
+    unsigned long long first = best;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
+    const uint32_t highest = __reduce_max_sync(0xffffffffu, tid < a.slices && best != ~0ull && rank_value(best) != -INFINITY ? order_key(cut) : 0u);
+    if (lane == 0) {
+        if (first != ~0ull) atomicMin(&sm.answer, first);
+        atomicMax(&sm.lo[0], highest);
+    }
+    __syncthreads();
+    const float M = rank_value(sm.answer);
+    if (l.bad || M == -INFINITY || l.one) {
+        if (tid == 0) {
+            const bool none = l.bad || M == -INFINITY;
+            a.tokens[row] = none ? -1 : (int)(uint32_t)sm.answer;
+            if (a.logprob) a.logprob[row] = none ? __int_as_float(0x7fffffff) : 0.f;
+        }
+        return;
+    }
+    Row r;
+    set_row(r, l, M);
+    cut = key_value(sm.lo[0]);            // all elements of the row that are not below it are in the lists
+    // ---- sums of the slices' weights, four stretches a thread, in terms of the row's largest
+    const bool plain = !l.use_k && !l.use_p && !l.use_m;
+    double S = 0.0;
+    if (plain || (l.use_p && !l.use_k)) {
+        constexpr int PER = SAMPLE_MAX_SLICES * SCAN_WARPS / NT;
+        double w[PER], run = 0.0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int i = tid * PER + e, sl = i / SCAN_WARPS;
+            w[e] = 0.0;
+            if (sl < a.slices) w[e] = __ldcg(&slice[sl].stretch[i % SCAN_WARPS]) * weight(r, sm.tab, rank_value(__ldcg(&slice[sl].best)));
+            if (w[e] < 0x1p-110) w[e] = 0.0;                       // (2^10 elements that count as nothing one by one)
+            run += w[e];
+        }
+        const double in = warp_scan_f64(run, lane);
+        if (lane == 31) sm.warp_sum[warp] = in;
+        __syncthreads();
+        double upto = in - run;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            if (k == warp) upto += S;
+            S += sm.warp_sum[k];
+        }
+        if (plain) {
+            // the stretch in which the target lies, or the last one with weight, then its element
+            const double target = (double)l.uniform * S;
+            int found = BINS * LIST, last = -1;
+            double before = 0.0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (w[e] > 0.0) {
+                    last = tid * PER + e;
+                    if (found == BINS * LIST && upto + w[e] > target) { found = tid * PER + e; before = upto; }
+                }
+                upto += w[e];
+            }
+            const int f = __reduce_min_sync(0xffffffffu, found), z = __reduce_max_sync(0xffffffffu, last);
+            if (tid == 0) { sm.bin = BINS * LIST; sm.end_bin = -1; }
+            __syncthreads();
+            if (lane == 0) { atomicMin(&sm.bin, f); atomicMax(&sm.end_bin, z); }
+            __syncthreads();
+            const bool none = sm.bin == BINS * LIST;
+            const int at = none ? sm.end_bin : sm.bin;
+            if (!none && found == at) sm.kept_sum = before;
+            if (none && last == at) {
+                double b = upto;
+#pragma unroll
+                for (int e = PER - 1; e >= 0; --e)
+                    if (tid * PER + e >= at) b -= w[e];
+                sm.kept_sum = b;
+            }
+            __syncthreads();
+            const double front = sm.kept_sum;
+            // two neighbours a thread
+            const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
+            constexpr int E = STRETCH / NT;
+            const int i0 = at * STRETCH + tid * E;
+            float x[E];
+            double v[E], sum = 0.0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[e] = i0 + e < a.vocab ? number(to_f32(logits[i0 + e])) : -INFINITY;
+                v[e] = weight(r, sm.tab, x[e]);
+                sum += v[e];
+            }
+            const double scan = warp_scan_f64(sum, lane);
+            if (lane == 31) sm.warp_sum2[warp] = scan;
+            if (tid == 0) { sm.bin = BINS * LIST; sm.end_bin = -1; }
+            __syncthreads();
+            double here = front + scan - sum;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) here += k < warp ? sm.warp_sum2[k] : 0.0;
+            int hit = BINS * LIST, some = -1;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                here += v[e];
+                if (v[e] > 0.0) {
+                    some = tid * E + e;
+                    if (hit == BINS * LIST && here > target) hit = tid * E + e;
+                }
+            }
+            const int h = __reduce_min_sync(0xffffffffu, hit), y = __reduce_max_sync(0xffffffffu, some);
+            if (lane == 0) { atomicMin(&sm.bin, h); atomicMax(&sm.end_bin, y); }
+            __syncthreads();
+            const int token = sm.bin < BINS * LIST ? sm.bin : sm.end_bin;
+            if (token / E == tid) {
+                a.tokens[row] = at * STRETCH + token;
+                if (a.logprob) a.logprob[row] = (float)log((token % E ? v[E - 1] : v[0]) / S);
+            }
+            return;
+        }
+    }
+    // ---- where the front ends, from a histogram of the lists; then what lies in front of that
+    bool done = cut == -INFINITY;                                  // everything is in the lists
+    if (cut < INFINITY && l.use_m && !(l.use_k && l.use_p)) done = done || weight(r, sm.tab, cut) < r.min_p * 0.999;
+    const bool weigh = l.use_p && !l.use_k;
+    const unsigned long long* entries = a.entries + (size_t)row * a.slices * CAP;
+    const int slots = a.slices * CAP;
+    auto entry = [&](int i) {                                      // ~0: none
+        const int sl = i / CAP;
+        return i - sl * CAP < (int)sm.all[sl] ? __ldcg(entries + i) : ~0ull;
+    };
+    int last_bin = BINS - 1;
+    if (cut < INFINITY && (l.use_k || l.use_p)) {
+        for (int i = tid; i < slots; i += NT) {
+            const unsigned long long v = entry(i);
+            if (v == ~0ull || rank_value(v) < cut) continue;
+            if (weigh) {
+                const float d = depth_of(r, rank_value(v));
+                const int b = (int)d;
+                if (b < BINS - 1) atomicAdd(&sm.hist[b], (unsigned)UNIT - (unsigned)((d - (float)b) * (UNIT * (1.f - 0.97153194f))));
+            } else {
+                const int b = wide_bin(r, rank_value(v));
+                if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
+            }
+        }
+        __syncthreads();
+        const unsigned mine = sm.hist[tid];
+        const float v = weigh ? (float)mine * (1.f / UNIT) * exp2f((float)tid * (-1.f / STEPS)) : (float)mine;
+        float in = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const float y = __shfl_up_sync(0xffffffffu, in, o);
+            if (lane >= o) in += y;
+        }
+        if (lane == 31) sm.warp_f[warp] = in;
+        if (tid == 0) sm.bin = BINS;
+        __syncthreads();
+        float before = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) before += w < warp ? sm.warp_f[w] : 0.f;
+        const float goal = weigh ? (float)((double)l.top_p * S) * 1.001f : (float)l.top_k;
+        if (before + in >= goal) atomicMin(&sm.bin, tid);
+        __syncthreads();
+        if (sm.bin < BINS - 1) {
+            done = true;
+            last_bin = weigh && sm.bin >= FINE ? min(FINE + (sm.bin - FINE) / COARSE, BINS - 1) : sm.bin;
+        }
+    }
+    int count = LIST + 1;
+    if (done) {
+        for (int i = tid; i < slots; i += NT) {
+            const unsigned long long v = entry(i);
+            if (v == ~0ull || rank_value(v) < cut || wide_bin(r, rank_value(v)) > last_bin) continue;
+            const unsigned at = atomicAdd(&sm.n_list, 1u);
+            if (at < LIST) sm.list[at] = v;
+        }
+        __syncthreads();
+        count = (int)sm.n_list;
+    }
+    if (count > LIST) {
+        if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = row;
+        return;
+    }
+    from_list(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform);
+}
+
+template <typename T>
+int run(SampleArgs a, int n_sm, cudaStream_t s) {
+    k_sample_scan<T><<<(unsigned)((long long)a.n_rows * a.slices), SCAN_THREADS, 0, s>>>(a);
+    if (launch_k(k_sample_list<T>, dim3(a.n_rows), dim3(NT), 0, s, true, a) != cudaSuccess) return -1;
     constexpr int STRIDE = 32 * Raw<T>::VEC;
     int cl = 1;
     while (cl < MAX_CL && a.vocab > cl * 4096) cl *= 2;
     a.chunk = ((a.vocab + cl - 1) / cl + STRIDE - 1) / STRIDE * STRIDE;
     const size_t bytes = (size_t)a.chunk * sizeof(T);
     const bool resident = bytes <= SMEM_ROW;
+    const int clusters = 2 * n_sm / cl < a.n_rows ? 2 * n_sm / cl : a.n_rows;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.n_rows * cl);
+    cfg.gridDim = dim3((unsigned)clusters * cl);
     cfg.blockDim = dim3(NT);
     cfg.dynamicSmemBytes = resident ? bytes : 0;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cl;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (resident) {
-        if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_sample<T, true>), SMEM_ROW)) return -1;
-        return cudaLaunchKernelEx(&cfg, k_sample<T, true>, a) != cudaSuccess;
+        if (ensure_dynamic_smem(reinterpret_cast<const void*>(&k_sample_rest<T, true>), SMEM_ROW)) return -1;
+        return cudaLaunchKernelEx(&cfg, k_sample_rest<T, true>, a) != cudaSuccess;
     }
-    return cudaLaunchKernelEx(&cfg, k_sample<T, false>, a) != cudaSuccess;
+    return cudaLaunchKernelEx(&cfg, k_sample_rest<T, false>, a) != cudaSuccess;
 }
 
 }  // namespace
 
 int launch_sample(int dtype, SampleArgs a, int n_sm, cudaStream_t s) {
-    (void)n_sm;
-    return dtype == 0 ? run<float>(a, s) : run<__nv_bfloat16>(a, s);
+    return dtype == 0 ? run<float>(a, n_sm, s) : run<__nv_bfloat16>(a, n_sm, s);
 }
 
 }  // namespace esp
@@ -1067,9 +1445,11 @@ using namespace esp;
 
 extern "C" {
 
+// scratch layout: [rows][slices] SampleSlice, [rows][slices][SAMPLE_CAP] entries, [rows] the rest, how many
 int esp_sample_scratch_bytes(int32_t n_rows, int32_t vocab, size_t* bytes_out) {
-    if (!bytes_out || n_rows < 0 || vocab < 1) return ESP_E_ARG;
-    *bytes_out = 256;
+    if (!bytes_out || n_rows < 0 || n_rows > (1 << 24) || vocab < 1 || vocab > MAX_VOCAB) return ESP_E_ARG;
+    const size_t slices = (size_t)n_rows * ((vocab + SAMPLE_SLICE - 1) / SAMPLE_SLICE);
+    *bytes_out = slices * (sizeof(SampleSlice) + SAMPLE_CAP * sizeof(unsigned long long)) + ((size_t)n_rows + 1) * sizeof(int32_t);
     return ESP_OK;
 }
 
@@ -1078,7 +1458,7 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     if (dtype != 0 && dtype != 1) return ESP_E_BADCFG;
     const int size = dtype == 0 ? 4 : 2;
     auto off = [](const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; };
-    if (n_rows < 0 || n_rows > (1 << 27) || vocab < 1 || vocab > MAX_VOCAB || row_stride < 0 || row_stride > ((int64_t)1 << 40) || !sampling) return ESP_E_ARG;
+    if (n_rows < 0 || n_rows > (1 << 24) || vocab < 1 || vocab > MAX_VOCAB || row_stride < 0 || row_stride > ((int64_t)1 << 40) || !sampling) return ESP_E_ARG;
     if (off(logits, size) || off(sampling->temperature, 4) || off(sampling->top_k, 4) || off(sampling->top_p, 4) || off(sampling->min_p, 4) || off(uniform, 4) ||
         off(tokens, 4) || off(logprob, 4)) return ESP_E_ARG;
     if (n_rows == 0) return ESP_OK;
@@ -1089,6 +1469,12 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     const int n_sm = current_sm_count();
     if (n_sm < 1) return ESP_E_CUDA;
     SampleArgs a;
+    a.slices = (vocab + SAMPLE_SLICE - 1) / SAMPLE_SLICE;
+    if ((int64_t)n_rows * a.slices > 0x7fffffff) return ESP_E_ARG;
+    a.slice = reinterpret_cast<SampleSlice*>(scratch);
+    a.entries = reinterpret_cast<unsigned long long*>(a.slice + (size_t)n_rows * a.slices);
+    a.rest = reinterpret_cast<int32_t*>(a.entries + (size_t)n_rows * a.slices * SAMPLE_CAP);
+    a.n_rest = a.rest + n_rows;
     a.logits = logits; a.row_stride = row_stride; a.n_rows = n_rows; a.vocab = vocab;
     a.temperature = sampling->temperature; a.top_k = sampling->top_k; a.top_p = sampling->top_p; a.min_p = sampling->min_p;
     a.uniform = uniform; a.tokens = tokens; a.logprob = logprob; a.chunk = 0;
