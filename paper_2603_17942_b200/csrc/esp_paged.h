@@ -116,6 +116,11 @@ struct SampleSlice {        // what the first pass leaves of a slice of a row
     int32_t n;                        // elements of the list
     double stretch[8];                // sums of weights of its eighths, in terms of its own largest
 };
+struct SampleRest {
+    double S;               // the row's weights, where top-p goes by them
+    float M;                // its largest logit
+    int32_t row;
+};
 struct SampleArgs {
     const void* logits;
     long long row_stride;
@@ -128,7 +133,8 @@ struct SampleArgs {
     int32_t slices;         // of a row
     SampleSlice* slice;     // [n_rows][slices]
     unsigned long long* entries;      // [n_rows][slices][SAMPLE_CAP]
-    int32_t *rest, *n_rest; // rows that the lists do not settle
+    SampleRest* rest;       // rows that the lists do not settle
+    int32_t* n_rest;
 };
 
 // Partials a launch may need at most: two tiles of 256 pairs for each of 148 SMs, or as much in smaller tiles.

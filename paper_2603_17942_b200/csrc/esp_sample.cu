@@ -36,6 +36,20 @@ constexpr float UNIT = 8192.f;            // a histogram of weights counts in 1 
 constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
 constexpr int WANT = 110;                 // elements of a slice that go to its list, more or less
 
+// 2^(j / TAB), as the compiler works it out: the series of exp(j ln 2 / TAB)
+struct PowTable {
+    double v[TAB];
+    constexpr PowTable() : v() {
+        for (int j = 0; j < TAB; ++j) {
+            const double x = j * (0.6931471805599453 / TAB);
+            double sum = 0.0;
+            for (int k = 24; k > 0; --k) sum = (sum + 1.0) * x / k;
+            v[j] = sum + 1.0;
+        }
+    }
+};
+__device__ const PowTable POW_TABLE;
+
 __device__ __forceinline__ uint32_t order_key(float x) {        // no NaN comes here
     const uint32_t b = __float_as_uint(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -59,7 +73,6 @@ __device__ __forceinline__ double warp_scan_f64(double v, int lane) {
 
 struct Shared {
     double tab[TAB];
-    unsigned long long best[MAX_CL];      // the first of each block
     double sum[2][MAX_CL];                // a sum of each block
     unsigned count[MAX_CL];
     uint32_t lo[MAX_CL], hi[MAX_CL];      // smallest and largest key of an interval in each block
@@ -91,22 +104,15 @@ struct Row {
 __device__ __forceinline__ unsigned long long rank_of(float x, int index) { return ((unsigned long long)~order_key(x) << 32) | (unsigned)index; }
 __device__ __forceinline__ float rank_value(unsigned long long r) { return key_value(~(uint32_t)(r >> 32)); }
 
-// A float as a double by its bits (the conversion instruction runs at a quarter of the rate of the sums).  Zero comes out as 2^-127, infinity as 2^128.
-__device__ __forceinline__ double widen(float x) {
-    const uint32_t b = __float_as_uint(x);
-    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + (896u << 20))), (int)(b << 29));
-}
-// exp((x - M) / temperature): 2^n * 2^(j / 256) from a table * a polynomial of degree 3 on what is left, |r| <= 1/512 octave: (ln 2 / 512)^4 / 24 = 1.4e-13 of the
-// weight.  Weights below 2^-120 of the largest count as nothing.
+// exp((x - M) / temperature), M finite: 2^n * 2^(j / 256) from a table * a polynomial of degree 3 on what is left, |d| <= 1/512 octave: (ln 2 / 512)^4 / 24 = 1.4e-13 of the
+// weight.  Weights below 2^-120 of the largest count as nothing.  Passes over whole rows are bound by how many instructions this takes.
 __device__ __forceinline__ double weight(const Row& r, const double* tab, float x) {
-    constexpr double C1 = 0.6931471805599453 / TAB, C2 = C1 * C1 / 2, C3 = C1 * C1 * C1 / 6, MAGIC = 6755399441055744.0;
-    const double t = (widen(x) - r.Md) * r.A;
-    const double y = t + MAGIC;
-    const int n = __double2loint(y);
-    const double d = t - (y - MAGIC);
-    const double p = fma(d, fma(d, fma(d, C3, C2), C1), 1.0) * tab[n & (TAB - 1)];
-    const double w = __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
-    return t > -120.0 * TAB && x != -INFINITY ? w : 0.0;
+    constexpr double C1 = 0.6931471805599453 / TAB, C2 = C1 * C1 / 2, C3 = C1 * C1 * C1 / 6, MAGIC = 6755399441055744.0;      // 1.5 * 2^52: the sum's last bits are the whole number
+    const double diff = (double)x - r.Md, u = fma(diff, r.A, MAGIC), d = fma(diff, r.A, MAGIC - u);
+    const int n = __double2loint(u);
+    const double v = tab[n & (TAB - 1)], p = fma(v * d, fma(d, fma(d, C3, C2), C1), v);
+    const double w = __hiloint2double(__double2hiint(p) + ((n & ~(TAB - 1)) << 12), __double2loint(p));
+    return u > MAGIC - 120.0 * TAB ? w : 0.0;
 }
 // Fine bins from the largest logit down; BINS - 1: somewhere behind.
 __device__ __forceinline__ float depth_of(const Row& r, float x) { return x == r.M ? 0.f : fminf((r.M - x) * r.steps, (float)(BINS - 1)); }
@@ -380,9 +386,9 @@ __device__ __forceinline__ Limits limits_of(const SampleArgs& a, int row) {
     return l;
 }
 __device__ __forceinline__ void set_row(Row& r, const Limits& l, float M) {
-    const double inv_t = isinf(M) ? 1e300 : 1.0 / (double)l.temperature;      // (next to an infinite logit no other has weight)
+    const double inv_t = 1.0 / (double)l.temperature;
     r.M = M;
-    r.Md = widen(M);
+    r.Md = (double)M;
     r.A = inv_t * (TAB * 1.4426950408889634);
     r.steps = (float)fmin(inv_t * ((double)STEPS * 1.4426950408889634), 3e38);
     r.bound = ~0ull;
@@ -390,7 +396,8 @@ __device__ __forceinline__ void set_row(Row& r, const Limits& l, float M) {
 }
 
 template <typename T, bool RESIDENT>
-__device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_raw, int row) {
+__device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_raw, const SampleRest& known) {
+    const int row = known.row;
     constexpr int VEC = Raw<T>::VEC, STRIDE = 32 * VEC;
     cg::cluster_group cluster = cg::this_cluster();
     const int CL = cluster.num_blocks(), me = cluster.block_rank();
@@ -411,35 +418,39 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[e] = number(x[e]);
     };
+    // next to infinite logits no other has weight: they count as 0 and the others as -infinity
+    const bool infinite = isinf(known.M);
+    auto only_infinite = [&](float (&x)[VEC]) {
+        if (infinite)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] = x[e] == INFINITY ? 0.f : -INFINITY;
+    };
     auto load = [&](int i, float (&x)[VEC]) {
         if (RESIDENT) Raw<T>::unpack(kept_row[i / VEC], x);
-        else fetch(i, x);
+        else {
+            fetch(i, x);
+            only_infinite(x);
+        }
     };
 
     Row r;
     const Limits l = limits_of(a, row);
-    const float uniform = l.uniform, top_p = l.top_p, min_p = l.min_p;
+    const float uniform = l.uniform, top_p = l.top_p;
     const int top_k = l.top_k;
     const bool use_k = l.use_k, use_p = l.use_p, use_m = l.use_m;
 
     if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
-    if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
+    if (tid < TAB) sm.tab[tid] = POW_TABLE.v[tid];
     sm.hist[tid] = 0;
     cluster.barrier_arrive();             // (before anybody looks into another block's shared memory, all have to have started)
 
-    // ---- the largest
-    unsigned long long best = ~0ull;
+    // ---- the row into shared memory, each thread's largest
+    float own_best = -INFINITY;
     auto take = [&](int i, float (&x)[VEC]) {
+        only_infinite(x);
         if (RESIDENT) kept_row[i / VEC] = Raw<T>::pack(x);
-        float m = x[0];
 #pragma unroll
-        for (int e = 1; e < VEC; ++e) m = fmaxf(m, x[e]);
-        if (best == ~0ull || m > rank_value(best)) {
-            int at = VEC - 1;
-#pragma unroll
-            for (int e = VEC - 2; e >= 0; --e) at = x[e] == m ? e : at;
-            best = rank_of(m, first + i + at);
-        }
+        for (int e = 0; e < VEC; ++e) own_best = fmaxf(own_best, x[e]);
     };
     constexpr int AHEAD = 8;              // loads of a lane under way
     int i_load = w0 + lane * VEC;
@@ -462,19 +473,8 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
         fetch(i_load, x);
         take(i_load, x);
     }
-    const unsigned long long own_best = best;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
-    __syncthreads();
-    if (lane == 0) atomicMin(&sm.answer, best);
-    __syncthreads();
     cluster.barrier_wait();
-    if (tid < CL) cluster.map_shared_rank(sm.best, tid)[me] = sm.answer;
-    cluster.sync();
-    best = sm.best[0];
-#pragma unroll
-    for (int c = 1; c < MAX_CL; ++c) best = min(best, c < CL ? sm.best[c] : ~0ull);
-    r.M = rank_value(best);
+    r.M = infinite ? 0.f : known.M;
     set_row(r, l, r.M);
 
     int flip = 0;
@@ -521,17 +521,28 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
         }
     };
 
-    double S = 0.0, front_w = 0.0;        // weights of the whole row; of this thread's elements in front of the bin that a front ends in
-    bool have_s = false, have_front = false;
+    double S = known.S;
+    if (infinite) {                       // (a weight of 1 each)
+        double s = 0.0;
+        for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
+            float x[VEC];
+            load(i, x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += x[e] == 0.f ? 1.0 : 0.0;
+        }
+        publish(s);
+        cluster.sync();
+        S = total();
+    }
+    double front_w = 0.0;                 // weights of this thread's elements in front of the bin that a front ends in
+    bool have_front = false;
     int end_bin = 0;
     if (use_k || use_p || use_m) {
         const bool weigh = use_p && !use_k;
         int last_bin = -1;                // wide bins up to here go to the list; -1: too many
         if (a.vocab <= LIST) last_bin = BINS - 1;
         if (weigh) {
-            // the whole row's weights, and a histogram of them
-            double s = 0.0;
-            // what lies at this or below is in no bin (a little lower, so that rounding does not matter)
+            // a histogram of the weights.  What lies at `cut` or below is in no bin (a little lower, so that rounding does not matter)
             const float cut = r.M - ((float)BINS / r.steps) * 1.00001f;
 #pragma unroll 2
             for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
@@ -540,8 +551,6 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
                 float top = x[0];
 #pragma unroll
                 for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) s += weight(r, sm.tab, x[e]);
                 if (!(top < cut)) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
@@ -552,13 +561,10 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
                     }
                 }
             }
-            publish(s);
         } else if (use_k && last_bin < 0) {
             // the threads' largest logits (equal shares of the row for each, or one element more)
-            if (own_best != ~0ull) {
-                const int b = wide_bin(r, rank_value(own_best));
-                if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
-            }
+            const int b = wide_bin(r, own_best);
+            if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
         }
         if (weigh || (use_k && last_bin < 0)) {
             cluster.sync();
@@ -568,10 +574,6 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
             unsigned long long mine = 0;
 #pragma unroll
             for (int c = 0; c < MAX_CL; ++c) mine += part[c];
-            if (weigh) {
-                S = total();
-                have_s = true;
-            }
             // sums along the bins: elements, or weights (a fine bin's smaller by 2^(1/24) than those of the one in front of it)
             const float v = weigh ? (float)mine * (1.f / UNIT) * exp2f((float)tid * (-1.f / STEPS)) : (float)mine;
             float in = v;
@@ -641,20 +643,29 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
             if (tid == 0) sm.n_list = 0;
             cluster.sync();                                        // (histograms, counts and lists have been read)
             front_w = 0.0;
-            const float cut = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
+            // above `over` an element is in front of the bin for certain, below `under` behind it; between them its depth says
+            const float over = r.M - ((float)end_bin / r.steps) * 0.99999f, under = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
 #pragma unroll 2
             for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
                 float x[VEC];
                 load(i, x);
+                float top = x[0];
+#pragma unroll
+                for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
+                if (!__any_sync(__activemask(), top >= under)) continue;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    if (x[e] < cut) continue;
-                    const int b = (int)depth_of(r, x[e]);
-                    if (b < end_bin) front_w += weight(r, sm.tab, x[e]);
-                    else if (b == end_bin) {
-                        const unsigned p = atomicAdd(&sm.n_list, 1u);
-                        if (p < LIST) sm.list[p] = rank_of(x[e], first + i + e);
+                    bool front = x[e] > over;
+                    if (!front && x[e] >= under) {
+                        const int b = (int)depth_of(r, x[e]);
+                        front = b < end_bin;
+                        if (b == end_bin) {
+                            const unsigned p = atomicAdd(&sm.n_list, 1u);
+                            if (p < LIST) sm.list[p] = rank_of(x[e], first + i + e);
+                        }
                     }
+                    const double w = weight(r, sm.tab, x[e]);
+                    front_w += front ? w : 0.0;
                 }
             }
             publish(front_w);
@@ -719,7 +730,7 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
         if (what == 0 ? !use_k : !use_p) continue;
         double theta = 0.0;               // top-p: the weights that have to be reached
         if (what == 1) {
-            if (!have_s || use_k) {
+            if (use_k) {
                 double s = 0.0;
                 for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
                     float x[VEC];
@@ -959,15 +970,19 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
     double s = 0.0;
     if (have_front && !use_m) {
         // what is in front of the last bin has been added up
-        const float from_x = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
+        const float over = r.M - ((float)end_bin / r.steps) * 0.99999f, under = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
         s = front_w;
 #pragma unroll 4
         for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
             float x[VEC];
             load(i, x);
+            bool near = false;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (!(x[e] < from_x) && (int)depth_of(r, x[e]) == end_bin && rank_of(x[e], first + i + e) <= r.bound) s += weight(r, sm.tab, x[e]);
+            for (int e = 0; e < VEC; ++e) near = near || (x[e] >= under && x[e] <= over);
+            if (near)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (x[e] >= under && x[e] <= over && (int)depth_of(r, x[e]) == end_bin && rank_of(x[e], first + i + e) <= r.bound) s += weight(r, sm.tab, x[e]);
         }
     } else {
 #pragma unroll 2
@@ -1038,26 +1053,32 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
 }
 
 template <typename T, bool RESIDENT>
-__global__ void __launch_bounds__(NT) k_sample_rest(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(NT, 2) k_sample_rest(const __grid_constant__ SampleArgs a) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ Shared sm;
     pdl_wait();
     const int CL = cg::this_cluster().num_blocks(), count = __ldcg(a.n_rest);
     for (int i = blockIdx.x / CL; i < count; i += gridDim.x / CL) {
-        sample_row<T, RESIDENT>(a, sm, smem_raw, __ldcg(a.rest + i));
+        sample_row<T, RESIDENT>(a, sm, smem_raw, a.rest[i]);
         __syncthreads();                  // (a warp may still have been reading the row)
     }
 }
 
 // ---- first pass: a block has a slice of a row in its registers, reads it once and leaves what the second pass needs
+#ifndef SCANB
+#define SCANB 4
+#endif
+constexpr int SCAN_BLOCKS = SCANB;
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = SCAN_THREADS / 32, SLICE = SAMPLE_SLICE, CAP = SAMPLE_CAP, STRETCH = SLICE / SCAN_WARPS;
 template <typename T>
-__global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const __grid_constant__ SampleArgs a) {
     constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
     __shared__ double s_tab[TAB], s_sum[SCAN_WARPS];
     __shared__ uint32_t s_hist[BINS], s_key[SCAN_WARPS], s_index, s_n;
     __shared__ unsigned s_count[SCAN_WARPS];
     __shared__ int s_bin;
+    __shared__ unsigned s_before, s_near_n;
+    __shared__ float s_near[SCAN_THREADS], s_cut;
     const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();
     const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
@@ -1081,18 +1102,14 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_co
         }
     }
     const Limits l = limits_of(a, row);
-    if (tid < TAB) s_tab[tid] = exp2((double)tid / TAB);
+    if (tid < TAB) s_tab[tid] = POW_TABLE.v[tid];
     for (int i = tid; i < BINS; i += SCAN_THREADS) s_hist[i] = 0;
     if (tid == 0) {
         s_index = ~0u;
-        s_n = 0;
+        s_n = s_near_n = 0;
         if (blockIdx.x == 0) *a.n_rest = 0;
     }
-    auto unpack = [&](int j, float (&x)[VEC]) {
-        Raw<T>::unpack(raw[j], x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[e] = number(x[e]);
-    };
+    auto unpack = [&](int j, float (&x)[VEC]) { Raw<T>::unpack(raw[j], x); };
     // ---- the largest
     float mine = -INFINITY;
 #pragma unroll
@@ -1100,7 +1117,11 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_co
         float x[VEC];
         unpack(j, x);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, x[e]);
+        for (int e = 0; e < VEC; ++e) {
+            x[e] = number(x[e]);
+            mine = fmaxf(mine, x[e]);
+        }
+        raw[j] = Raw<T>::pack(x);
     }
     const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(mine));
     if (lane == 0) s_key[warp] = key;
@@ -1124,7 +1145,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_co
     SampleSlice* out = a.slice + (size_t)row * a.slices + slice;
     Row r;
     set_row(r, l, M);
-    const bool skip = l.bad || l.one || M == -INFINITY;
+    const bool skip = l.bad || l.one || isinf(M);         // (rows with an infinite logit are the rest's)
     // ---- its weights, as far as sums over the row are asked for
     const bool weigh = !skip && !l.use_k && (l.use_p || !l.use_m);
     if (weigh) {
@@ -1159,34 +1180,57 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) k_sample_scan(const __grid_co
                 unsigned before = in - n0 - n1;
 #pragma unroll
                 for (int w = 0; w < SCAN_WARPS; ++w) before += w < warp ? s_count[w] : 0u;
-                if (before < of && of <= before + n0) s_bin = 2 * tid;
-                else if (before + n0 < of && of <= before + n0 + n1) s_bin = 2 * tid + 1;
+                if (before < of && of <= before + n0) { s_bin = 2 * tid; s_before = before; }
+                else if (before + n0 < of && of <= before + n0 + n1) { s_bin = 2 * tid + 1; s_before = before + n0; }
                 __syncthreads();
-                int bin = s_bin;
-                if (l.use_m && !(l.use_k && l.use_p)) {
-                    // what min_p takes away from the largest here it takes away from the row's
-                    const double d = -log(r.min_p) * (1.4426950408889634 * STEPS) * 1.00001 + 1.0;
-                    bin = min(bin, d < FINE ? (int)d : min(FINE + (int)((fmin(d, 1e6) - FINE) / COARSE), BINS - 1));
+                if (s_bin < BINS - 1) {
+                    // of the largest in that bin the one itself
+                    if (b == s_bin) s_near[atomicAdd(&s_near_n, 1u)] = mine;
+                    __syncthreads();
+                    if (b == s_bin) {
+                        unsigned over = s_before, same = 0;
+                        for (unsigned i = 0; i < s_near_n; ++i) {
+                            over += s_near[i] > mine;
+                            same += s_near[i] == mine;
+                        }
+                        if (over < of && of <= over + same) s_cut = mine;
+                    }
+                    __syncthreads();
+                    cut = s_cut;
+                    if (l.use_m && !(l.use_k && l.use_p)) {
+                        // what min_p takes away from the largest here it takes away from the row's
+                        const double d = -log(r.min_p) * (1.4426950408889634 * STEPS) * 1.00001 + 1.0;
+                        cut = fmaxf(cut, M - (float)fmin(d, 3e38) / r.steps);
+                    }
                 }
-                if (bin < BINS - 1) cut = M - wide_end(bin) / r.steps;
             }
         }
         unsigned long long* list = a.entries + ((size_t)row * a.slices + slice) * CAP;
         if (cut < INFINITY) {
+            // which of a thread's elements as bits, the warp's places by one addition
+            uint32_t bits = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                float x[VEC], most = -INFINITY;
+                float x[VEC];
                 unpack(j, x);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) most = fmaxf(most, x[e]);
-                if (most < cut) continue;
+                for (int e = 0; e < VEC; ++e) bits |= (uint32_t)(x[e] >= cut && i0 + j * 32 * VEC + e < n) << (j * VEC + e);
+            }
+            const unsigned upto = warp_scan_u32(__popc(bits), lane);
+            unsigned at = 0;
+            if (lane == 31) at = atomicAdd(&s_n, upto);
+            at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(bits);
+            if (__any_sync(0xffffffffu, bits)) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const int i = i0 + j * 32 * VEC + e;
-                    if (x[e] >= cut && i < n) {
-                        const unsigned at = atomicAdd(&s_n, 1u);
-                        if (at < CAP) list[at] = rank_of(x[e], first + i);
-                    }
+                for (int j = 0; j < PER; ++j) {
+                    float x[VEC];
+                    unpack(j, x);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if ((bits >> (j * VEC + e)) & 1) {
+                            if (at < CAP) list[at] = rank_of(x[e], first + i0 + j * 32 * VEC + e);
+                            ++at;
+                        }
                 }
             }
         }
@@ -1207,7 +1251,7 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
     __shared__ Shared sm;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();
-    if (tid < TAB) sm.tab[tid] = exp2((double)tid / TAB);
+    if (tid < TAB) sm.tab[tid] = POW_TABLE.v[tid];
     sm.hist[tid] = 0;
     if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; sm.bin = BINS; sm.lo[0] = 0; }
     const Limits l = limits_of(a, row);
@@ -1242,6 +1286,10 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
         }
         return;
     }
+    if (isinf(M)) {
+        if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = {0.0, M, row};
+        return;
+    }
     Row r;
     set_row(r, l, M);
     cut = key_value(sm.lo[0]);            // all elements of the row that are not below it are in the lists
@@ -1255,7 +1303,7 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
         for (int e = 0; e < PER; ++e) {
             const int i = tid * PER + e, sl = i / SCAN_WARPS;
             w[e] = 0.0;
-            if (sl < a.slices) w[e] = __ldcg(&slice[sl].stretch[i % SCAN_WARPS]) * weight(r, sm.tab, rank_value(__ldcg(&slice[sl].best)));
+            if (sl < a.slices) w[e] = __ldcg(&slice[sl].stretch[i % SCAN_WARPS]) * weight(r, sm.tab, rank_value(__ldcg(&slice[sl].best)));      // (no sums without a finite logit: 0)
             if (w[e] < 0x1p-110) w[e] = 0.0;                       // (2^10 elements that count as nothing one by one)
             run += w[e];
         }
@@ -1396,7 +1444,7 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
         count = (int)sm.n_list;
     }
     if (count > LIST) {
-        if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = row;
+        if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = {S, M, row};
         return;
     }
     from_list(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform);
@@ -1449,7 +1497,7 @@ extern "C" {
 int esp_sample_scratch_bytes(int32_t n_rows, int32_t vocab, size_t* bytes_out) {
     if (!bytes_out || n_rows < 0 || n_rows > (1 << 24) || vocab < 1 || vocab > MAX_VOCAB) return ESP_E_ARG;
     const size_t slices = (size_t)n_rows * ((vocab + SAMPLE_SLICE - 1) / SAMPLE_SLICE);
-    *bytes_out = slices * (sizeof(SampleSlice) + SAMPLE_CAP * sizeof(unsigned long long)) + ((size_t)n_rows + 1) * sizeof(int32_t);
+    *bytes_out = slices * (sizeof(SampleSlice) + SAMPLE_CAP * sizeof(unsigned long long)) + (size_t)n_rows * sizeof(SampleRest) + sizeof(int32_t);
     return ESP_OK;
 }
 
@@ -1473,8 +1521,8 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     if ((int64_t)n_rows * a.slices > 0x7fffffff) return ESP_E_ARG;
     a.slice = reinterpret_cast<SampleSlice*>(scratch);
     a.entries = reinterpret_cast<unsigned long long*>(a.slice + (size_t)n_rows * a.slices);
-    a.rest = reinterpret_cast<int32_t*>(a.entries + (size_t)n_rows * a.slices * SAMPLE_CAP);
-    a.n_rest = a.rest + n_rows;
+    a.rest = reinterpret_cast<SampleRest*>(a.entries + (size_t)n_rows * a.slices * SAMPLE_CAP);
+    a.n_rest = reinterpret_cast<int32_t*>(a.rest + n_rows);
     a.logits = logits; a.row_stride = row_stride; a.n_rows = n_rows; a.vocab = vocab;
     a.temperature = sampling->temperature; a.top_k = sampling->top_k; a.top_p = sampling->top_p; a.min_p = sampling->min_p;
     a.uniform = uniform; a.tokens = tokens; a.logprob = logprob; a.chunk = 0;
