@@ -1510,6 +1510,7 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     if (off(logits, size) || off(sampling->temperature, 4) || off(sampling->top_k, 4) || off(sampling->top_p, 4) || off(sampling->min_p, 4) || off(uniform, 4) ||
         off(tokens, 4) || off(logprob, 4)) return ESP_E_ARG;
     if (n_rows == 0) return ESP_OK;
+    if ((int64_t)n_rows * ((vocab + SAMPLE_SLICE - 1) / SAMPLE_SLICE) > 0x7fffffff) return ESP_E_ARG;
     if (!logits || !uniform || !tokens) return ESP_E_ARG;
     size_t need = 0;
     if (const int rc = esp_sample_scratch_bytes(n_rows, vocab, &need)) return rc;
@@ -1518,7 +1519,6 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     if (n_sm < 1) return ESP_E_CUDA;
     SampleArgs a;
     a.slices = (vocab + SAMPLE_SLICE - 1) / SAMPLE_SLICE;
-    if ((int64_t)n_rows * a.slices > 0x7fffffff) return ESP_E_ARG;
     a.slice = reinterpret_cast<SampleSlice*>(scratch);
     a.entries = reinterpret_cast<unsigned long long*>(a.slice + (size_t)n_rows * a.slices);
     a.rest = reinterpret_cast<SampleRest*>(a.entries + (size_t)n_rows * a.slices * SAMPLE_CAP);
