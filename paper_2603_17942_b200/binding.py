@@ -378,16 +378,18 @@ def _need(ok: bool, where: str, what: str):
 
 _torch = None
 _DTYPES: Dict[object, int] = {}        # torch dtype -> dtype of the library
+_device_now = None                     # the current device's number (torch.cuda.current_device without its detour through the interpreter, where torch has that)
 
 
 def _on_current_device(device: int, where: str):
     """The tensors' device (their get_device()) has to be the current one: the library launches there."""
-    global _torch
+    global _torch, _device_now
     if _torch is None:
         import torch
         _DTYPES.update({torch.float32: 0, torch.bfloat16: 1})
+        _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _torch = torch
-    if device < 0 or device != _torch.cuda.current_device():
+    if device < 0 or device != _device_now():
         raise EspError(-8, f"{where} (tensors on device {device}, which is not the current one)")
 
 
