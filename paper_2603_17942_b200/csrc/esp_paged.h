@@ -109,7 +109,7 @@ struct AcceptArgs {
     int32_t out_stride, Hkv, D, vec;
 };
 
-constexpr int SAMPLE_SLICE = 8192, SAMPLE_CAP = 160, SAMPLE_MAX_SLICES = 256;
+constexpr int SAMPLE_SLICE = 8192, SAMPLE_CAP = 160, SAMPLE_MAX_SLICES = 256, SAMPLE_BINS = 512;
 struct SampleSlice {        // what the first pass leaves of a slice of a row
     unsigned long long best;          // its first element in the order
     float cut;                        // its elements that are not below this are in its list (infinity: it has none)

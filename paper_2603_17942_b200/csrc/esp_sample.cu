@@ -1,16 +1,20 @@
 // Sampling from rows of logits: temperature, top-k, top-p and min-p, from one given random number a row.
 //
-// A cluster of blocks has a row, each block a stretch of it that it copies into its shared memory once; everything else reads it there.
-//   order      larger logits first, of equal ones the lower index: a 32-bit key of the logit (its bits in the order of the values) and the index.  top-k, top-p and min-p each
-//              keep a front of that order.
-//   weights    exp in 64 bits, summed in 64 bits in a fixed order, wherever a sum decides.
-//   list       A value that the front does not reach below is found first.  For top-k, of the largest logits of each thread the k-th one: k elements are not below it, and of elements
-//              that lie anywhere hardly more.  For top-p, from a histogram of the weights along (largest - logit) / temperature, in steps of 1/24 octave.  For min-p it
-//              is given.  What lies above, a few dozen to a few hundred elements, goes to the first block, the others are done.  It sorts them, takes exact sums along the
-//              order, cuts, and finds the lowest index at which the kept weights exceed uniform times their sum.
-//   long front of top-p: exact sums up to the bin that holds its end, that bin's elements sorted by the first block for the end itself, and the draw
-//              by sums of the kept weights over stretches in the order of indices, the stretch in which uniform * total lies, the element.
-//   the rest   (long fronts of top-k, thousands of equal logits): the last element of a front by histograms that close in on it; then the draw as above.
+// The order: larger logits first, of equal ones the lower index.  top-k, top-p and min-p each keep a front of it.  Weights are exp((x - M) / temperature) in 64 bits, M the row's
+// largest, and their sums are in 64 bits in a fixed order wherever a sum decides: the front of top-p ends where a sum meets top_p times another, and the draw where one exceeds
+// uniform times another.  The token is found along the indices, not along the order, so that nothing has to be sorted but what the limits ask for.
+//
+//   scan   a block for each slice of 8192 logits of a row, which it holds in its registers and reads once: the slice's largest element, the sums of its weights by stretches of 1024
+//          (for top-p and for rows without limits), and a list of its largest elements, about 110, with the value below which it leaves things out.  How many weights it has to
+//          work out is what bounds it where sums are asked for (us, 272 fp32 rows of 128256, 20 us to read: greedy 28, temperature alone 54, min-p 60).
+//   list   a block for each row: the slices' largest give M, and the sums scaled to it the row's S.  What the limits keep lies nearly always within the lists: histograms say how far,
+//          those elements are sorted, their exact sums cut, and the draw is among them.  Rows without limits draw by stretches: the one the target lies in, then its element.
+//   rest   clusters of up to eight blocks for the rows that the lists do not settle.
+//          Long fronts of top-p (thousands of elements): a histogram of the weights over the whole row says in which bin of 1/25 of a logit the front ends; then sums of what lies in
+//          front of the bin, with that bin's elements as lists; the end by exact sums along them; the draw by stretches.  About 45 us for a row, 18 rows at a time.
+//          Everything else (long fronts of top-k, thousands of equal logits, infinite logits): a value that the front does not reach below, or, where too much lies above it, the
+//          front's last element by histograms that close in on it; then the draw by stretches.
+// Sorting whole rows is what this avoids: with the row in a cluster's shared memory and every limit's end found there, the same 272 rows took 200 to 480 us instead of 54 to 180.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -25,14 +29,15 @@ namespace {
 using paged::warp_scan_u32;
 
 constexpr int NT = 512, NW = NT / 32;
-constexpr int BINS = NT;                  // of a histogram, a thread for each
+constexpr int BINS = SAMPLE_BINS;         // of a histogram, a thread for each
+static_assert(BINS == NT, "");
 constexpr float STEPS = 24.f;             // fine bins of an octave of weights: 21 octaves
 constexpr int FINE = 256, COARSE = 8;     // wide bins: that many fine ones, then as wide as eight of them: 95 octaves
 constexpr int MAX_CL = 8;                 // blocks of a cluster at most
 constexpr int LIST = 2048;                // elements that are sorted at most
 constexpr int SMEM_ROW = 160 * 1024;      // bytes of a row that a block keeps at most
 constexpr int TAB = 256;                  // 2^(j / TAB)
-constexpr float UNIT = 8192.f;            // a histogram of weights counts in 1 / UNIT of a bin's largest: 2^19 elements of a block fit 32 bits
+constexpr float UNIT = 32768.f, GRID = 25.f;       // a histogram of weights counts in 1 / UNIT of what a bin's upper end weighs, bins are 1 / GRID of a logit
 constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
 constexpr int WANT = 110;                 // elements of a slice that go to its list, more or less
 
@@ -247,9 +252,9 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
     __syncthreads();
 }
 
-// What the first block does with a list of `count` elements that holds the front: sorts it, cuts it and draws.  S: the weights of the whole row that top_p goes by (below 0: those of
-// the first top_k).
-__device__ __forceinline__ void from_list(const Row& r, Shared& sm, const SampleArgs& a, int row, int count, int top_k, float top_p, double S, float uniform) {
+// What a block does with a list of `count` elements, the first ones of the order: sorts it, cuts it and draws.  S: the weights of the whole row that top_p goes by (below 0: those of
+// the first top_k).  whole: what is not in the list is not kept.  false: top_p reaches beyond the list.
+__device__ __forceinline__ bool from_list(const Row& r, Shared& sm, const SampleArgs& a, int row, int count, int top_k, float top_p, double S, float uniform, bool whole) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     sort_list(r, sm, count);
 
@@ -279,6 +284,7 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
             upto += before;
         }
         const double theta = top_p < 1.f ? (double)top_p * (S < 0.0 ? all : S) : INFINITY;
+        if (tid == 0) sm.verdict = !whole && S >= 0.0 && top_p < 1.f && all < theta;
         int stay = 0;
         double sum = 0.0;
 #pragma unroll
@@ -296,6 +302,7 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
         } else if (lane == 0) { sm.warp_count[warp] = stay; sm.warp_sum[warp] = sum; }
     }
     __syncthreads();
+    if (sm.verdict) return false;
     int kept = 0;
     double W = 0.0;
     if (one_warp) {
@@ -310,7 +317,7 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
     // ---- the smallest index at which the kept weights in the order of indices exceed the target; with a target that nothing exceeds, the last kept one with weight
     if (kept <= 128) {
         // each element adds up those that its index has in front of it.  (0xffffffff: no candidate)
-        if (warp >= 4) return;
+        if (warp >= 4) return true;
         if (warp == 0 || warp * 32 < kept) {
             const int mine = tid < kept ? (int)(uint32_t)sm.list[tid] : -1;
             double upto = 0.0;
@@ -331,7 +338,7 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
             a.tokens[row] = (int)token;
             if (a.logprob) a.logprob[row] = (float)log(sm.list_w[tid] / W);
         }
-        return;
+        return true;
     }
     // the range of indices in NW parts at a time: a warp sums up to each border
     int lo = -1, hi = a.vocab - 1;                                  // the sum up to lo does not exceed the target; up to hi it does, or nothing does
@@ -363,6 +370,7 @@ __device__ __forceinline__ void from_list(const Row& r, Shared& sm, const Sample
                 if (a.logprob) a.logprob[row] = (float)log(sm.list_w[i] / W);
             }
     }
+    return true;
 }
 
 // A row's settings.
@@ -393,6 +401,318 @@ __device__ __forceinline__ void set_row(Row& r, const Limits& l, float M) {
     r.steps = (float)fmin(inv_t * ((double)STEPS * 1.4426950408889634), 3e38);
     r.bound = ~0ull;
     r.min_p = fmin((double)l.min_p, 1.0);
+}
+
+constexpr int SCAN_THREADS = 256, SCAN_WARPS = SCAN_THREADS / 32, SLICE = SAMPLE_SLICE, CAP = SAMPLE_CAP, STRETCH = SLICE / SCAN_WARPS;
+constexpr int PER_STRETCH = SAMPLE_MAX_SLICES * SCAN_WARPS / NT;      // stretches of a thread of the second pass
+
+// The token, given the kept weights w of PER_STRETCH stretches of each thread in their order and their sum W: the stretch in which the target lies, or the last one with
+// weight, then its element.  All threads of a block.
+template <typename T>
+__device__ __forceinline__ void draw_from(const Row& r, Shared& sm, const SampleArgs& a, int row, const double (&w)[PER_STRETCH], double W, double target) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int NONE = 1 << 30, E = STRETCH / NT;
+    double run = 0.0;
+#pragma unroll
+    for (int e = 0; e < PER_STRETCH; ++e) run += w[e];
+    const double in = warp_scan_f64(run, lane);
+    __syncthreads();
+    if (lane == 31) sm.warp_sum[warp] = in;
+    if (tid == 0) { sm.bin = NONE; sm.end_bin = -1; }
+    __syncthreads();
+    double upto = in - run;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) upto += k < warp ? sm.warp_sum[k] : 0.0;
+    int found = NONE, last = -1;
+    double found_front = 0.0, last_front = 0.0;
+#pragma unroll
+    for (int e = 0; e < PER_STRETCH; ++e) {
+        if (w[e] > 0.0) {
+            last = tid * PER_STRETCH + e;
+            last_front = upto;
+            if (found == NONE && upto + w[e] > target) { found = last; found_front = upto; }
+        }
+        upto += w[e];
+    }
+    const int f = __reduce_min_sync(0xffffffffu, found), z = __reduce_max_sync(0xffffffffu, last);
+    if (lane == 0) { atomicMin(&sm.bin, f); atomicMax(&sm.end_bin, z); }
+    __syncthreads();
+    const bool none = sm.bin == NONE;
+    const int at = none ? sm.end_bin : sm.bin;
+    if (none ? last == at : found == at) sm.kept_sum = none ? last_front : found_front;
+    __syncthreads();
+    // neighbours a thread
+    const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
+    const int i0 = at * STRETCH + tid * E;
+    double v[E], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float x = i0 + e < a.vocab ? number(to_f32(logits[i0 + e])) : -INFINITY;
+        v[e] = rank_of(x, i0 + e) <= r.bound ? weight(r, sm.tab, x) : 0.0;
+        sum += v[e];
+    }
+    const double scan = warp_scan_f64(sum, lane);
+    if (lane == 31) sm.warp_sum2[warp] = scan;
+    if (tid == 0) { sm.bin = NONE; sm.end_bin = -1; }
+    __syncthreads();
+    double here = sm.kept_sum + scan - sum;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) here += k < warp ? sm.warp_sum2[k] : 0.0;
+    int hit = NONE, some = -1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        here += v[e];
+        if (v[e] > 0.0) {
+            some = tid * E + e;
+            if (hit == NONE && here > target) hit = some;
+        }
+    }
+    const int h = __reduce_min_sync(0xffffffffu, hit), y = __reduce_max_sync(0xffffffffu, some);
+    if (lane == 0) { atomicMin(&sm.bin, h); atomicMax(&sm.end_bin, y); }
+    __syncthreads();
+    const int token = sm.bin < NONE ? sm.bin : sm.end_bin;
+    if (token / E == tid) {
+        a.tokens[row] = at * STRETCH + token;
+        if (a.logprob) a.logprob[row] = (float)log((token % E ? v[E - 1] : v[0]) / W);
+    }
+}
+
+// Bins on a grid that all rows share, 1/25 of a logit each: bin k holds the logits from k / GRID on.
+__device__ __forceinline__ int grid_bin(float x) { return __float2int_rd(x * GRID); }
+// What an element adds to its bin of weights, in 1 / UNIT of the weight of the bin's upper end; per: log2 e / (GRID temperature).
+__device__ __forceinline__ unsigned grid_weight(float x, int k, float per) { return __float2uint_rn(UNIT * exp2f((x * GRID - (float)(k + 1)) * per)); }
+
+// A slice of n logits, VEC of them to a lane at i0, i0 + 32 VEC, ...; -infinity behind its end.
+template <typename T>
+__device__ __forceinline__ void load_slice(const T* x0, int n, int i0, uint4 (&raw)[SLICE / SCAN_THREADS / Raw<T>::VEC]) {
+    constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
+    const bool aligned = reinterpret_cast<uintptr_t>(x0) % 16 == 0;
+    if (n == SLICE && aligned) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) raw[j] = __ldg(reinterpret_cast<const uint4*>(x0 + i0 + j * 32 * VEC));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = i0 + j * 32 * VEC;
+        if (aligned && i + VEC <= n) raw[j] = __ldg(reinterpret_cast<const uint4*>(x0 + i));
+        else {
+            float x[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] = i + e < n ? to_f32(x0[i + e]) : -INFINITY;
+            raw[j] = Raw<T>::pack(x);
+        }
+    }
+}
+// The elements that `bits` marks of SCAN_THREADS threads' into a list of CAP, in the order of warps and lanes; how many there are.  All threads of the block (s_count: their part's).
+template <typename T>
+__device__ __forceinline__ unsigned put_bits(const uint4 (&raw)[SLICE / SCAN_THREADS / Raw<T>::VEC], uint32_t bits, unsigned* s_count, unsigned long long* list, int index0) {
+    constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x % SCAN_THREADS) >> 5;
+    const unsigned upto = warp_scan_u32(__popc(bits), lane);
+    __syncthreads();
+    if (lane == 31) s_count[warp] = upto;
+    __syncthreads();
+    unsigned at = upto - __popc(bits), all = 0;
+#pragma unroll
+    for (int w = 0; w < SCAN_WARPS; ++w) {
+        at += w < warp ? s_count[w] : 0u;
+        all += s_count[w];
+    }
+    if (all <= CAP && __any_sync(0xffffffffu, bits)) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            float x[VEC];
+            Raw<T>::unpack(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if ((bits >> (j * VEC + e)) & 1) list[at++] = rank_of(x[e], index0 + j * 32 * VEC + e);
+        }
+    }
+    return all;
+}
+
+// A long front of top-p, first step: a histogram of the row's weights.  The cluster's blocks take the row's slices, half a block for each.  Gives the bin in which the front ends (or its neighbour, at a border
+// of bins); false: it is not known.
+template <typename T>
+__device__ __forceinline__ bool front_bins(const Row& r, Shared& sm, const SampleArgs& a, const SampleRest& known, float top_p, int& bin, int me, int CL) {
+    constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, base = grid_bin(known.M);
+    const float per = r.steps * (1.f / (STEPS * GRID));
+    for (int s0 = 2 * me; s0 < a.slices; s0 += 2 * CL) {
+        const int first = (s0 + tid / SCAN_THREADS) * SLICE, n = max(0, min(SLICE, a.vocab - first)), i0 = warp % SCAN_WARPS * STRETCH + lane * VEC;
+        uint4 raw[PER];
+        load_slice<T>(reinterpret_cast<const T*>(a.logits) + (long long)known.row * a.row_stride + first, n, i0, raw);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            float x[VEC];
+            Raw<T>::unpack(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const int k = grid_bin(x[e]);
+                if ((uint32_t)base - (uint32_t)k < BINS && x[e] == x[e]) atomicAdd(&sm.hist[base - k], grid_weight(x[e], k, per));
+            }
+        }
+    }
+    cluster.sync();
+    uint32_t part[MAX_CL];
+#pragma unroll
+    for (int c = 0; c < MAX_CL; ++c) part[c] = c < CL ? cluster.map_shared_rank(sm.hist, c)[tid] : 0u;
+    unsigned long long mine = 0;
+#pragma unroll
+    for (int c = 0; c < MAX_CL; ++c) mine += part[c];
+    // sums along the bins, by what each one's upper end weighs
+    const float v = (float)mine * (1.f / UNIT) * exp2f(((float)(base - tid + 1) - known.M * GRID) * per);
+    float in = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float y = __shfl_up_sync(0xffffffffu, in, o);
+        if (lane >= o) in += y;
+    }
+    if (lane == 31) sm.warp_f[warp] = in;
+    if (tid == 0) sm.bin = BINS;
+    __syncthreads();
+    float before = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) before += w < warp ? sm.warp_f[w] : 0.f;
+    if (before + in >= (float)((double)top_p * known.S)) atomicMin(&sm.bin, tid);
+    __syncthreads();
+    bin = base - sm.bin;
+    const bool found = sm.bin < BINS;
+    cluster.sync();                       // (the histograms have been read)
+    return found;
+}
+
+// A long front of top-p, second step: what lies in front of the bin is added up, by stretches, and its elements go to the slices' lists.
+template <typename T>
+__device__ __forceinline__ void front_slices(const Row& r, Shared& sm, const SampleArgs& a, const SampleRest& known, int bin, int me, int CL) {
+    constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
+    const int tid = threadIdx.x, lane = tid & 31, half = tid / SCAN_THREADS, warp = (tid % SCAN_THREADS) >> 5;
+    for (int s0 = 2 * me; s0 < a.slices; s0 += 2 * CL) {                 // the same trips in every thread
+        const int slice = s0 + half, first = slice * SLICE, n = max(0, min(SLICE, a.vocab - first)), i0 = warp * STRETCH + lane * VEC;
+        uint4 raw[PER];
+        load_slice<T>(reinterpret_cast<const T*>(a.logits) + (long long)known.row * a.row_stride + first, n, i0, raw);
+        double s = 0.0;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            float x[VEC];
+            Raw<T>::unpack(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                x[e] = number(x[e]);
+                const int k = grid_bin(x[e]);
+                const double w = weight(r, sm.tab, x[e]);
+                s += k > bin ? w : 0.0;
+                bits |= (uint32_t)(k == bin && i0 + j * 32 * VEC + e < n) << (j * VEC + e);
+            }
+            raw[j] = Raw<T>::pack(x);
+        }
+        s = warp_sum_f64(s);
+        const unsigned listed = put_bits<T>(raw, bits, sm.warp_count + half * SCAN_WARPS, a.entries + ((size_t)known.row * a.slices + slice) * CAP, first + i0);
+        if (slice < a.slices) {
+            SampleSlice* out = a.slice + (size_t)known.row * a.slices + slice;
+            if (lane == 0) out->stretch[warp] = s;
+            if (tid % SCAN_THREADS == 0) {
+                out->n = listed <= CAP ? (int)listed : 0;
+                out->cut = listed <= CAP ? 0.f : INFINITY;
+            }
+        }
+    }
+}
+
+// Third step, by one block: the end of the front is found among the listed elements, the draw is by stretches.  -1: it ends in a bin of larger logits,
+// 1: of smaller ones, 2: there are too many elements.
+template <typename T>
+__device__ __forceinline__ int from_front(Row& r, Shared& sm, const SampleArgs& a, const SampleRest& known, float top_p, float uniform) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const SampleSlice* slice = a.slice + (size_t)known.row * a.slices;
+    const unsigned long long* entries = a.entries + (size_t)known.row * a.slices * CAP;
+    double w[PER_STRETCH], run = 0.0;
+#pragma unroll
+    for (int e = 0; e < PER_STRETCH; ++e) {
+        const int i = tid * PER_STRETCH + e;
+        w[e] = i / SCAN_WARPS < a.slices ? __ldcg(&slice[i / SCAN_WARPS].stretch[i % SCAN_WARPS]) : 0.0;
+        run += w[e];
+    }
+    if (tid < a.slices) sm.all[tid] = __ldcg(&slice[tid].n);
+    const bool over = __syncthreads_or(tid < a.slices && __ldcg(&slice[tid].cut) == INFINITY);
+    if (over) return 2;
+    for (int i = tid; i < a.slices * CAP; i += NT)
+        if (i % CAP < (int)sm.all[i / CAP]) {
+            const unsigned at = atomicAdd(&sm.n_list, 1u);
+            if (at < LIST) sm.list[at] = __ldcg(entries + i);
+        }
+    const double all_in = warp_scan_f64(run, lane);
+    if (lane == 31) sm.warp_sum[warp] = all_in;
+    __syncthreads();
+    const int count = (int)sm.n_list;
+    double before = 0.0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) before += sm.warp_sum[k];
+    const double theta = (double)top_p * known.S;
+    if (before >= theta) return -1;
+    if (count < 1) return 1;
+    if (count > LIST) return 2;
+    // the first element at which the sums along the order reach theta, four neighbours a thread
+    sort_list(r, sm, count);
+    constexpr int PER = LIST / NT, NONE = 1 << 30;
+    double v[PER], part = 0.0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        v[e] = tid * PER + e < count ? sm.list_w[tid * PER + e] : 0.0;
+        part += v[e];
+    }
+    const double in = warp_scan_f64(part, lane);
+    if (lane == 31) sm.warp_sum2[warp] = in;
+    if (tid == 0) sm.bin = NONE;
+    __syncthreads();
+    double upto = before + in - part, W = 0.0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) upto += k < warp ? sm.warp_sum2[k] : 0.0;
+    int end = NONE;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        upto += v[e];
+        if (end == NONE && tid * PER + e < count && upto >= theta) { end = tid * PER + e; W = upto; }
+    }
+    const int first = __reduce_min_sync(0xffffffffu, end);
+    if (lane == 0) atomicMin(&sm.bin, first);
+    __syncthreads();
+    if (sm.bin == NONE) return 1;
+    if (end == sm.bin) { sm.kept_sum = W; sm.answer = sm.list[end]; }
+    __syncthreads();
+    W = sm.kept_sum;
+    r.bound = sm.answer;
+    // what of the lists is kept, by stretches (the sorted list is done with: its place has the sums)
+    double* kept = reinterpret_cast<double*>(sm.list);
+    for (int s = warp; s < a.slices; s += NW) {
+        const int n = (int)__ldcg(&slice[s].n);
+        double sum[SCAN_WARPS];
+#pragma unroll
+        for (int e = 0; e < SCAN_WARPS; ++e) sum[e] = 0.0;
+        for (int i = lane; i < n; i += 32) {
+            const unsigned long long x = __ldcg(entries + (size_t)s * CAP + i);
+            const double y = x <= r.bound ? weight(r, sm.tab, rank_value(x)) : 0.0;
+            const int at = ((int)(uint32_t)x - s * SLICE) / STRETCH;
+#pragma unroll
+            for (int e = 0; e < SCAN_WARPS; ++e) sum[e] += e == at ? y : 0.0;
+        }
+#pragma unroll
+        for (int e = 0; e < SCAN_WARPS; ++e) {
+            const double y = warp_sum_f64(sum[e]);
+            if (lane == 0) kept[s * SCAN_WARPS + e] = y;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < PER_STRETCH; ++e) {
+        const int i = tid * PER_STRETCH + e;
+        if (i / SCAN_WARPS < a.slices) w[e] += kept[i];
+    }
+    draw_from<T>(r, sm, a, known.row, w, W, (double)uniform * W);
+    return 0;
 }
 
 template <typename T, bool RESIDENT>
@@ -441,6 +761,28 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
 
     if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
     if (tid < TAB) sm.tab[tid] = POW_TABLE.v[tid];
+    sm.hist[tid] = 0;
+    set_row(r, l, known.M);
+    int bin = 0;
+    __syncthreads();
+    // a long front of top-p (not with logits so large that their last bit is 3e-5 of a weight, or that a bin's number does not fit)
+    if (use_p && !use_k && !use_m && fabsf(known.M) * r.steps < 17000.f && fabsf(known.M) < 1e7f && front_bins<T>(r, sm, a, known, top_p, bin, me, CL))
+        for (int tries = 0; tries < 3; ++tries) {
+            front_slices<T>(r, sm, a, known, bin, me, CL);
+            cluster.sync();
+            int verdict = 0;
+            if (me == 0) verdict = from_front<T>(r, sm, a, known, top_p, uniform);
+            if (me == 0 && tid < CL) *cluster.map_shared_rank(&sm.verdict, tid) = verdict;
+            cluster.sync();
+            verdict = sm.verdict;
+            if (verdict == 0) return;
+            if (verdict == 2) break;
+            bin -= verdict;
+            if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
+            cluster.sync();
+        }
+    __syncthreads();
+    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; }
     sm.hist[tid] = 0;
     cluster.barrier_arrive();             // (before anybody looks into another block's shared memory, all have to have started)
 
@@ -534,72 +876,31 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
         cluster.sync();
         S = total();
     }
-    double front_w = 0.0;                 // weights of this thread's elements in front of the bin that a front ends in
-    bool have_front = false;
-    int end_bin = 0;
     if (use_k || use_p || use_m) {
         const bool weigh = use_p && !use_k;
         int last_bin = -1;                // wide bins up to here go to the list; -1: too many
         if (a.vocab <= LIST) last_bin = BINS - 1;
-        if (weigh) {
-            // a histogram of the weights.  What lies at `cut` or below is in no bin (a little lower, so that rounding does not matter)
-            const float cut = r.M - ((float)BINS / r.steps) * 1.00001f;
-#pragma unroll 2
-            for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-                float x[VEC];
-                load(i, x);
-                float top = x[0];
-#pragma unroll
-                for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
-                if (!(top < cut)) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float d = depth_of(r, x[e]);
-                        const int b = (int)d;
-                        // (2^(-1/24) = 0.97153; linear in between, off by 1.1e-4 at most)
-                        if (b < BINS - 1) atomicAdd(&sm.hist[b], (unsigned)UNIT - (unsigned)((d - (float)b) * (UNIT * (1.f - 0.97153194f))));
-                    }
-                }
-            }
-        } else if (use_k && last_bin < 0) {
+        else if (use_k) {
             // the threads' largest logits (equal shares of the row for each, or one element more)
             const int b = wide_bin(r, own_best);
             if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
-        }
-        if (weigh || (use_k && last_bin < 0)) {
             cluster.sync();
-            unsigned part[MAX_CL];
+            unsigned part[MAX_CL], mine = 0;
 #pragma unroll
             for (int c = 0; c < MAX_CL; ++c) part[c] = c < CL ? cluster.map_shared_rank(sm.hist, c)[tid] : 0u;
-            unsigned long long mine = 0;
 #pragma unroll
             for (int c = 0; c < MAX_CL; ++c) mine += part[c];
-            // sums along the bins: elements, or weights (a fine bin's smaller by 2^(1/24) than those of the one in front of it)
-            const float v = weigh ? (float)mine * (1.f / UNIT) * exp2f((float)tid * (-1.f / STEPS)) : (float)mine;
-            float in = v;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const float y = __shfl_up_sync(0xffffffffu, in, o);
-                if (lane >= o) in += y;
-            }
-            const unsigned cnt = warp_scan_u32(weigh ? (unsigned)ceilf((float)mine * (1.03f / UNIT)) : (unsigned)mine, lane);
-            if (lane == 31) { sm.warp_f[warp] = in; sm.warp_count[warp] = cnt; }
-            if (tid == 0) { sm.bin = BINS; sm.end_bin = BINS; }
+            const unsigned in = warp_scan_u32(mine, lane);
+            if (lane == 31) sm.warp_count[warp] = in;
+            if (tid == 0) sm.bin = BINS;
             __syncthreads();
-            float before = 0.f;
-            unsigned n_before = 0;
+            unsigned before = 0;
 #pragma unroll
-            for (int w = 0; w < NW; ++w)
-                if (w < warp) { before += sm.warp_f[w]; n_before += sm.warp_count[w]; }
-            // the border is in front of here at the latest: sums in steps of 2^-24 of themselves, the histogram's own error below 2e-4
-            const float goal = weigh ? (float)((double)top_p * S) : (float)top_k;
-            if (before + in >= goal * (weigh ? 1.001f : 1.f) && n_before + cnt <= LIST) atomicMin(&sm.bin, tid);
-            if (weigh && before + in >= goal) atomicMin(&sm.end_bin, tid);
+            for (int w = 0; w < NW; ++w) before += w < warp ? sm.warp_count[w] : 0u;
+            if (before + in >= (unsigned)top_k && before + in <= LIST) atomicMin(&sm.bin, tid);
             __syncthreads();
-            // (a bin that reaches the goal behind one that holds too much is no answer: sums only grow)
-            end_bin = sm.end_bin;
-            if (last_bin < 0 && sm.bin < BINS - 1) last_bin = weigh && sm.bin >= FINE ? min(FINE + (sm.bin - FINE) / COARSE, BINS - 1) : sm.bin;
-        } else if (last_bin < 0) {
+            if (sm.bin < BINS - 1) last_bin = sm.bin;
+        } else if (!weigh) {
             const double d = -log((double)r.min_p) * 1.4426950408889634 * STEPS * 1.00001 + 1.0;
             if (d < FINE) last_bin = (int)d;
         }
@@ -631,102 +932,20 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
                 }
                 fetch_parts();
                 cluster.barrier_arrive();
-                from_list(r, sm, a, row, count, use_k ? top_k : count, use_p ? top_p : 2.f, use_k ? -1.0 : S, uniform);
+                from_list(r, sm, a, row, count, use_k ? top_k : count, use_p ? top_p : 2.f, use_k ? -1.0 : S, uniform, true);
                 cluster.barrier_wait();
                 return;
             }
         }
-        // ---- a long front of top-p that ends in a fine bin
-        const double theta = (double)top_p * S;
-        for (int tries = 0; weigh && end_bin < BINS - 1 && tries < 4; ++tries) {
-            __syncthreads();
-            if (tid == 0) sm.n_list = 0;
-            cluster.sync();                                        // (histograms, counts and lists have been read)
-            front_w = 0.0;
-            // above `over` an element is in front of the bin for certain, below `under` behind it; between them its depth says
-            const float over = r.M - ((float)end_bin / r.steps) * 0.99999f, under = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
-#pragma unroll 2
-            for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-                float x[VEC];
-                load(i, x);
-                float top = x[0];
-#pragma unroll
-                for (int e = 1; e < VEC; ++e) top = fmaxf(top, x[e]);
-                if (!__any_sync(__activemask(), top >= under)) continue;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    bool front = x[e] > over;
-                    if (!front && x[e] >= under) {
-                        const int b = (int)depth_of(r, x[e]);
-                        front = b < end_bin;
-                        if (b == end_bin) {
-                            const unsigned p = atomicAdd(&sm.n_list, 1u);
-                            if (p < LIST) sm.list[p] = rank_of(x[e], first + i + e);
-                        }
-                    }
-                    const double w = weight(r, sm.tab, x[e]);
-                    front_w += front ? w : 0.0;
-                }
-            }
-            publish(front_w);
-            count_parts();
-            const double before = total();
-            if (count > LIST || count == 0) break;
-            if (me == 0) {
-                fetch_parts();
-                sort_list(r, sm, count);
-                // sums along it, four neighbours a thread: the first element at which they reach theta
-                double w[LIST / NT], run = 0.0;
-#pragma unroll
-                for (int e = 0; e < LIST / NT; ++e) {
-                    w[e] = tid * (LIST / NT) + e < count ? sm.list_w[tid * (LIST / NT) + e] : 0.0;
-                    run += w[e];
-                }
-                const double in = warp_scan_f64(run, lane);
-                if (lane == 31) sm.warp_sum2[warp] = in;
-                if (tid == 0) sm.bin = BINS * LIST;
-                __syncthreads();
-                double upto = before + in - run, all = before;
-#pragma unroll
-                for (int k = 0; k < NW; ++k) {
-                    if (k < warp) upto += sm.warp_sum2[k];
-                    all += sm.warp_sum2[k];
-                }
-                int end = BINS * LIST;
-#pragma unroll
-                for (int e = 0; e < LIST / NT; ++e) {
-                    upto += w[e];
-                    if (end == BINS * LIST && tid * (LIST / NT) + e < count && upto >= theta) end = tid * (LIST / NT) + e;
-                }
-                end = __reduce_min_sync(0xffffffffu, end);
-                if (lane == 0) atomicMin(&sm.bin, end);
-                __syncthreads();
-                if (tid < CL) {
-                    // (the histogram's sums may be off at a border of bins: the next one then)
-                    const int verdict = before >= theta && end_bin > 0 ? -1 : (sm.bin >= count && all < theta * (1.0 - 1e-13) ? 1 : 0);
-                    *cluster.map_shared_rank(&sm.verdict, tid) = verdict;
-                    *cluster.map_shared_rank(&sm.answer, tid) = sm.list[min(sm.bin, count - 1)];
-                }
-            }
-            cluster.sync();
-            if (sm.verdict == 0) {
-                r.bound = sm.answer;
-                have_front = true;
-                break;
-            }
-            end_bin += sm.verdict;
-        }
-        if (!have_front) {
-            cluster.sync();
-            if (tid == 0) sm.n_list = 0;
-        }
+        cluster.sync();                                            // histograms and counts have been read
+        if (tid == 0) sm.n_list = 0;
     }
 
     // ---- fronts too long for the list: what = 0 top-k, 1 top-p
     auto inside = [&](uint32_t k, uint32_t lo, uint32_t hi, int index) {
         return k >= lo && k <= hi && (((unsigned long long)~k << 32) | (unsigned)index) <= r.bound;
     };
-    for (int what = 0; what < 2 && !have_front; ++what) {
+    for (int what = 0; what < 2; ++what) {
         if (what == 0 ? !use_k : !use_p) continue;
         double theta = 0.0;               // top-p: the weights that have to be reached
         if (what == 1) {
@@ -968,30 +1187,12 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
         return w >= r.min_p ? w : 0.0;
     };
     double s = 0.0;
-    if (have_front && !use_m) {
-        // what is in front of the last bin has been added up
-        const float over = r.M - ((float)end_bin / r.steps) * 0.99999f, under = r.M - (float)(end_bin + 1) / r.steps * 1.00001f;
-        s = front_w;
-#pragma unroll 4
-        for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-            float x[VEC];
-            load(i, x);
-            bool near = false;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) near = near || (x[e] >= under && x[e] <= over);
-            if (near)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (x[e] >= under && x[e] <= over && (int)depth_of(r, x[e]) == end_bin && rank_of(x[e], first + i + e) <= r.bound) s += weight(r, sm.tab, x[e]);
-        }
-    } else {
 #pragma unroll 2
-        for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
-            float x[VEC];
-            load(i, x);
+    for (int i = w0 + lane * VEC; i < w1; i += STRIDE) {
+        float x[VEC];
+        load(i, x);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s += kept_weight(x[e], first + i + e);
-        }
+        for (int e = 0; e < VEC; ++e) s += kept_weight(x[e], first + i + e);
     }
     publish(s);
     cluster.sync();
@@ -1065,16 +1266,12 @@ __global__ void __launch_bounds__(NT, 2) k_sample_rest(const __grid_constant__ S
 }
 
 // ---- first pass: a block has a slice of a row in its registers, reads it once and leaves what the second pass needs
-#ifndef SCANB
-#define SCANB 4
-#endif
-constexpr int SCAN_BLOCKS = SCANB;
-constexpr int SCAN_THREADS = 256, SCAN_WARPS = SCAN_THREADS / 32, SLICE = SAMPLE_SLICE, CAP = SAMPLE_CAP, STRETCH = SLICE / SCAN_WARPS;
+constexpr int SCAN_BLOCKS = 5;            // (us, 272 rows of 128256 with a nucleus each: 3 205, 4 203, 5 200)
 template <typename T>
 __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const __grid_constant__ SampleArgs a) {
     constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
     __shared__ double s_tab[TAB], s_sum[SCAN_WARPS];
-    __shared__ uint32_t s_hist[BINS], s_key[SCAN_WARPS], s_index, s_n;
+    __shared__ uint32_t s_hist[BINS], s_key[SCAN_WARPS], s_index;
     __shared__ unsigned s_count[SCAN_WARPS];
     __shared__ int s_bin;
     __shared__ unsigned s_before, s_near_n;
@@ -1084,29 +1281,13 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const
     const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
     const int first = slice * SLICE, n = min(SLICE, a.vocab - first), i0 = warp * STRETCH + lane * VEC;       // a warp has a stretch, lanes side by side
     uint4 raw[PER];
-    if (n == SLICE && reinterpret_cast<uintptr_t>(logits + first) % 16 == 0) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j) raw[j] = __ldg(reinterpret_cast<const uint4*>(logits + first + i0 + j * 32 * VEC));
-    } else {
-        const bool aligned = reinterpret_cast<uintptr_t>(logits + first) % 16 == 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int i = i0 + j * 32 * VEC;
-            if (aligned && i + VEC <= n) raw[j] = __ldg(reinterpret_cast<const uint4*>(logits + first + i));
-            else {
-                float x[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) x[e] = i + e < n ? to_f32(logits[first + i + e]) : -INFINITY;
-                raw[j] = Raw<T>::pack(x);
-            }
-        }
-    }
+    load_slice<T>(logits + first, n, i0, raw);
     const Limits l = limits_of(a, row);
     if (tid < TAB) s_tab[tid] = POW_TABLE.v[tid];
     for (int i = tid; i < BINS; i += SCAN_THREADS) s_hist[i] = 0;
     if (tid == 0) {
         s_index = ~0u;
-        s_n = s_near_n = 0;
+        s_near_n = 0;
         if (blockIdx.x == 0) *a.n_rest = 0;
     }
     auto unpack = [&](int j, float (&x)[VEC]) { Raw<T>::unpack(raw[j], x); };
@@ -1160,6 +1341,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const
         s = warp_sum_f64(s);
         if (lane == 0) s_sum[warp] = s;
     }
+    unsigned listed = 0;
     // ---- its largest elements: the ones not below a value that so many of the threads' largest reach that `want` elements do, more or less
     float cut = INFINITY;
     if (!skip && (l.use_k || l.use_p || l.use_m)) {
@@ -1207,7 +1389,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const
         }
         unsigned long long* list = a.entries + ((size_t)row * a.slices + slice) * CAP;
         if (cut < INFINITY) {
-            // which of a thread's elements as bits, the warp's places by one addition
+            // which of a thread's elements as bits, places in the order of the warps and lanes
             uint32_t bits = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
@@ -1216,31 +1398,14 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_sample_scan(const
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) bits |= (uint32_t)(x[e] >= cut && i0 + j * 32 * VEC + e < n) << (j * VEC + e);
             }
-            const unsigned upto = warp_scan_u32(__popc(bits), lane);
-            unsigned at = 0;
-            if (lane == 31) at = atomicAdd(&s_n, upto);
-            at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(bits);
-            if (__any_sync(0xffffffffu, bits)) {
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    float x[VEC];
-                    unpack(j, x);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if ((bits >> (j * VEC + e)) & 1) {
-                            if (at < CAP) list[at] = rank_of(x[e], first + i0 + j * 32 * VEC + e);
-                            ++at;
-                        }
-                }
-            }
+            listed = put_bits<T>(raw, bits, s_count, list, first + i0);
         }
     }
     __syncthreads();
     if (tid == 0) {
         out->best = ((unsigned long long)~top << 32) | s_index;
-        const int count = (int)s_n;
-        out->n = min(count, CAP);
-        out->cut = count <= CAP ? cut : INFINITY;
+        out->n = listed <= CAP ? (int)listed : 0;
+        out->cut = listed <= CAP ? cut : INFINITY;
     }
     if (tid < SCAN_WARPS) out->stretch[tid] = weigh ? s_sum[tid] : 0.0;
 }
@@ -1253,7 +1418,7 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
     pdl_launch_dependents();
     if (tid < TAB) sm.tab[tid] = POW_TABLE.v[tid];
     sm.hist[tid] = 0;
-    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; sm.bin = BINS; sm.lo[0] = 0; }
+    if (tid == 0) { sm.answer = ~0ull; sm.n_list = 0; sm.lo[0] = 0; }
     const Limits l = limits_of(a, row);
     __syncthreads();
     pdl_wait();
@@ -1294,122 +1459,56 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
     set_row(r, l, M);
     cut = key_value(sm.lo[0]);            // all elements of the row that are not below it are in the lists
     // ---- sums of the slices' weights, four stretches a thread, in terms of the row's largest
-    const bool plain = !l.use_k && !l.use_p && !l.use_m;
+    const bool plain = !l.use_k && !l.use_p && !l.use_m, weigh = l.use_p && !l.use_k;
     double S = 0.0;
-    if (plain || (l.use_p && !l.use_k)) {
-        constexpr int PER = SAMPLE_MAX_SLICES * SCAN_WARPS / NT;
-        double w[PER], run = 0.0;
+    if (plain || weigh) {
+        double w[PER_STRETCH], run = 0.0;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const int i = tid * PER + e, sl = i / SCAN_WARPS;
+        for (int e = 0; e < PER_STRETCH; ++e) {
+            const int i = tid * PER_STRETCH + e, sl = i / SCAN_WARPS;
             w[e] = 0.0;
-            if (sl < a.slices) w[e] = __ldcg(&slice[sl].stretch[i % SCAN_WARPS]) * weight(r, sm.tab, rank_value(__ldcg(&slice[sl].best)));      // (no sums without a finite logit: 0)
+            // (no sums without a finite logit: 0)
+            if (sl < a.slices) w[e] = __ldcg(&slice[sl].stretch[i % SCAN_WARPS]) * weight(r, sm.tab, rank_value(__ldcg(&slice[sl].best)));
             if (w[e] < 0x1p-110) w[e] = 0.0;                       // (2^10 elements that count as nothing one by one)
             run += w[e];
         }
         const double in = warp_scan_f64(run, lane);
-        if (lane == 31) sm.warp_sum[warp] = in;
+        if (lane == 31) sm.warp_sum2[warp] = in;
         __syncthreads();
-        double upto = in - run;
 #pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            if (k == warp) upto += S;
-            S += sm.warp_sum[k];
-        }
+        for (int k = 0; k < NW; ++k) S += sm.warp_sum2[k];
         if (plain) {
-            // the stretch in which the target lies, or the last one with weight, then its element
-            const double target = (double)l.uniform * S;
-            int found = BINS * LIST, last = -1;
-            double before = 0.0;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                if (w[e] > 0.0) {
-                    last = tid * PER + e;
-                    if (found == BINS * LIST && upto + w[e] > target) { found = tid * PER + e; before = upto; }
-                }
-                upto += w[e];
-            }
-            const int f = __reduce_min_sync(0xffffffffu, found), z = __reduce_max_sync(0xffffffffu, last);
-            if (tid == 0) { sm.bin = BINS * LIST; sm.end_bin = -1; }
-            __syncthreads();
-            if (lane == 0) { atomicMin(&sm.bin, f); atomicMax(&sm.end_bin, z); }
-            __syncthreads();
-            const bool none = sm.bin == BINS * LIST;
-            const int at = none ? sm.end_bin : sm.bin;
-            if (!none && found == at) sm.kept_sum = before;
-            if (none && last == at) {
-                double b = upto;
-#pragma unroll
-                for (int e = PER - 1; e >= 0; --e)
-                    if (tid * PER + e >= at) b -= w[e];
-                sm.kept_sum = b;
-            }
-            __syncthreads();
-            const double front = sm.kept_sum;
-            // two neighbours a thread
-            const T* logits = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
-            constexpr int E = STRETCH / NT;
-            const int i0 = at * STRETCH + tid * E;
-            float x[E];
-            double v[E], sum = 0.0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] = i0 + e < a.vocab ? number(to_f32(logits[i0 + e])) : -INFINITY;
-                v[e] = weight(r, sm.tab, x[e]);
-                sum += v[e];
-            }
-            const double scan = warp_scan_f64(sum, lane);
-            if (lane == 31) sm.warp_sum2[warp] = scan;
-            if (tid == 0) { sm.bin = BINS * LIST; sm.end_bin = -1; }
-            __syncthreads();
-            double here = front + scan - sum;
-#pragma unroll
-            for (int k = 0; k < NW; ++k) here += k < warp ? sm.warp_sum2[k] : 0.0;
-            int hit = BINS * LIST, some = -1;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                here += v[e];
-                if (v[e] > 0.0) {
-                    some = tid * E + e;
-                    if (hit == BINS * LIST && here > target) hit = tid * E + e;
-                }
-            }
-            const int h = __reduce_min_sync(0xffffffffu, hit), y = __reduce_max_sync(0xffffffffu, some);
-            if (lane == 0) { atomicMin(&sm.bin, h); atomicMax(&sm.end_bin, y); }
-            __syncthreads();
-            const int token = sm.bin < BINS * LIST ? sm.bin : sm.end_bin;
-            if (token / E == tid) {
-                a.tokens[row] = at * STRETCH + token;
-                if (a.logprob) a.logprob[row] = (float)log((token % E ? v[E - 1] : v[0]) / S);
-            }
+            draw_from<T>(r, sm, a, row, w, S, (double)l.uniform * S);
             return;
         }
     }
-    // ---- where the front ends, from a histogram of the lists; then what lies in front of that
-    bool done = cut == -INFINITY;                                  // everything is in the lists
-    if (cut < INFINITY && l.use_m && !(l.use_k && l.use_p)) done = done || weight(r, sm.tab, cut) < r.min_p * 0.999;
-    const bool weigh = l.use_p && !l.use_k;
+    // ---- where the front ends; what lies in front of that, if the lists hold it
     const unsigned long long* entries = a.entries + (size_t)row * a.slices * CAP;
     const int slots = a.slices * CAP;
     auto entry = [&](int i) {                                      // ~0: none
         const int sl = i / CAP;
         return i - sl * CAP < (int)sm.all[sl] ? __ldcg(entries + i) : ~0ull;
     };
+    bool done = cut == -INFINITY;                                  // everything is in the lists
+    if (cut < INFINITY && l.use_m && !(l.use_k && l.use_p)) done = done || weight(r, sm.tab, cut) < r.min_p * 0.999;
+    const bool whole = done;
     int last_bin = BINS - 1;
     if (cut < INFINITY && (l.use_k || l.use_p)) {
         for (int i = tid; i < slots; i += NT) {
             const unsigned long long v = entry(i);
             if (v == ~0ull || rank_value(v) < cut) continue;
+            const float x = rank_value(v);
             if (weigh) {
-                const float d = depth_of(r, rank_value(v));
+                const float d = depth_of(r, x);
                 const int b = (int)d;
-                if (b < BINS - 1) atomicAdd(&sm.hist[b], (unsigned)UNIT - (unsigned)((d - (float)b) * (UNIT * (1.f - 0.97153194f))));
+                if (b < BINS - 1) atomicAdd(&sm.hist[b], __float2uint_rn(UNIT * exp2f(((float)b - d) * (1.f / STEPS))));
             } else {
-                const int b = wide_bin(r, rank_value(v));
+                const int b = wide_bin(r, x);
                 if (b < BINS - 1) atomicAdd(&sm.hist[b], 1u);
             }
         }
         __syncthreads();
+        // sums along the bins: elements, or weights by what each bin's upper end weighs
         const unsigned mine = sm.hist[tid];
         const float v = weigh ? (float)mine * (1.f / UNIT) * exp2f((float)tid * (-1.f / STEPS)) : (float)mine;
         float in = v;
@@ -1424,7 +1523,8 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
         float before = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) before += w < warp ? sm.warp_f[w] : 0.f;
-        const float goal = weigh ? (float)((double)l.top_p * S) * 1.001f : (float)l.top_k;
+        // the border is in front of here (a little further for weights, of which these are not exact; the sorted list's sums are, and say so if it was not far enough)
+        const float goal = weigh ? (float)((double)l.top_p * S) * 1.0002f : (float)l.top_k;
         if (before + in >= goal) atomicMin(&sm.bin, tid);
         __syncthreads();
         if (sm.bin < BINS - 1) {
@@ -1436,18 +1536,16 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
     if (done) {
         for (int i = tid; i < slots; i += NT) {
             const unsigned long long v = entry(i);
-            if (v == ~0ull || rank_value(v) < cut || wide_bin(r, rank_value(v)) > last_bin) continue;
+            if (v == ~0ull || rank_value(v) < cut) continue;
+            if (wide_bin(r, rank_value(v)) > last_bin) continue;
             const unsigned at = atomicAdd(&sm.n_list, 1u);
             if (at < LIST) sm.list[at] = v;
         }
         __syncthreads();
         count = (int)sm.n_list;
     }
-    if (count > LIST) {
+    if (count > LIST || !from_list(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform, whole))
         if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = {S, M, row};
-        return;
-    }
-    from_list(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform);
 }
 
 template <typename T>
