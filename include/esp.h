@@ -434,6 +434,7 @@ typedef struct {
  * [0, kv_len) of each sequence that has new tokens, the positions that no observed token sees among them; where the table names no page for these, they are passed over, and their
  * keys are not read.  Positions of the new tokens begin at zero whatever they hold, and with keep 0 nothing is read.  What a token does
  * not see does not reach a score; an lse that is no number reaches what its token sees.
+ * Sequences of one call that have new tokens must not share pages (which one's scores such a page then has is open).
  * The same call gives the same bits.  scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
 int esp_paged_key_weights_scratch_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
 int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const float* lse, const uint64_t* anc,

@@ -572,7 +572,7 @@ def _slots(x, cache: PagedCache, dtype, where: str, name: str):
 
 
 def _scratch(scratch, scratch_bytes: int, device: int, where: str) -> int:
-    if scratch.get_device() != device or scratch.numel() * scratch.element_size() < scratch_bytes or not scratch.is_contiguous():
+    if scratch.get_device() != device or not 0 <= scratch_bytes <= scratch.numel() * scratch.element_size() or not scratch.is_contiguous():
         raise EspError(-8, f"{where} (scratch: {scratch_bytes} dense bytes on device {device})")
     return scratch.data_ptr()
 

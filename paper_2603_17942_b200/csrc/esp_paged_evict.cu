@@ -339,8 +339,9 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_co
         walk([&](int s, uint32_t k) {
             const bool st = stays(k);
             const uint32_t gm = __ballot_sync(0xffffffffu, st && s >= c.budget), tm = __ballot_sync(0xffffffffu, k != 0 && !st && s < c.budget);
-            if ((gm >> lane) & 1) list[m + __popc(gm & low)].x = s;
-            if ((tm >> lane) & 1) list[e + __popc(tm & low)].y = s;
+            const int mi = m + __popc(gm & low), ei = e + __popc(tm & low);      // (pages that are not the sequence's own may have changed since they were counted)
+            if (((gm >> lane) & 1) && mi < a.list_cap) list[mi].x = s;
+            if (((tm >> lane) & 1) && ei < a.list_cap) list[ei].y = s;
             m += __popc(gm);
             e += __popc(tm);
         });
@@ -350,7 +351,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_co
         a.count[list_no] = few ? 0 : total;
         if (h == 0) a.info[b] = make_int4(c.budget, c.settled, c.base, 0);
     }
-    // positions of slots that had none
+    // positions of slots that had none, once nobody reads any
+    if (CL > 1) cluster.sync();
     if (a.positions.p)
         for (int s = max(c.settled, f0) + (int)threadIdx.x; s < min(c.budget, f1); s += THREADS) {
             const int index = page_index(a.pages, s), page = named(a.pages, table_entry(a.seq, b, index));
@@ -360,7 +362,6 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_co
         __syncthreads();
         if (warp < total) move_one<VEC>(a, elem, b, h, c, list[warp], lane);
     }
-    if (CL > 1) cluster.sync();                         // nobody leaves while others may look into its shared memory
 }
 
 // A warp takes up to 32 moves of a list at a time: each lane looks up one of them and moves its score and position, then all lanes move the rows together, four loads of each under way.
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 5) k_evict_move(const __grid_con
     const int list = blockIdx.x / blocks, part = blockIdx.x - list * blocks;
     const int b = list / a.Hkv, h = list - b * a.Hkv, lane = threadIdx.x & 31;
     pdl_wait();
-    const int n = a.count[list];
+    const int n = min(a.count[list], a.list_cap);
     const bool tells = part == 0 && h == 0 && threadIdx.x == 0;
     if (n == 0 && !tells) return;
     const int4 info = a.info[b];
@@ -385,7 +386,9 @@ __global__ void __launch_bounds__(MOVE_THREADS, 5) k_evict_move(const __grid_con
         const int have = (int)min((long long)each, n - m0);
         long long from = 0, to = -1;                // bytes behind k and behind v
         if (lane < have) {
-            const int2 x = moves[m0 + lane];
+            int2 x = moves[m0 + lane];
+            x.x = min(max(x.x, 0), a.seq.kv_cap - 1);
+            x.y = min(max(x.y, 0), a.seq.kv_cap - 1);
             const int fi = page_index(a.pages, x.x), ti = page_index(a.pages, x.y), fs = x.x - fi * a.pages.page_size, ts = x.y - ti * a.pages.page_size;
             int fp = table_entry(a.seq, b, fi), tp = table_entry(a.seq, b, ti);
             fp = named(a.pages, fp);

@@ -136,6 +136,23 @@ def test_lists_that_no_block_keeps(kv, budget):
     b.ok()
 
 
+@pytest.mark.parametrize("kv,budget,settled", [([9001, 12000], [300, 11990], [300, 8000]), ([70001, 30], [40000, 29], [69000, 11]), ([66000, 131073], [65999, 5000], [0, 66000])])
+def test_positions_of_long_lists(kv, budget, settled):
+    """Lists that several blocks have, also ones whose keys these do not keep, with positions of their own in front of `settled`; many equal scores."""
+    Hkv, recent = 2, 25
+    b = _batch(kv, 64, Hkv, 32, "bf16", "head", seed=2)
+    scores, positions = Scores(b, seed=5), Scores(b, fill=-5, dtype=torch.int32)
+    scores.x.copy_((scores.x * 700).floor())
+    seen = [t + 1000 for t in kv]
+    for s in range(len(kv)):                            # a cut has left every head with slots in an order of its own
+        page, slot = b.slots(s)
+        for h in range(Hkv):
+            order = torch.randperm(kv[s] + 1000, generator=_gen(h + s), device="cuda")[:settled[s]].to(torch.int32)
+            positions.view(b)[page[:settled[s]], slot[:settled[s]], h] = order
+    _cut(b, scores, budget, recent, positions, settled, seen)
+    b.ok()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("offset,pad", [(1, 0), (2, 1), (0, 3), (4, 4)])
 def test_strides_and_alignment(dtype, offset, pad):

@@ -202,6 +202,19 @@ def test_the_vocabulary_that_no_block_keeps():
             _check(x, np.array([0.2, 0.9], np.float32), tokens, lp, **settings)
 
 
+@pytest.mark.parametrize("dtype,rows,vocab", [("fp32", 60, 30011), ("bf16", 60, 30011), ("fp32", 3, 2 ** 21), ("bf16", 2, 2 ** 21)])
+def test_long_fronts(dtype, rows, vocab):
+    """Nuclei of thousands of tokens, more rows of them than there are clusters for; logits far from zero, temperatures that make a bin of logits wide or narrow."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    u = np.random.default_rng(vocab).random(rows).astype(np.float32)
+    p = np.linspace(0.6, 0.9999, rows)
+    for scale, offset, t in ((1.0, 0.0, 1.0), (3.0, -200.0, 4.0), (0.01, 7.0, 0.01), (1e5, 0.0, 9e4), (30.0, 1e6, 50.0), (1e9, 3e9, 1e9), (1e-4, 0.0, 1e-4), (1.0, 0.0, 20.0)):
+        x = (scale * torch.randn(rows, vocab, generator=g, device="cuda") + offset).to(DT[dtype])
+        settings = dict(top_p=p, temperature=t)
+        tokens, lp = _call(x, u, **settings)
+        _check(x, u, tokens, lp, **settings)
+
+
 def test_streams_and_graphs():
     x = _rows(20, 20011, 6, "bf16", "peaks")
     u = torch.rand(20, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")

@@ -124,3 +124,14 @@ def test_what_the_binding_refuses():
                  lambda: P.esp_paged_accept(cache, batch, i(2), i(2), i(2), i(2, 1), i(2), i(2)), lambda: P.esp_sample(f(2, 100), f(2), i(2), f(4), 16)):
         with pytest.raises(P.EspError):
             call()
+
+
+def test_scratch_sizes_that_the_binding_refuses():
+    from paper_2603_17942_b200 import binding
+    scratch = torch.empty(1024, dtype=torch.uint8)
+    assert binding._scratch(scratch, 1024, -1, "here") == scratch.data_ptr()
+    for size in (-1, 1025, 2 ** 63):
+        with pytest.raises(P.EspError):
+            binding._scratch(scratch, size, -1, "here")
+    with pytest.raises(P.EspError):
+        binding._scratch(scratch[::2], 100, -1, "here")
