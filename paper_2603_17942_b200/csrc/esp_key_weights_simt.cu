@@ -12,6 +12,7 @@ namespace {
 using namespace paged;
 
 constexpr int CK = 64, MP = 32, THREADS = 256;
+constexpr int BLOCKS = KEY_WEIGHT_KEYS / CK;      // of an SM: as many as the scratch has room for
 
 template <int D>
 struct Smem {
@@ -33,7 +34,7 @@ __device__ __forceinline__ float4 load4(const T* x) {
 }
 
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(THREADS) k_key_weights_simt(const __grid_constant__ KeyWeightArgs w) {
+__global__ void __launch_bounds__(THREADS, BLOCKS) k_key_weights_simt(const __grid_constant__ KeyWeightArgs w) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
     const PagedAttnArgs& a = w.a;
@@ -60,10 +61,19 @@ __global__ void __launch_bounds__(THREADS) k_key_weights_simt(const __grid_const
             sm.base[tid] = base;
         }
         __syncthreads();
-        for (int i = tid; i < CK * (D / 4); i += THREADS) {
-            const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-            *reinterpret_cast<float4*>(&sm.k[r][d]) =
-                sm.base[r] >= 0 ? load4<T, VEC>(reinterpret_cast<const T*>(a.pages.k) + sm.base[r] + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+        {
+            constexpr int N = CK * (D / 4) / THREADS;        // all of a thread's loads under way
+            float4 x[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int i = tid + j * THREADS, r = i / (D / 4), d = (i % (D / 4)) * 4;
+                x[j] = sm.base[r] >= 0 ? load4<T, VEC>(reinterpret_cast<const T*>(a.pages.k) + sm.base[r] + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int i = tid + j * THREADS;
+                *reinterpret_cast<float4*>(&sm.k[i / (D / 4)][(i % (D / 4)) * 4]) = x[j];
+            }
         }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         for (int t = pc.t0; t < pc.t0 + pc.n; ++t) {
@@ -122,7 +132,7 @@ __global__ void __launch_bounds__(THREADS) k_key_weights_simt(const __grid_const
 #pragma unroll
             for (int i = 0; i < 16; ++i) total += sm.sum[i][tid];
             if (pc.slot < 0) store_score(w, c, p0 + tid, total);
-            else w.part[((size_t)blockIdx.x * 2 + pc.slot) * KEY_WEIGHT_KEYS + tid] = total;
+            else w.part[((size_t)blockIdx.x * 2 + pc.slot) * CK + tid] = total;
         }
         u += max(pc.n, 1);
         if (u < end) next_chunk<CK>(w, c);
@@ -148,7 +158,7 @@ __global__ void __launch_bounds__(KEYS) k_key_weights_join(const __grid_constant
     float sum = 0.f;
     for (int k = cta; k <= last; ++k) {
         const int slot = k == cta && share.begin(k) < n.chunk_u ? 1 : 0;
-        sum += __ldcg(w.part + ((size_t)k * 2 + slot) * KEY_WEIGHT_KEYS + threadIdx.x);
+        sum += __ldcg(w.part + ((size_t)k * 2 + slot) * KEYS + threadIdx.x);
     }
     store_score(w, n, pos, sum);
 }
@@ -169,12 +179,14 @@ int launch_key_weights_simt(int dtype, KeyWeightArgs w, int n_sm, cudaStream_t s
     PagedAttnArgs& a = w.a;
     a.rows = a.group <= MP ? MP / a.group : 1;
     a.rows_shift = shift_of(a.rows);
-    a.n_cta = n_sm;
+    a.n_cta = n_sm * BLOCKS;
     a.min_units = 1;
     int rc;
     if (dtype == 0) rc = a.D == 32 ? run<float, 32>(w, s) : (a.D == 64 ? run<float, 64>(w, s) : run<float, 128>(w, s));
     else rc = a.D == 32 ? run<__nv_bfloat16, 32>(w, s) : (a.D == 64 ? run<__nv_bfloat16, 64>(w, s) : run<__nv_bfloat16, 128>(w, s));
-    return rc ? rc : launch_key_weights_join(w, CK, s);
+    const int observed = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;
+    // (no chunk has two owners where all observed tokens are one tile)
+    return rc || observed <= a.rows ? rc : launch_key_weights_join(w, CK, s);
 }
 
 int launch_key_weights_join(const KeyWeightArgs& w, int keys, cudaStream_t s) {
