@@ -54,11 +54,19 @@ __device__ __forceinline__ uint32_t warp_units(const KeyWeightArgs& w, const WSe
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum >> 31 ? 1u << 31 : (uint32_t)sum;
 }
-// The same for a sequence of each lane; one that has a single tile has a unit for each chunk.
+// The same for a sequence of each lane.  One that has a single tile has a unit for each chunk; without a window all chunks up to the first observed token meet all tiles, and where
+// only a few chunks are behind that a lane counts them by itself.
 template <int CK>
 __device__ __forceinline__ uint32_t seq_units(const KeyWeightArgs& w, const WSeq& x, int lane) {
-    uint32_t n = x.T == 1 ? (uint32_t)n_chunks<CK>(x) : 0u;
-    for (uint32_t many = __ballot_sync(0xffffffffu, x.T > 1); many; many &= many - 1) {
+    const int C = n_chunks<CK>(x), full = w.a.anc ? C : (int)min((long long)C, ((long long)x.s.kv - x.s.n + x.i0 + w.a.rows + CK - 1) / CK);
+    const bool alone = x.T <= 1 || (w.a.window <= 0 && C - full <= 16);
+    uint32_t n = x.T == 1 ? (uint32_t)C : 0u;
+    if (x.T > 1 && alone) {
+        unsigned long long sum = (unsigned long long)full * x.T;
+        for (int c = full; c < C; ++c) sum += make_chunk<CK>(w, x, c).units();
+        n = sum >> 31 ? 1u << 31 : (uint32_t)sum;
+    }
+    for (uint32_t many = __ballot_sync(0xffffffffu, !alone); many; many &= many - 1) {
         const int src = __ffs(many) - 1;
         WSeq o;
         o.s.start = 0;

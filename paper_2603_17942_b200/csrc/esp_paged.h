@@ -156,7 +156,8 @@ int launch_paged_merge(int dtype, const PagedAttnArgs& a, cudaStream_t s);
 int paged_page_map5(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows);      // [pages][heads][halves][slots][64], box 64 x box_rows x halves
 int paged_page_map(CUtensorMap* map, const PagedAttnArgs& a, const void* base, int box_rows);       // [pages][heads][slots][D], box 64 x box_rows
 int launch_key_weights_join(const KeyWeightArgs& w, int keys, cudaStream_t s);
-bool key_weights_few_supported(int dtype, const KeyWeightArgs& w);
+bool key_weights_few_supported(int dtype, const KeyWeightArgs& w);      // a handful of pairs
+bool key_weights_rows_supported(int dtype, const KeyWeightArgs& w);     // any number of them
 int launch_key_weights_few(KeyWeightArgs w, int n_sm, cudaStream_t s);
 bool key_weights_tc_supported(int dtype, const KeyWeightArgs& w);
 int launch_key_weights_tc(KeyWeightArgs w, int n_sm, cudaStream_t s);

@@ -372,9 +372,10 @@ int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const 
     w.keep = keep;
     w.part = reinterpret_cast<float*>(scratch);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const int rc = key_weights_few_supported(cache->dtype, w)  ? launch_key_weights_few(w, n_sm, s)
-                   : key_weights_tc_supported(cache->dtype, w) ? launch_key_weights_tc(w, n_sm, s)
-                                                               : launch_key_weights_simt(cache->dtype, w, n_sm, s);
+    const int rc = key_weights_few_supported(cache->dtype, w)    ? launch_key_weights_few(w, n_sm, s)
+                   : key_weights_tc_supported(cache->dtype, w)   ? launch_key_weights_tc(w, n_sm, s)
+                   : key_weights_rows_supported(cache->dtype, w) ? launch_key_weights_few(w, n_sm, s)
+                                                                 : launch_key_weights_simt(cache->dtype, w, n_sm, s);
     const cudaError_t e = cudaGetLastError();
     return rc ? ESP_E_CUDA : cuda_ok(e);
 }

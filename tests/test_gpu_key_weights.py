@@ -155,6 +155,18 @@ def test_trees(dtype, Hq, Hkv, D, n, kv, last):
     _run(b, q, 0.5, anc=_trees(b, 6), last=last)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,page,pad", [(8, 2, 128, 17, 0), (14, 2, 64, 9, 0), (40, 1, 128, 5, 0), (64, 1, 64, 17, 2), (3, 3, 128, 1, 0), (28, 4, 128, 16, 2), (6, 2, 64, 24, 4)])
+@pytest.mark.parametrize("n,kv", [([1, 1, 1], [700, 30, 1]), ([5, 130, 2], [600, 400, 1000]), ([60], [61])])
+@pytest.mark.parametrize("window,last,tree", [(0, 0, False), (33, 0, False), (300, 40, False), (0, 3, False), (0, 0, True), (0, 9, True)])
+def test_rows_that_no_box_fits(Hq, Hkv, D, page, pad, n, kv, window, last, tree):
+    """bf16 in pages that are no whole eights of slots, and queries whose heads do not lie on 16 bytes; passes that end inside a token's group of heads."""
+    if tree and max(n) > 128:
+        n = [min(x, 128) for x in n]
+    b = Batch(n, kv, page, Hkv, D, "bf16", "token" if page % 2 else "head", seed=window + last + D, front=1)
+    q = _randn(_gen(4), b.tokens, Hq, D + pad, dtype=DT["bf16"])[..., :D]
+    _run(b, q, 0.9, window=window, last=last, anc=_trees(b, 6) if tree else None)
+
+
 @pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 8, 2, 128), ("bf16", 32, 2, 64), ("fp32", 8, 2, 64)])
 @pytest.mark.parametrize("n,kv,window", [([1, 1], [900, 300], 0), ([40, 3], [900, 300], 0), ([1, 70], [1000, 1000], 130)])
 def test_with_the_lse_of_the_attention(dtype, Hq, Hkv, D, n, kv, window):
