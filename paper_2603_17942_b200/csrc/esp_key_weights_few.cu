@@ -7,6 +7,9 @@
 // columns in registers, two shuffles, one number written for each key.  All tokens count as one tile, so no chunk has several owners and nothing is joined; more than 32 pairs are
 // taken 32 at a time, with the queries read anew (from the first-level cache) for every chunk.
 // Pages that boxes of eight slots do not fit into (PLAIN) are copied row by row, each lane 16 bytes at a time, to where a box would have put them.
+// 64 single tokens over 1k to 8k positions, 32/8 heads of 128: 85 us, 0.90 of the copy rate; one over 4k 5.3 us, of which 3 are the way to the first keys.  Pages of 17, 25 x 4 tokens
+// over up to 7109 positions, 16/4 heads of 64: 28 us (on CUDA cores 173).  Which products are weights is a bit of a word that each column makes once: asked product by product, the
+// chunks that masks cut took up to twice as long (16 x 8 tokens over 1606 positions, 32/8 heads of 128: 40 us, now 28).
 #include <string.h>
 
 #include "esp_attn_tc.cuh"
