@@ -35,7 +35,7 @@ constexpr float STEPS = 24.f;             // fine bins of an octave of weights: 
 constexpr int FINE = 256, COARSE = 8;     // wide bins: that many fine ones, then as wide as eight of them: 95 octaves
 constexpr int MAX_CL = 8;                 // blocks of a cluster at most
 constexpr int LIST = 2048;                // elements that are sorted at most
-constexpr int SMEM_ROW = 160 * 1024;      // bytes of a row that a block keeps at most
+constexpr int SMEM_ROW = 64 * 1024;      // bytes of a row that a block keeps at most
 constexpr int TAB = 256;                  // 2^(j / TAB)
 constexpr float UNIT = 32768.f, GRID = 25.f;       // a histogram of weights counts in 1 / UNIT of what a bin's upper end weighs, bins are 1 / GRID of a logit
 constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
@@ -153,7 +153,8 @@ template <> struct Raw<__nv_bfloat16> {
 };
 
 // Sorts the block's list along the order and puts the elements' weights beside it.  Called by all threads.
-__device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
+template <typename T>
+__device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int vocab, int count) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __syncthreads();
     if (count <= 128) {
@@ -173,7 +174,9 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
         __syncthreads();
         return;
     }
-    // by bins of keys, then each element counts the ones in front of it in its bin
+    // by bins of (key, index), then each element counts the ones in front of it in its bin.  bf16 has few different keys in a list, with bits that are the same in all: without
+    // these the numbers that are cut into bins lie dense, by the indices (several hundred equal logits in one bin took 20 us to be put in order)
+    constexpr int SAME = sizeof(T) == 2 ? 16 : 0;
     constexpr int PER = LIST / NT;
     unsigned long long v[PER];
     uint32_t lo = ~0u, hi = 0;
@@ -192,9 +195,10 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) { lo = min(lo, sm.warp_lo[w]); hi = max(hi, sm.warp_hi[w]); }
-    int width = 0;
-    while (((hi - lo) >> width) >= BINS) ++width;
-    auto bin = [&](unsigned long long x) { return ((uint32_t)(x >> 32) - lo) >> width; };
+    lo >>= SAME;
+    const int bits = 32 - __clz(vocab - 1), width = max(0, bits + 32 - __clz((hi >> SAME) - lo) - 9);
+    static_assert(BINS == 1 << 9, "");
+    auto bin = [&](unsigned long long x) { return (unsigned)((((unsigned long long)((uint32_t)(x >> 32) >> SAME) - lo) << bits | (uint32_t)x) >> width); };
 #pragma unroll
     for (int e = 0; e < PER; ++e)
         if (e * NT + tid < count) atomicAdd(&sm.hist[bin(v[e])], 1u);
@@ -254,9 +258,10 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int count) {
 
 // What a block does with a list of `count` elements, the first ones of the order: sorts it, cuts it and draws.  S: the weights of the whole row that top_p goes by (below 0: those of
 // the first top_k).  whole: what is not in the list is not kept.  false: top_p reaches beyond the list.
+template <typename T>
 __device__ __forceinline__ bool from_list(const Row& r, Shared& sm, const SampleArgs& a, int row, int count, int top_k, float top_p, double S, float uniform, bool whole) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    sort_list(r, sm, count);
+    sort_list<T>(r, sm, a.vocab, count);
 
     // ---- exact sums along it, four neighbours a lane, and where the front ends
     const int n_k = min(count, top_k);
@@ -656,7 +661,7 @@ __device__ __forceinline__ int from_front(Row& r, Shared& sm, const SampleArgs& 
     if (count < 1) return 1;
     if (count > LIST) return 2;
     // the first element at which the sums along the order reach theta, four neighbours a thread
-    sort_list(r, sm, count);
+    sort_list<T>(r, sm, a.vocab, count);
     constexpr int PER = LIST / NT, NONE = 1 << 30;
     double v[PER], part = 0.0;
 #pragma unroll
@@ -932,7 +937,7 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
                 }
                 fetch_parts();
                 cluster.barrier_arrive();
-                from_list(r, sm, a, row, count, use_k ? top_k : count, use_p ? top_p : 2.f, use_k ? -1.0 : S, uniform, true);
+                from_list<T>(r, sm, a, row, count, use_k ? top_k : count, use_p ? top_p : 2.f, use_k ? -1.0 : S, uniform, true);
                 cluster.barrier_wait();
                 return;
             }
@@ -1544,7 +1549,7 @@ __global__ void __launch_bounds__(NT) k_sample_list(const __grid_constant__ Samp
         __syncthreads();
         count = (int)sm.n_list;
     }
-    if (count > LIST || !from_list(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform, whole))
+    if (count > LIST || !from_list<T>(r, sm, a, row, count, l.use_k ? l.top_k : count, l.use_p ? l.top_p : 2.f, l.use_k ? -1.0 : S, l.uniform, whole))
         if (tid == 0) a.rest[atomicAdd(a.n_rest, 1)] = {S, M, row};
 }
 
@@ -1553,8 +1558,9 @@ int run(SampleArgs a, int n_sm, cudaStream_t s) {
     k_sample_scan<T><<<(unsigned)((long long)a.n_rows * a.slices), SCAN_THREADS, 0, s>>>(a);
     if (launch_k(k_sample_list<T>, dim3(a.n_rows), dim3(NT), 0, s, true, a) != cudaSuccess) return -1;
     constexpr int STRIDE = 32 * Raw<T>::VEC;
+    const int most = a.n_rows > 4 * (2 * n_sm / MAX_CL) ? MAX_CL / 2 : MAX_CL;
     int cl = 1;
-    while (cl < MAX_CL && a.vocab > cl * 4096) cl *= 2;
+    while (cl < most && a.vocab > cl * 4096) cl *= 2;
     a.chunk = ((a.vocab + cl - 1) / cl + STRIDE - 1) / STRIDE * STRIDE;
     const size_t bytes = (size_t)a.chunk * sizeof(T);
     const bool resident = bytes <= SMEM_ROW;
