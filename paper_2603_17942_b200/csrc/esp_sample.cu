@@ -11,10 +11,10 @@
 //          those elements are sorted, their exact sums cut, and the draw is among them.  Rows without limits draw by stretches: the one the target lies in, then its element.
 //   rest   clusters of up to eight blocks for the rows that the lists do not settle.
 //          Long fronts of top-p (thousands of elements): a histogram of the weights over the whole row says in which bin of 1/25 of a logit the front ends; then sums of what lies in
-//          front of the bin, with that bin's elements as lists; the end by exact sums along them; the draw by stretches.  About 45 us for a row, 18 rows at a time.
+//          front of the bin, with that bin's elements as lists; the end by exact sums along them; the draw by stretches.  About 30 us for one row of 128256.
 //          Everything else (long fronts of top-k, thousands of equal logits, infinite logits): a value that the front does not reach below, or, where too much lies above it, the
 //          front's last element by histograms that close in on it; then the draw by stretches.
-// Sorting whole rows is what this avoids: with the row in a cluster's shared memory and every limit's end found there, the same 272 rows took 200 to 480 us instead of 54 to 180.
+// Sorting whole rows is what this avoids: with the row in a cluster's shared memory and every limit's end found there, the same 272 rows took 200 to 480 us instead of 54 to 157.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -35,7 +35,7 @@ constexpr float STEPS = 24.f;             // fine bins of an octave of weights: 
 constexpr int FINE = 256, COARSE = 8;     // wide bins: that many fine ones, then as wide as eight of them: 95 octaves
 constexpr int MAX_CL = 8;                 // blocks of a cluster at most
 constexpr int LIST = 2048;                // elements that are sorted at most
-constexpr int SMEM_ROW = 64 * 1024;      // bytes of a row that a block keeps at most
+constexpr int SMEM_ROW = 64 * 1024;       // bytes of a row that a block keeps at most: two blocks an SM (us, 64 fp32 rows of 128256, top-k 2500: kept 141, read anew 175)
 constexpr int TAB = 256;                  // 2^(j / TAB)
 constexpr float UNIT = 32768.f, GRID = 25.f;       // a histogram of weights counts in 1 / UNIT of what a bin's upper end weighs, bins are 1 / GRID of a logit
 constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
@@ -195,15 +195,27 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int vocab, i
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) { lo = min(lo, sm.warp_lo[w]); hi = max(hi, sm.warp_hi[w]); }
+    // values far from each other: by their distance from the largest instead, for keys would leave most bins to what is next to zero; what has no weight is last, in any order
+    const bool wide = hi - lo > 2u << 23;
+    const float top = key_value(~lo), scale = (BINS - 2) / fminf(top - key_value(~hi), (float)(121.0 * TAB / r.A));
     lo >>= SAME;
     const int bits = 32 - __clz(vocab - 1), width = max(0, bits + 32 - __clz((hi >> SAME) - lo) - 9);
     static_assert(BINS == 1 << 9, "");
-    auto bin = [&](unsigned long long x) { return (unsigned)((((unsigned long long)((uint32_t)(x >> 32) >> SAME) - lo) << bits | (uint32_t)x) >> width); };
+    int bin[PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
-        if (e * NT + tid < count) atomicAdd(&sm.hist[bin(v[e])], 1u);
+    for (int e = 0; e < PER; ++e) {
+        bin[e] = -1;
+        if (e * NT + tid < count) {
+            if (!wide) bin[e] = (int)((((unsigned long long)((uint32_t)(v[e] >> 32) >> SAME) - lo) << bits | (uint32_t)v[e]) >> width);
+            else {
+                const float x = rank_value(v[e]);
+                bin[e] = weight(r, sm.tab, x) == 0.0 ? BINS - 1 : min((int)((top - x) * scale), BINS - 2);
+            }
+            atomicAdd(&sm.hist[bin[e]], 1u);
+        }
+    }
     __syncthreads();
-    const unsigned mine = sm.hist[tid], in = warp_scan_u32(mine, lane), most = __reduce_max_sync(0xffffffffu, mine);
+    const unsigned mine = sm.hist[tid], in = warp_scan_u32(mine, lane), most = __reduce_max_sync(0xffffffffu, wide && tid == BINS - 1 ? 0u : mine);
     if (lane == 31) { sm.warp_count[warp] = in; sm.warp_hi[warp] = most; }
     __syncthreads();
     unsigned begin = in - mine, largest = 0;
@@ -216,15 +228,18 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int vocab, i
     sm.hist[tid] = begin;
     __syncthreads();
     if (largest <= 512) {
-#pragma unroll
-        for (int e = 0; e < PER; ++e)
-            if (e * NT + tid < count) sm.list[atomicAdd(&sm.hist[bin(v[e])], 1u)] = v[e];
-        __syncthreads();
         int rank[PER];
 #pragma unroll
         for (int e = 0; e < PER; ++e)
-            if (e * NT + tid < count) {
-                const int j0 = sm.all[bin(v[e])], j1 = sm.hist[bin(v[e])];
+            if (bin[e] >= 0) {
+                rank[e] = atomicAdd(&sm.hist[bin[e]], 1u);
+                sm.list[rank[e]] = v[e];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (bin[e] >= 0 && !(wide && bin[e] == BINS - 1)) {
+                const int j0 = sm.all[bin[e]], j1 = sm.hist[bin[e]];
                 int at = j0;
 #pragma unroll 4
                 for (int j = j0; j < j1; ++j) at += sm.list[j] < v[e];
@@ -233,7 +248,7 @@ __device__ __forceinline__ void sort_list(const Row& r, Shared& sm, int vocab, i
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < PER; ++e)
-            if (e * NT + tid < count) {
+            if (bin[e] >= 0) {
                 sm.list[rank[e]] = v[e];
                 sm.list_w[rank[e]] = weight(r, sm.tab, rank_value(v[e]));
             }
@@ -1558,7 +1573,9 @@ int run(SampleArgs a, int n_sm, cudaStream_t s) {
     k_sample_scan<T><<<(unsigned)((long long)a.n_rows * a.slices), SCAN_THREADS, 0, s>>>(a);
     if (launch_k(k_sample_list<T>, dim3(a.n_rows), dim3(NT), 0, s, true, a) != cudaSuccess) return -1;
     constexpr int STRIDE = 32 * Raw<T>::VEC;
-    const int most = a.n_rows > 4 * (2 * n_sm / MAX_CL) ? MAX_CL / 2 : MAX_CL;
+    // Clusters of eight are soonest done with one row (16 slices at a time: 43 us for a call of one row of 128256; in two rounds 55), of four with many, as one block of a cluster orders the list
+    // while the others wait: where a fifth of the rows may be more than there are clusters of eight (272 rows of which 55 come here: 187 us with eight, 157 with four).
+    const int most = a.n_rows > 5 * (2 * n_sm / MAX_CL) ? MAX_CL / 2 : MAX_CL;
     int cl = 1;
     while (cl < most && a.vocab > cl * 4096) cl *= 2;
     a.chunk = ((a.vocab + cl - 1) / cl + STRIDE - 1) / STRIDE * STRIDE;
