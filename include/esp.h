@@ -467,8 +467,8 @@ int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, 
  * tokens [device] [n_rows]; logprob [device] [n_rows] or NULL: the logarithm of the token's share of the kept weights.
  * A logit that is no number counts as -infinity.  With an infinite largest logit only those equal to it have weight.  A row without a finite or +infinite logit, or with a
  * setting that is no number, a temperature that is negative or infinite, or a uniform that is no number or negative, gets token -1 and a logprob that is no number.
- * Sums and weights are taken in 64 bits: the draw is that of the formulas unless uniform or top_p meets a border to 1e-12.  The same row gives the same token whatever
- * other rows there are.  scratch as esp_sample_scratch_bytes says, [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap. */
+ * Sums and weights are taken in 64 bits: the draw is that of the formulas unless uniform or top_p meets a border to 1e-12, and but for such borders the same row
+ * gives the same token whatever other rows there are.  scratch as esp_sample_scratch_bytes says, [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap. */
 typedef struct {
     const float* temperature;
     const int32_t* top_k;
