@@ -785,8 +785,8 @@ __device__ void sample_row(const SampleArgs& a, Shared& sm, unsigned char* smem_
     set_row(r, l, known.M);
     int bin = 0;
     __syncthreads();
-    // a long front of top-p (not with logits so large that their last bit is 3e-5 of a weight, or that a bin's number does not fit)
-    if (use_p && !use_k && !use_m && fabsf(known.M) * r.steps < 17000.f && fabsf(known.M) < 1e7f && front_bins<T>(r, sm, a, known, top_p, bin, me, CL))
+    // a long front of top-p (not of a row that the list holds as it is, nor with logits so large that their last bit is 3e-5 of a weight or that a bin's number does not fit)
+    if (use_p && !use_k && !use_m && a.vocab > LIST && fabsf(known.M) * r.steps < 17000.f && fabsf(known.M) < 1e7f && front_bins<T>(r, sm, a, known, top_p, bin, me, CL))
         for (int tries = 0; tries < 3; ++tries) {
             front_slices<T>(r, sm, a, known, bin, me, CL);
             cluster.sync();
