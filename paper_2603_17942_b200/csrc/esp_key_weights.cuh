@@ -17,9 +17,10 @@ struct WSeq {
 };
 struct WChunk {
     int t0, nt;           // tiles [t0, t0 + nt) meet it; nt 0: none does
-    __device__ __forceinline__ int units() const { return max(nt, 1); }
+    __host__ __device__ __forceinline__ int units() const { return max(nt, 1); }
 };
-__device__ __forceinline__ WSeq observed(const KeyWeightArgs& w, const Seq& s) {
+// (what does not touch device memory is compiled for the host too, where tests count with it)
+__host__ __device__ __forceinline__ WSeq observed(const KeyWeightArgs& w, const Seq& s) {
     WSeq x;
     x.s = s;
     x.i0 = w.last > 0 ? max(0, s.n - w.last) : 0;
@@ -27,9 +28,9 @@ __device__ __forceinline__ WSeq observed(const KeyWeightArgs& w, const Seq& s) {
     return x;
 }
 template <int CK>
-__device__ __forceinline__ int n_chunks(const WSeq& x) { return x.T > 0 ? (int)(((unsigned)x.s.kv + CK - 1) / CK) : 0; }
+__host__ __device__ __forceinline__ int n_chunks(const WSeq& x) { return x.T > 0 ? (int)(((unsigned)x.s.kv + CK - 1) / CK) : 0; }
 template <int CK>
-__device__ __forceinline__ WChunk make_chunk(const KeyWeightArgs& w, const WSeq& x, int c) {
+__host__ __device__ __forceinline__ WChunk make_chunk(const KeyWeightArgs& w, const WSeq& x, int c) {
     WChunk k;
     k.t0 = 0;
     k.nt = x.T;
@@ -54,18 +55,29 @@ __device__ __forceinline__ uint32_t warp_units(const KeyWeightArgs& w, const WSe
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum >> 31 ? 1u << 31 : (uint32_t)sum;
 }
-// The same for a sequence of each lane.  One that has a single tile has a unit for each chunk; without a window all chunks up to the first observed token meet all tiles, and where
-// only a few chunks are behind that a lane counts them by itself.
+// The same for one sequence, by one thread.  A single tile has a unit for each chunk; without a window all chunks up to the first observed token meet all tiles, and where
+// only a few chunks are behind that they are counted one by one.  false: there are many to count, n is 0.
+template <int CK>
+__host__ __device__ __forceinline__ bool lane_units(const KeyWeightArgs& w, const WSeq& x, uint32_t& n) {
+    n = 0;
+    if (x.T <= 1) {
+        n = x.T == 1 ? (uint32_t)n_chunks<CK>(x) : 0u;
+        return true;
+    }
+    const int C = n_chunks<CK>(x);
+    // (padding may reach so far that the first tiles see nothing at all: then no chunk meets all of them)
+    const int full = w.a.anc ? C : (int)max(0ll, min((long long)C, ((long long)x.s.kv - x.s.n + x.i0 + w.a.rows + CK - 1) / CK));
+    if (w.a.window > 0 || C - full > 16) return false;
+    unsigned long long sum = (unsigned long long)full * x.T;
+    for (int c = full; c < C; ++c) sum += make_chunk<CK>(w, x, c).units();
+    n = sum >> 31 ? 1u << 31 : (uint32_t)sum;
+    return true;
+}
+// The same for a sequence of each lane.
 template <int CK>
 __device__ __forceinline__ uint32_t seq_units(const KeyWeightArgs& w, const WSeq& x, int lane) {
-    const int C = n_chunks<CK>(x), full = w.a.anc ? C : (int)min((long long)C, ((long long)x.s.kv - x.s.n + x.i0 + w.a.rows + CK - 1) / CK);
-    const bool alone = x.T <= 1 || (w.a.window <= 0 && C - full <= 16);
-    uint32_t n = x.T == 1 ? (uint32_t)C : 0u;
-    if (x.T > 1 && alone) {
-        unsigned long long sum = (unsigned long long)full * x.T;
-        for (int c = full; c < C; ++c) sum += make_chunk<CK>(w, x, c).units();
-        n = sum >> 31 ? 1u << 31 : (uint32_t)sum;
-    }
+    uint32_t n;
+    const bool alone = lane_units<CK>(w, x, n);
     for (uint32_t many = __ballot_sync(0xffffffffu, !alone); many; many &= many - 1) {
         const int src = __ffs(many) - 1;
         WSeq o;
