@@ -144,21 +144,24 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) k_key_weights_simt(const __gr
 template <int KEYS>
 __global__ void __launch_bounds__(KEYS) k_key_weights_join(const __grid_constant__ KeyWeightArgs w) {
     Share share;
-    WCursor c;
+    WCursor c, n;
     const int cta = blockIdx.x;
-    if (!deal_keys<KEYS>(w, cta, threadIdx.x & 31, share, c)) return;
-    const uint32_t begin = share.begin(cta), end = share.begin(cta + 1);
-    if (cta + 1 >= share.ctas) return;
-    // the chunk in which the next CTA starts, if it is one that this CTA starts
-    WCursor n;
-    deal_keys<KEYS>(w, cta + 1, threadIdx.x & 31, share, n);
-    if (n.chunk_u >= end || n.chunk_u < begin) return;        // nobody shares, or another CTA has the first piece
-    pdl_wait();
+    uint32_t begin = 0, end = 0;
+    bool joins = deal_keys<KEYS>(w, cta, threadIdx.x & 31, share, c) && cta + 1 < share.ctas;
+    if (joins) {
+        begin = share.begin(cta);
+        end = share.begin(cta + 1);
+        // the chunk in which the next CTA starts, if it is one that this CTA starts (otherwise nobody shares, or another CTA has the first piece)
+        deal_keys<KEYS>(w, cta + 1, threadIdx.x & 31, share, n);
+        joins = n.chunk_u >= begin && n.chunk_u < end;
+    }
+    pdl_wait();                           // by every block: who comes behind this grid has to find the sums written
+    if (!joins) return;
     const int last = share.cta_of(n.chunk_u + n.k.units() - 1), pos = n.c * KEYS + threadIdx.x;
     if (pos >= n.x.s.kv) return;
     float sum = 0.f;
     for (int k = cta; k <= last; ++k) {
-        const int slot = k == cta && share.begin(k) < n.chunk_u ? 1 : 0;
+        const int slot = k == cta && begin < n.chunk_u ? 1 : 0;
         sum += __ldcg(w.part + ((size_t)k * 2 + slot) * KEYS + threadIdx.x);
     }
     store_score(w, n, pos, sum);
