@@ -110,6 +110,9 @@ struct AcceptArgs {
 };
 
 constexpr int SAMPLE_SLICE = 8192, SAMPLE_CAP = 160, SAMPLE_MAX_SLICES = 256, SAMPLE_BINS = 512;
+// Weights are added up in 32-bit counters in 1 / unit of the most that one of them can be: the unit for a counter that `elements` may be added to.
+constexpr unsigned SAMPLE_UNIT = 32768;
+__host__ __device__ constexpr unsigned sample_unit(unsigned elements) { return 0xffffffffu / elements < SAMPLE_UNIT ? 0xffffffffu / elements : SAMPLE_UNIT; }
 struct SampleSlice {        // what the first pass leaves of a slice of a row
     unsigned long long best;          // its first element in the order
     float cut;                        // its elements that are not below this are in its list (infinity: it has none)
@@ -131,6 +134,7 @@ struct SampleArgs {
     float* logprob;
     int32_t chunk;          // logits of a row that each block of its cluster has (the rest)
     int32_t slices;         // of a row
+    float unit, per_unit;   // of the rest's histograms of weights (sample_unit), and its inverse
     SampleSlice* slice;     // [n_rows][slices]
     unsigned long long* entries;      // [n_rows][slices][SAMPLE_CAP]
     SampleRest* rest;       // rows that the lists do not settle

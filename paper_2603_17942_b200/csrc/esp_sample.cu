@@ -37,7 +37,8 @@ constexpr int MAX_CL = 8;                 // blocks of a cluster at most
 constexpr int LIST = 2048;                // elements that are sorted at most
 constexpr int SMEM_ROW = 64 * 1024;       // bytes of a row that a block keeps at most: two blocks an SM (us, 64 fp32 rows of 128256, top-k 2500: kept 141, read anew 175)
 constexpr int TAB = 256;                  // 2^(j / TAB)
-constexpr float UNIT = 32768.f, GRID = 25.f;       // a histogram of weights counts in 1 / UNIT of what a bin's upper end weighs, bins are 1 / GRID of a logit
+constexpr float UNIT = SAMPLE_UNIT, GRID = 25.f;   // a histogram of weights counts in 1 / UNIT (or less: sample_unit) of what a bin's upper end weighs, bins are 1 / GRID of a logit
+static_assert(sample_unit(SAMPLE_MAX_SLICES * SAMPLE_CAP) == SAMPLE_UNIT, "all lists' elements may be in one bin");
 constexpr int MAX_VOCAB = SAMPLE_MAX_SLICES * SAMPLE_SLICE;      // 2^21
 constexpr int WANT = 110;                 // elements of a slice that go to its list, more or less
 
@@ -499,8 +500,8 @@ __device__ __forceinline__ void draw_from(const Row& r, Shared& sm, const Sample
 
 // Bins on a grid that all rows share, 1/25 of a logit each: bin k holds the logits from k / GRID on.
 __device__ __forceinline__ int grid_bin(float x) { return __float2int_rd(x * GRID); }
-// What an element adds to its bin of weights, in 1 / UNIT of the weight of the bin's upper end; per: log2 e / (GRID temperature).
-__device__ __forceinline__ unsigned grid_weight(float x, int k, float per) { return __float2uint_rn(UNIT * exp2f((x * GRID - (float)(k + 1)) * per)); }
+// What an element adds to its bin of weights, in 1 / unit of the weight of the bin's upper end; per: log2 e / (GRID temperature).
+__device__ __forceinline__ unsigned grid_weight(float x, int k, float per, float unit) { return __float2uint_rn(unit * exp2f((x * GRID - (float)(k + 1)) * per)); }
 
 // A slice of n logits, VEC of them to a lane at i0, i0 + 32 VEC, ...; -infinity behind its end.
 template <typename T>
@@ -553,7 +554,7 @@ __device__ __forceinline__ unsigned put_bits(const uint4 (&raw)[SLICE / SCAN_THR
 }
 
 // A long front of top-p, first step: a histogram of the row's weights.  The cluster's blocks take the row's slices, half a block for each.  Gives the bin in which the front ends (or its neighbour, at a border
-// of bins); false: it is not known.
+// of bins); false: it is not known, or has more elements than can be sorted (each adds one unit at most, so the bin's sum tells).
 template <typename T>
 __device__ __forceinline__ bool front_bins(const Row& r, Shared& sm, const SampleArgs& a, const SampleRest& known, float top_p, int& bin, int me, int CL) {
     constexpr int VEC = Raw<T>::VEC, PER = SLICE / SCAN_THREADS / VEC;
@@ -571,7 +572,7 @@ __device__ __forceinline__ bool front_bins(const Row& r, Shared& sm, const Sampl
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int k = grid_bin(x[e]);
-                if ((uint32_t)base - (uint32_t)k < BINS && x[e] == x[e]) atomicAdd(&sm.hist[base - k], grid_weight(x[e], k, per));
+                if ((uint32_t)base - (uint32_t)k < BINS && x[e] == x[e]) atomicAdd(&sm.hist[base - k], grid_weight(x[e], k, per, a.unit));
             }
         }
     }
@@ -583,7 +584,7 @@ __device__ __forceinline__ bool front_bins(const Row& r, Shared& sm, const Sampl
 #pragma unroll
     for (int c = 0; c < MAX_CL; ++c) mine += part[c];
     // sums along the bins, by what each one's upper end weighs
-    const float v = (float)mine * (1.f / UNIT) * exp2f(((float)(base - tid + 1) - known.M * GRID) * per);
+    const float v = (float)mine * a.per_unit * exp2f(((float)(base - tid + 1) - known.M * GRID) * per);
     float in = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -599,7 +600,7 @@ __device__ __forceinline__ bool front_bins(const Row& r, Shared& sm, const Sampl
     if (before + in >= (float)((double)top_p * known.S)) atomicMin(&sm.bin, tid);
     __syncthreads();
     bin = base - sm.bin;
-    const bool found = sm.bin < BINS;
+    const bool found = sm.bin < BINS && !__syncthreads_or(tid == sm.bin && mine > (unsigned long long)LIST * (unsigned)a.unit);
     cluster.sync();                       // (the histograms have been read)
     return found;
 }
@@ -1590,6 +1591,9 @@ int run(SampleArgs a, int n_sm, cudaStream_t s) {
     int cl = 1;
     while (cl < most && a.vocab > cl * 4096) cl *= 2;
     a.chunk = ((a.vocab + cl - 1) / cl + STRIDE - 1) / STRIDE * STRIDE;
+    // (a nearly flat row has all the elements of a block's slices in one bin)
+    a.unit = (float)sample_unit((unsigned)((a.slices + 2 * cl - 1) / (2 * cl) * 2 * SLICE));
+    a.per_unit = 1.f / a.unit;
     const size_t bytes = (size_t)a.chunk * sizeof(T);
     const bool resident = bytes <= SMEM_ROW;
     const int clusters = 2 * n_sm / cl < a.n_rows ? 2 * n_sm / cl : a.n_rows;
@@ -1657,7 +1661,7 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
     a.n_rest = reinterpret_cast<int32_t*>(a.rest + n_rows);
     a.logits = logits; a.row_stride = row_stride; a.n_rows = n_rows; a.vocab = vocab;
     a.temperature = sampling->temperature; a.top_k = sampling->top_k; a.top_p = sampling->top_p; a.min_p = sampling->min_p;
-    a.uniform = uniform; a.tokens = tokens; a.logprob = logprob; a.chunk = 0;
+    a.uniform = uniform; a.tokens = tokens; a.logprob = logprob; a.chunk = 0; a.unit = a.per_unit = 0.f;
     const int rc = launch_sample(dtype, a, n_sm, reinterpret_cast<cudaStream_t>(cuda_stream));
     const cudaError_t e = cudaGetLastError();
     return rc ? ESP_E_CUDA : (e == cudaSuccess ? ESP_OK : ESP_E_CUDA);
