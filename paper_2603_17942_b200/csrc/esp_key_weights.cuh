@@ -19,6 +19,11 @@ struct WChunk {
     int t0, nt;           // tiles [t0, t0 + nt) meet it; nt 0: none does
     __host__ __device__ __forceinline__ int units() const { return max(nt, 1); }
 };
+// A bound for the observed tokens of a sequence, so that they all are one tile.  (max_new may be far above the tokens of the call; what is added to such a bound has to fit.)
+inline int one_tile(const KeyWeightArgs& w) {
+    const int most = w.last > 0 && w.last < w.a.seq.max_new ? w.last : w.a.seq.max_new;
+    return most < w.a.seq.n_tokens ? most : w.a.seq.n_tokens;
+}
 // (what does not touch device memory is compiled for the host too, where tests count with it)
 __host__ __device__ __forceinline__ WSeq observed(const KeyWeightArgs& w, const Seq& s) {
     WSeq x;

@@ -321,7 +321,7 @@ int launch_key_weights_few(KeyWeightArgs w, int n_sm, cudaStream_t s) {
     if (plain) box = keys;
     else if (paged_page_map5(&p.map_k, a, a.pages.k, box)) return -1;
     p.box_shift = shift_of(box);
-    a.rows = w.last > 0 && w.last < a.seq.max_new ? w.last : a.seq.max_new;       // one tile
+    a.rows = one_tile(w);
     a.rows_shift = shift_of(a.rows);
     a.min_units = 1;
     p.w = w;

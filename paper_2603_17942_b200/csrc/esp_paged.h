@@ -22,7 +22,7 @@ struct PagesView {
 // log2 of x, -1 if x is no power of two: what is divided by on the way to a kernel's first load is a shift where it can be
 inline int shift_of(int x) {
     int s = 0;
-    while ((1 << s) < x) ++s;
+    while (s < 30 && (1 << s) < x) ++s;         // (2^30 is the largest there is)
     return (1 << s) == x ? s : -1;
 }
 

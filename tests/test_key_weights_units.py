@@ -1,8 +1,6 @@
 """How the weights of cached positions count their work (no GPU): the host-side compilation of the counting functions against the definition, chunk by chunk and token by token."""
 import subprocess
 
-import pytest
-
 from paper_2603_17942_b200 import build as esp_build
 
 PROGRAM = r"""
@@ -78,18 +76,62 @@ int main() {
 }
 """
 
+BOUNDS = r"""
+#include <stdio.h>
+#include <string.h>
+#include "esp_key_weights.cuh"
 
-@pytest.fixture(scope="module")
-def program(tmp_path_factory):
-    at = tmp_path_factory.mktemp("units")
+using namespace esp;
+using namespace esp::paged;
+
+int main() {
+    const long long most = 0x7fffffff;
+    for (long long near : {1ll, 2ll, 3ll, 64ll, 1000ll, 1ll << 29, 1ll << 30, most})
+        for (long long x = near - 1; x <= near + 1 && x <= most; ++x) {
+            int want = -1;
+            for (int s = 0; s < 31; ++s)
+                if (x == 1ll << s) want = s;
+            if (x > 0 && shift_of((int)x) != want) { printf("shift_of(%lld) is %d\n", x, shift_of((int)x)); return 1; }
+        }
+    // all observed tokens of any sequence are one tile, whatever bound the caller gives
+    for (int tokens : {1, 60, 1 << 30})
+        for (int max_new : {tokens, 100, (1 << 30) + 1, 0x7fffffff})
+            for (int last : {0, 1, 40, 0x7fffffff}) {
+                KeyWeightArgs w;
+                memset(&w, 0, sizeof(w));
+                w.a.seq.n_tokens = tokens;
+                w.a.seq.max_new = max_new;
+                w.last = last;
+                w.a.rows = one_tile(w);
+                w.a.rows_shift = shift_of(w.a.rows);
+                for (int n : {0, 1, 2, 59, 60, 100, 1 << 30}) {
+                    if (n > tokens || n > max_new) continue;
+                    Seq s;
+                    s.start = 0; s.n = s.kv = n;
+                    const WSeq x = observed(w, s);
+                    if (x.T != (n > 0) || w.a.rows < 1) { printf("tokens %d max_new %d last %d n %d: %d tiles of %d\n", tokens, max_new, last, n, x.T, w.a.rows); return 1; }
+                }
+            }
+    return 0;
+}
+"""
+
+
+def _compile(source, at):
     src, exe = str(at / "units.cu"), str(at / "units")
     with open(src, "w") as f:
-        f.write(PROGRAM)
+        f.write(source)
     subprocess.run([esp_build.NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-O1", "-std=c++17", "-I", esp_build.CSRC, "-o", exe, src], check=True, capture_output=True, text=True)
     return exe
 
 
-def test_units_of_every_sequence(program):
+def test_units_of_every_sequence(tmp_path):
     """Single tokens, prompts, observed tails, windows and trees; as many positions as tokens, more, fewer (padding), a few of them only and none."""
-    done = subprocess.run([program], capture_output=True, text=True, timeout=300)
+    done = subprocess.run([_compile(PROGRAM, tmp_path)], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stdout
+
+
+def test_bounds_far_above_the_tokens(tmp_path):
+    """max_new is a bound: 2^31 - 1 is one too.  (A power of two that was looked for beyond 2^30 was never found.)"""
+    done = subprocess.run([_compile(BOUNDS, tmp_path)], capture_output=True, text=True, timeout=20)
     assert done.returncode == 0, done.stdout
