@@ -487,7 +487,8 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
  *   tokens_out[b] = the tokens chosen along the path, rows_out[b] (or NULL) = its rows, rows of out_stride numbers, -1 behind the last.
  * parents, drafted, chosen [device] [n_tokens]; the others [device] [batch] and [batch][out_stride], out_stride >= max_new.  A sequence without new tokens
  * keeps its kv_len.  One that does not hold together, or has kv_len < n, keeps it too, with n_out 0, and is recorded in the batch's status.  A page that
- * the table does not name where a row has to move is recorded, and the row's keys and values are lost.  kv_len_out must not be batch->kv_len. */
+ * the table does not name where a row has to move is recorded, and the row's keys and values are lost.  kv_len_out must not be batch->kv_len.
+ * Up to 2^20 KV heads (ESP_E_ARG otherwise), as many as esp_paged_append takes. */
 int esp_paged_accept(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const int32_t* parents, const int32_t* drafted, const int32_t* chosen,
                      int32_t* tokens_out, int32_t* rows_out, int32_t out_stride, int32_t* n_out, int32_t* kv_len_out, void* cuda_stream);
 

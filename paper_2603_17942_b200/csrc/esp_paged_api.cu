@@ -436,6 +436,7 @@ int esp_paged_accept(int32_t n_tokens, const esp_paged_cache* cache, const esp_p
     if (const int rc = check_slots(cache)) return rc;
     if (const int rc = check_batch(batch)) return rc;
     if (batch->max_new > RT || out_stride < batch->max_new) return ESP_E_ARG;
+    if (cache->n_kv_heads > MAX_HEADS) return ESP_E_ARG;        // (as in the append: a row's units are counted in 32 bits)
     if (off(parents, 4) || off(drafted, 4) || off(chosen, 4) || off(tokens_out, 4) || off(rows_out, 4) || off(n_out, 4) || off(kv_len_out, 4)) return ESP_E_ARG;
     if (batch->batch == 0) return ESP_OK;
     if ((n_tokens > 0 && (!parents || !drafted || !chosen)) || !tokens_out || !n_out || !kv_len_out) return ESP_E_ARG;
