@@ -452,7 +452,8 @@ int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const 
  * their own numbers as positions, which is so until a first cut.
  * budget, settled, seen, kv_len_out [device] [batch]; kv_len_out may be batch->kv_len.  q_start and max_new are not read.  A sequence is left as it is, its kv_len copied and the
  * batch's status set, if its kv_len is out of range, its budget negative or below `recent` while kv_len is above it, or it is above its budget with more positions
- * than the scratch was made for (max_kv).  Cut sequences must not share pages.  scratch [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap. */
+ * than the scratch was made for (max_kv).  Cut sequences must not share pages.  scratch [device] 256-byte aligned, contents of no account, one for each of two calls that may overlap; many short
+ * lists are cut soonest where scratch_bytes is that of their max_kv, however large the scratch is. */
 int esp_paged_evict_scratch_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_kv, size_t* bytes_out);
 int esp_paged_evict(const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_paged_slots* scores, const esp_paged_slots* positions, const int32_t* seen,
                     int32_t* settled, int32_t recent, const int32_t* budget, int32_t* kv_len_out, void* scratch, size_t scratch_bytes, void* cuda_stream);

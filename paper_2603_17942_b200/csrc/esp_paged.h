@@ -87,6 +87,22 @@ struct KeyWeightArgs {
     float* part;            // [n_cta][2][keys of a chunk] sums of the pieces of chunks that several CTAs share
 };
 
+// Blocks for a list of eviction: as many as hold the keys of the longest one that the table has room for, up to EVICT_BLOCKS.  Where that is more than the GPU takes at a time, blocks that a
+// short list does not need cost it (barriers, and the moves within the first kernel), and rows of a table are often as long as the longest context: then it goes by what the scratch is
+// made for, and each list that fits into one block has one (`as_needed`).  us, 256 lists of 2049 keys and 128 of 8000, cut to 2048 and 1000, with 1, 2, 4 and 8 blocks: 19, 33, 64,
+// 139 and 51, 51, 59, 82; where the GPU is not full, others read a list sooner: 32 of 8000 27, 24, 22, 24.
+constexpr int EVICT_KEYS = 8192, EVICT_BLOCKS = 8;        // keys that a block keeps, blocks of a cluster at most
+inline int evict_blocks(int kv_cap, int list_cap, int lists, int n_sm, int32_t* as_needed) {
+    auto holding = [](long long keys) {
+        int n = 1;
+        while (n < EVICT_BLOCKS && keys > (long long)n * EVICT_KEYS) n *= 2;
+        return n;
+    };
+    const int n = holding(kv_cap);
+    *as_needed = (long long)lists * n > 2ll * n_sm;
+    return *as_needed ? holding(2ll * list_cap < kv_cap ? 2ll * list_cap : kv_cap) : n;
+}
+
 struct EvictArgs {
     PagesView pages;
     SlotsView scores, positions;
@@ -96,6 +112,7 @@ struct EvictArgs {
     int32_t recent, Hkv, D;
     int32_t list_cap;       // moves of a list at most
     int32_t vec;            // elements of a row that can be moved at a time
+    int32_t as_needed;      // a list whose keys fit into one block has one, whatever the others of the call need
     int32_t* count;         // [batch * Hkv] moves
     int4* info;             // [batch] (kv_len from now on, -1: as it was; settled slots and their positions' base as the call found them)
     int2* list;             // [batch * Hkv][list_cap] (from, to)

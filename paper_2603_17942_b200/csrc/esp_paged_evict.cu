@@ -38,8 +38,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 constexpr uint32_t KEY_INF = 0xff800000u;      // order_key(INFINITY)
 
-constexpr int BINS = 256, MAX_CL = 8, NEAR = 255;
-constexpr int KEYS = 8192;            // keys that a block keeps; those of a longer stretch are made anew in every pass
+constexpr int BINS = 256, MAX_CL = EVICT_BLOCKS, NEAR = 255;
+constexpr int KEYS = EVICT_KEYS;      // keys that a block keeps; those of a longer stretch are made anew in every pass
 
 struct SeqCut {
     int kv, budget;
@@ -146,7 +146,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_co
     __shared__ uint32_t s_near[MAX_CL][NEAR + 1];       // [block] the keys that share the digits found so far; the last one: how many
     __shared__ int s_near_n;
     cg::cluster_group cluster = cg::this_cluster();
-    const int CL = cluster.num_blocks(), me = cluster.block_rank(), list_no = blockIdx.x / CL;
+    int CL = cluster.num_blocks();
+    const int me = cluster.block_rank(), list_no = blockIdx.x / CL;
     const int b = list_no / a.Hkv, h = list_no - b * a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t low = (1u << lane) - 1u;
     pdl_launch_dependents();
@@ -157,6 +158,10 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_evict_select(const __grid_co
             if (h == 0) a.info[b] = make_int4(-1, 0, 0, 0);
         }
         return;
+    }
+    if (a.as_needed && c.kv <= KEYS) {                  // the first block has the list alone (and nothing to do with the others)
+        if (me != 0) return;
+        CL = 1;
     }
     if (CL > 1) cluster.barrier_arrive();               // (before anybody looks into another block's shared memory, all have to have started)
     // the block's stretch of slots, and each warp's of it
@@ -527,10 +532,8 @@ cudaError_t run_select(const EvictArgs& a, int elem, int cl, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, k_evict_select<VEC>, a, elem);
 }
 template <int VEC>
-int run_evict(const EvictArgs& a, int elem, int n_sm, cudaStream_t s) {
-    const int lists = a.seq.batch * a.Hkv;
-    int cl = 1;
-    while (cl < MAX_CL && a.seq.kv_cap > cl * KEYS) cl *= 2;
+int run_evict(EvictArgs a, int elem, int n_sm, cudaStream_t s) {
+    const int lists = a.seq.batch * a.Hkv, cl = evict_blocks(a.seq.kv_cap, a.list_cap, lists, n_sm, &a.as_needed);
     if (run_select<VEC>(a, elem, cl, s) != cudaSuccess) return -1;
     const long long want = (long long)n_sm * 8 / lists;
     const int blocks = want < 1 ? 1 : (int)want;
