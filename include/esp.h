@@ -435,6 +435,7 @@ typedef struct {
  * keys are not read.  Positions of the new tokens begin at zero whatever they hold, and with keep 0 nothing is read.  What a token does
  * not see does not reach a score; an lse that is no number reaches what its token sees.
  * Sequences of one call that have new tokens must not share pages (which one's scores such a page then has is open).
+ * A call with 2^31 or more pairs of a chunk of keys (32 to 256 positions) and a tile of tokens writes nothing and records the capacity code in *status.
  * The same call gives the same bits.  scratch [device] 256-byte aligned, contents of no account; two calls that may overlap on the GPU need one each. */
 int esp_paged_key_weights_scratch_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t head_dim, size_t* bytes_out);
 int esp_paged_key_weights(int32_t n_tokens, const esp_paged_cache* cache, const esp_paged_batch* batch, const esp_heads* q, const float* lse, const uint64_t* anc,
@@ -483,7 +484,8 @@ int esp_sample(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
 /* Verification of draft trees whose keys and values were appended to pages.  The new tokens of a sequence are the rows of its tree (at most ESP_MAX_ROWS): row 0 the root,
  * parents[i] in 0 .. i - 1 the row that row i hangs on (any other value: on none, as the rows of probes), drafted[i] its token, chosen[i] the
  * token that the model put behind it (esp_sample, or the largest logit; below 0: none).  From the root on, the next row is the lowest one that hangs on the present row and
- * carries its chosen token.  The path's r rows become the cache: the keys and values of its i-th row move to position kv_len[b] - n + i, and
+ * carries its chosen token.  The path's r rows become the cache: the keys and values of its i-th row move to position kv_len[b] - n + i (numbers of slots, as scores, stay
+ * where they are: the path's weights are taken behind this call, by its own rows' queries over the new lengths), and
  *   kv_len_out[b] = kv_len[b] - n + r,  n_out[b] = r (one less if the last row chose none),
  *   tokens_out[b] = the tokens chosen along the path, rows_out[b] (or NULL) = its rows, rows of out_stride numbers, -1 behind the last.
  * parents, drafted, chosen [device] [n_tokens]; the others [device] [batch] and [batch][out_stride], out_stride >= max_new.  A sequence without new tokens

@@ -3,7 +3,8 @@
 //
 // A block holds a chunk of 64 keys in shared memory as fp32 and walks the tiles of 32 (token, query head) pairs that see it: thread (ty, tx), 16 x 16, has
 // pairs 2 ty and 2 ty + 1 and keys tx + 16 j.  The weights exp(scale q k - lse) add up in registers, one number for each of a thread's keys, and over the ty at the end.
-// Multiply-adds bound long calls (fp32, 4 x 1000 tokens, 8/2 heads of 128: 188 us, 22 TFLOP/s; with one block an SM 322), the chain from lengths over pages to keys small ones (6 to 10 us).
+// Shared memory bounds long calls: for four elements of a head a warp reads six float4, about 10 cycles of its pipe, for multiply-adds that take the SM 8 (fp32, 4 x 1000 tokens, 8/2 heads of
+// 128: 190 us, 22 TFLOP/s, the pipe busy for 85 % of the cycles and the multiply-adds' for 41 %; with one block an SM 322).  The chain from lengths over pages to keys bounds small ones (6 to 10 us).
 #include "esp_key_weights.cuh"
 
 namespace esp {

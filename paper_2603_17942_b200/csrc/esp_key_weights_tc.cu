@@ -6,7 +6,7 @@
 // So a key's sum never leaves its thread while the chunk stays, keys are read once and queries once for every 256 keys.
 // What bounds it: one exponential a pair and key, 2048 cycles of an SM's special-function units for 256 keys and 128 pairs, twice what the products take.  2048 tokens at
 // the end of 8192, 32/8 heads of 128: 2750 cycles a tile, 165 us (71 us of products at the cuBLAS rate).  Built and slower (us there): 8 warps of weights 190; a part of the
-// exponentials as polynomials 175 to 188 (an eighth to a half of them: the multiply-add pipes have the scaling and the sums already); the two groups of warps on alternate tiles
+// exponentials as polynomials 175 to 188 (an eighth to a half of them; what they cost was not looked into: the kernel uses 39 % of its issue slots); the two groups of warps on alternate tiles
 // 179; masks by comparing every column 170.  For few tiles the start counts: 64 tokens of one sequence took 22 us with one warp issuing the keys' boxes, 17.5 with two.
 // Roles: warps 0 and 3 TMA (a subtile's keys each, warp 0 the queries too), warp 1 issues the products, warp 2 brings the tiles' lse, warps 4-19 have the weights.  Every wait is bounded; one
 // that runs out is recorded, the tensor memory is given back and the kernel returns.

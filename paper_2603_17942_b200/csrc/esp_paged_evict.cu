@@ -6,7 +6,7 @@
 // k_evict_move moves the lists' rows, scores and positions, spread over the whole GPU.  Both are chains of short steps: what counts is that the loads of a step are all under
 // way before the first is waited for, and that the code is short (loops unrolled over 32 keys in registers took longer to fetch than to run).
 // Clusters with the keys in shared memory, and the last two digits from the keys themselves where few share the first two, took 8 sequences of 32k positions cut to 4k, 8 heads of
-// 128, from 121 to 78 us: 28 for the choice and 50 for 235 MB of rows, at 0.73 of the copy rate.  32 sequences that are one position above their budget: 14 us.
+// 128, from 121 to 78 us: 28 for the choice and 50 for 235 MB of rows, at 0.73 of the copy rate.  32 sequences that are one position above their budget: 14 us, 42 with table and scratch for 64k positions (seven blocks of eight that leave at once).
 #include <cooperative_groups.h>
 
 #include "esp_paged.cuh"

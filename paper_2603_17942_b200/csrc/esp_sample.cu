@@ -6,7 +6,7 @@
 //
 //   scan   a block for each slice of 8192 logits of a row, which it holds in its registers and reads once: the slice's largest element, the sums of its weights by stretches of 1024
 //          (for top-p and for rows without limits), and a list of its largest elements, about 110, with the value below which it leaves things out.  How many weights it has to
-//          work out is what bounds it where sums are asked for (us, 272 fp32 rows of 128256, 20 us to read: greedy 28, temperature alone 54, min-p 60).
+//          work out is what bounds it where sums are asked for (us, 272 fp32 rows of 128256, 20 us to read: greedy 28, temperature alone 54, min-p 62).
 //   list   a block for each row: the slices' largest give M, and the sums scaled to it the row's S.  What the limits keep lies nearly always within the lists: histograms say how far,
 //          those elements are sorted, their exact sums cut, and the draw is among them.  Rows without limits draw by stretches: the one the target lies in, then its element.
 //   rest   clusters of up to eight blocks for the rows that the lists do not settle.
